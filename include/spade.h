@@ -293,6 +293,121 @@ spade_status spade_accept_from_logits_noalloc(int B, int gamma, int V, const flo
                                               float temperature, int32_t* d_n_accepted,
                                               int32_t* d_correction, uint32_t* d_err, void* stream);
 
+/*
+ * K/V caches in 4 bits
+ * --------------------
+ * A cache of its own next to the model's: the attention state of a stack of
+ * layers in a quarter of bfloat16's bytes, for a program that computes its
+ * projections itself.  Every position and K/V head holds a key and a value of
+ * head_dim features as codes n of 4 bits, with one scale s and one minimum m
+ * (bfloat16) each:
+ *   m = bf16(min_f x_f), s = bf16((max_f x_f - m) * (1 / 15))  (in float32)
+ *   n_f = clamp((x_f - m) / s to the nearest integer, ties to even, 0, 15)
+ *   (0 where s = 0), and the cache stands for x_f ~ m + n_f s.
+ * A row with a feature that is not finite, or whose span max - m is not, is
+ * held as NaN.  head_dim bytes and 8 more per position and K/V head (bfloat16
+ * takes 4 head_dim).
+ *
+ * The calls share a shape, given by value of its fields at every call:
+ *   n_layers, batch    layers and requests of the cache
+ *   n_heads            query heads, a multiple of n_kv_heads (grouped-query:
+ *                      query head h reads K/V head h / (n_heads / n_kv_heads))
+ *   head_dim           64 or 128
+ *   max_len            positions per request, at most 1048576
+ * Layouts: a cache is n_layers x batch x n_kv_heads regions, whose inner order
+ * is the library's; weights are float32 [n_layers][batch][n_kv_heads][max_len]
+ * (the calls of one layer take that layer's part).  lens[b] counts the
+ * positions request b holds: the calls read it, and only spade_kvq_evict
+ * changes it (the caller adds the rows it keeps).  Requests are 0 .. B - 1.
+ * Inputs of `dtype` SPADE_F32 or SPADE_BF16 are rows of contiguous heads, `ld`
+ * elements from one row to the next (a multiple of 4), from addresses that
+ * divide by 16 (SPADE_F32) or 8 (SPADE_BF16); other float arrays divide by 16.
+ * Row i of request b is row b R + i.  d_rows: int32 [B], how many of its R
+ * rows each request uses (clamped to [0, R]); NULL: all.  d_err: a device
+ * uint32 that gets SPADE_DERR_CAPACITY ORed in where a length leaves the
+ * range a call was given (nothing is read or written out of the cache then);
+ * may be NULL.  All calls are asynchronous, allocate nothing and can be
+ * captured.
+ */
+typedef struct {
+  int32_t n_layers, batch, n_heads, n_kv_heads, head_dim, max_len;
+} spade_kvq_shape;
+
+/* Bytes of a cache (256-byte aligned; needs no initial contents). */
+size_t spade_kvq_bytes(const spade_kvq_shape* shape);
+
+/* Bytes of the workspace of spade_kvq_attend calls of up to max_rows rows (1
+ * to 16) per request.  Calls that may overlap need a workspace each; it needs
+ * no initial contents and keeps nothing between calls. */
+size_t spade_kvq_workspace_bytes(const spade_kvq_shape* shape, int max_rows);
+
+/* New rows of one layer: queries, keys and values as a projection leaves them.
+ * Every query and key head is divided by its root mean square over head_dim
+ * (x / sqrt(mean(x^2) + eps) * gain; d_gain_q / d_gain_k float32 [head_dim],
+ * NULL: no norm), then rotated by its position as in the verifier (feature i
+ * with i + head_dim / 2; d_rope float32 [rope_len][head_dim / 2][2], the cosine
+ * and sine of every angle; NULL: no rotation).  Row i of request b is at
+ * position (d_pos ? d_pos[b] : lens[b]) + i of the table (clamped to it,
+ * flagged) and is stored as position lens[b] + i of the cache (dropped and
+ * flagged at max_len and beyond).  Keys are normed and rotated in double and
+ * rounded once to float32 before they are quantised, so their codes do not
+ * depend on the order of a sum.  d_q NULL: no queries (d_q_out is not used);
+ * else d_q_out gets the queries in `dtype` (it may be d_q itself), zeros for
+ * rows that a request does not use.  d_weights (NULL: none): the new
+ * positions' weights of this layer become 0.  R is any number of rows. */
+spade_status spade_kvq_append(const spade_kvq_shape* shape, int layer, void* d_cache, int B, int R, int dtype,
+                              const void* d_q, int64_t q_ld, const void* d_k, int64_t k_ld, const void* d_v,
+                              int64_t v_ld, const float* d_gain_q, const float* d_gain_k, float eps,
+                              const float* d_rope, int rope_len, const int32_t* d_pos, const int32_t* d_lens,
+                              const int32_t* d_rows, void* d_q_out, int64_t q_out_ld, float* d_weights,
+                              uint32_t* d_err, void* stream);
+
+/* Causal attention of R rows per request (1 to 16) over one layer of the cache,
+ * which already holds those rows at positions lens[b] .. lens[b] + R - 1
+ * (spade_kvq_append): row i sees positions 0 .. lens[b] + i,
+ *   out = softmax(scale q . k) v   per query head,
+ * d_q and d_out [B R] rows of n_heads heads in `dtype`; rows that a request
+ * does not use give zeros.  max_keys: the host's bound of lens[b] + rows, in
+ * [R, max_len], or 0 for max_len (a longer request is cut to it and flagged).
+ * d_weights_out (NULL: none): out = in + sum of the probabilities that the
+ * first weight_rows rows in use of request b gave a position, over the query
+ * heads of its K/V head, for the positions below lens[b] + rows; the others are
+ * left as they were.  d_weights_in may be NULL (zeros) or d_weights_out.
+ * Float32 calls keep their queries and the products of probabilities and
+ * scales in 24 bits (three bfloat16 terms); bfloat16 calls round those products
+ * to bfloat16 once.  Sums are float32. */
+spade_status spade_kvq_attend(const spade_kvq_shape* shape, int layer, const void* d_cache, int B, int R, int dtype,
+                              const void* d_q, int64_t q_ld, float scale, const int32_t* d_lens,
+                              const int32_t* d_rows, int max_keys, void* d_out, int64_t out_ld,
+                              const float* d_weights_in, float* d_weights_out, int weight_rows, void* d_workspace,
+                              size_t workspace_bytes, uint32_t* d_err, void* stream);
+
+/* Rows of one layer as the values they stand for: positions start[b] + i (NULL:
+ * i), i < R, as [B][R][n_kv_heads][head_dim] in `dtype`; zeros for rows past
+ * d_rows[b] and for positions outside [0, max_len). */
+spade_status spade_kvq_read(const spade_kvq_shape* shape, int layer, const void* d_cache, int B, int R,
+                            const int32_t* d_start, const int32_t* d_rows, int dtype, void* d_k, void* d_v,
+                            void* stream);
+
+/* Eviction by accumulated attention weight.  Every (layer, request, K/V head)
+ * of a request with more than `budget` positions keeps the last `recent` of
+ * them and, of the others, the budget - recent with the largest weights (ties:
+ * the lower position; NaN counts as larger than any number), closed up in
+ * order; shorter requests keep all.  lens_out[b] = min(lens[b], budget).  The
+ * positions' angles stay what they were, so later rows are appended with
+ * d_pos counting the evicted positions too.
+ * d_kept int32 [n_layers][batch][n_kv_heads][budget] gets the kept positions
+ * of requests 0 .. B - 1, then -1.  The cache goes to d_cache_out of shape_out
+ * (its batch >= B, its max_len >= budget, other fields equal), which is
+ * another buffer, or d_cache itself with the same shape: then in place.
+ * d_weights_out (NULL: none) gets the kept positions' weights, those behind
+ * stay as they were; it may be d_weights if the shapes are the same.
+ * d_lens_out may be d_lens.  0 <= recent <= budget, budget >= 1. */
+spade_status spade_kvq_evict(const spade_kvq_shape* shape, const void* d_cache, const spade_kvq_shape* shape_out,
+                             void* d_cache_out, int B, int budget, int recent, const float* d_weights,
+                             float* d_weights_out, const int32_t* d_lens, int32_t* d_lens_out, int32_t* d_kept,
+                             void* stream);
+
 /* Read and clear the device error word.  Synchronises the stream. */
 spade_status spade_get_device_error(spade_model m, uint32_t* h_flags, void* stream);
 

@@ -11,6 +11,7 @@
 #include <new>
 #include <vector>
 
+#include "kvq.h"
 #include "spade_internal.h"
 
 using namespace spade;
@@ -176,6 +177,40 @@ WsPlan plan_ws(const Dims& D, int max_batch, int max_gamma, int max_len) {
   p.prefill_off = take((kPrefillPack + 1) * 4);
   p.total = off;
   return p;
+}
+
+spade_status check_kvq(const spade_kvq_shape* s) {
+  if (!s) return fail(SPADE_EINVAL, "null shape");
+  if (s->n_layers < 1 || s->batch < 1 || s->n_kv_heads < 1 || s->n_heads < 1 || s->n_heads % s->n_kv_heads != 0)
+    return fail(SPADE_EINVAL, "shape: layers, batch and heads must be positive, n_heads a multiple of n_kv_heads");
+  if (s->head_dim != 64 && s->head_dim != 128) return fail(SPADE_EUNSUPPORTED, "head_dim must be 64 or 128");
+  if (s->max_len < 1 || s->max_len > kKvqMaxLen) return fail(SPADE_ECAPACITY, "max_len must be in [1, %d]", kKvqMaxLen);
+  // every count of heads fits 31 bits, also times the rows of an attention call
+  if ((int64_t)s->n_layers * s->batch > 0x7fffffff / s->n_heads / kKvqMaxRows)
+    return fail(SPADE_ECAPACITY, "too many layers, requests and heads");
+  return SPADE_OK;
+}
+
+spade_status check_kvq_call(const spade_kvq_shape* s, int layer, int B, int dtype) {
+  const spade_status r = check_kvq(s);
+  if (r != SPADE_OK) return r;
+  if (layer < 0 || layer >= s->n_layers) return fail(SPADE_EINVAL, "layer %d out of range", layer);
+  if (B < 1 || B > s->batch) return fail(SPADE_ECAPACITY, "B=%d out of range", B);
+  if (dtype != SPADE_F32 && dtype != SPADE_BF16) return fail(SPADE_EINVAL, "dtype must be SPADE_F32 or SPADE_BF16");
+  return SPADE_OK;
+}
+
+// Rows of `heads` heads, ld elements apart: alignment of the vector accesses.
+bool kvq_rows_ok(const void* p, int64_t ld, int64_t heads, int hd, int dtype) {
+  return ((uintptr_t)p & (dtype == SPADE_F32 ? 15 : 7)) == 0 && ld >= heads * hd && ld % 4 == 0;
+}
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+}
+
+size_t kvq_layer_bytes(const spade_kvq_shape* s) {
+  return (size_t)s->batch * s->n_kv_heads * kvq_head_bytes(s->max_len, s->head_dim);
 }
 
 }  // namespace
@@ -726,6 +761,216 @@ spade_status spade_tile_tiling(int kind, int rows, int n_units, int k, int n_cu,
   *row_tiles = c.rt;
   *panels = c.p;
   *k_splits = c.ks;
+  return SPADE_OK;
+}
+
+size_t spade_kvq_bytes(const spade_kvq_shape* s) {
+  if (check_kvq(s) != SPADE_OK) return 0;
+  return align256(s->n_layers * kvq_layer_bytes(s));
+}
+
+size_t spade_kvq_workspace_bytes(const spade_kvq_shape* s, int max_rows) {
+  if (check_kvq(s) != SPADE_OK) return 0;
+  if (max_rows < 1 || max_rows > kKvqMaxRows) {
+    fail(SPADE_ECAPACITY, "max_rows must be in [1, %d]", kKvqMaxRows);
+    return 0;
+  }
+  size_t ml, lse;
+  const size_t o = kvq_attend_floats(s->batch, s->n_heads, s->n_kv_heads, s->head_dim, s->max_len, max_rows, &ml, &lse);
+  return align256(o * 4) + align256(ml * 4) + align256(lse * 4);
+}
+
+spade_status spade_kvq_append(const spade_kvq_shape* s, int layer, void* d_cache, int B, int R, int dtype,
+                              const void* d_q, int64_t q_ld, const void* d_k, int64_t k_ld, const void* d_v,
+                              int64_t v_ld, const float* d_gain_q, const float* d_gain_k, float eps,
+                              const float* d_rope, int rope_len, const int32_t* d_pos, const int32_t* d_lens,
+                              const int32_t* d_rows, void* d_q_out, int64_t q_out_ld, float* d_weights,
+                              uint32_t* d_err, void* stream) {
+  const spade_status r = check_kvq_call(s, layer, B, dtype);
+  if (r != SPADE_OK) return r;
+  if (!d_cache || !d_k || !d_v || !d_lens || (d_q && !d_q_out)) return fail(SPADE_EINVAL, "null pointer");
+  if (R < 1) return fail(SPADE_EINVAL, "R must be >= 1");
+  const int hd = s->head_dim;
+  if (!kvq_rows_ok(d_k, k_ld, s->n_kv_heads, hd, dtype) || !kvq_rows_ok(d_v, v_ld, s->n_kv_heads, hd, dtype) ||
+      (d_q && (!kvq_rows_ok(d_q, q_ld, s->n_heads, hd, dtype) || !kvq_rows_ok(d_q_out, q_out_ld, s->n_heads, hd, dtype))))
+    return fail(SPADE_EINVAL, "rows: alignment or leading dimension");
+  if ((uintptr_t)d_cache & 255) return fail(SPADE_EINVAL, "the cache must be 256-byte aligned");
+  if (!aligned16(d_gain_q) || !aligned16(d_gain_k) || !aligned16(d_rope))
+    return fail(SPADE_EINVAL, "gains and rope must be 16-byte aligned");
+  if (!(eps >= 0.f && std::isfinite(eps))) return fail(SPADE_EINVAL, "eps must be finite and >= 0");
+  if (d_rope && rope_len < 1) return fail(SPADE_EINVAL, "rope_len must be >= 1");
+  if ((int64_t)B * R > (int64_t)0x7fffffff / (s->n_heads + 2 * s->n_kv_heads))
+    return fail(SPADE_ECAPACITY, "too many rows");
+  KvqAppend a{};
+  a.cache = (uint8_t*)d_cache + layer * kvq_layer_bytes(s);
+  a.head_bytes = kvq_head_bytes(s->max_len, hd);
+  a.B = B;
+  a.R = R;
+  a.H = s->n_heads;
+  a.KVH = s->n_kv_heads;
+  a.hd = hd;
+  a.max_len = s->max_len;
+  a.q = d_q;
+  a.k = d_k;
+  a.v = d_v;
+  a.q_ld = q_ld;
+  a.k_ld = k_ld;
+  a.v_ld = v_ld;
+  a.bf16 = dtype == SPADE_BF16;
+  a.gain_q = d_gain_q;
+  a.gain_k = d_gain_k;
+  a.eps = eps;
+  a.rope = d_rope;
+  a.rope_len = rope_len;
+  a.pos = d_pos;
+  a.lens = d_lens;
+  a.rows = d_rows;
+  a.q_out = d_q_out;
+  a.qo_ld = q_out_ld;
+  a.weights = d_weights;
+  a.err = d_err;
+  const hipError_t e = launch_kvq_append(a, (hipStream_t)stream);
+  if (e != hipSuccess) return hipfail(e, "kvq_append");
+  return SPADE_OK;
+}
+
+spade_status spade_kvq_read(const spade_kvq_shape* s, int layer, const void* d_cache, int B, int R,
+                            const int32_t* d_start, const int32_t* d_rows, int dtype, void* d_k, void* d_v,
+                            void* stream) {
+  const spade_status r = check_kvq_call(s, layer, B, dtype);
+  if (r != SPADE_OK) return r;
+  if (!d_cache || !d_k || !d_v) return fail(SPADE_EINVAL, "null pointer");
+  if (R < 1) return fail(SPADE_EINVAL, "R must be >= 1");
+  if ((uintptr_t)d_cache & 255) return fail(SPADE_EINVAL, "the cache must be 256-byte aligned");
+  if (!aligned16(d_k) || !aligned16(d_v)) return fail(SPADE_EINVAL, "outputs must be 16-byte aligned");
+  if ((int64_t)B * R > (int64_t)0x7fffffff / s->n_kv_heads) return fail(SPADE_ECAPACITY, "too many rows");
+  KvqRead a{};
+  a.cache = (const uint8_t*)d_cache + layer * kvq_layer_bytes(s);
+  a.head_bytes = kvq_head_bytes(s->max_len, s->head_dim);
+  a.B = B;
+  a.R = R;
+  a.KVH = s->n_kv_heads;
+  a.hd = s->head_dim;
+  a.max_len = s->max_len;
+  a.bf16 = dtype == SPADE_BF16;
+  a.start = d_start;
+  a.rows = d_rows;
+  a.k = d_k;
+  a.v = d_v;
+  const hipError_t e = launch_kvq_read(a, (hipStream_t)stream);
+  if (e != hipSuccess) return hipfail(e, "kvq_read");
+  return SPADE_OK;
+}
+
+spade_status spade_kvq_attend(const spade_kvq_shape* s, int layer, const void* d_cache, int B, int R, int dtype,
+                              const void* d_q, int64_t q_ld, float scale, const int32_t* d_lens,
+                              const int32_t* d_rows, int max_keys, void* d_out, int64_t out_ld,
+                              const float* d_weights_in, float* d_weights_out, int weight_rows, void* d_workspace,
+                              size_t workspace_bytes, uint32_t* d_err, void* stream) {
+  const spade_status r = check_kvq_call(s, layer, B, dtype);
+  if (r != SPADE_OK) return r;
+  if (!d_cache || !d_q || !d_out || !d_lens || !d_workspace) return fail(SPADE_EINVAL, "null pointer");
+  if (R < 1 || R > kKvqMaxRows) return fail(SPADE_ECAPACITY, "R must be in [1, %d]", kKvqMaxRows);
+  const int hd = s->head_dim;
+  if (!kvq_rows_ok(d_q, q_ld, s->n_heads, hd, dtype) || !kvq_rows_ok(d_out, out_ld, s->n_heads, hd, dtype))
+    return fail(SPADE_EINVAL, "rows: alignment or leading dimension");
+  if (((uintptr_t)d_cache | (uintptr_t)d_workspace) & 255)
+    return fail(SPADE_EINVAL, "cache and workspace must be 256-byte aligned");
+  if (!(scale > 0.f && std::isfinite(scale))) return fail(SPADE_EINVAL, "scale must be finite and > 0");
+  if (max_keys == 0) max_keys = s->max_len;
+  if (max_keys < R || max_keys > s->max_len) return fail(SPADE_ECAPACITY, "max_keys must be in [R, max_len]");
+  if (d_weights_out && (weight_rows < 0 || weight_rows > R)) return fail(SPADE_EINVAL, "weight_rows must be in [0, R]");
+  if (d_weights_in && !d_weights_out) return fail(SPADE_EINVAL, "weights_in without weights_out");
+  const size_t wb = (size_t)s->batch * s->n_kv_heads * s->max_len * 4;
+  if (d_weights_in && d_weights_in != d_weights_out && overlap(d_weights_in, wb, d_weights_out, wb))
+    return fail(SPADE_EINVAL, "weights_in and weights_out overlap");
+  // the part of the layout that B requests of R rows use
+  size_t ml, lse;
+  const size_t o = kvq_attend_floats(B, s->n_heads, s->n_kv_heads, hd, max_keys, R, &ml, &lse);
+  if (align256(o * 4) + align256(ml * 4) + align256(lse * 4) > workspace_bytes)
+    return fail(SPADE_ECAPACITY, "workspace of %zu bytes is too small", workspace_bytes);
+  KvqAttend a{};
+  a.cache = (const uint8_t*)d_cache + layer * kvq_layer_bytes(s);
+  a.head_bytes = kvq_head_bytes(s->max_len, hd);
+  a.B = B;
+  a.R = R;
+  a.H = s->n_heads;
+  a.KVH = s->n_kv_heads;
+  a.G = s->n_heads / s->n_kv_heads;
+  a.hd = hd;
+  a.max_len = s->max_len;
+  a.q = d_q;
+  a.q_ld = q_ld;
+  a.bf16 = dtype == SPADE_BF16;
+  a.scale = scale;
+  a.lens = d_lens;
+  a.rows = d_rows;
+  a.max_keys = max_keys;
+  a.out = d_out;
+  a.out_ld = out_ld;
+  a.w_in = d_weights_in;
+  a.w_out = d_weights_out;
+  a.w_rows = weight_rows;
+  a.part_o = (float*)d_workspace;
+  a.part_ml = (float*)((uint8_t*)d_workspace + align256(o * 4));
+  a.lse = (float*)((uint8_t*)d_workspace + align256(o * 4) + align256(ml * 4));
+  a.err = d_err;
+  const hipError_t e = launch_kvq_attend(a, (hipStream_t)stream);
+  if (e != hipSuccess) return hipfail(e, "kvq_attend");
+  return SPADE_OK;
+}
+
+spade_status spade_kvq_evict(const spade_kvq_shape* s, const void* d_cache, const spade_kvq_shape* s_out,
+                             void* d_cache_out, int B, int budget, int recent, const float* d_weights,
+                             float* d_weights_out, const int32_t* d_lens, int32_t* d_lens_out, int32_t* d_kept,
+                             void* stream) {
+  spade_status r = check_kvq_call(s, 0, B, SPADE_F32);
+  if (r == SPADE_OK) r = check_kvq_call(s_out, 0, B, SPADE_F32);
+  if (r != SPADE_OK) return r;
+  if (!d_cache || !d_cache_out || !d_weights || !d_lens || !d_lens_out || !d_kept)
+    return fail(SPADE_EINVAL, "null pointer");
+  if (s->n_layers != s_out->n_layers || s->n_heads != s_out->n_heads || s->n_kv_heads != s_out->n_kv_heads ||
+      s->head_dim != s_out->head_dim)
+    return fail(SPADE_EINVAL, "the shapes differ in more than batch and max_len");
+  if (budget < 1 || budget > s_out->max_len) return fail(SPADE_ECAPACITY, "budget must be in [1, max_len of the output]");
+  if (recent < 0 || recent > budget) return fail(SPADE_EINVAL, "recent must be in [0, budget]");
+  if (((uintptr_t)d_cache | (uintptr_t)d_cache_out) & 255) return fail(SPADE_EINVAL, "caches must be 256-byte aligned");
+  const bool same = s->batch == s_out->batch && s->max_len == s_out->max_len;
+  if (d_cache == d_cache_out) {
+    if (!same) return fail(SPADE_EINVAL, "in place the shapes must be the same");
+  } else if (overlap(d_cache, spade_kvq_bytes(s), d_cache_out, spade_kvq_bytes(s_out))) {
+    return fail(SPADE_EINVAL, "the caches overlap");
+  }
+  if (d_weights_out) {
+    const size_t n = (size_t)s->n_layers * s->n_kv_heads * 4;
+    if (d_weights == d_weights_out) {
+      if (!same) return fail(SPADE_EINVAL, "in place the shapes must be the same");
+    } else if (overlap(d_weights, n * s->batch * s->max_len, d_weights_out, n * s_out->batch * s_out->max_len)) {
+      return fail(SPADE_EINVAL, "the weights overlap");
+    }
+  }
+  KvqEvict a{};
+  a.cache = (const uint8_t*)d_cache;
+  a.head_bytes = kvq_head_bytes(s->max_len, s->head_dim);
+  a.out = (uint8_t*)d_cache_out;
+  a.out_head_bytes = kvq_head_bytes(s_out->max_len, s->head_dim);
+  a.L = s->n_layers;
+  a.batch = s->batch;
+  a.B = B;
+  a.KVH = s->n_kv_heads;
+  a.hd = s->head_dim;
+  a.max_len = s->max_len;
+  a.out_batch = s_out->batch;
+  a.out_max_len = s_out->max_len;
+  a.budget = budget;
+  a.recent = recent;
+  a.w = d_weights;
+  a.w_out = d_weights_out;
+  a.lens = d_lens;
+  a.lens_out = d_lens_out;
+  a.kept = d_kept;
+  const hipError_t e = launch_kvq_evict(a, (hipStream_t)stream);
+  if (e != hipSuccess) return hipfail(e, "kvq_evict");
   return SPADE_OK;
 }
 

@@ -1,0 +1,116 @@
+// Internal declarations of the 4-bit K/V cache: its layout and the launchers
+// of its kernels (kvq.hip), shared with the C ABI (api.cpp) and the model's
+// forward (kernels.hip).
+#pragma once
+
+#include "spade_internal.h"
+
+namespace spade {
+
+// A cache row (one position of one K/V head) is x_f = m + n_f s: codes n_f of
+// 4 bits, one scale s and one minimum m (bfloat16) for the keys and one pair
+// for the values.  Positions are stored in blocks of 32, each one contiguous
+// run: the keys' codes, the values' codes, then (key pair, value pair) per
+// position.
+//   keys    position t: head_dim / 2 bytes at t head_dim / 2, feature f in
+//           nibble f % 8 of word f / 8.  Sixteen positions are the A operand of
+//           S^T = K Q^T: lane 16 q + c loads the q-th quarter of position c.
+//   values  word (f / 8) of position t at ((t / 4) (head_dim / 8) + f / 8) 16
+//           + (t % 4) 4: four positions of eight features are one 16-byte
+//           piece, so a lane's load holds four positions (the k index of O^T =
+//           V^T P^T) of its own eight features, and appending a position
+//           writes whole words.
+//   pairs   8 bytes per position: scale and minimum (low and high half) of
+//           the keys, then of the values.
+constexpr int kKvqBlock = 32;
+__host__ __device__ inline uint32_t kvq_block_bytes(int hd) { return (uint32_t)kKvqBlock * (hd + 8); }
+__host__ __device__ inline uint32_t kvq_k_word(int t, int w, int hd) { return (uint32_t)(t * (hd >> 1) + 4 * w); }
+__host__ __device__ inline uint32_t kvq_v_word(int t, int w, int hd) {
+  return (uint32_t)(kKvqBlock * (hd >> 1) + ((t >> 2) * (hd >> 3) + w) * 16 + (t & 3) * 4);
+}
+__host__ __device__ inline uint32_t kvq_pair(int t, int hd) { return (uint32_t)(kKvqBlock * hd + 8 * t); }
+// bytes of one (layer, request, K/V head)
+inline size_t kvq_head_bytes(int max_len, int hd) {
+  return (size_t)((max_len + kKvqBlock - 1) / kKvqBlock) * kvq_block_bytes(hd);
+}
+constexpr int kKvqMaxLen = 1 << 20;
+constexpr int kKvqMaxRows = 16;  // rows per request of one attention call
+
+struct KvqAppend {
+  uint8_t* cache;  // the layer's [batch][KVH] heads
+  size_t head_bytes;
+  int B, R, H, KVH, hd, max_len;
+  // element (request b, row i, head h, feature f) of an input at (b R + i) ld + h hd + f
+  const void* q;
+  const void* k;
+  const void* v;
+  int64_t q_ld, k_ld, v_ld;
+  int bf16;  // inputs and q_out: bfloat16, else float32
+  const float* gain_q;
+  const float* gain_k;
+  float eps;
+  const float* rope;
+  int rope_len;
+  const int32_t* pos;
+  const int32_t* lens;
+  const int32_t* rows;
+  void* q_out;
+  int64_t qo_ld;
+  float* weights;  // the layer's [batch][KVH][max_len], or NULL
+  uint32_t* err;
+};
+hipError_t launch_kvq_append(const KvqAppend& a, hipStream_t st);
+
+struct KvqRead {
+  const uint8_t* cache;
+  size_t head_bytes;
+  int B, R, KVH, hd, max_len, bf16;
+  const int32_t* start;
+  const int32_t* rows;
+  void* k;
+  void* v;
+};
+hipError_t launch_kvq_read(const KvqRead& a, hipStream_t st);
+
+struct KvqAttend {
+  const uint8_t* cache;
+  size_t head_bytes;
+  int B, R, H, KVH, G, hd, max_len;
+  const void* q;
+  int64_t q_ld;
+  int bf16;  // q and out
+  float scale;
+  const int32_t* lens;
+  const int32_t* rows;
+  int max_keys;  // bound of lens + rows
+  void* out;
+  int64_t out_ld;
+  const float* w_in;
+  float* w_out;  // the layer's [batch][KVH][max_len], or NULL
+  int w_rows;
+  float* part_o;   // [B][KVH][NC][G R][hd] chunk partials
+  float* part_ml;  // [B][KVH][NC][G R][2]
+  float* lse;      // [B][KVH][G R]
+  uint32_t* err;
+  // set by the launcher
+  int CK, NC, TG;
+};
+size_t kvq_attend_floats(int B, int H, int KVH, int hd, int max_len, int R, size_t* part_ml, size_t* lse);
+hipError_t launch_kvq_attend(const KvqAttend& a, hipStream_t st);
+
+struct KvqEvict {
+  const uint8_t* cache;
+  size_t head_bytes;
+  uint8_t* out;
+  size_t out_head_bytes;
+  int L, batch, B, KVH, hd, max_len, out_batch, out_max_len;
+  int budget, recent;
+  const float* w;
+  float* w_out;
+  const int32_t* lens;
+  int32_t* lens_out;
+  int32_t* kept;  // [L][batch][KVH][budget]
+};
+hipError_t launch_kvq_evict(const KvqEvict& a, hipStream_t st);
+
+}  // namespace spade

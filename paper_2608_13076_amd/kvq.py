@@ -1,0 +1,192 @@
+"""K/V caches in 4 bits (``spade_kvq_*`` of include/spade.h).
+
+``QuantCache`` owns the buffers of one cache -- the codes, the lengths, the
+attention's workspace and an error word -- and marshals its calls: ``append``
+new rows (head norms, rotation, quantisation), ``attend`` over the cache,
+``evict`` positions by accumulated attention weight and ``read`` rows back.
+Every call runs on the current stream of the cache's device.
+"""
+
+from __future__ import annotations
+
+import ctypes
+import math
+from typing import Optional, Tuple
+
+import torch
+
+from . import spade
+from .spade import BF16, F32, KVQShape, _check, load_library
+
+_DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+def rope_table(n: int, head_dim: int, theta: float = 10000.0, device="cuda:0") -> torch.Tensor:
+    """float32 [n][head_dim / 2][2]: cosine and sine of pos theta^(-2 i /
+    head_dim), the angles in double."""
+    pos = torch.arange(n, dtype=torch.float64, device=device)[:, None]
+    inv = float(theta) ** (-2.0 * torch.arange(head_dim // 2, dtype=torch.float64, device=device) / head_dim)
+    return torch.stack([torch.cos(pos * inv), torch.sin(pos * inv)], -1).float().contiguous()
+
+
+class QuantCache:
+    """A 4-bit K/V cache of ``n_layers`` layers and ``batch`` requests.
+
+    ``lens`` (int32 [batch], on the device) counts the positions each request
+    holds; ``append`` and ``attend`` leave it alone, so a program adds the rows
+    it keeps itself (``cache.lens += n``).  ``max_rows``: most rows per request
+    of an ``attend`` call."""
+
+    def __init__(self, n_layers: int, batch: int, n_heads: int, n_kv_heads: int, head_dim: int, max_len: int,
+                 max_rows: int = 16, device="cuda:0"):
+        self.lib = load_library()
+        self.device = torch.device(device)
+        if self.device.type == "cuda" and self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self.shape = KVQShape(n_layers, batch, n_heads, n_kv_heads, head_dim, max_len)
+        self.n_layers, self.batch, self.n_heads, self.n_kv_heads = n_layers, batch, n_heads, n_kv_heads
+        self.head_dim, self.max_len, self.max_rows = head_dim, max_len, max_rows
+        nbytes = self.lib.spade_kvq_bytes(self._shape())
+        ws = self.lib.spade_kvq_workspace_bytes(self._shape(), max_rows)
+        if nbytes == 0 or ws == 0:
+            raise spade.SpadeError(-1, "cache shape: " + self.lib.spade_last_error().decode())
+        with torch.cuda.device(self.device):
+            self.buf = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+            self.workspace = torch.empty(ws, dtype=torch.uint8, device=self.device)
+            self.lens = torch.zeros(batch, dtype=torch.int32, device=self.device)
+            self.err = torch.zeros(1, dtype=torch.int32, device=self.device)
+
+    def _shape(self):
+        return ctypes.byref(self.shape)
+
+    def _stream(self):
+        return ctypes.c_void_p(torch.cuda.current_stream(self.device).cuda_stream)
+
+    def _arg(self, t: Optional[torch.Tensor], dtype, shape, name: str):
+        """Pointer of a contiguous tensor of this dtype and shape on the cache's device."""
+        if t is None:
+            return None
+        if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != self.device:
+            raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {self.device}")
+        return ctypes.c_void_p(t.data_ptr())
+
+    def _rows(self, t: torch.Tensor, B: int, R: int, heads: int, dtype, name: str):
+        """(pointer, ld) of rows [B, R, heads, head_dim]: contiguous heads, the
+        rows of all requests one stride apart."""
+        if t.dtype != dtype or tuple(t.shape) != (B, R, heads, self.head_dim) or t.device != self.device:
+            raise ValueError(f"{name}: expected {dtype} [{B}, {R}, {heads}, {self.head_dim}] on {self.device}")
+        sb, sr, sh, sf = t.stride()
+        ld = sr if R > 1 else (sb if B > 1 else heads * self.head_dim)
+        if sf != 1 or (heads > 1 and sh != self.head_dim) or (R > 1 and B > 1 and sb != R * sr):
+            raise ValueError(f"{name}: heads must be contiguous and rows one stride apart")
+        return ctypes.c_void_p(t.data_ptr()), ld
+
+    def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None,
+               gain_q: Optional[torch.Tensor] = None, gain_k: Optional[torch.Tensor] = None, eps: float = 1e-5,
+               rope: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None,
+               rows: Optional[torch.Tensor] = None, weights: Optional[torch.Tensor] = None,
+               q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+        """Store rows k, v [B, R, n_kv_heads, head_dim] as positions lens[b] ..
+        lens[b] + R - 1 and return the queries q [B, R, n_heads, head_dim]
+        (q_out where given), normed and rotated like the keys.  ``weights``: the
+        layer's running weights [batch, n_kv_heads, max_len], zeroed for the new
+        positions.  See spade_kvq_append."""
+        B, R = int(k.shape[0]), int(k.shape[1])
+        dt = k.dtype
+        if dt not in _DTYPES:
+            raise ValueError("k: float32 or bfloat16")
+        kp, kld = self._rows(k, B, R, self.n_kv_heads, dt, "k")
+        vp, vld = self._rows(v, B, R, self.n_kv_heads, dt, "v")
+        qp, qld, op, old = None, 0, None, 0
+        if q is not None:
+            qp, qld = self._rows(q, B, R, self.n_heads, dt, "q")
+            if q_out is None:
+                q_out = torch.empty((B, R, self.n_heads, self.head_dim), dtype=dt, device=self.device)
+            op, old = self._rows(q_out, B, R, self.n_heads, dt, "q_out")
+        f32, i32, half = torch.float32, torch.int32, self.head_dim // 2
+        n_rope = 0 if rope is None else int(rope.shape[0])
+        with torch.cuda.device(self.device):
+            _check(self.lib.spade_kvq_append(
+                self._shape(), layer, ctypes.c_void_p(self.buf.data_ptr()), B, R, _DTYPES[dt], qp, qld, kp, kld, vp, vld,
+                self._arg(gain_q, f32, (self.head_dim,), "gain_q"), self._arg(gain_k, f32, (self.head_dim,), "gain_k"),
+                float(eps), self._arg(rope, f32, (n_rope, half, 2), "rope"), n_rope, self._arg(pos, i32, (B,), "pos"),
+                self._arg(self.lens, i32, (self.batch,), "lens"), self._arg(rows, i32, (B,), "rows"), op, old,
+                self._arg(weights, f32, (self.batch, self.n_kv_heads, self.max_len), "weights"),
+                ctypes.c_void_p(self.err.data_ptr()), self._stream()))
+        return q_out
+
+    def attend(self, layer: int, q: torch.Tensor, out: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+               rows: Optional[torch.Tensor] = None, max_keys: int = 0, weights: Optional[torch.Tensor] = None,
+               weights_out: Optional[torch.Tensor] = None, weight_rows: int = 0) -> torch.Tensor:
+        """Causal attention of q [B, R, n_heads, head_dim], whose rows ``append``
+        has stored, over the layer; returns out (same shape and dtype).  scale:
+        1 / sqrt(head_dim) unless given.  max_keys: the host's bound of lens +
+        rows (0: max_len).  weights_out = weights + the probabilities of the
+        first weight_rows rows, both [batch, n_kv_heads, max_len] (may be one
+        tensor).  See spade_kvq_attend."""
+        B, R = int(q.shape[0]), int(q.shape[1])
+        dt = q.dtype
+        if dt not in _DTYPES:
+            raise ValueError("q: float32 or bfloat16")
+        qp, qld = self._rows(q, B, R, self.n_heads, dt, "q")
+        if out is None:
+            out = torch.empty((B, R, self.n_heads, self.head_dim), dtype=dt, device=self.device)
+        op, old = self._rows(out, B, R, self.n_heads, dt, "out")
+        f32, i32 = torch.float32, torch.int32
+        ws = (self.batch, self.n_kv_heads, self.max_len)
+        with torch.cuda.device(self.device):
+            _check(self.lib.spade_kvq_attend(
+                self._shape(), layer, ctypes.c_void_p(self.buf.data_ptr()), B, R, _DTYPES[dt], qp, qld,
+                1.0 / math.sqrt(self.head_dim) if scale is None else float(scale),
+                self._arg(self.lens, i32, (self.batch,), "lens"), self._arg(rows, i32, (B,), "rows"), int(max_keys), op,
+                old, self._arg(weights, f32, ws, "weights"), self._arg(weights_out, f32, ws, "weights_out"),
+                int(weight_rows), ctypes.c_void_p(self.workspace.data_ptr()), self.workspace.numel(),
+                ctypes.c_void_p(self.err.data_ptr()), self._stream()))
+        return out
+
+    def read(self, layer: int, n: int, start: Optional[torch.Tensor] = None, rows: Optional[torch.Tensor] = None,
+             dtype: torch.dtype = torch.float32) -> Tuple[torch.Tensor, torch.Tensor]:
+        """Keys and values [batch, n, n_kv_heads, head_dim] of positions start[b]
+        (0) .. + n - 1 as they are held; zeros past rows[b].  See spade_kvq_read."""
+        if dtype not in _DTYPES:
+            raise ValueError("dtype: float32 or bfloat16")
+        k = torch.empty((self.batch, n, self.n_kv_heads, self.head_dim), dtype=dtype, device=self.device)
+        v = torch.empty_like(k)
+        i32 = torch.int32
+        with torch.cuda.device(self.device):
+            _check(self.lib.spade_kvq_read(
+                self._shape(), layer, ctypes.c_void_p(self.buf.data_ptr()), self.batch, n,
+                self._arg(start, i32, (self.batch,), "start"), self._arg(rows, i32, (self.batch,), "rows"), _DTYPES[dtype],
+                ctypes.c_void_p(k.data_ptr()), ctypes.c_void_p(v.data_ptr()), self._stream()))
+        return k, v
+
+    def evict(self, weights: torch.Tensor, budget: int, recent: int, kept: Optional[torch.Tensor] = None,
+              into: Optional["QuantCache"] = None, weights_out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Keep, per layer, request and K/V head, the last ``recent`` positions
+        and the heaviest others, ``budget`` in all; in place, or into another
+        cache of the same layers and heads, whose lens become the new ones.
+        weights [n_layers, batch, n_kv_heads, max_len]; weights_out likewise
+        with the other cache's sizes (may be weights in place).  Returns kept
+        int32 [n_layers, batch, n_kv_heads, budget].  See spade_kvq_evict."""
+        dst = self if into is None else into
+        if dst.device != self.device:
+            raise ValueError("the caches are on different devices")
+        i32, f32 = torch.int32, torch.float32
+        kshape = (self.n_layers, self.batch, self.n_kv_heads, budget)
+        if kept is None:
+            kept = torch.empty(tuple(max(int(x), 0) for x in kshape), dtype=i32, device=self.device)
+        with torch.cuda.device(self.device):
+            _check(self.lib.spade_kvq_evict(
+                self._shape(), ctypes.c_void_p(self.buf.data_ptr()), dst._shape(), ctypes.c_void_p(dst.buf.data_ptr()),
+                self.batch, int(budget), int(recent),
+                self._arg(weights, f32, (self.n_layers, self.batch, self.n_kv_heads, self.max_len), "weights"),
+                dst._arg(weights_out, f32, (dst.n_layers, dst.batch, dst.n_kv_heads, dst.max_len), "weights_out"),
+                self._arg(self.lens, i32, (self.batch,), "lens"), dst._arg(dst.lens, i32, (dst.batch,), "lens"),
+                self._arg(kept, i32, kshape, "kept"), self._stream()))
+        return kept
+
+    def device_error(self) -> int:
+        """Read and clear the error word (synchronises)."""
+        v = int(self.err.item())
+        self.err.zero_()
+        return v

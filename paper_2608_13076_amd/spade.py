@@ -25,7 +25,7 @@ KINDS = {"wq": 0, "wk": 1, "wv": 2, "wo": 3, "wg": 4, "wu": 5, "wd": 6,
 GLOBAL_KINDS = ("embed", "g_final", "lm_head")
 DERR_TOKEN, DERR_NAN, DERR_RESIDUAL, DERR_NOQ, DERR_CAPACITY, DERR_COMMIT = 1, 2, 4, 8, 16, 32
 
-# include/spade.h: the calls of the method
+# include/spade.h: the calls of the method and of 4-bit caches
 EXPORTED = (
     "spade_weight_bytes", "spade_workspace_bytes", "spade_kv_bytes", "spade_model_create",
     "spade_model_load_tensor", "spade_kv_create", "spade_kv_set_state", "spade_kv_get_state",
@@ -33,6 +33,8 @@ EXPORTED = (
     "spade_accept_from_logits", "spade_get_device_error", "spade_last_error",
     "spade_model_destroy", "spade_kv_destroy", "spade_softmax", "spade_prefill_batch",
     "spade_accept_from_logits_noalloc",
+    "spade_kvq_bytes", "spade_kvq_workspace_bytes", "spade_kvq_append", "spade_kvq_read", "spade_kvq_attend",
+    "spade_kvq_evict",
 )
 # include/spade_tuning.h: schedule controls and measurement hooks
 EXPORTED_TUNING = (
@@ -58,6 +60,11 @@ class SpadeConfig(ctypes.Structure):
                 ("n_kv_heads", ctypes.c_int32)]
 
 
+class KVQShape(ctypes.Structure):
+    _fields_ = [("n_layers", ctypes.c_int32), ("batch", ctypes.c_int32), ("n_heads", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("max_len", ctypes.c_int32)]
+
+
 def config_from(shape) -> SpadeConfig:
     """spade_config from any object with the ModelShape attributes."""
     return SpadeConfig(shape.n_layers, shape.d_model, shape.n_heads, shape.head_dim, shape.d_ffn,
@@ -68,6 +75,7 @@ def config_from(shape) -> SpadeConfig:
 
 _LIB = None
 P, I, SZ, F = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_float
+L64 = ctypes.c_int64
 
 
 def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
@@ -79,6 +87,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
                            "(there is no CPU fallback)")
     lib = ctypes.CDLL(path)
     cfgp = ctypes.POINTER(SpadeConfig)
+    kvqp = ctypes.POINTER(KVQShape)
     sig = {
         "spade_weight_bytes": (SZ, [cfgp]),
         "spade_workspace_bytes": (SZ, [cfgp, I, I, I]),
@@ -112,6 +121,12 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "spade_wide_tiling": (I, [I, I, I, I, I, P, P, P]),
         "spade_tile_tiling": (I, [I, I, I, I, I, P, P, P]),
         "spade_model_gemm_engine": (I, [P, I, I, P]),
+        "spade_kvq_bytes": (SZ, [kvqp]),
+        "spade_kvq_workspace_bytes": (SZ, [kvqp, I]),
+        "spade_kvq_append": (I, [kvqp, I, P, I, I, I, P, L64, P, L64, P, L64, P, P, F, P, I, P, P, P, P, L64, P, P, P]),
+        "spade_kvq_read": (I, [kvqp, I, P, I, I, P, P, I, P, P, P]),
+        "spade_kvq_attend": (I, [kvqp, I, P, I, I, I, P, L64, F, P, P, I, P, L64, P, P, I, P, SZ, P, P]),
+        "spade_kvq_evict": (I, [kvqp, P, kvqp, P, I, I, I, P, P, P, P, P, P]),
         "spade_last_error": (ctypes.c_char_p, []),
         "spade_model_destroy": (None, [P]),
         "spade_kv_destroy": (None, [P]),

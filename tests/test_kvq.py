@@ -1,0 +1,163 @@
+"""4-bit K/V caches without a GPU: buffer sizes, refusals on the host, and the
+oracle's own rows (every row within half a step of its values)."""
+
+import ctypes
+
+import numpy as np
+import pytest
+
+from oracle import kvq as okvq
+from paper_2608_13076_amd import spade
+
+OK, EINVAL, ECAP, EUNSUP = 0, -1, -2, -4
+PTR = 1 << 20  # an aligned address that no refused call touches
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return spade.load_library()
+
+
+def shape(**kw):
+    d = dict(n_layers=2, batch=3, n_heads=8, n_kv_heads=2, head_dim=128, max_len=1000)
+    d.update(kw)
+    return spade.KVQShape(*(d[k] for k in ("n_layers", "batch", "n_heads", "n_kv_heads", "head_dim", "max_len")))
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("max_len", [1, 31, 32, 33, 1000, 1 << 20])
+def test_sizes(lib, hd, max_len):
+    s = shape(head_dim=hd, max_len=max_len)
+    n = lib.spade_kvq_bytes(ctypes.byref(s))
+    rows = 2 * 3 * 2 * max_len
+    assert rows * (hd + 8) <= n <= (rows + 2 * 3 * 2 * 31) * (hd + 8) + 255
+    assert n % 256 == 0
+    w = [lib.spade_kvq_workspace_bytes(ctypes.byref(s), r) for r in (1, 16)]
+    assert 0 < w[0] <= w[1]
+    assert lib.spade_kvq_workspace_bytes(ctypes.byref(s), 0) == 0
+    assert lib.spade_kvq_workspace_bytes(ctypes.byref(s), 17) == 0
+
+
+@pytest.mark.parametrize("kw", [dict(n_layers=0), dict(batch=0), dict(n_heads=0), dict(n_kv_heads=0),
+                                dict(n_kv_heads=3), dict(head_dim=96), dict(head_dim=256), dict(max_len=0),
+                                dict(max_len=(1 << 20) + 1), dict(batch=1 << 20, n_layers=1 << 10), dict(batch=-1)])
+def test_bad_shapes(lib, kw):
+    s = shape(**kw)
+    assert lib.spade_kvq_bytes(ctypes.byref(s)) == 0
+    assert lib.spade_kvq_workspace_bytes(ctypes.byref(s), 1) == 0
+    assert lib.spade_last_error().decode()
+
+
+def call_append(lib, s=None, **kw):
+    d = dict(layer=0, cache=PTR, B=3, R=2, dtype=1, q=PTR, q_ld=1024, k=PTR, k_ld=256, v=PTR, v_ld=256, gq=None, gk=None,
+             eps=1e-5, rope=None, n_rope=0, pos=None, lens=PTR, rows=None, qo=PTR, qo_ld=1024, w=None, err=None)
+    d.update(kw)
+    s = s or shape()
+    return lib.spade_kvq_append(ctypes.byref(s) if s != "null" else None, d["layer"], d["cache"], d["B"], d["R"],
+                                d["dtype"], d["q"], d["q_ld"], d["k"], d["k_ld"], d["v"], d["v_ld"], d["gq"], d["gk"],
+                                d["eps"], d["rope"], d["n_rope"], d["pos"], d["lens"], d["rows"], d["qo"], d["qo_ld"],
+                                d["w"], d["err"], None)
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(s="null"), EINVAL), (dict(layer=2), EINVAL), (dict(layer=-1), EINVAL), (dict(B=0), ECAP), (dict(B=4), ECAP),
+    (dict(R=0), EINVAL), (dict(dtype=2), EINVAL), (dict(cache=None), EINVAL), (dict(k=None), EINVAL), (dict(v=None), EINVAL),
+    (dict(lens=None), EINVAL), (dict(qo=None), EINVAL), (dict(q_ld=1020), EINVAL), (dict(k_ld=258), EINVAL),
+    (dict(v_ld=252), EINVAL), (dict(k=PTR + 4), EINVAL), (dict(dtype=0, v=PTR + 8), EINVAL), (dict(qo_ld=1022), EINVAL),
+    (dict(cache=PTR + 16), EINVAL), (dict(gq=PTR + 4), EINVAL), (dict(rope=PTR + 8, n_rope=4), EINVAL),
+    (dict(rope=PTR, n_rope=0), EINVAL), (dict(eps=-1.0), EINVAL), (dict(eps=float("nan")), EINVAL),
+    (dict(R=1 << 30), ECAP),
+])
+def test_append_refuses(lib, kw, want):
+    assert call_append(lib, **kw) == want
+    assert lib.spade_last_error().decode()
+
+
+def call_attend(lib, s=None, **kw):
+    d = dict(layer=0, cache=PTR, B=3, R=2, dtype=1, q=PTR, q_ld=1024, scale=0.1, lens=PTR, rows=None, max_keys=0, out=PTR,
+             out_ld=1024, wi=None, wo=None, wr=0, ws=PTR, wsb=1 << 30, err=None)
+    d.update(kw)
+    s = s or shape()
+    return lib.spade_kvq_attend(ctypes.byref(s) if s != "null" else None, d["layer"], d["cache"], d["B"], d["R"],
+                                d["dtype"], d["q"], d["q_ld"], d["scale"], d["lens"], d["rows"], d["max_keys"], d["out"],
+                                d["out_ld"], d["wi"], d["wo"], d["wr"], d["ws"], d["wsb"], d["err"], None)
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(s="null"), EINVAL), (dict(layer=2), EINVAL), (dict(B=0), ECAP), (dict(B=4), ECAP), (dict(R=0), ECAP),
+    (dict(R=17), ECAP), (dict(dtype=5), EINVAL), (dict(cache=None), EINVAL), (dict(q=None), EINVAL), (dict(out=None), EINVAL),
+    (dict(lens=None), EINVAL), (dict(ws=None), EINVAL), (dict(q_ld=512), EINVAL), (dict(out=PTR + 4), EINVAL),
+    (dict(cache=PTR + 128), EINVAL), (dict(ws=PTR + 64), EINVAL), (dict(scale=0.0), EINVAL), (dict(scale=-1.0), EINVAL),
+    (dict(scale=float("inf")), EINVAL), (dict(max_keys=1), ECAP), (dict(max_keys=1001), ECAP), (dict(wo=PTR, wr=3), EINVAL),
+    (dict(wo=PTR, wr=-1), EINVAL), (dict(wi=PTR), EINVAL), (dict(wi=PTR, wo=PTR + 4096), EINVAL), (dict(wsb=0), ECAP),
+])
+def test_attend_refuses(lib, kw, want):
+    assert call_attend(lib, **kw) == want
+    assert lib.spade_last_error().decode()
+
+
+def test_attend_refuses_a_small_workspace(lib):
+    s = shape()
+    one = lib.spade_kvq_workspace_bytes(ctypes.byref(s), 1)
+    assert call_attend(lib, R=16, wsb=one) == ECAP
+
+
+def call_read(lib, **kw):
+    d = dict(layer=0, cache=PTR, B=3, R=2, start=None, rows=None, dtype=0, k=PTR, v=PTR)
+    d.update(kw)
+    s = shape()
+    return lib.spade_kvq_read(ctypes.byref(s), d["layer"], d["cache"], d["B"], d["R"], d["start"], d["rows"], d["dtype"],
+                              d["k"], d["v"], None)
+
+
+@pytest.mark.parametrize("kw,want", [(dict(layer=9), EINVAL), (dict(B=0), ECAP), (dict(R=0), EINVAL), (dict(k=None), EINVAL),
+                                     (dict(v=PTR + 8), EINVAL), (dict(dtype=-1), EINVAL), (dict(cache=None), EINVAL),
+                                     (dict(R=1 << 30), ECAP)])
+def test_read_refuses(lib, kw, want):
+    assert call_read(lib, **kw) == want
+
+
+def call_evict(lib, s=None, so=None, **kw):
+    d = dict(cache=PTR, out=1 << 30, B=3, budget=100, recent=10, w=1 << 32, wo=None, lens=PTR, lo=PTR, kept=PTR)
+    d.update(kw)
+    s, so = s or shape(), so or shape()
+    return lib.spade_kvq_evict(ctypes.byref(s), d["cache"], ctypes.byref(so) if so != "null" else None, d["out"], d["B"],
+                               d["budget"], d["recent"], d["w"], d["wo"], d["lens"], d["lo"], d["kept"], None)
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(so="null"), EINVAL), (dict(so=shape(n_layers=1)), EINVAL), (dict(so=shape(head_dim=64)), EINVAL),
+    (dict(so=shape(n_kv_heads=4)), EINVAL), (dict(so=shape(batch=2)), ECAP), (dict(so=shape(max_len=99)), ECAP),
+    (dict(cache=None), EINVAL), (dict(out=None), EINVAL), (dict(w=None), EINVAL), (dict(lens=None), EINVAL),
+    (dict(lo=None), EINVAL), (dict(kept=None), EINVAL), (dict(budget=0), ECAP), (dict(budget=1001), ECAP),
+    (dict(recent=-1), EINVAL), (dict(recent=101), EINVAL), (dict(B=4), ECAP), (dict(out=PTR + 256), EINVAL),
+    (dict(out=PTR, so=shape(max_len=500)), EINVAL), (dict(wo=1 << 32, so=shape(max_len=500)), EINVAL),
+    (dict(wo=(1 << 32) + 64), EINVAL), (dict(out=(1 << 30) + 8), EINVAL),
+])
+def test_evict_refuses(lib, kw, want):
+    assert call_evict(lib, **kw) == want
+    assert lib.spade_last_error().decode()
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_oracle_rows_are_near_their_values(hd):
+    """A code is at most half a step off, the ends by what the minimum's and
+    the scale's rounding to bfloat16 (2^-8 of |m| + 15 s) moves them."""
+    rng = np.random.default_rng(1)
+    x = rng.normal(size=(200, hd)).astype(np.float32) * np.exp(rng.normal(size=(200, 1)) * 3)
+    n, s, m = okvq.codes(x)
+    assert n.min() == 0 and n.max() == 15
+    off = np.abs(okvq.held(x) - x)
+    assert (off <= s / 2 + 2.0 ** -8 * (np.abs(m) + 15 * s)).all()
+    assert (okvq.held(np.full((1, hd), 2.5)) == 2.5).all()
+    y = x[:2].copy()
+    y[0, 3] = np.inf
+    assert np.isnan(okvq.held(y)[0]).all() and np.isfinite(okvq.held(y)[1]).all()
+
+
+def test_oracle_keep():
+    w = np.array([1, 0, 3, 3, 0, 2, np.nan, 3, 9], np.float32)
+    assert okvq.keep(w, 9, 4, 1).tolist() == [2, 3, 6, 8]
+    assert okvq.keep(w, 9, 4, 4).tolist() == [5, 6, 7, 8]
+    assert okvq.keep(w, 9, 9, 1).tolist() == list(range(9))
+    assert okvq.keep(np.zeros(6, np.float32), 6, 3, 0).tolist() == [0, 1, 2]

@@ -776,7 +776,7 @@ size_t spade_kvq_workspace_bytes(const spade_kvq_shape* s, int max_rows) {
     return 0;
   }
   size_t ml, lse;
-  const size_t o = kvq_attend_floats(s->batch, s->n_heads, s->n_kv_heads, s->head_dim, s->max_len, max_rows, &ml, &lse);
+  const size_t o = kvq_attend_floats(s->batch, s->n_heads, s->n_kv_heads, s->head_dim, max_rows, &ml, &lse);
   return align256(o * 4) + align256(ml * 4) + align256(lse * 4);
 }
 
@@ -886,7 +886,7 @@ spade_status spade_kvq_attend(const spade_kvq_shape* s, int layer, const void* d
     return fail(SPADE_EINVAL, "weights_in and weights_out overlap");
   // the part of the layout that B requests of R rows use
   size_t ml, lse;
-  const size_t o = kvq_attend_floats(B, s->n_heads, s->n_kv_heads, hd, max_keys, R, &ml, &lse);
+  const size_t o = kvq_attend_floats(B, s->n_heads, s->n_kv_heads, hd, R, &ml, &lse);
   if (align256(o * 4) + align256(ml * 4) + align256(lse * 4) > workspace_bytes)
     return fail(SPADE_ECAPACITY, "workspace of %zu bytes is too small", workspace_bytes);
   KvqAttend a{};
@@ -912,6 +912,7 @@ spade_status spade_kvq_attend(const spade_kvq_shape* s, int layer, const void* d
   a.w_out = d_weights_out;
   a.w_rows = weight_rows;
   a.part_o = (float*)d_workspace;
+  a.part_rows = o / hd;
   a.part_ml = (float*)((uint8_t*)d_workspace + align256(o * 4));
   a.lse = (float*)((uint8_t*)d_workspace + align256(o * 4) + align256(ml * 4));
   a.err = d_err;

@@ -88,14 +88,16 @@ struct KvqAttend {
   const float* w_in;
   float* w_out;  // the layer's [batch][KVH][max_len], or NULL
   int w_rows;
-  float* part_o;   // [B][KVH][NC][G R][hd] chunk partials
-  float* part_ml;  // [B][KVH][NC][G R][2]
+  float* part_o;   // [slot][G R][hd] segments' partials
+  float* part_ml;  // [slot][G R][2]
   float* lse;      // [B][KVH][G R]
+  size_t part_rows;  // rows that part_o holds
   uint32_t* err;
   // set by the launcher
-  int CK, NC, TG;
+  int WG;  // ranges (0: a head per workgroup)
+  int TG;  // 16-row tiles of a K/V head's rows
 };
-size_t kvq_attend_floats(int B, int H, int KVH, int hd, int max_len, int R, size_t* part_ml, size_t* lse);
+size_t kvq_attend_floats(int B, int H, int KVH, int hd, int R, size_t* part_ml, size_t* lse);
 hipError_t launch_kvq_attend(const KvqAttend& a, hipStream_t st);
 
 struct KvqEvict {

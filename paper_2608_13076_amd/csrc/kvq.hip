@@ -112,6 +112,17 @@ __device__ __forceinline__ void norm_rotate(F (&x)[8], const float* g, float eps
   }
 }
 
+// The integer nearest to (v - m) / s, ties to even, by its exact remainder.
+__device__ __noinline__ float exact_code(float v, float m, float s) {
+  const double ds = s, d = (double)v - (double)m;
+  double n = rint(d / ds);
+  const double e = __builtin_fma(-n, ds, d), h = 0.5 * ds;
+  const bool odd = fmod(n, 2.0) != 0.0;
+  if (e > h || (e == h && odd)) n += 1.0;
+  else if (e < -h || (e == -h && odd)) n -= 1.0;
+  return (float)fmin(fmax(n, -1.0), 16.0);
+}
+
 // Codes of a lane's features: nibbles 0..3 of word c / 2 (even lanes' half) in
 // the low half, those of the partners in the high half; pair = scale | minimum.
 template <int HD>
@@ -133,17 +144,14 @@ __device__ __forceinline__ uint32_t quantise(const float (&v)[8], uint32_t* pair
   const float s = bf2f(sb);
   uint32_t code = 0;
   if (bad == 0.f && s > 0.f) {
-    const double ds = s, inv = 1.0 / ds;
+    const float inv = 1.0f / s;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const double d = (double)v[j] - (double)m;
-      double n = rint(d * inv);
-      // exact remainder: the nearest integer, ties to even
-      const double e = __builtin_fma(-n, ds, d), h = 0.5 * ds;
-      const bool odd = ((int)n) & 1;
-      if (e > h || (e == h && odd)) n += 1.0;
-      else if (e < -h || (e == -h && odd)) n -= 1.0;
-      const int ni = (int)fmin(fmax(n, 0.0), 15.0);
+      // three roundings of 2^-24 of a quotient below 17: within 4e-6
+      const float t = (v[j] - m) * inv;
+      float n = rintf(t);
+      if (fabsf(fabsf(t - n) - 0.5f) < 1e-5f || !(t < 17.f)) n = exact_code(v[j], m, s);
+      const int ni = (int)fminf(fmaxf(n, 0.f), 15.f);
       code |= (uint32_t)ni << (j < 4 ? 4 * j : 16 + 4 * (j - 4));
     }
   }
@@ -157,12 +165,10 @@ __global__ void __launch_bounds__(256) kvq_append_kernel(KvqAppend p) {
   const int c = threadIdx.x % LPH;
   const int HQ = p.q != nullptr ? p.H : 0;
   const int heads = HQ + 2 * p.KVH;
-  const int64_t items = (int64_t)p.B * p.R * heads;
-  const int64_t it = (int64_t)blockIdx.x * (256 / LPH) + threadIdx.x / LPH;
-  if (it >= items) return;  // whole groups of LPH lanes
-  const int64_t row = it / heads;
-  int h = (int)(it - row * heads);
-  const int b = (int)(row / p.R), i = (int)(row - (int64_t)b * p.R);
+  int h = (int)blockIdx.y * (256 / LPH) + threadIdx.x / LPH;
+  if (h >= heads) return;  // whole groups of LPH lanes
+  const int64_t row = blockIdx.x;
+  const int b = (int)blockIdx.x / p.R, i = (int)blockIdx.x - b * p.R;
   const int n_rows = p.rows != nullptr ? min(p.rows[b], p.R) : p.R;
   const int f0 = 4 * c, f1 = HD / 2 + 4 * c;
   if (i >= n_rows) {  // a row the request does not use
@@ -237,12 +243,12 @@ template <int HD, bool BF16>
 __global__ void __launch_bounds__(256) kvq_read_kernel(KvqRead p) {
   constexpr int LPH = HD / 8;
   const int c = threadIdx.x % LPH;
-  const int64_t items = (int64_t)p.B * p.R * p.KVH;
-  const int64_t it = (int64_t)blockIdx.x * (256 / LPH) + threadIdx.x / LPH;
+  const unsigned items = (unsigned)p.B * p.R * p.KVH;
+  const unsigned it = blockIdx.x * (256 / LPH) + threadIdx.x / LPH;
   if (it >= items) return;
-  const int64_t row = it / p.KVH;
+  const unsigned row = it / (unsigned)p.KVH;
   const int h = (int)(it - row * p.KVH);
-  const int b = (int)(row / p.R), i = (int)(row - (int64_t)b * p.R);
+  const int b = (int)(row / (unsigned)p.R), i = (int)(row - (unsigned)b * p.R);
   const int n_rows = p.rows != nullptr ? min(p.rows[b], p.R) : p.R;
   const int t = (p.start != nullptr ? p.start[b] : 0) + i;
   const bool live = i < n_rows && t >= 0 && t < p.max_len;
@@ -261,7 +267,7 @@ __global__ void __launch_bounds__(256) kvq_read_kernel(KvqRead p) {
       for (int j = 0; j < 8; ++j) x[o][j] = m + (float)((w[o] >> (4 * j)) & 15u) * s;
     }
   }
-  const int64_t at = it * HD + 8 * c;
+  const int64_t at = (int64_t)it * HD + 8 * c;
   store4<BF16>(p.k, at, x[0]);
   store4<BF16>(p.k, at + 4, x[0] + 4);
   store4<BF16>(p.v, at, x[1]);
@@ -296,14 +302,22 @@ constexpr int kWaves = 4;
 constexpr float kLog2e = 1.4426950408889634f;
 
 __device__ __forceinline__ uint32_t pk_bf16(float a, float b) {
-  return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)a) | ((uint32_t)__builtin_bit_cast(uint16_t, (__bf16)b) << 16);
+  typedef __attribute__((ext_vector_type(2))) float f2;
+  typedef __attribute__((ext_vector_type(2))) __bf16 b2;
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2){a, b}, b2));  // one v_cvt_pk_bf16_f32
 }
 __device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_f(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
-// the codes at bits 3..6 and 19..22 of x as the bf16 pair (16 + n, 16 + n')
-__device__ __forceinline__ uint32_t code16(uint32_t x) { return (x & 0x00780078u) | 0x41804180u; }
-__device__ __forceinline__ uint32_t code_pair(uint32_t w, int j) { return code16(j == 0 ? w << 3 : w >> (4 * j - 3)); }
+// Codes j and j + 4 of a word as the bf16 pair (16 + n, 16 + n'): n goes to bits
+// 3..6 of the mantissa of 16.  One and-or takes both constants from registers
+// (the compiler would emit two instructions with a literal each).
+__device__ __forceinline__ uint32_t code_pair(uint32_t w, int j) {
+  const uint32_t x = j == 0 ? w << 3 : w >> (4 * j - 3);
+  uint32_t r;
+  asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "s"(0x00780078u), "v"(0x41804180u));
+  return r;
+}
 
 __device__ __forceinline__ bf16x8 op(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   return __builtin_bit_cast(bf16x8, make_uint4(a, b, c, d));
@@ -337,6 +351,41 @@ __device__ __forceinline__ float sum_q(float v) {
   return __uint_as_float(t[0]) + __uint_as_float(t[1]);
 }
 
+// A lane's quarter of a query as loaded (nothing waits for it before get).
+template <int HD, bool QB>
+struct RawQuery {
+  static constexpr int V = HD / 32 * (QB ? 1 : 2);  // 16-byte (QB: eight-feature) pieces
+  uint4 v[V];
+  __device__ __forceinline__ void load(const void* base, int64_t at, int q) {
+    if constexpr (QB) {
+      const uint16_t* p = (const uint16_t*)base + at + q * (HD / 4);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {  // (rows are aligned to 8 bytes)
+        const uint2 a = *(const uint2*)(p + 8 * i), b = *(const uint2*)(p + 8 * i + 4);
+        v[i] = make_uint4(a.x, a.y, b.x, b.y);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] = *(const uint4*)((const float*)base + at + q * (HD / 4) + 4 * i);
+    }
+  }
+  __device__ __forceinline__ void get(int s, float (&x)[8]) const {
+    if constexpr (QB) {
+      const uint32_t w[4] = {v[s].x, v[s].y, v[s].z, v[s].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        x[2 * j] = lo_f(w[j]);
+        x[2 * j + 1] = hi_f(w[j]);
+      }
+    } else {
+      const uint4 a = v[2 * s], b = v[2 * s + 1];
+      const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(w[j]);
+    }
+  }
+};
+
 // Queries of one row in a lane: its quarter of the features (HD / 4 from q HD / 4
 // on), as the B operands of the HD / 32 steps; dword j of step s holds
 // features 8 s + j and 8 s + j + 4 of the quarter, the order of a code word.
@@ -345,23 +394,20 @@ struct Queries {
   static constexpr int S = HD / 32, N = QB ? 1 : 3;
   uint32_t w[N][S][4];
   float sum;  // of the row's features
-  __device__ __forceinline__ void load(const void* base, int64_t at, bool ok, int q) {
-    float x[8], t = 0.f;
+  __device__ __forceinline__ void convert(const RawQuery<HD, QB>& raw, bool ok) {
+    float t = 0.f;
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = 0.f;
-      if (ok) {
-        load4<QB>(base, at + q * (HD / 4) + 8 * s, x);
-        load4<QB>(base, at + q * (HD / 4) + 8 * s + 4, x + 4);
-      }
+      float x[8];
+      raw.get(s, x);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
+        const float a = ok ? x[j] : 0.f, b = ok ? x[j + 4] : 0.f;
         uint32_t e[N];
-        terms<N>(x[j], x[j + 4], e);
+        terms<N>(a, b, e);
 #pragma unroll
         for (int n = 0; n < N; ++n) w[n][s][j] = e[n];
-        t += x[j] + x[j + 4];
+        t += a + b;
       }
     }
     sum = sum_q(t);
@@ -377,71 +423,86 @@ struct Block {
   uint4 pr[2][2];  // (key pair, value pair) of positions 16 u + 4 q .. + 3
 };
 
+// Loads of block `blk` of a head (r: its region, nt policy: every block is read
+// by one workgroup or by the tile groups of one XCD).
 template <int HD>
-__device__ __forceinline__ void load_keys(Block<HD>& b, const uint8_t* blk, int q, int c) {
-#pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const uint8_t* p = blk + (16 * u + c) * (HD / 2) + q * (HD / 8);
-    if constexpr (HD == 128) {
-      const uint4 w = *(const uint4*)p;
-      b.k[u][0] = w.x;
-      b.k[u][1] = w.y;
-      b.k[u][2] = w.z;
-      b.k[u][3] = w.w;
-    } else {
-      const uint2 w = *(const uint2*)p;
-      b.k[u][0] = w.x;
-      b.k[u][1] = w.y;
-    }
-    const uint4* pr = (const uint4*)(blk + kvq_pair(16 * u + 4 * q, HD));
-    b.pr[u][0] = pr[0];
-    b.pr[u][1] = pr[1];
+struct BlockLoader {
+  Rsrc r;
+  uint32_t k, v, pr;  // the lane's offsets
+  __device__ __forceinline__ void init(const uint8_t* head, size_t bytes, int q, int c) {
+    r = make_rsrc(head, (uint32_t)bytes);
+    k = (uint32_t)(c * (HD / 2) + q * (HD / 8));
+    v = kvq_v_word(4 * q, HD == 128 ? c : c / 2, HD);
+    pr = kvq_pair(4 * q, HD);
   }
-}
-
-template <int HD>
-__device__ __forceinline__ void load_values(Block<HD>& b, const uint8_t* blk, int q, int c) {
+  __device__ __forceinline__ uint4 b128(uint32_t off, uint32_t so) const {
+    return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, (int)so, kAuxStream));
+  }
+  __device__ __forceinline__ void keys(Block<HD>& b, int blk) const {
+    const uint32_t so = (uint32_t)blk * kvq_block_bytes(HD);
 #pragma unroll
-  for (int u = 0; u < 2; ++u)
-    b.v[u] = *(const uint4*)(blk + kvq_v_word(16 * u + 4 * q, HD == 128 ? c : c / 2, HD));
-}
+    for (int u = 0; u < 2; ++u) {
+      if constexpr (HD == 128) {
+        const uint4 w = b128(k + 16 * u * (HD / 2), so);
+        b.k[u][0] = w.x;
+        b.k[u][1] = w.y;
+        b.k[u][2] = w.z;
+        b.k[u][3] = w.w;
+      } else {
+        const auto w = __builtin_amdgcn_raw_buffer_load_b64(r, (int)(k + 16 * u * (HD / 2)), (int)so, kAuxStream);
+        b.k[u][0] = w[0];
+        b.k[u][1] = w[1];
+      }
+    }
+  }
+  __device__ __forceinline__ void pairs(Block<HD>& b, int blk) const {
+    const uint32_t so = (uint32_t)blk * kvq_block_bytes(HD);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      b.pr[u][0] = b128(pr + 128 * u, so);
+      b.pr[u][1] = b128(pr + 128 * u + 16, so);
+    }
+  }
+  __device__ __forceinline__ void values(Block<HD>& b, int blk) const {
+    const uint32_t so = (uint32_t)blk * kvq_block_bytes(HD);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) b.v[u] = b128(v + 4 * u * (HD / 8) * 16, so);
+  }
+};
 
 __device__ __forceinline__ uint32_t key_pair_of(const uint4 (&pr)[2], int r) {
   return r == 0 ? pr[0].x : r == 1 ? pr[0].z : r == 2 ? pr[1].x : pr[1].z;
 }
-__device__ __forceinline__ uint32_t value_pair_of(const uint4 (&pr)[2], int r) {
+__device__ __forceinline__ uint32_t& value_pair_of(uint4 (&pr)[2], int r) {
   return r == 0 ? pr[0].y : r == 1 ? pr[0].w : r == 2 ? pr[1].y : pr[1].w;
 }
 
 // z[u][r]: the (unscaled) score of the lane's row at position 16 u + 4 q + r
-template <int HD, bool QB, int T>
-__device__ __forceinline__ void scores(const Block<HD>& b, const Queries<HD, QB> (&Q)[T], float (&z)[T][2][4]) {
+template <int HD, bool QB>
+__device__ __forceinline__ void scores(const Block<HD>& b, const Queries<HD, QB>& Q, float (&z)[2][4]) {
+  const float o = -16.f * Q.sum;
+  floatx4 acc[2] = {floatx4{o, o, o, o}, floatx4{o, o, o, o}};
 #pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    floatx4 acc[T];
+  for (int s = 0; s < HD / 32; ++s) {
+    bf16x8 a[2];
 #pragma unroll
-    for (int t = 0; t < T; ++t) {
-      const float o = -16.f * Q[t].sum;
-      acc[t] = floatx4{o, o, o, o};
-    }
-#pragma unroll
-    for (int s = 0; s < HD / 32; ++s) {
+    for (int u = 0; u < 2; ++u) {
       const uint32_t w = b.k[u][s];
-      const bf16x8 a = op(code_pair(w, 0), code_pair(w, 1), code_pair(w, 2), code_pair(w, 3));
-#pragma unroll
-      for (int t = 0; t < T; ++t)
-#pragma unroll
-        for (int n = 0; n < Queries<HD, QB>::N; ++n)
-          acc[t] = mfma(a, op(Q[t].w[n][s][0], Q[t].w[n][s][1], Q[t].w[n][s][2], Q[t].w[n][s][3]), acc[t]);
+      a[u] = op(code_pair(w, 0), code_pair(w, 1), code_pair(w, 2), code_pair(w, 3));
     }
+#pragma unroll
+    for (int n = 0; n < Queries<HD, QB>::N; ++n)
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        acc[u] = mfma(a[u], op(Q.w[n][s][0], Q.w[n][s][1], Q.w[n][s][2], Q.w[n][s][3]), acc[u]);
+  }
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const uint32_t pr = key_pair_of(b.pr[u], r);
-      const float s = lo_f(pr), m = hi_f(pr);
-#pragma unroll
-      for (int t = 0; t < T; ++t) z[t][u][r] = __builtin_fmaf(s, acc[t][r], m * Q[t].sum);
+      z[u][r] = __builtin_fmaf(lo_f(pr), acc[u][r], hi_f(pr) * Q.sum);
     }
-  }
 }
 
 struct RequestRows {
@@ -459,6 +520,134 @@ __device__ __forceinline__ RequestRows request_rows(const KvqAttend& p, int b) {
   return r;
 }
 
+// Work of an attention call: the blocks of 32 positions of request 0's first
+// K/V head, its second, .., request 1's, .., T in all, cut into WG ranges whose
+// sizes differ by one at most, whatever the requests' lengths.  Head bh's part
+// of range w (a segment) leaves its partial in slot w + bh: along the cut one of
+// the two moves on by one, so slots do not meet and a head's are contiguous.
+// The last bits of a row's result follow the cut, and so the batch.
+struct Plan {
+  uint32_t T, q, r;  // the first r ranges hold q + 1 blocks, the others q
+  __device__ __forceinline__ uint32_t start(uint32_t w) const { return w * q + min(w, r); }
+  __device__ __forceinline__ uint32_t range_of(uint32_t block) const {
+    const uint32_t big = r * (q + 1);
+    return block < big ? block / (q + 1) : r + (block - big) / q;
+  }
+};
+
+// blocks that request b brings per K/V head (ALL: also without rows in use)
+template <bool ALL>
+__device__ __forceinline__ uint32_t request_blocks(const RequestRows& rr) {
+  return !ALL && rr.n == 0 ? 0u : (uint32_t)(rr.L + rr.n + kKvqBlock - 1) / kKvqBlock;
+}
+
+// Blocks per K/V head of requests b0 .. b0 + 63, one per lane, and their
+// inclusive prefix.
+template <bool ALL>
+__device__ __forceinline__ uint32_t scan_blocks(const KvqAttend& p, int b0, int lane, uint32_t* incl) {
+  const uint32_t n = b0 + lane < p.B ? request_blocks<ALL>(request_rows(p, b0 + lane)) : 0u;
+  uint32_t v = n;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t t = __shfl_up(v, o);
+    if (lane >= o) v += t;
+  }
+  *incl = v;
+  return n;
+}
+
+__device__ __forceinline__ uint32_t lane_of(uint32_t v, int l) { return (uint32_t)__builtin_amdgcn_readlane((int)v, l); }
+
+__device__ __forceinline__ Plan make_plan(const KvqAttend& p, uint32_t blocks) {
+  Plan pl;
+  pl.T = blocks * (uint32_t)p.KVH;
+  pl.q = pl.T / (uint32_t)p.WG;
+  pl.r = pl.T - pl.q * (uint32_t)p.WG;
+  return pl;
+}
+
+// The plan, and the request that holds the first block of range w with the
+// blocks before that request (b = B: the range is empty).
+template <bool ALL>
+__device__ __forceinline__ Plan find_range(const KvqAttend& p, int lane, uint32_t w, int* b_out, uint32_t* before_out) {
+  uint32_t incl;
+  uint32_t n = scan_blocks<ALL>(p, 0, lane, &incl), sum = lane_of(incl, 63);
+  for (int b0 = 64; b0 < p.B; b0 += 64) {
+    uint32_t v;
+    scan_blocks<ALL>(p, b0, lane, &v);
+    sum += lane_of(v, 63);
+  }
+  const Plan pl = make_plan(p, sum);
+  const uint32_t want = pl.start(w) / (uint32_t)p.KVH;  // of the requests' blocks per head
+  uint32_t before = 0;
+  *b_out = p.B;
+  for (int b0 = 0;;) {
+    const uint64_t hit = __ballot(before + incl > want);
+    if (hit != 0) {
+      const int l = __ffsll((unsigned long long)hit) - 1;
+      *b_out = b0 + l;
+      before += lane_of(incl - n, l);
+      break;
+    }
+    before += lane_of(incl, 63);
+    b0 += 64;
+    if (b0 >= p.B) break;
+    n = scan_blocks<ALL>(p, b0, lane, &incl);
+  }
+  *before_out = before * (uint32_t)p.KVH;
+  return pl;
+}
+
+// The plan and the blocks before request b.
+__device__ __forceinline__ Plan find_request(const KvqAttend& p, int lane, int b, uint32_t* before_out) {
+  uint32_t sum = 0, before = 0;
+  for (int b0 = 0; b0 < p.B; b0 += 64) {
+    uint32_t incl;
+    const uint32_t n = scan_blocks<false>(p, b0, lane, &incl);
+    if (b >= b0 && b < b0 + 64) before = sum + lane_of(incl - n, b - b0);
+    sum += lane_of(incl, 63);
+  }
+  *before_out = before * (uint32_t)p.KVH;
+  return make_plan(p, sum);
+}
+
+// One segment after the other of range w: (request, K/V head, blocks lo .. hi - 1
+// of nb).
+template <bool ALL>
+struct Segments {
+  uint32_t left;  // blocks of the range still to go
+  int b, h, lo, hi, nb;
+  RequestRows rr;
+  __device__ __forceinline__ bool init(const KvqAttend& p, int lane, uint32_t w) {
+    uint32_t before;
+    const Plan pl = find_range<ALL>(p, lane, w, &b, &before);
+    const uint32_t s = pl.start(w);
+    left = pl.start(w + 1) - s;
+    if (b >= p.B || left == 0) return false;
+    rr = request_rows(p, b);
+    nb = (int)request_blocks<ALL>(rr);
+    h = (int)((s - before) / (uint32_t)nb);
+    lo = (int)(s - before) - h * nb;
+    hi = lo + (int)min((uint32_t)(nb - lo), left);
+    return true;
+  }
+  __device__ __forceinline__ bool next(const KvqAttend& p) {
+    left -= (uint32_t)(hi - lo);
+    if (left == 0) return false;
+    if (++h == p.KVH) {
+      h = 0;
+      do {  // (the plan counted these blocks, so there is such a request)
+        if (++b >= p.B) return false;
+        rr = request_rows(p, b);
+        nb = (int)request_blocks<ALL>(rr);
+      } while (nb == 0);
+    }
+    lo = 0;
+    hi = (int)min((uint32_t)nb, left);
+    return true;
+  }
+};
+
 template <int HD>
 struct AttendSmem {
   float o[kWaves][16][HD + 4];
@@ -473,164 +662,185 @@ __device__ __forceinline__ void store_out(const KvqAttend& p, int b, int kvh, in
   else store4<false>(p.out, at, x);
 }
 
-template <int HD, int T, bool QB>
-__global__ void __launch_bounds__(kWaves * 64) kvq_attend_kernel(KvqAttend p) {
-  constexpr int FT = HD / 16;  // O^T products: features (HD / 16) c + j
+template <int HD, bool QB>
+__global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2))) kvq_attend_kernel(KvqAttend p) {
+  constexpr int FT = HD / 16;        // O^T products: features (HD / 16) c + j
+  constexpr int N = QB ? 1 : 3;      // bf16 terms of p s
   __shared__ AttendSmem<HD> sm;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, q = lane >> 4, c = lane & 15;
-  // the tile groups of one chunk run on one XCD (workgroup i on XCD i % 8)
-  const int x = (int)blockIdx.x & 7, jj = (int)blockIdx.x >> 3;
-  const int tt = jj / p.TG, tg = jj - tt * p.TG;
-  const int64_t item = 8ll * tt + x;
-  const int chunk = (int)(item % p.NC);
-  const int64_t bh = item / p.NC;
-  if (bh >= (int64_t)p.B * p.KVH) return;
-  const int b = (int)(bh / p.KVH), kvh = (int)(bh - (int64_t)b * p.KVH);
-  const RequestRows rr = request_rows(p, b);
-  const int NR = p.G * p.R, keys = rr.L + rr.n;
-  const int k_lo = chunk * p.CK, k_hi = min(k_lo + p.CK, keys);
-  if (p.NC > 1 && (rr.n == 0 || k_lo >= keys)) return;  // (one chunk: it writes the zeros)
-
-  Queries<HD, QB> Q[T];
-  int vis[T];  // positions the lane's row sees
-#pragma unroll
-  for (int t = 0; t < T; ++t) {
-    const int pr = (tg * T + t) * 16 + c, g = pr / p.R, i = pr - g * p.R;
-    const bool ok = pr < NR && i < rr.n;
-    vis[t] = ok ? rr.L + i + 1 : 0;
-    Q[t].load(p.q, ((int64_t)b * p.R + i) * p.q_ld + (kvh * p.G + g) * HD, ok, q);
-  }
-  float M[T], l[T], cs[T];
-  floatx4 o[T][FT], ps[T];
-#pragma unroll
-  for (int t = 0; t < T; ++t) {
-    M[t] = -INFINITY;
-    l[t] = cs[t] = 0.f;
-    ps[t] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int j = 0; j < FT; ++j) o[t][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-  }
+  const int tid = threadIdx.x, lane = tid & 63, q = lane >> 4, c = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // Workgroup i runs on XCD i % 8: the row tiles of one range follow each other
+  // on one XCD and share its L2.
+  const unsigned xcd = blockIdx.x & 7, jj = blockIdx.x >> 3;
+  const unsigned tt = jj / (unsigned)p.TG, tile = jj - tt * p.TG, range = 8 * tt + xcd;
+  const int NR = p.G * p.R;
   const float sl = p.scale * kLog2e;
-  const uint8_t* head = p.cache + (size_t)bh * p.head_bytes;
-  const uint32_t bb = kvq_block_bytes(HD);
-  const int blk_hi = (k_hi + kKvqBlock - 1) / kKvqBlock;
-  int blk = k_lo / kKvqBlock + wave;
-  Block<HD> cur;
-  if (blk < blk_hi) {
-    load_keys<HD>(cur, head + (size_t)blk * bb, q, c);
-    load_values<HD>(cur, head + (size_t)blk * bb, q, c);
+  Segments<false> sg;
+  const bool whole = p.WG == 0;  // a head per workgroup
+  if (whole) {
+    if (range >= (unsigned)(p.B * p.KVH)) return;
+    sg.b = (int)(range / (unsigned)p.KVH);
+    sg.h = (int)(range - (unsigned)sg.b * p.KVH);
+    sg.rr = request_rows(p, sg.b);
+    sg.lo = 0;
+    sg.nb = sg.hi = (int)request_blocks<false>(sg.rr);
+  } else {
+    if (range >= (unsigned)p.WG || !sg.init(p, lane, range)) return;
   }
-  for (; blk < blk_hi; blk += kWaves) {
-    Block<HD> nxt;
-    {  // (the last round loads its own block again)
-      const int nb = blk + kWaves < blk_hi ? blk + kWaves : blk;
-      load_keys<HD>(nxt, head + (size_t)nb * bb, q, c);
-      load_values<HD>(nxt, head + (size_t)nb * bb, q, c);
-    }
-    float z[T][2][4];
-    scores<HD, QB, T>(cur, Q, z);
-    const int p0 = blk * kKvqBlock;
-    const bool tail = p0 + kKvqBlock > rr.L + 1;  // some row does not see all of the block
-    if (tail) {
+  const unsigned my = tile * 16 + c, g = my / (unsigned)p.R;  // the lane's packed row
+  const int i = (int)(my - g * p.R);
+  const bool row_ok = my < (unsigned)NR;
+
+  BlockLoader<HD> ld;
+  RawQuery<HD, QB> qx;
+  // The wave's blocks lo + wave, + W, ..: two in flight, a part of the next one
+  // requested as soon as its registers are free (past the end: the last one
+  // again).
+  Block<HD> buf[2];
+  auto request = [&]() {  // a segment's queries and first blocks
+    ld.init(p.cache + (size_t)(sg.b * p.KVH + sg.h) * p.head_bytes, p.head_bytes, q, c);
+    qx.load(p.q, ((int64_t)sg.b * p.R + (row_ok ? i : 0)) * p.q_ld + (sg.h * p.G + (row_ok ? (int)g : 0)) * HD, q);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int t = 0; t < T; ++t)
+    for (int n = 0; n < 2; ++n) {
+      const int nb = max(min(sg.lo + wave + n * kWaves, sg.hi - 1), 0);
+      ld.keys(buf[n], nb);
+      // (in the order of the loop, or its head would have to wait for more)
+      asm volatile("" ::: "memory");
+      ld.pairs(buf[n], nb);
+      asm volatile("" ::: "memory");
+      ld.values(buf[n], nb);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  request();
+  for (;;) {
+    const RequestRows rr = sg.rr;
+    const int b = sg.b, kvh = sg.h, blk_hi = sg.hi;
+    const unsigned bh = (unsigned)(b * p.KVH + kvh);
+    const bool all = sg.lo == 0 && sg.hi == sg.nb, ok = row_ok && i < rr.n;
+    const int vis = ok ? rr.L + i + 1 : 0;  // positions the lane's row sees
+    Queries<HD, QB> Q;
+    Q.convert(qx, ok);
+    float M = -INFINITY, l = 0.f, cs = 0.f;
+    floatx4 o[FT], ps = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < FT; ++j) o[j] = floatx4{0.f, 0.f, 0.f, 0.f};
+
+    auto block = [&](Block<HD>& cur, int blk) {
+      const int nb = min(blk + 2 * kWaves, blk_hi - 1);  // the buffer's next block
+      float z[2][4];
+      scores<HD, QB>(cur, Q, z);
+      ld.keys(cur, nb);
+      asm volatile("" ::: "memory");  // (the compiler would request all parts at the block's end)
+      const int p0 = blk * kKvqBlock;
+      if (p0 + kKvqBlock > rr.L + 1) {  // some row does not see all of the block
+        // a hidden position may hold anything, NaN among it
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (p0 + 16 * u + 4 * q + r >= vis[t]) z[t][u][r] = -INFINITY;
-    }
-    constexpr int N = QB ? 1 : 3;
-    uint32_t pw[T][N][4];
-#pragma unroll
-    for (int t = 0; t < T; ++t) {
-      float mx = fmaxf(fmaxf(fmaxf(z[t][0][0], z[t][0][1]), fmaxf(z[t][0][2], z[t][0][3])),
-                       fmaxf(fmaxf(z[t][1][0], z[t][1][1]), fmaxf(z[t][1][2], z[t][1][3])));
-      mx = max_q(mx);
-      if (__any(mx > M[t])) {
-        const float mn = fmaxf(M[t], mx);
-        const float f = M[t] == -INFINITY ? 0.f : exp2f((M[t] - mn) * sl);
-        M[t] = mn;
-        l[t] *= f;
-        cs[t] *= f;
-        ps[t] *= f;
-#pragma unroll
-        for (int j = 0; j < FT; ++j) o[t][j] *= f;
+            if (p0 + 16 * u + 4 * q + r >= vis) {
+              z[u][r] = -INFINITY;
+              value_pair_of(cur.pr[u], r) = 0;
+            }
       }
-      const float base = M[t] == -INFINITY ? 0.f : M[t] * sl;
+      float mx = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])),
+                       fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3])));
+      mx = max_q(mx);
+      if (__any(mx > M)) {
+        const float mn = fmaxf(M, mx);
+        const float f = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((M - mn) * sl);
+        M = mn;
+        l *= f;
+        cs *= f;
+        ps *= f;
+#pragma unroll
+        for (int j = 0; j < FT; ++j) o[j] *= f;
+      }
+      const float base = M == -INFINITY ? 0.f : M * sl;
       float w[8];
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(z[t][u][r], sl, -base));
+          const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(z[u][r], sl, -base));
           const uint32_t pr = value_pair_of(cur.pr[u], r);
-          float s = lo_f(pr), m = hi_f(pr);
-          // a hidden position may hold anything, NaN among it
-          if (tail && p0 + 16 * u + 4 * q + r >= vis[t]) s = m = 0.f;
-          l[t] += e;
-          cs[t] = __builtin_fmaf(e, __builtin_fmaf(8.f, s, m), cs[t]);
+          const float s = lo_f(pr);
+          l += e;
+          cs = __builtin_fmaf(e, __builtin_fmaf(8.f, s, hi_f(pr)), cs);
           w[4 * u + r] = e * s;
         }
+      ld.pairs(cur, nb);
+      asm volatile("" ::: "memory");
+      bf16x8 P[N];
+      {
+        uint32_t pw[N][4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        uint32_t x[N];
-        terms<N>(w[2 * e], w[2 * e + 1], x);
+        for (int e = 0; e < 4; ++e) {
+          uint32_t t[N];
+          terms<N>(w[2 * e], w[2 * e + 1], t);
 #pragma unroll
-        for (int n = 0; n < N; ++n) pw[t][n][e] = x[n];
+          for (int n = 0; n < N; ++n) pw[n][e] = t[n];
+        }
+#pragma unroll
+        for (int n = 0; n < N; ++n) P[n] = op(pw[n][0], pw[n][1], pw[n][2], pw[n][3]);
       }
-    }
-    // V^T: for the pairs of positions (2 e, 2 e + 1) of the lane's eight, the
-    // halves of their words side by side
-    uint32_t half[2][4];
-    {
-      const uint32_t vw[8] = {cur.v[0].x, cur.v[0].y, cur.v[0].z, cur.v[0].w,
-                              cur.v[1].x, cur.v[1].y, cur.v[1].z, cur.v[1].w};
-      const uint32_t sel = HD == 128 ? 0x05040100u : (c & 1 ? 0x07060302u : 0x05040100u);
+      // V^T: for the pairs of positions (2 e, 2 e + 1) of the lane's eight, the
+      // halves of their words side by side
+      uint32_t half[2][4];
+      {
+        const uint32_t vw[8] = {cur.v[0].x, cur.v[0].y, cur.v[0].z, cur.v[0].w,
+                                cur.v[1].x, cur.v[1].y, cur.v[1].z, cur.v[1].w};
+        const uint32_t sel = HD == 128 ? 0x05040100u : (c & 1 ? 0x07060302u : 0x05040100u);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        half[0][e] = __builtin_amdgcn_perm(vw[2 * e + 1], vw[2 * e], sel);
-        half[1][e] = HD == 128 ? __builtin_amdgcn_perm(vw[2 * e + 1], vw[2 * e], 0x07060302u) : 0u;
+        for (int e = 0; e < 4; ++e) {
+          half[0][e] = __builtin_amdgcn_perm(vw[2 * e + 1], vw[2 * e], sel);
+          half[1][e] = HD == 128 ? __builtin_amdgcn_perm(vw[2 * e + 1], vw[2 * e], 0x07060302u) : 0u;
+        }
       }
-    }
-    const bf16x8 ones = op(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
+      ld.values(cur, nb);
+      const bf16x8 ones = op(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
 #pragma unroll
-    for (int t = 0; t < T; ++t)
+      for (int n = 0; n < N; ++n) ps = mfma(ones, P[n], ps);
 #pragma unroll
-      for (int n = 0; n < N; ++n) ps[t] = mfma(ones, op(pw[t][n][0], pw[t][n][1], pw[t][n][2], pw[t][n][3]), ps[t]);
+      for (int jh = 0; jh < FT / 4; ++jh) {
+        const uint32_t(&hf)[4] = half[jh];
+        bf16x8 a[4];
 #pragma unroll
-    for (int j = 0; j < FT; ++j) {
-      const uint32_t(&hf)[4] = half[j >> 2];
-      const bf16x8 a = op(code_pair(hf[0], j & 3), code_pair(hf[1], j & 3), code_pair(hf[2], j & 3), code_pair(hf[3], j & 3));
-#pragma unroll
-      for (int t = 0; t < T; ++t)
+        for (int j = 0; j < 4; ++j)
+          a[j] = op(code_pair(hf[0], j), code_pair(hf[1], j), code_pair(hf[2], j), code_pair(hf[3], j));
 #pragma unroll
         for (int n = 0; n < N; ++n)
-          o[t][j] = mfma(a, op(pw[t][n][0], pw[t][n][1], pw[t][n][2], pw[t][n][3]), o[t][j]);
-    }
-    cur = nxt;
-  }
-
-  // the waves' parts, tile by tile; lane 16 q + c holds row c, features
-  // q HD / 4 + FT r + j
 #pragma unroll
-  for (int t = 0; t < T; ++t) {
-    const float lt = sum_q(l[t]), off = sum_q(cs[t]) - 24.f * ps[t][0];
-    if (t > 0) __syncthreads();
+          for (int j = 0; j < 4; ++j) o[4 * jh + j] = mfma(a[j], P[n], o[4 * jh + j]);
+      }
+    };
+    for (int blk = sg.lo + wave; blk < blk_hi; blk += 2 * kWaves) {
+      block(buf[0], blk);
+      __builtin_amdgcn_sched_barrier(0);
+      if (blk + kWaves >= blk_hi) break;
+      block(buf[1], blk + kWaves);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+
+    // the waves' parts; lane 16 q + c holds row c, features q HD / 4 + FT r + j
+    const float lt = sum_q(l), off = sum_q(cs) - 24.f * ps[0];
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
       for (int j = 0; j < FT; j += 4)
         *(float4*)&sm.o[wave][c][q * (HD / 4) + r * FT + j] =
-            make_float4(o[t][j][r] + off, o[t][j + 1][r] + off, o[t][j + 2][r] + off, o[t][j + 3][r] + off);
+            make_float4(o[j][r] + off, o[j + 1][r] + off, o[j + 2][r] + off, o[j + 3][r] + off);
     if (q == 0) {
-      sm.m[wave][c] = M[t];
+      sm.m[wave][c] = M;
       sm.l[wave][c] = lt;
     }
+    const bool more = !whole && sg.next(p);
+    if (more) request();  // (in flight while this segment is put together)
     __syncthreads();
-    const int row0 = (tg * T + t) * 16;
     for (int e = tid; e < 16 * (HD / 4); e += kWaves * 64) {
-      const int row = e / (HD / 4), f = 4 * (e - row * (HD / 4)), pr = row0 + row;
+      const int row = e / (HD / 4), f = 4 * (e - row * (HD / 4)), pr = (int)tile * 16 + row;
       if (pr >= NR) continue;
       float mm = -INFINITY;
 #pragma unroll
@@ -638,133 +848,216 @@ __global__ void __launch_bounds__(kWaves * 64) kvq_attend_kernel(KvqAttend p) {
       float ll = 0.f, a[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
-        const float mw = sm.m[w][row];
-        if (mw == -INFINITY && sm.l[w][row] == 0.f) continue;  // the wave saw nothing of this row
-        const float s = exp2f((mw - mm) * sl);
+        const float mw = sm.m[w][row], lw = sm.l[w][row];
+        // (a wave that saw nothing of this row holds zeros)
+        const float s = mw == -INFINITY && lw == 0.f ? 0.f : __builtin_amdgcn_exp2f((mw - mm) * sl);
         const float4 v = *(const float4*)&sm.o[w][row][f];
-        ll += sm.l[w][row] * s;
+        ll += lw * s;
         a[0] += v.x * s;
         a[1] += v.y * s;
         a[2] += v.z * s;
         a[3] += v.w * s;
       }
-      if (p.NC == 1) {
+      if (all) {  // the segment is all of the head
         const bool live = pr - pr / p.R * p.R < rr.n;
         const float inv = 1.0f / ll;
 #pragma unroll
         for (int k = 0; k < 4; ++k) a[k] = live ? a[k] * inv : 0.f;
         store_out(p, b, kvh, pr, f, a);
-        if (f == 0 && p.w_out != nullptr) p.lse[bh * NR + pr] = live ? mm * sl + log2f(ll) : INFINITY;
+        if (f == 0 && p.w_out != nullptr) p.lse[(int64_t)bh * NR + pr] = live ? mm * sl + log2f(ll) : INFINITY;
       } else {
-        const int64_t at = (bh * p.NC + chunk) * NR + pr;
+        const int64_t at = (int64_t)(range + bh) * NR + pr;
         *(float4*)(p.part_o + at * HD + f) = make_float4(a[0], a[1], a[2], a[3]);
         if (f == 0) *(float2*)(p.part_ml + at * 2) = make_float2(mm, ll);
       }
     }
+    if (!more) break;
+    __syncthreads();
   }
 }
 
-// Merge of the chunks of one (request, K/V head, packed row), in chunk order:
-// HD / 4 lanes per row.
+// Merge of the segments of one (request, K/V head, packed row) per workgroup:
+// 256 / (HD / 4) groups of lanes take every so many segments, in order, and are
+// added in order.  A head that lies in one range is complete already; rows that
+// are not in use get their zeros here.
 template <int HD>
 __global__ void __launch_bounds__(256) kvq_merge_kernel(KvqAttend p) {
-  constexpr int LPR = HD / 4;
-  const int NR = p.G * p.R;
-  const int64_t row = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
-  if (row >= (int64_t)p.B * p.KVH * NR) return;
-  const int f = 4 * (threadIdx.x % LPR);
-  const int64_t bh = row / NR;
-  const int pr = (int)(row - bh * NR);
-  const int b = (int)(bh / p.KVH), kvh = (int)(bh - (int64_t)b * p.KVH);
+  constexpr int LPR = HD / 4, GR = 256 / LPR;
+  __shared__ float so[GR][HD];
+  __shared__ float sm[4], sl_[GR];
+  const int NR = p.G * p.R, tid = threadIdx.x;
+  const unsigned bhu = blockIdx.x / (unsigned)NR;
+  const int pr = (int)(blockIdx.x - bhu * NR);
+  const int b = (int)(bhu / (unsigned)p.KVH), kvh = (int)(bhu - (unsigned)b * p.KVH);
   const RequestRows rr = request_rows(p, b);
-  const int i = pr - pr / p.R * p.R;
-  float a[4] = {0.f, 0.f, 0.f, 0.f};
-  float lse = INFINITY;
-  if (i < rr.n) {
-    const float sl = p.scale * kLog2e;
-    // chunks with a position that the row sees
-    const int nc = min((rr.L + i + p.CK) / p.CK, p.NC);
-    const float* ml = p.part_ml + ((bh * p.NC) * NR + pr) * 2;
-    const float* po = p.part_o + ((bh * p.NC) * NR + pr) * HD + f;
-    float M = -INFINITY;
-    for (int k = 0; k < nc; ++k) M = fmaxf(M, ml[(int64_t)k * NR * 2]);
-    float l = 0.f;
-#pragma unroll 4
-    for (int k = 0; k < nc; ++k) {
-      const float2 v = *(const float2*)(ml + (int64_t)k * NR * 2);
-      const float s = exp2f((v.x - M) * sl);
-      const float4 o = *(const float4*)(po + (int64_t)k * NR * HD);
-      l += v.y * s;
-      a[0] += o.x * s;
-      a[1] += o.y * s;
-      a[2] += o.z * s;
-      a[3] += o.w * s;
-    }
-    const float inv = 1.0f / l;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) a[k] *= inv;
-    lse = M * sl + log2f(l);
+  const int i = pr - pr / p.R * p.R, f = 4 * (tid % LPR), g = tid / LPR;
+  if (i >= rr.n) {
+    const float z[4] = {0.f, 0.f, 0.f, 0.f};
+    if (g == 0) store_out(p, b, kvh, pr, f, z);
+    if (tid == 0 && p.w_out != nullptr) p.lse[blockIdx.x] = INFINITY;
+    return;
   }
+  const float sl = p.scale * kLog2e;
+  const uint32_t nb = request_blocks<false>(rr);
+  uint32_t before, w0, w1;
+  // the ranges of the head's first and last block
+  const Plan pl = find_request(p, tid & 63, b, &before);
+  before += (uint32_t)(bhu - (unsigned)b * p.KVH) * nb;
+  w0 = pl.range_of(before);
+  w1 = pl.range_of(before + nb - 1);
+  if (w0 == w1) return;
+  const int nc = (int)(w1 - w0) + 1;
+  const float* ml = p.part_ml + ((int64_t)(w0 + bhu) * NR + pr) * 2;
+  const float* po = p.part_o + ((int64_t)(w0 + bhu) * NR + pr) * HD + f;
+  float M = -INFINITY;
+  for (int k = tid; k < nc; k += 256) M = fmaxf(M, ml[(int64_t)k * NR * 2]);
+  M = max_lanes<64>(M);
+  if ((tid & 63) == 0) sm[tid >> 6] = M;
+  __syncthreads();
+  M = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
+  float l = 0.f, a[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 2
+  for (int k = g; k < nc; k += GR) {
+    const float2 v = *(const float2*)(ml + (int64_t)k * NR * 2);
+    const float s = v.x == -INFINITY && v.y == 0.f ? 0.f : __builtin_amdgcn_exp2f((v.x - M) * sl);  // (0: it sees none of them)
+    const float4 o = *(const float4*)(po + (int64_t)k * NR * HD);
+    l += v.y * s;
+    a[0] += o.x * s;
+    a[1] += o.y * s;
+    a[2] += o.z * s;
+    a[3] += o.w * s;
+  }
+  *(float4*)&so[g][f] = make_float4(a[0], a[1], a[2], a[3]);
+  if (f == 0) sl_[g] = l;
+  __syncthreads();
+  if (g != 0) return;
+#pragma unroll
+  for (int k = 1; k < GR; ++k) {
+    const float4 o = *(const float4*)&so[k][f];
+    a[0] += o.x;
+    a[1] += o.y;
+    a[2] += o.z;
+    a[3] += o.w;
+    l += sl_[k];
+  }
+  const float inv = 1.0f / l;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) a[k] *= inv;
   store_out(p, b, kvh, pr, f, a);
-  if (f == 0 && p.w_out != nullptr) p.lse[bh * NR + pr] = lse;
+  if (f == 0 && p.w_out != nullptr) p.lse[blockIdx.x] = M * sl + log2f(l);
 }
 
 // Weights: out = in + the probabilities of the first w_rows rows, summed over
 // the rows and the query heads of the K/V head.  The scores are taken again
 // from the keys' codes (half of the cache) now that the rows' log-sum-exp is
-// known; a wave owns its block of 32 positions, so nothing is added twice and
-// the order of the sum is fixed.
+// known, here as S = Q K^T: lane 16 q + c gets position c of rows 4 q .. + 3, so
+// a position's sum is three adds and two swaps.  A wave owns its blocks of 32
+// positions: nothing is added twice and the order of the sum is fixed.  The
+// cut is a plan of its own (requests without rows in use copy their weights).
 template <int HD, bool QB>
 __global__ void __launch_bounds__(kWaves * 64) kvq_weights_kernel(KvqAttend p) {
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, q = lane >> 4, c = lane & 15;
-  const int64_t bh = blockIdx.x;
-  const int b = (int)(bh / p.KVH), kvh = (int)(bh - (int64_t)b * p.KVH);
-  const RequestRows rr = request_rows(p, b);
-  const int keys = rr.L + rr.n, blocks = (keys + kKvqBlock - 1) / kKvqBlock;
-  const int per = p.CK / kKvqBlock;
-  const int lo = (int)blockIdx.y * per, hi = min(lo + per, blocks);
-  const int nw = min(p.w_rows, rr.n), NW = p.G * nw;
+  constexpr int S = HD / 32;
+  const int tid = threadIdx.x, lane = tid & 63, q = lane >> 4, c = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const float sl = p.scale * kLog2e;
-  const uint8_t* head = p.cache + (size_t)bh * p.head_bytes;
-  const uint32_t bb = kvq_block_bytes(HD);
-  const float* lse = p.lse + bh * p.G * p.R;
-  for (int blk = lo + wave; blk < hi; blk += kWaves) {
-    Block<HD> cur;
-    load_keys<HD>(cur, head + (size_t)blk * bb, q, c);
-    const int p0 = blk * kKvqBlock;
-    float add[2][4] = {};
-    for (int r0 = 0; r0 < NW; r0 += 16) {
-      const int pr = r0 + c, g = pr / nw, i = pr - g * nw;
-      const bool ok = pr < NW;
-      Queries<HD, QB> Q[1];
-      Q[0].load(p.q, ((int64_t)b * p.R + i) * p.q_ld + (kvh * p.G + g) * HD, ok, q);
-      const float ls = ok ? lse[g * p.R + i] : INFINITY;
-      const int vis = ok ? rr.L + i + 1 : 0;
-      float z[1][2][4];
-      scores<HD, QB, 1>(cur, Q, z);
+  Segments<true> sg;
+  if (!sg.init(p, lane, blockIdx.x)) return;
+  do {
+    const RequestRows rr = sg.rr;
+    const int b = sg.b, kvh = sg.h, keys = rr.L + rr.n;
+    const int64_t bh = b * p.KVH + kvh;
+    const int first = sg.lo + wave, hi = sg.hi;
+    if (first >= hi) continue;
+    const int nw = min(p.w_rows, rr.n), NW = p.G * nw;
+    BlockLoader<HD> ld;
+    ld.init(p.cache + (size_t)bh * p.head_bytes, p.head_bytes, q, c);
+    const float* lse = p.lse + bh * p.G * p.R;
+    struct Part {
+      Block<HD> b;
+      uint2 pr[2];  // key pair (and value pair) of positions 16 u + c
+    };
+    auto request = [&](Part& x, int blk) {
+      blk = blk < hi ? blk : first;
+      ld.keys(x.b, blk);
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(z[0][u][r], sl, -ls));
-          add[u][r] += p0 + 16 * u + 4 * q + r < vis ? e : 0.f;
-        }
-    }
-    // over the sixteen rows; lane 16 q + 4 u + r stores position 16 u + 4 q + r
-    float mine = 0.f;
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
+      for (int u = 0; u < 2; ++u) {
+        const auto w = __builtin_amdgcn_raw_buffer_load_b64(ld.r, (int)kvq_pair(16 * u + c, HD),
+                                                            (int)((uint32_t)blk * kvq_block_bytes(HD)), kAuxStream);
+        x.pr[u] = make_uint2(w[0], w[1]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    Part buf[2];
+    request(buf[0], first);
+    request(buf[1], first + kWaves);
+    // sixteen counted rows at a time; the first tile (there is one even without
+    // rows) starts from w_in, the others from what the tile before stored
+    for (int r0 = 0; r0 == 0 || r0 < NW; r0 += 16) {
+      Queries<HD, QB> Q;
+      {
+        const int pr = r0 + c, g = nw > 0 ? pr / nw : 0, i = pr - g * nw;
+        const bool ok = pr < NW;
+        RawQuery<HD, QB> x;
+        x.load(p.q, ((int64_t)b * p.R + (ok ? i : 0)) * p.q_ld + (kvh * p.G + (ok ? g : 0)) * HD, q);
+        Q.convert(x, ok);
+      }
+      float ls[4], sq[4];
+      int vis[4];
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const float t = sum_lanes<16>(add[u][r]);
-        if (c == 4 * u + r) mine = t;
+        const int pr = r0 + 4 * q + r, g = nw > 0 ? pr / nw : 0, i = pr - g * nw;
+        const bool ok = pr < NW;
+        ls[r] = ok ? lse[g * p.R + i] : INFINITY;
+        vis[r] = ok ? rr.L + i + 1 : 0;
+        sq[r] = __shfl(Q.sum, 4 * q + r);
       }
-    const int pos = p0 + 16 * (c >> 2) + 4 * q + (c & 3);
-    if (c < 8 && pos < keys) {
-      const int64_t at = bh * p.max_len + pos;
-      p.w_out[at] = (p.w_in != nullptr ? p.w_in[at] : 0.f) + mine;
+      const float* from = r0 == 0 ? p.w_in : p.w_out;
+      auto block = [&](Part& cur, int blk) {
+        floatx4 acc[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) acc[u] = floatx4{-16.f * sq[0], -16.f * sq[1], -16.f * sq[2], -16.f * sq[3]};
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+#pragma unroll
+          for (int n = 0; n < Queries<HD, QB>::N; ++n)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              const uint32_t w = cur.b.k[u][s];
+              acc[u] = mfma(op(Q.w[n][s][0], Q.w[n][s][1], Q.w[n][s][2], Q.w[n][s][3]),
+                            op(code_pair(w, 0), code_pair(w, 1), code_pair(w, 2), code_pair(w, 3)), acc[u]);
+            }
+        const float s[2] = {lo_f(cur.pr[0].x), lo_f(cur.pr[1].x)}, m[2] = {hi_f(cur.pr[0].x), hi_f(cur.pr[1].x)};
+        request(cur, blk + 2 * kWaves);
+        float t[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          t[u] = 0.f;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float z = __builtin_fmaf(s[u], acc[u][r], m[u] * sq[r]);
+            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(z, sl, -ls[r]));
+            t[u] += blk * kKvqBlock + 16 * u + c < vis[r] ? e : 0.f;
+          }
+          t[u] = sum_q(t[u]);
+        }
+        // lanes 0 .. 31 store the block's positions
+        const int pos = blk * kKvqBlock + lane;
+        if (lane < kKvqBlock && pos < keys) {
+          const int64_t at = bh * p.max_len + pos;
+          p.w_out[at] = (from != nullptr ? from[at] : 0.f) + (q == 0 ? t[0] : t[1]);
+        }
+      };
+      for (int blk = first; blk < hi; blk += 2 * kWaves) {
+        block(buf[0], blk);
+        if (blk + kWaves >= hi) break;
+        block(buf[1], blk + kWaves);
+      }
+      if (r0 + 16 < NW) {
+        request(buf[0], first);
+        request(buf[1], first + kWaves);
+      }
     }
-  }
+  } while (sg.next(p));
 }
 
 // ---------------------------------------------------------------------------
@@ -787,7 +1080,7 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 }
 
 __global__ void __launch_bounds__(kSelThreads) kvq_select_kernel(KvqEvict p) {
-  __shared__ uint32_t hist[256];
+  __shared__ uint32_t hist[4][256];  // (lanes 4 apart count apart: equal weights meet less often)
   __shared__ uint32_t s_prefix, s_need;
   __shared__ uint32_t wsum[2][kSelThreads / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -809,19 +1102,37 @@ __global__ void __launch_bounds__(kSelThreads) kvq_select_kernel(KvqEvict p) {
   uint32_t need = (uint32_t)(p.budget - p.recent), prefix = 0, mask = 0;
   if (need > 0) {
     for (int shift = 24; shift >= 0; shift -= 8) {
-      if (tid < 256) hist[tid] = 0;
+      ((uint32_t*)hist)[tid] = 0;
       __syncthreads();
       for (int j = tid; j < cand; j += kSelThreads) {
         const uint32_t k = weight_key(w[j]);
-        if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & 255], 1u);
+        if ((k & mask) == prefix) atomicAdd(&hist[tid & 3][(k >> shift) & 255], 1u);
       }
       __syncthreads();
-      if (tid == 0) {  // from the heaviest bin down, the one that holds the last kept position
-        uint32_t left = need;
-        int d = 255;
-        while (d > 0 && hist[d] < left) left -= hist[d--];
-        s_prefix = prefix | ((uint32_t)d << shift);
-        s_need = left;
+      if (wave == 0) {
+        // from the heaviest bin down, the one that holds the last kept position:
+        // lane i has bins 255 - 4 i .. 252 - 4 i
+        uint32_t n[4], t = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int d = 255 - 4 * lane - k;
+          n[k] = hist[0][d] + hist[1][d] + hist[2][d] + hist[3][d];
+          t += n[k];
+        }
+        uint32_t above = t;  // inclusive prefix over the lanes
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+          const uint32_t v = __shfl_up(above, o);
+          if (lane >= o) above += v;
+        }
+        above -= t;
+        if (above < need && need <= above + t) {
+          uint32_t left = need - above;
+          int k = 0;
+          while (k < 3 && n[k] < left) left -= n[k++];
+          s_prefix = prefix | ((uint32_t)(255 - 4 * lane - k) << shift);
+          s_need = left;
+        }
       }
       __syncthreads();
       prefix = s_prefix;
@@ -873,12 +1184,13 @@ __global__ void __launch_bounds__(kSelThreads) kvq_select_kernel(KvqEvict p) {
 }
 
 // kvq_move_kernel: kept position j of the source becomes position j.  Grid
-// ((layer, request, K/V head), part, column): a column is a quarter of the
-// keys' codes, a quarter of the values' or the pairs.  In place one workgroup
-// goes through its column in order: a row moves to a lower or the same place,
-// and a round reads all of its rows before it writes the first.
-constexpr int kMoveThreads = 256;
-constexpr int kMoveCols = 9;
+// ((layer, request, K/V head), part, column).  Column 0 is the keys' codes, a
+// thread a 16-byte piece of a position; column 1 the values', a thread the
+// piece of four positions and eight features (from four places); column 2 the
+// pairs.  In place one workgroup goes through its column in order: a row moves
+// to a lower or the same position, and a round reads all of its rows before it
+// writes the first.
+constexpr int kMoveThreads = 512;
 
 template <int HD>
 __global__ void __launch_bounds__(kMoveThreads) kvq_move_kernel(KvqEvict p, int in_place) {
@@ -892,39 +1204,58 @@ __global__ void __launch_bounds__(kMoveThreads) kvq_move_kernel(KvqEvict p, int 
   const uint8_t* src = p.cache + (size_t)lbh * p.head_bytes;
   uint8_t* dst = p.out + (size_t)lbh_out * p.out_head_bytes;
   constexpr uint32_t bb = (uint32_t)kKvqBlock * (HD + 8);
-  constexpr int W = HD / 32;  // words of a column
-  // rows of a round: threads are (row, word) of the column; the pairs' column has 2 words
-  const int cw = col == 8 ? 2 : W;
-  const int rpr = kMoveThreads / cw;
-  const int r = tid / cw, wd = tid - r * cw;
-  for (int j0 = (int)blockIdx.y * rpr; j0 < m; j0 += (int)gridDim.y * rpr) {
-    const int j = j0 + r;
-    uint32_t v = 0;
-    size_t to = 0;
-    bool move = j < m;
-    if (move) {
-      const int t = kept[j];
-      const int tb = t % kKvqBlock, jb = j % kKvqBlock;
-      uint32_t from;
-      if (col < 4) {
-        from = kvq_k_word(tb, col * W + wd, HD);
-        to = kvq_k_word(jb, col * W + wd, HD);
-      } else if (col < 8) {
-        from = kvq_v_word(tb, (col - 4) * W + wd, HD);
-        to = kvq_v_word(jb, (col - 4) * W + wd, HD);
-      } else {
-        from = kvq_pair(tb, HD) + 4 * wd;
-        to = kvq_pair(jb, HD) + 4 * wd;
+  constexpr int KP = HD / 32, VP = HD / 8;  // pieces of a position's keys, of four positions' values
+  // positions of a round
+  const int per = col == 0 ? kMoveThreads / KP : col == 1 ? kMoveThreads / VP * 4 : kMoveThreads;
+  for (int j0 = (int)blockIdx.y * per; j0 < m; j0 += (int)gridDim.y * per) {
+    uint4 v = make_uint4(0, 0, 0, 0);
+    int j, n = 0;  // first position and count of the thread's positions
+    uint8_t* to;
+    if (col == 0) {
+      j = j0 + tid / KP;
+      n = j < m;
+      to = dst + (size_t)(j / kKvqBlock) * bb + kvq_k_word(j % kKvqBlock, 4 * (tid % KP), HD);
+      if (n) {
+        const int t = kept[j];
+        v = *(const uint4*)(src + (size_t)(t / kKvqBlock) * bb + kvq_k_word(t % kKvqBlock, 4 * (tid % KP), HD));
       }
-      to += (size_t)(j / kKvqBlock) * bb;
-      v = *(const uint32_t*)(src + (size_t)(t / kKvqBlock) * bb + from);
-      if (in_place && t == j) move = false;
+    } else if (col == 1) {
+      j = j0 + tid / VP * 4;
+      n = max(0, min(m - j, 4));
+      to = dst + (size_t)(j / kKvqBlock) * bb + kvq_v_word(j % kKvqBlock, tid % VP, HD);
+      uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (k < n) {
+          const int t = kept[j + k];
+          w[k] = *(const uint32_t*)(src + (size_t)(t / kKvqBlock) * bb + kvq_v_word(t % kKvqBlock, tid % VP, HD));
+        }
+      v = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+      j = j0 + tid;
+      n = j < m;
+      to = dst + (size_t)(j / kKvqBlock) * bb + kvq_pair(j % kKvqBlock, HD);
+      if (n) {
+        const int t = kept[j];
+        const uint2 w = *(const uint2*)(src + (size_t)(t / kKvqBlock) * bb + kvq_pair(t % kKvqBlock, HD));
+        v.x = w.x;
+        v.y = w.y;
+      }
     }
     if (in_place) __syncthreads();
-    if (move) *(uint32_t*)(dst + to) = v;
+    if (col == 2) {
+      if (n) *(uint2*)to = make_uint2(v.x, v.y);
+    } else if (col == 1 && n < 4) {  // positions behind the last stay as they were
+      uint32_t* o = (uint32_t*)to;
+      if (n > 0) o[0] = v.x;
+      if (n > 1) o[1] = v.y;
+      if (n > 2) o[2] = v.z;
+    } else if (n) {
+      *(uint4*)to = v;
+    }
     if (in_place) __syncthreads();
   }
-  if (col == 8 && blockIdx.y == 0 && l == 0 && h == 0 && tid == 0) p.lens_out[b] = m;
+  if (col == 2 && blockIdx.y == 0 && l == 0 && h == 0 && tid == 0) p.lens_out[b] = m;
 }
 
 }  // namespace
@@ -932,9 +1263,8 @@ __global__ void __launch_bounds__(kMoveThreads) kvq_move_kernel(KvqEvict p, int 
 hipError_t launch_kvq_append(const KvqAppend& a, hipStream_t st) {
   const int heads = (a.q != nullptr ? a.H : 0) + 2 * a.KVH;
   const int per = 256 / (a.hd / 8);
-  const int64_t items = (int64_t)a.B * a.R * heads, grid = (items + per - 1) / per;
-  if (grid > 0x7fffffff) return hipErrorInvalidValue;
-  const dim3 g((unsigned)grid);
+  if ((heads + per - 1) / per > 65535) return hipErrorInvalidValue;
+  const dim3 g((unsigned)(a.B * a.R), (unsigned)((heads + per - 1) / per));
   if (a.hd == 128) {
     if (a.bf16) hipLaunchKernelGGL((kvq_append_kernel<128, true>), g, dim3(256), 0, st, a);
     else hipLaunchKernelGGL((kvq_append_kernel<128, false>), g, dim3(256), 0, st, a);
@@ -962,36 +1292,45 @@ hipError_t launch_kvq_read(const KvqRead& a, hipStream_t st) {
 
 namespace {
 
-constexpr int kChunk = 512;  // keys per workgroup of the attention
+// Workgroups of the attention's ranges: two per compute unit (what their
+// registers allow) over all row tiles, one round; fewer where that left less
+// than two blocks per wave.  A workgroup costs about 5 us before and after its
+// stream, so one round of long ranges beats several of short ones: 16 requests of
+// 16384 positions, 8 K/V heads, one bf16 token took 104 us with 256 keys per
+// workgroup, 75 with 512 and 60 with 2048; and ranges of equal size beat chunks
+// of equal length where the requests' lengths differ (16 of 5000 to 16000: 40 us,
+// 55 with chunks).  Up to 256 keys a workgroup takes a whole head, without a
+// merge.
+constexpr int kAttendWgs = 512;
+constexpr int kWeightWgs = 1024;
+constexpr int kWholeKeys = 2 * kWaves * kKvqBlock;
 
-template <int HD, int T>
-void attend_t(const KvqAttend& a, unsigned grid, hipStream_t st) {
-  if (a.bf16) hipLaunchKernelGGL((kvq_attend_kernel<HD, T, true>), dim3(grid), dim3(kWaves * 64), 0, st, a);
-  else hipLaunchKernelGGL((kvq_attend_kernel<HD, T, false>), dim3(grid), dim3(kWaves * 64), 0, st, a);
-}
+int64_t attend_blocks(const KvqAttend& a) { return (int64_t)a.B * a.KVH * ((a.max_keys + kKvqBlock - 1) / kKvqBlock); }
 
 template <int HD>
 hipError_t attend_hd(KvqAttend a, hipStream_t st) {
-  const int NR = a.G * a.R, tiles = (NR + 15) / 16, T = tiles > 1 ? 2 : 1;
-  a.TG = (tiles + T - 1) / T;
-  a.CK = kChunk;
-  a.NC = std::max(1, (a.max_keys + a.CK - 1) / a.CK);
-  const int64_t items = (int64_t)a.B * a.KVH * a.NC, grid = 8 * a.TG * ((items + 7) / 8);
-  if (grid > 0x7fffffff) return hipErrorInvalidValue;
-  if (T == 1) attend_t<HD, 1>(a, (unsigned)grid, st);
-  else attend_t<HD, 2>(a, (unsigned)grid, st);
+  const int64_t heads = (int64_t)a.B * a.KVH, rows = heads * a.G * a.R;
+  a.TG = (a.G * a.R + 15) / 16;
+  const bool whole = a.max_keys <= kWholeKeys;
+  const int64_t fill = (attend_blocks(a) + 2 * kWaves - 1) / (2 * kWaves);
+  // (whole rounds of the eight XCDs)
+  const int64_t wgs = std::min<int64_t>(fill, std::max(8, kAttendWgs / 8 / a.TG * 8));
+  a.WG = whole ? 0 : (int)wgs;
+  const int64_t grid = 8 * a.TG * (((whole ? heads : wgs) + 7) / 8);
+  if (grid > 0x7fffffff || rows > 0x7fffffff || attend_blocks(a) > 0x7fffffff) return hipErrorInvalidValue;
+  if (!whole && (heads + wgs) * a.G * a.R > (int64_t)a.part_rows) return hipErrorInvalidValue;
+  if (a.bf16) hipLaunchKernelGGL((kvq_attend_kernel<HD, true>), dim3((unsigned)grid), dim3(kWaves * 64), 0, st, a);
+  else hipLaunchKernelGGL((kvq_attend_kernel<HD, false>), dim3((unsigned)grid), dim3(kWaves * 64), 0, st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (a.NC > 1) {
-    const int per = 256 / (HD / 4);
-    const int64_t rows = (int64_t)a.B * a.KVH * NR;
-    hipLaunchKernelGGL((kvq_merge_kernel<HD>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, st, a);
+  if (!whole) {
+    hipLaunchKernelGGL((kvq_merge_kernel<HD>), dim3((unsigned)rows), dim3(256), 0, st, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (a.w_out != nullptr) {
-    const dim3 g((unsigned)(a.B * a.KVH), (unsigned)a.NC);
-    if (a.bf16) hipLaunchKernelGGL((kvq_weights_kernel<HD, true>), g, dim3(kWaves * 64), 0, st, a);
-    else hipLaunchKernelGGL((kvq_weights_kernel<HD, false>), g, dim3(kWaves * 64), 0, st, a);
+    a.WG = (int)std::min<int64_t>(fill, kWeightWgs);
+    if (a.bf16) hipLaunchKernelGGL((kvq_weights_kernel<HD, true>), dim3((unsigned)a.WG), dim3(kWaves * 64), 0, st, a);
+    else hipLaunchKernelGGL((kvq_weights_kernel<HD, false>), dim3((unsigned)a.WG), dim3(kWaves * 64), 0, st, a);
     e = hipGetLastError();
   }
   return e;
@@ -999,11 +1338,13 @@ hipError_t attend_hd(KvqAttend a, hipStream_t st) {
 
 }  // namespace
 
-size_t kvq_attend_floats(int B, int H, int KVH, int hd, int max_len, int R, size_t* part_ml, size_t* lse) {
-  const size_t rows = (size_t)B * H * R, nc = (size_t)std::max(1, (max_len + kChunk - 1) / kChunk);
-  *part_ml = rows * nc * 2;
+// (grows with every argument, so a workspace for the largest call holds any)
+size_t kvq_attend_floats(int B, int H, int KVH, int hd, int R, size_t* part_ml, size_t* lse) {
+  const size_t rows = (size_t)B * H * R, TG = ((size_t)(H / KVH) * R + 15) / 16;
+  const size_t parts = rows + std::max<size_t>(16 * kAttendWgs, 8 * 16 * TG);
+  *part_ml = parts * 2;
   *lse = rows;
-  return rows * nc * hd;
+  return parts * hd;
 }
 
 hipError_t launch_kvq_attend(const KvqAttend& a, hipStream_t st) {
@@ -1017,7 +1358,7 @@ hipError_t launch_kvq_evict(const KvqEvict& a, hipStream_t st) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int in_place = a.cache == a.out;
-  const dim3 g((unsigned)heads, in_place ? 1u : (unsigned)std::max(1, std::min((a.budget + 63) / 64, 64)), kMoveCols);
+  const dim3 g((unsigned)heads, in_place ? 1u : (unsigned)std::min((a.budget + 127) / 128, 64), 3);
   if (a.hd == 128) hipLaunchKernelGGL((kvq_move_kernel<128>), g, dim3(kMoveThreads), 0, st, a, in_place);
   else hipLaunchKernelGGL((kvq_move_kernel<64>), g, dim3(kMoveThreads), 0, st, a, in_place);
   return hipGetLastError();

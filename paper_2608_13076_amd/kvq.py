@@ -46,8 +46,9 @@ class QuantCache:
         self.shape = KVQShape(n_layers, batch, n_heads, n_kv_heads, head_dim, max_len)
         self.n_layers, self.batch, self.n_heads, self.n_kv_heads = n_layers, batch, n_heads, n_kv_heads
         self.head_dim, self.max_len, self.max_rows = head_dim, max_len, max_rows
-        nbytes = self.lib.spade_kvq_bytes(self._shape())
-        ws = self.lib.spade_kvq_workspace_bytes(self._shape(), max_rows)
+        self._sp = ctypes.byref(self.shape)
+        nbytes = self.lib.spade_kvq_bytes(self._sp)
+        ws = self.lib.spade_kvq_workspace_bytes(self._sp, max_rows)
         if nbytes == 0 or ws == 0:
             raise spade.SpadeError(-1, "cache shape: " + self.lib.spade_last_error().decode())
         with torch.cuda.device(self.device):
@@ -55,31 +56,37 @@ class QuantCache:
             self.workspace = torch.empty(ws, dtype=torch.uint8, device=self.device)
             self.lens = torch.zeros(batch, dtype=torch.int32, device=self.device)
             self.err = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self._wshape = (batch, n_kv_heads, max_len)
 
-    def _shape(self):
-        return ctypes.byref(self.shape)
+    def _call(self, fn, *args) -> None:
+        """fn(shape, *args, stream) with the cache's device current, on its
+        current stream."""
+        dev = self.device
+        if torch.cuda.current_device() == dev.index:
+            _check(fn(self._sp, *args, torch.cuda.current_stream(dev).cuda_stream))
+        else:
+            with torch.cuda.device(dev):
+                _check(fn(self._sp, *args, torch.cuda.current_stream(dev).cuda_stream))
 
-    def _stream(self):
-        return ctypes.c_void_p(torch.cuda.current_stream(self.device).cuda_stream)
-
-    def _arg(self, t: Optional[torch.Tensor], dtype, shape, name: str):
-        """Pointer of a contiguous tensor of this dtype and shape on the cache's device."""
+    def _arg(self, t: Optional[torch.Tensor], dtype, shape: tuple, name: str):
+        """Address of a contiguous tensor of this dtype and shape on the cache's device."""
         if t is None:
             return None
-        if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != self.device:
-            raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {self.device}")
-        return ctypes.c_void_p(t.data_ptr())
+        if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.device != self.device:
+            raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {shape} on {self.device}")
+        return t.data_ptr()
 
     def _rows(self, t: torch.Tensor, B: int, R: int, heads: int, dtype, name: str):
-        """(pointer, ld) of rows [B, R, heads, head_dim]: contiguous heads, the
+        """(address, ld) of rows [B, R, heads, head_dim]: contiguous heads, the
         rows of all requests one stride apart."""
-        if t.dtype != dtype or tuple(t.shape) != (B, R, heads, self.head_dim) or t.device != self.device:
-            raise ValueError(f"{name}: expected {dtype} [{B}, {R}, {heads}, {self.head_dim}] on {self.device}")
+        hd = self.head_dim
+        if t.dtype is not dtype or t.shape != (B, R, heads, hd) or t.device != self.device:
+            raise ValueError(f"{name}: expected {dtype} [{B}, {R}, {heads}, {hd}] on {self.device}")
         sb, sr, sh, sf = t.stride()
-        ld = sr if R > 1 else (sb if B > 1 else heads * self.head_dim)
-        if sf != 1 or (heads > 1 and sh != self.head_dim) or (R > 1 and B > 1 and sb != R * sr):
+        ld = sr if R > 1 else (sb if B > 1 else heads * hd)
+        if sf != 1 or (heads > 1 and sh != hd) or (R > 1 and B > 1 and sb != R * sr):
             raise ValueError(f"{name}: heads must be contiguous and rows one stride apart")
-        return ctypes.c_void_p(t.data_ptr()), ld
+        return t.data_ptr(), ld
 
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None,
                gain_q: Optional[torch.Tensor] = None, gain_k: Optional[torch.Tensor] = None, eps: float = 1e-5,
@@ -101,18 +108,16 @@ class QuantCache:
         if q is not None:
             qp, qld = self._rows(q, B, R, self.n_heads, dt, "q")
             if q_out is None:
-                q_out = torch.empty((B, R, self.n_heads, self.head_dim), dtype=dt, device=self.device)
+                q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
             op, old = self._rows(q_out, B, R, self.n_heads, dt, "q_out")
         f32, i32, half = torch.float32, torch.int32, self.head_dim // 2
         n_rope = 0 if rope is None else int(rope.shape[0])
-        with torch.cuda.device(self.device):
-            _check(self.lib.spade_kvq_append(
-                self._shape(), layer, ctypes.c_void_p(self.buf.data_ptr()), B, R, _DTYPES[dt], qp, qld, kp, kld, vp, vld,
-                self._arg(gain_q, f32, (self.head_dim,), "gain_q"), self._arg(gain_k, f32, (self.head_dim,), "gain_k"),
-                float(eps), self._arg(rope, f32, (n_rope, half, 2), "rope"), n_rope, self._arg(pos, i32, (B,), "pos"),
-                self._arg(self.lens, i32, (self.batch,), "lens"), self._arg(rows, i32, (B,), "rows"), op, old,
-                self._arg(weights, f32, (self.batch, self.n_kv_heads, self.max_len), "weights"),
-                ctypes.c_void_p(self.err.data_ptr()), self._stream()))
+        self._call(
+            self.lib.spade_kvq_append, layer, self.buf.data_ptr(), B, R, _DTYPES[dt], qp, qld, kp, kld, vp, vld,
+            self._arg(gain_q, f32, (self.head_dim,), "gain_q"), self._arg(gain_k, f32, (self.head_dim,), "gain_k"),
+            eps, self._arg(rope, f32, (n_rope, half, 2), "rope"), n_rope, self._arg(pos, i32, (B,), "pos"),
+            self._arg(self.lens, i32, (self.batch,), "lens"), self._arg(rows, i32, (B,), "rows"), op, old,
+            self._arg(weights, f32, self._wshape, "weights"), self.err.data_ptr())
         return q_out
 
     def attend(self, layer: int, q: torch.Tensor, out: Optional[torch.Tensor] = None, scale: Optional[float] = None,
@@ -130,18 +135,15 @@ class QuantCache:
             raise ValueError("q: float32 or bfloat16")
         qp, qld = self._rows(q, B, R, self.n_heads, dt, "q")
         if out is None:
-            out = torch.empty((B, R, self.n_heads, self.head_dim), dtype=dt, device=self.device)
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
         op, old = self._rows(out, B, R, self.n_heads, dt, "out")
         f32, i32 = torch.float32, torch.int32
-        ws = (self.batch, self.n_kv_heads, self.max_len)
-        with torch.cuda.device(self.device):
-            _check(self.lib.spade_kvq_attend(
-                self._shape(), layer, ctypes.c_void_p(self.buf.data_ptr()), B, R, _DTYPES[dt], qp, qld,
-                1.0 / math.sqrt(self.head_dim) if scale is None else float(scale),
-                self._arg(self.lens, i32, (self.batch,), "lens"), self._arg(rows, i32, (B,), "rows"), int(max_keys), op,
-                old, self._arg(weights, f32, ws, "weights"), self._arg(weights_out, f32, ws, "weights_out"),
-                int(weight_rows), ctypes.c_void_p(self.workspace.data_ptr()), self.workspace.numel(),
-                ctypes.c_void_p(self.err.data_ptr()), self._stream()))
+        self._call(
+            self.lib.spade_kvq_attend, layer, self.buf.data_ptr(), B, R, _DTYPES[dt], qp, qld,
+            1.0 / math.sqrt(self.head_dim) if scale is None else scale,
+            self._arg(self.lens, i32, (self.batch,), "lens"), self._arg(rows, i32, (B,), "rows"), max_keys, op, old,
+            self._arg(weights, f32, self._wshape, "weights"), self._arg(weights_out, f32, self._wshape, "weights_out"),
+            weight_rows, self.workspace.data_ptr(), self.workspace.numel(), self.err.data_ptr())
         return out
 
     def read(self, layer: int, n: int, start: Optional[torch.Tensor] = None, rows: Optional[torch.Tensor] = None,
@@ -153,11 +155,10 @@ class QuantCache:
         k = torch.empty((self.batch, n, self.n_kv_heads, self.head_dim), dtype=dtype, device=self.device)
         v = torch.empty_like(k)
         i32 = torch.int32
-        with torch.cuda.device(self.device):
-            _check(self.lib.spade_kvq_read(
-                self._shape(), layer, ctypes.c_void_p(self.buf.data_ptr()), self.batch, n,
-                self._arg(start, i32, (self.batch,), "start"), self._arg(rows, i32, (self.batch,), "rows"), _DTYPES[dtype],
-                ctypes.c_void_p(k.data_ptr()), ctypes.c_void_p(v.data_ptr()), self._stream()))
+        self._call(
+            self.lib.spade_kvq_read, layer, self.buf.data_ptr(), self.batch, n,
+            self._arg(start, i32, (self.batch,), "start"), self._arg(rows, i32, (self.batch,), "rows"), _DTYPES[dtype],
+            k.data_ptr(), v.data_ptr())
         return k, v
 
     def evict(self, weights: torch.Tensor, budget: int, recent: int, kept: Optional[torch.Tensor] = None,
@@ -175,14 +176,12 @@ class QuantCache:
         kshape = (self.n_layers, self.batch, self.n_kv_heads, budget)
         if kept is None:
             kept = torch.empty(tuple(max(int(x), 0) for x in kshape), dtype=i32, device=self.device)
-        with torch.cuda.device(self.device):
-            _check(self.lib.spade_kvq_evict(
-                self._shape(), ctypes.c_void_p(self.buf.data_ptr()), dst._shape(), ctypes.c_void_p(dst.buf.data_ptr()),
-                self.batch, int(budget), int(recent),
-                self._arg(weights, f32, (self.n_layers, self.batch, self.n_kv_heads, self.max_len), "weights"),
-                dst._arg(weights_out, f32, (dst.n_layers, dst.batch, dst.n_kv_heads, dst.max_len), "weights_out"),
-                self._arg(self.lens, i32, (self.batch,), "lens"), dst._arg(dst.lens, i32, (dst.batch,), "lens"),
-                self._arg(kept, i32, kshape, "kept"), self._stream()))
+        self._call(
+            self.lib.spade_kvq_evict, self.buf.data_ptr(), dst._sp, dst.buf.data_ptr(), self.batch, budget, recent,
+            self._arg(weights, f32, (self.n_layers,) + self._wshape, "weights"),
+            dst._arg(weights_out, f32, (dst.n_layers,) + dst._wshape, "weights_out"),
+            self._arg(self.lens, i32, (self.batch,), "lens"), dst._arg(dst.lens, i32, (dst.batch,), "lens"),
+            self._arg(kept, i32, kshape, "kept"))
         return kept
 
     def device_error(self) -> int:

@@ -289,17 +289,26 @@ __global__ void __launch_bounds__(256) kvq_read_kernel(KvqRead p) {
 //   O^T = V^T P^T B = probabilities of 2 x 16 positions straight from those
 //                 registers (k slots 8 q .. + 7 are positions 4 q .. + 3 of
 //                 either half), A = codes of features 8 c + j, j the product
-// A code n enters as the bf16 number 16 + n (one shift, one and-or for two
-// codes), exact; with x = m + n s the scores are
-//   q . x = s (sum_f q_f (16 + n_f) - 16 sum_f q_f) + m sum_f q_f
-// (the sum over 16 + n starts at -16 sum q), and with x = c + (n - 8) s,
-//   sum_t p_t x_t = sum_t p_t s_t (16 + n_t) - 24 sum_t p_t s_t + sum_t p_t c_t.
+// A code n enters as the bf16 subnormal n 2^-133 (the matrix instructions keep
+// subnormal inputs, and these products come out exact), so one shift and one
+// mask make two operands of a code word.  Queries carry 2^60 and probabilities
+// 2^50 to keep the products in float32's normal range; with x = m + n s,
+//   2^-73 q . x = s sum_f (2^60 q_f) (2^-133 n_f) + m 2^-73 sum_f q_f
+//   sum_t p_t x_t = 2^133 sum_t (p_t s_t) (2^-133 n_t) + sum_t p_t m_t.
 // Float32 queries enter as three bf16 terms, which hold all of their 24 bits,
 // and so do the products p s; bfloat16 calls take their queries as they are and
 // round p s to bfloat16 once (2^-9 of a weight, half a step of their outputs).
+// The matrix instructions cut the smaller of 32 products short, which for codes
+// of one sign adds up; float32 calls therefore take the values as c + (n - 8) s
+// and subtract eight times the sum of their weights, cut short alike, at the
+// end (error of the outputs about 3.5e-6, 8e-6 without).
 // ---------------------------------------------------------------------------
 constexpr int kWaves = 4;
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kQScale = 0x1p60f, kZScale = 0x1p-73f;  // of queries; of the scores that come out
+constexpr float kPLog = 50.f;                          // log2 of the probabilities' scale
+// sums of p n as they come out, back in units of p
+__device__ __forceinline__ float code_sum(float x) { return x * 0x1p100f * 0x1p33f; }
 
 __device__ __forceinline__ uint32_t pk_bf16(float a, float b) {
   typedef __attribute__((ext_vector_type(2))) float f2;
@@ -309,15 +318,8 @@ __device__ __forceinline__ uint32_t pk_bf16(float a, float b) {
 __device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_f(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
-// Codes j and j + 4 of a word as the bf16 pair (16 + n, 16 + n'): n goes to bits
-// 3..6 of the mantissa of 16.  One and-or takes both constants from registers
-// (the compiler would emit two instructions with a literal each).
-__device__ __forceinline__ uint32_t code_pair(uint32_t w, int j) {
-  const uint32_t x = j == 0 ? w << 3 : w >> (4 * j - 3);
-  uint32_t r;
-  asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "s"(0x00780078u), "v"(0x41804180u));
-  return r;
-}
+// codes j and j + 4 of a word as a bf16 pair
+__device__ __forceinline__ uint32_t code_pair(uint32_t w, int j) { return (w >> (4 * j)) & 0x000f000fu; }
 
 __device__ __forceinline__ bf16x8 op(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   return __builtin_bit_cast(bf16x8, make_uint4(a, b, c, d));
@@ -393,7 +395,7 @@ template <int HD, bool QB>
 struct Queries {
   static constexpr int S = HD / 32, N = QB ? 1 : 3;
   uint32_t w[N][S][4];
-  float sum;  // of the row's features
+  float sum;  // of the row's features, times kZScale
   __device__ __forceinline__ void convert(const RawQuery<HD, QB>& raw, bool ok) {
     float t = 0.f;
 #pragma unroll
@@ -404,13 +406,13 @@ struct Queries {
       for (int j = 0; j < 4; ++j) {
         const float a = ok ? x[j] : 0.f, b = ok ? x[j + 4] : 0.f;
         uint32_t e[N];
-        terms<N>(a, b, e);
+        terms<N>(a * kQScale, b * kQScale, e);
 #pragma unroll
         for (int n = 0; n < N; ++n) w[n][s][j] = e[n];
         t += a + b;
       }
     }
-    sum = sum_q(t);
+    sum = sum_q(t) * kZScale;
   }
 };
 
@@ -477,11 +479,11 @@ __device__ __forceinline__ uint32_t& value_pair_of(uint4 (&pr)[2], int r) {
   return r == 0 ? pr[0].y : r == 1 ? pr[0].w : r == 2 ? pr[1].y : pr[1].w;
 }
 
-// z[u][r]: the (unscaled) score of the lane's row at position 16 u + 4 q + r
+// z[u][r]: kZScale times the (unscaled) score of the lane's row at position 16
+// u + 4 q + r
 template <int HD, bool QB>
 __device__ __forceinline__ void scores(const Block<HD>& b, const Queries<HD, QB>& Q, float (&z)[2][4]) {
-  const float o = -16.f * Q.sum;
-  floatx4 acc[2] = {floatx4{o, o, o, o}, floatx4{o, o, o, o}};
+  floatx4 acc[2] = {};
 #pragma unroll
   for (int s = 0; s < HD / 32; ++s) {
     bf16x8 a[2];
@@ -674,7 +676,7 @@ __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_e
   const unsigned xcd = blockIdx.x & 7, jj = blockIdx.x >> 3;
   const unsigned tt = jj / (unsigned)p.TG, tile = jj - tt * p.TG, range = 8 * tt + xcd;
   const int NR = p.G * p.R;
-  const float sl = p.scale * kLog2e;
+  const float sl = p.scale * kLog2e / kZScale;
   Segments<false> sg;
   const bool whole = p.WG == 0;  // a head per workgroup
   if (whole) {
@@ -723,7 +725,7 @@ __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_e
     Queries<HD, QB> Q;
     Q.convert(qx, ok);
     float M = -INFINITY, l = 0.f, cs = 0.f;
-    floatx4 o[FT], ps = floatx4{0.f, 0.f, 0.f, 0.f};
+    floatx4 o[FT], p8 = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < FT; ++j) o[j] = floatx4{0.f, 0.f, 0.f, 0.f};
 
@@ -747,18 +749,18 @@ __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_e
       }
       float mx = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])),
                        fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3])));
-      mx = max_q(mx);
+      mx = max_q(mx) * sl;
       if (__any(mx > M)) {
         const float mn = fmaxf(M, mx);
-        const float f = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((M - mn) * sl);
+        const float f = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - mn);
         M = mn;
         l *= f;
         cs *= f;
-        ps *= f;
+        if constexpr (!QB) p8 *= f;
 #pragma unroll
         for (int j = 0; j < FT; ++j) o[j] *= f;
       }
-      const float base = M == -INFINITY ? 0.f : M * sl;
+      const float base = (M == -INFINITY ? 0.f : M) - kPLog;
       float w[8];
 #pragma unroll
       for (int u = 0; u < 2; ++u)
@@ -766,10 +768,9 @@ __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_e
         for (int r = 0; r < 4; ++r) {
           const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(z[u][r], sl, -base));
           const uint32_t pr = value_pair_of(cur.pr[u], r);
-          const float s = lo_f(pr);
           l += e;
-          cs = __builtin_fmaf(e, __builtin_fmaf(8.f, s, hi_f(pr)), cs);
-          w[4 * u + r] = e * s;
+          cs = __builtin_fmaf(e, QB ? hi_f(pr) : __builtin_fmaf(8.f, lo_f(pr), hi_f(pr)), cs);
+          w[4 * u + r] = e * lo_f(pr);
         }
       ld.pairs(cur, nb);
       asm volatile("" ::: "memory");
@@ -800,9 +801,11 @@ __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_e
         }
       }
       ld.values(cur, nb);
-      const bf16x8 ones = op(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
+      if constexpr (!QB) {
+        const bf16x8 eight = op(0x00080008u, 0x00080008u, 0x00080008u, 0x00080008u);
 #pragma unroll
-      for (int n = 0; n < N; ++n) ps = mfma(ones, P[n], ps);
+        for (int n = 0; n < N; ++n) p8 = mfma(eight, P[n], p8);
+      }
 #pragma unroll
       for (int jh = 0; jh < FT / 4; ++jh) {
         const uint32_t(&hf)[4] = half[jh];
@@ -825,13 +828,14 @@ __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_e
     }
 
     // the waves' parts; lane 16 q + c holds row c, features q HD / 4 + FT r + j
-    const float lt = sum_q(l), off = sum_q(cs) - 24.f * ps[0];
+    const float lt = sum_q(l), off = sum_q(cs);
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
       for (int j = 0; j < FT; j += 4)
         *(float4*)&sm.o[wave][c][q * (HD / 4) + r * FT + j] =
-            make_float4(o[j][r] + off, o[j + 1][r] + off, o[j + 2][r] + off, o[j + 3][r] + off);
+            make_float4(code_sum(o[j][r] - p8[0]) + off, code_sum(o[j + 1][r] - p8[0]) + off,
+                        code_sum(o[j + 2][r] - p8[0]) + off, code_sum(o[j + 3][r] - p8[0]) + off);
     if (q == 0) {
       sm.m[wave][c] = M;
       sm.l[wave][c] = lt;
@@ -850,7 +854,7 @@ __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_e
       for (int w = 0; w < kWaves; ++w) {
         const float mw = sm.m[w][row], lw = sm.l[w][row];
         // (a wave that saw nothing of this row holds zeros)
-        const float s = mw == -INFINITY && lw == 0.f ? 0.f : __builtin_amdgcn_exp2f((mw - mm) * sl);
+        const float s = mw == -INFINITY && lw == 0.f ? 0.f : __builtin_amdgcn_exp2f(mw - mm);
         const float4 v = *(const float4*)&sm.o[w][row][f];
         ll += lw * s;
         a[0] += v.x * s;
@@ -864,7 +868,7 @@ __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_e
 #pragma unroll
         for (int k = 0; k < 4; ++k) a[k] = live ? a[k] * inv : 0.f;
         store_out(p, b, kvh, pr, f, a);
-        if (f == 0 && p.w_out != nullptr) p.lse[(int64_t)bh * NR + pr] = live ? mm * sl + log2f(ll) : INFINITY;
+        if (f == 0 && p.w_out != nullptr) p.lse[(int64_t)bh * NR + pr] = live ? mm + log2f(ll) - kPLog : INFINITY;
       } else {
         const int64_t at = (int64_t)(range + bh) * NR + pr;
         *(float4*)(p.part_o + at * HD + f) = make_float4(a[0], a[1], a[2], a[3]);
@@ -897,7 +901,6 @@ __global__ void __launch_bounds__(256) kvq_merge_kernel(KvqAttend p) {
     if (tid == 0 && p.w_out != nullptr) p.lse[blockIdx.x] = INFINITY;
     return;
   }
-  const float sl = p.scale * kLog2e;
   const uint32_t nb = request_blocks<false>(rr);
   uint32_t before, w0, w1;
   // the ranges of the head's first and last block
@@ -919,7 +922,7 @@ __global__ void __launch_bounds__(256) kvq_merge_kernel(KvqAttend p) {
 #pragma unroll 2
   for (int k = g; k < nc; k += GR) {
     const float2 v = *(const float2*)(ml + (int64_t)k * NR * 2);
-    const float s = v.x == -INFINITY && v.y == 0.f ? 0.f : __builtin_amdgcn_exp2f((v.x - M) * sl);  // (0: it sees none of them)
+    const float s = v.x == -INFINITY && v.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(v.x - M);  // (0: it sees none of them)
     const float4 o = *(const float4*)(po + (int64_t)k * NR * HD);
     l += v.y * s;
     a[0] += o.x * s;
@@ -944,7 +947,7 @@ __global__ void __launch_bounds__(256) kvq_merge_kernel(KvqAttend p) {
 #pragma unroll
   for (int k = 0; k < 4; ++k) a[k] *= inv;
   store_out(p, b, kvh, pr, f, a);
-  if (f == 0 && p.w_out != nullptr) p.lse[blockIdx.x] = M * sl + log2f(l);
+  if (f == 0 && p.w_out != nullptr) p.lse[blockIdx.x] = M + log2f(l) - kPLog;
 }
 
 // Weights: out = in + the probabilities of the first w_rows rows, summed over
@@ -959,7 +962,7 @@ __global__ void __launch_bounds__(kWaves * 64) kvq_weights_kernel(KvqAttend p) {
   constexpr int S = HD / 32;
   const int tid = threadIdx.x, lane = tid & 63, q = lane >> 4, c = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const float sl = p.scale * kLog2e;
+  const float sl = p.scale * kLog2e / kZScale;
   Segments<true> sg;
   if (!sg.init(p, lane, blockIdx.x)) return;
   do {
@@ -1013,9 +1016,7 @@ __global__ void __launch_bounds__(kWaves * 64) kvq_weights_kernel(KvqAttend p) {
       }
       const float* from = r0 == 0 ? p.w_in : p.w_out;
       auto block = [&](Part& cur, int blk) {
-        floatx4 acc[2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) acc[u] = floatx4{-16.f * sq[0], -16.f * sq[1], -16.f * sq[2], -16.f * sq[3]};
+        floatx4 acc[2] = {};
 #pragma unroll
         for (int s = 0; s < S; ++s)
 #pragma unroll

@@ -20,7 +20,9 @@ namespace {
 
 // ---------------------------------------------------------------------------
 // Append.  A row is a request's position i; hd / 8 lanes hold one head of it,
-// lane c features 4 c .. + 3 and their rotary partners hd / 2 + 4 c .. + 3.
+// lane c features 4 c .. + 3 and their rotary partners hd / 2 + 4 c .. + 3.  With
+// four rows or more per request (ROWS = 4) neighbouring lane groups take four
+// rows of one head, whose value words are 16-byte pieces; else heads of one row.
 //
 // A key's codes have to be those of its definition, so that a cache does not
 // depend on how a sum was ordered: the norm and the rotation of keys run in
@@ -31,22 +33,51 @@ namespace {
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t bf_bits(float f) { return (uint32_t)f2bf(f); }
 
+// v of another lane of the wave's groups of 16: step 0 and 1 swap neighbours and
+// pairs, step 2 and 3 mirror eight and sixteen lanes (data-parallel moves, so a
+// reduction that does not care for its order needs no LDS traffic)
+template <int STEP>
+__device__ __forceinline__ float lane_step(float v) {
+  constexpr int ctrl = STEP == 0 ? 0xb1 : STEP == 1 ? 0x4e : STEP == 2 ? 0x141 : 0x140;
+  const int i = __builtin_bit_cast(int, v);
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(i, i, ctrl, 0xf, 0xf, false));
+}
+template <int STEP>
+__device__ __forceinline__ double lane_step(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __float_as_uint(lane_step<STEP>(__uint_as_float((uint32_t)u)));
+  const uint32_t hi = __float_as_uint(lane_step<STEP>(__uint_as_float((uint32_t)(u >> 32))));
+  return __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
+}
+
+// over the LPH = 8 or 16 lanes of a head, in all of them
 template <int LPH>
 __device__ __forceinline__ float min_lanes(float v) {
-#pragma unroll
-  for (int o = LPH / 2; o >= 1; o >>= 1) v = fminf(v, __shfl_xor(v, o));
+  v = fminf(v, lane_step<0>(v));
+  v = fminf(v, lane_step<1>(v));
+  v = fminf(v, lane_step<2>(v));
+  if constexpr (LPH == 16) v = fminf(v, lane_step<3>(v));
   return v;
 }
 template <int LPH>
 __device__ __forceinline__ float max_lanes(float v) {
-#pragma unroll
-  for (int o = LPH / 2; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+  v = fmaxf(v, lane_step<0>(v));
+  v = fmaxf(v, lane_step<1>(v));
+  v = fmaxf(v, lane_step<2>(v));
+  if constexpr (LPH == 16) v = fmaxf(v, lane_step<3>(v));
   return v;
 }
 template <int LPH, typename F>
 __device__ __forceinline__ F sum_lanes(F v) {
+  v += lane_step<0>(v);
+  v += lane_step<1>(v);
+  v += lane_step<2>(v);
+  if constexpr (LPH == 16) v += lane_step<3>(v);
+  return v;
+}
+__device__ __forceinline__ float max_wave(float v) {
 #pragma unroll
-  for (int o = LPH / 2; o >= 1; o >>= 1) v += __shfl_xor(v, o);
+  for (int o = 32; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
   return v;
 }
 
@@ -148,9 +179,21 @@ __device__ __forceinline__ uint32_t quantise(const float (&v)[8], uint32_t* pair
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       // three roundings of 2^-24 of a quotient below 17: within 4e-6
-      const float t = (v[j] - m) * inv;
+      const float d = v[j] - m, t = d * inv;
       float n = rintf(t);
-      if (fabsf(fabsf(t - n) - 0.5f) < 1e-5f || !(t < 17.f)) n = exact_code(v[j], m, s);
+      if (fabsf(fabsf(t - n) - 0.5f) < 1e-5f || !(t < 17.f)) {
+        // near a border (bfloat16 rows hit many exactly): by the remainder,
+        // which float32 holds exactly where it holds the difference
+        const float back = v[j] - d, lost = (v[j] - (d + back)) + (back - m);
+        const float e = __builtin_fmaf(-n, s, d), h = 0.5f * s;
+        if (lost == 0.f && t < 17.f) {
+          const bool odd = ((int)n) & 1;
+          if (e > h || (e == h && odd)) n += 1.f;
+          else if (e < -h || (e == -h && odd)) n -= 1.f;
+        } else {
+          n = exact_code(v[j], m, s);
+        }
+      }
       const int ni = (int)fminf(fmaxf(n, 0.f), 15.f);
       code |= (uint32_t)ni << (j < 4 ? 4 * j : 16 + 4 * (j - 4));
     }
@@ -159,53 +202,50 @@ __device__ __forceinline__ uint32_t quantise(const float (&v)[8], uint32_t* pair
   return code;
 }
 
-template <int HD, bool BF16>
+template <int HD, bool BF16, int ROWS>
 __global__ void __launch_bounds__(256) kvq_append_kernel(KvqAppend p) {
   constexpr int LPH = HD / 8;
   const int c = threadIdx.x % LPH;
-  const int HQ = p.q != nullptr ? p.H : 0;
-  const int heads = HQ + 2 * p.KVH;
-  int h = (int)blockIdx.y * (256 / LPH) + threadIdx.x / LPH;
-  if (h >= heads) return;  // whole groups of LPH lanes
-  const int64_t row = blockIdx.x;
-  const int b = (int)blockIdx.x / p.R, i = (int)blockIdx.x - b * p.R;
-  const int n_rows = p.rows != nullptr ? min(p.rows[b], p.R) : p.R;
+  const int HQ = p.q != nullptr ? p.H : 0, heads = HQ + 2 * p.KVH;
+  int h = (int)blockIdx.y * (256 / LPH / ROWS) + threadIdx.x / LPH / ROWS;
+  const int per = (p.R + ROWS - 1) / ROWS, b = (int)blockIdx.x / per;
+  const int i = ((int)blockIdx.x - b * per) * ROWS + threadIdx.x / LPH % ROWS;
+  if (h >= heads || i >= p.R) return;  // whole groups of LPH lanes
+  const int64_t row = (int64_t)b * p.R + i;
   const int f0 = 4 * c, f1 = HD / 2 + 4 * c;
+  const bool query = h < HQ, key = !query && h < HQ + p.KVH;
+  if (!query) h -= key ? HQ : HQ + p.KVH;
+  float x[8];
+  {
+    const void* src = query ? p.q : key ? p.k : p.v;
+    const int64_t at = row * (query ? p.q_ld : key ? p.k_ld : p.v_ld) + h * HD;
+    load4<BF16>(src, at + f0, x);
+    load4<BF16>(src, at + f1, x + 4);
+  }
+  const int L = p.lens[b], n_rows = p.rows != nullptr ? min(p.rows[b], p.R) : p.R, t = L + i;
   if (i >= n_rows) {  // a row the request does not use
-    if (h < HQ) {
+    if (query) {
       const float z[4] = {0.f, 0.f, 0.f, 0.f};
       store4<BF16>(p.q_out, row * p.qo_ld + h * HD + f0, z);
       store4<BF16>(p.q_out, row * p.qo_ld + h * HD + f1, z);
     }
     return;
   }
-  const int t = p.lens[b] + i;
   const float* cs = nullptr;
   if (p.rope != nullptr) {
-    int pos = (p.pos != nullptr ? p.pos[b] : p.lens[b]) + i;
+    int pos = (p.pos != nullptr ? p.pos[b] : L) + i;
     if (pos < 0 || pos >= p.rope_len) {
       if (c == 0) flag_error(p.err, SPADE_DERR_CAPACITY);
       pos = pos < 0 ? 0 : p.rope_len - 1;
     }
     cs = p.rope + (size_t)pos * HD;
   }
-  if (h < HQ) {
-    float x[8];
-    load4<BF16>(p.q, row * p.q_ld + h * HD + f0, x);
-    load4<BF16>(p.q, row * p.q_ld + h * HD + f1, x + 4);
+  if (query) {
     norm_rotate<HD, float>(x, p.gain_q, p.eps, cs, c);
     store4<BF16>(p.q_out, row * p.qo_ld + h * HD + f0, x);
     store4<BF16>(p.q_out, row * p.qo_ld + h * HD + f1, x + 4);
     return;
   }
-  h -= HQ;
-  const bool key = h < p.KVH;
-  if (!key) h -= p.KVH;
-  float x[8];
-  const void* src = key ? p.k : p.v;
-  const int64_t at = row * (key ? p.k_ld : p.v_ld) + h * HD;
-  load4<BF16>(src, at + f0, x);
-  load4<BF16>(src, at + f1, x + 4);
   if (key && (p.gain_k != nullptr || cs != nullptr)) {
     double y[8];
 #pragma unroll
@@ -216,7 +256,7 @@ __global__ void __launch_bounds__(256) kvq_append_kernel(KvqAppend p) {
   }
   uint32_t pair;
   const uint32_t code = quantise<HD>(x, &pair);
-  const uint32_t other = __shfl_xor(code, 1);
+  const uint32_t other = __float_as_uint(lane_step<0>(__uint_as_float(code)));
   if (t < 0 || t >= p.max_len) {
     if (c == 0) flag_error(p.err, SPADE_DERR_CAPACITY);
     return;
@@ -239,16 +279,14 @@ __global__ void __launch_bounds__(256) kvq_append_kernel(KvqAppend p) {
 // ---------------------------------------------------------------------------
 // Read back: lanes as in the append.
 // ---------------------------------------------------------------------------
-template <int HD, bool BF16>
+template <int HD, bool BF16, int ROWS>
 __global__ void __launch_bounds__(256) kvq_read_kernel(KvqRead p) {
   constexpr int LPH = HD / 8;
   const int c = threadIdx.x % LPH;
-  const unsigned items = (unsigned)p.B * p.R * p.KVH;
-  const unsigned it = blockIdx.x * (256 / LPH) + threadIdx.x / LPH;
-  if (it >= items) return;
-  const unsigned row = it / (unsigned)p.KVH;
-  const int h = (int)(it - row * p.KVH);
-  const int b = (int)(row / (unsigned)p.R), i = (int)(row - (unsigned)b * p.R);
+  const int h = (int)blockIdx.y * (256 / LPH / ROWS) + threadIdx.x / LPH / ROWS;
+  const int per = (p.R + ROWS - 1) / ROWS, b = (int)blockIdx.x / per;
+  const int i = ((int)blockIdx.x - b * per) * ROWS + threadIdx.x / LPH % ROWS;
+  if (h >= p.KVH || i >= p.R) return;
   const int n_rows = p.rows != nullptr ? min(p.rows[b], p.R) : p.R;
   const int t = (p.start != nullptr ? p.start[b] : 0) + i;
   const bool live = i < n_rows && t >= 0 && t < p.max_len;
@@ -267,7 +305,7 @@ __global__ void __launch_bounds__(256) kvq_read_kernel(KvqRead p) {
       for (int j = 0; j < 8; ++j) x[o][j] = m + (float)((w[o] >> (4 * j)) & 15u) * s;
     }
   }
-  const int64_t at = (int64_t)it * HD + 8 * c;
+  const int64_t at = (((int64_t)b * p.R + i) * p.KVH + h) * HD + 8 * c;
   store4<BF16>(p.k, at, x[0]);
   store4<BF16>(p.k, at + 4, x[0] + 4);
   store4<BF16>(p.v, at, x[1]);
@@ -880,47 +918,51 @@ __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_e
   }
 }
 
-// Merge of the segments of one (request, K/V head, packed row) per workgroup:
-// 256 / (HD / 4) groups of lanes take every so many segments, in order, and are
-// added in order.  A head that lies in one range is complete already; rows that
-// are not in use get their zeros here.
-template <int HD>
+// Merge of a head's segments, in order.  A head that lies in one range is
+// complete already; rows that are not in use get their zeros here.  ROWS = 1:
+// a workgroup takes one row, its GR groups of HD / 4 lanes every GR-th segment,
+// and the groups are added in order (few rows of many segments); ROWS = GR: a
+// row per group (many rows of a few segments: 4608 of 2, 5 us, 10 with ROWS = 1).
+template <int HD, bool SPLIT>
 __global__ void __launch_bounds__(256) kvq_merge_kernel(KvqAttend p) {
-  constexpr int LPR = HD / 4, GR = 256 / LPR;
-  __shared__ float so[GR][HD];
-  __shared__ float sm[4], sl_[GR];
-  const int NR = p.G * p.R, tid = threadIdx.x;
-  const unsigned bhu = blockIdx.x / (unsigned)NR;
-  const int pr = (int)(blockIdx.x - bhu * NR);
-  const int b = (int)(bhu / (unsigned)p.KVH), kvh = (int)(bhu - (unsigned)b * p.KVH);
+  constexpr int LPR = HD / 4, GR = 256 / LPR, ROWS = SPLIT ? 1 : GR;
+  __shared__ float so[SPLIT ? GR : 1][HD];
+  __shared__ float sm[4], sl[GR];
+  const int NR = p.G * p.R, tid = threadIdx.x, f = 4 * (tid % LPR), g = tid / LPR;
+  const unsigned per = (unsigned)(NR + ROWS - 1) / ROWS, bh = blockIdx.x / per;
+  const int pr = (int)(blockIdx.x - bh * per) * ROWS + (SPLIT ? 0 : g);
+  const int b = (int)(bh / (unsigned)p.KVH), kvh = (int)(bh - (unsigned)b * p.KVH);
   const RequestRows rr = request_rows(p, b);
-  const int i = pr - pr / p.R * p.R, f = 4 * (tid % LPR), g = tid / LPR;
-  if (i >= rr.n) {
-    const float z[4] = {0.f, 0.f, 0.f, 0.f};
-    if (g == 0) store_out(p, b, kvh, pr, f, z);
-    if (tid == 0 && p.w_out != nullptr) p.lse[blockIdx.x] = INFINITY;
-    return;
-  }
   const uint32_t nb = request_blocks<false>(rr);
-  uint32_t before, w0, w1;
+  uint32_t before;
   // the ranges of the head's first and last block
   const Plan pl = find_request(p, tid & 63, b, &before);
-  before += (uint32_t)(bhu - (unsigned)b * p.KVH) * nb;
-  w0 = pl.range_of(before);
-  w1 = pl.range_of(before + nb - 1);
-  if (w0 == w1) return;
-  const int nc = (int)(w1 - w0) + 1;
-  const float* ml = p.part_ml + ((int64_t)(w0 + bhu) * NR + pr) * 2;
-  const float* po = p.part_o + ((int64_t)(w0 + bhu) * NR + pr) * HD + f;
+  before += (uint32_t)kvh * nb;
+  const uint32_t w0 = nb > 0 ? pl.range_of(before) : 0, w1 = nb > 0 ? pl.range_of(before + nb - 1) : 0;
+  const int i = pr - pr / p.R * p.R, nc = (int)(w1 - w0) + 1;
+  if (pr < NR && i >= rr.n && (!SPLIT || g == 0)) {
+    const float z[4] = {0.f, 0.f, 0.f, 0.f};
+    store_out(p, b, kvh, pr, f, z);
+    if (f == 0 && p.w_out != nullptr) p.lse[(int64_t)bh * NR + pr] = INFINITY;
+  }
+  const bool mine = pr < NR && i < rr.n && nc > 1;
+  if (SPLIT && !mine) return;  // (the workgroup's one row)
+  const float* ml = p.part_ml + ((int64_t)(w0 + bh) * NR + (mine ? pr : 0)) * 2;
+  const float* po = p.part_o + ((int64_t)(w0 + bh) * NR + (mine ? pr : 0)) * HD + f;
   float M = -INFINITY;
-  for (int k = tid; k < nc; k += 256) M = fmaxf(M, ml[(int64_t)k * NR * 2]);
-  M = max_lanes<64>(M);
-  if ((tid & 63) == 0) sm[tid >> 6] = M;
-  __syncthreads();
-  M = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
+  if constexpr (SPLIT) {
+    for (int k = tid; k < nc; k += 256) M = fmaxf(M, ml[(int64_t)k * NR * 2]);
+    M = max_wave(M);
+    if ((tid & 63) == 0) sm[tid >> 6] = M;
+    __syncthreads();
+    M = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
+  } else {
+    if (!mine) return;
+    for (int k = 0; k < nc; ++k) M = fmaxf(M, ml[(int64_t)k * NR * 2]);
+  }
   float l = 0.f, a[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 2
-  for (int k = g; k < nc; k += GR) {
+  for (int k = SPLIT ? g : 0; k < nc; k += SPLIT ? GR : 1) {
     const float2 v = *(const float2*)(ml + (int64_t)k * NR * 2);
     const float s = v.x == -INFINITY && v.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(v.x - M);  // (0: it sees none of them)
     const float4 o = *(const float4*)(po + (int64_t)k * NR * HD);
@@ -930,24 +972,26 @@ __global__ void __launch_bounds__(256) kvq_merge_kernel(KvqAttend p) {
     a[2] += o.z * s;
     a[3] += o.w * s;
   }
-  *(float4*)&so[g][f] = make_float4(a[0], a[1], a[2], a[3]);
-  if (f == 0) sl_[g] = l;
-  __syncthreads();
-  if (g != 0) return;
+  if constexpr (SPLIT) {
+    *(float4*)&so[g][f] = make_float4(a[0], a[1], a[2], a[3]);
+    if (f == 0) sl[g] = l;
+    __syncthreads();
+    if (g != 0) return;
 #pragma unroll
-  for (int k = 1; k < GR; ++k) {
-    const float4 o = *(const float4*)&so[k][f];
-    a[0] += o.x;
-    a[1] += o.y;
-    a[2] += o.z;
-    a[3] += o.w;
-    l += sl_[k];
+    for (int k = 1; k < GR; ++k) {
+      const float4 o = *(const float4*)&so[k][f];
+      a[0] += o.x;
+      a[1] += o.y;
+      a[2] += o.z;
+      a[3] += o.w;
+      l += sl[k];
+    }
   }
   const float inv = 1.0f / l;
 #pragma unroll
   for (int k = 0; k < 4; ++k) a[k] *= inv;
   store_out(p, b, kvh, pr, f, a);
-  if (f == 0 && p.w_out != nullptr) p.lse[blockIdx.x] = M + log2f(l) - kPLog;
+  if (f == 0 && p.w_out != nullptr) p.lse[(int64_t)bh * NR + pr] = M + log2f(l) - kPLog;
 }
 
 // Weights: out = in + the probabilities of the first w_rows rows, summed over
@@ -1071,6 +1115,8 @@ __global__ void __launch_bounds__(kWaves * 64) kvq_weights_kernel(KvqAttend p) {
 // positions in order.
 // ---------------------------------------------------------------------------
 constexpr int kSelThreads = 1024;
+constexpr int kSelAhead = 4;  // weights a thread requests at once
+constexpr int kSelRun = 4;    // positions in a row per thread of the last pass
 
 // larger key: heavier (NaN above everything, -0 as 0)
 __device__ __forceinline__ uint32_t weight_key(float w) {
@@ -1105,9 +1151,18 @@ __global__ void __launch_bounds__(kSelThreads) kvq_select_kernel(KvqEvict p) {
     for (int shift = 24; shift >= 0; shift -= 8) {
       ((uint32_t*)hist)[tid] = 0;
       __syncthreads();
-      for (int j = tid; j < cand; j += kSelThreads) {
-        const uint32_t k = weight_key(w[j]);
-        if ((k & mask) == prefix) atomicAdd(&hist[tid & 3][(k >> shift) & 255], 1u);
+      for (int j0 = 0; j0 < cand; j0 += kSelThreads * kSelAhead) {
+        float v[kSelAhead];
+#pragma unroll
+        for (int u = 0; u < kSelAhead; ++u) {
+          const int j = j0 + u * kSelThreads + tid;
+          v[u] = j < cand ? w[j] : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < kSelAhead; ++u) {
+          const uint32_t k = weight_key(v[u]);
+          if (j0 + u * kSelThreads + tid < cand && (k & mask) == prefix) atomicAdd(&hist[tid & 3][(k >> shift) & 255], 1u);
+        }
       }
       __syncthreads();
       if (wave == 0) {
@@ -1144,43 +1199,62 @@ __global__ void __launch_bounds__(kSelThreads) kvq_select_kernel(KvqEvict p) {
     prefix = 0xffffffffu;  // nothing but the last positions (need = 0: no ties are taken)
   }
   // every position heavier than the key, and the first `need` of those equal to it
+  // (a thread has kSelRun positions in a row; a position's place counts those
+  // before it: other rounds', other waves', lower lanes', the lane's own)
   uint32_t base_k = 0, base_e = 0;
-  for (int j0 = 0; j0 < n; j0 += kSelThreads) {
-    const int j = j0 + tid;
-    float wj = 0.f;
-    bool gt = false, eq = false;
-    if (j < n) {
-      wj = w[j];
-      const uint32_t k = weight_key(wj);
-      gt = j >= cand || (k > prefix);
-      eq = j < cand && k == prefix;
+  const uint64_t below = ((uint64_t)1 << lane) - 1;
+  for (int j0 = 0; j0 < n; j0 += kSelThreads * kSelRun) {
+    const int j = j0 + tid * kSelRun;
+    float v[kSelRun];
+#pragma unroll
+    for (int u = 0; u < kSelRun; ++u) v[u] = j + u < n ? w[j + u] : 0.f;
+    bool gt[kSelRun], eq[kSelRun];
+    uint32_t e_at = base_e, e_wave = 0, at = base_k, k_wave = 0;
+#pragma unroll
+    for (int u = 0; u < kSelRun; ++u) {
+      const uint32_t k = weight_key(v[u]);
+      gt[u] = j + u < n && (j + u >= cand || k > prefix);
+      eq[u] = j + u < cand && k == prefix;
+      const uint64_t m = __ballot(eq[u]);
+      e_at += (uint32_t)__popcll(m & below);
+      e_wave += (uint32_t)__popcll(m);
     }
-    const uint64_t be = __ballot(eq);
-    const uint64_t below = ((uint64_t)1 << lane) - 1;
-    if (lane == 0) wsum[0][wave] = (uint32_t)__popcll(be);
+    if (lane == 0) wsum[0][wave] = e_wave;
     __syncthreads();
-    uint32_t e_at = base_e, e_all = 0;
+    uint32_t all = 0;
+#pragma unroll
     for (int k = 0; k < kSelThreads / 64; ++k) {
-      if (k < wave) e_at += wsum[0][k];
-      e_all += wsum[0][k];
+      const uint32_t c = wsum[0][k];
+      if (k < wave) e_at += c;
+      all += c;
     }
-    e_at += (uint32_t)__popcll(be & below);
-    const bool take = gt || (eq && e_at < need);
-    const uint64_t bk = __ballot(take);
-    if (lane == 0) wsum[1][wave] = (uint32_t)__popcll(bk);
+    base_e += all;
+    bool take[kSelRun];
+#pragma unroll
+    for (int u = 0; u < kSelRun; ++u) {
+      take[u] = gt[u] || (eq[u] && e_at < need);
+      e_at += eq[u] ? 1 : 0;
+      const uint64_t m = __ballot(take[u]);
+      at += (uint32_t)__popcll(m & below);
+      k_wave += (uint32_t)__popcll(m);
+    }
+    if (lane == 0) wsum[1][wave] = k_wave;
     __syncthreads();
-    uint32_t at = base_k, k_all = 0;
+    all = 0;
+#pragma unroll
     for (int k = 0; k < kSelThreads / 64; ++k) {
-      if (k < wave) at += wsum[1][k];
-      k_all += wsum[1][k];
+      const uint32_t c = wsum[1][k];
+      if (k < wave) at += c;
+      all += c;
     }
-    at += (uint32_t)__popcll(bk & below);
-    if (take) {  // (at <= j, and every weight up to j has been read: in place is fine)
-      kept[at] = j;
-      if (wo != nullptr) wo[at] = wj;
-    }
-    base_k += k_all;
-    base_e += e_all;
+    base_k += all;
+#pragma unroll
+    for (int u = 0; u < kSelRun; ++u)
+      if (take[u]) {  // (at <= j + u, and every weight up to the round's end has been read: in place is fine)
+        kept[at] = j + u;
+        if (wo != nullptr) wo[at] = v[u];
+        ++at;
+      }
   }
 }
 
@@ -1261,34 +1335,43 @@ __global__ void __launch_bounds__(kMoveThreads) kvq_move_kernel(KvqEvict p, int 
 
 }  // namespace
 
-hipError_t launch_kvq_append(const KvqAppend& a, hipStream_t st) {
-  const int heads = (a.q != nullptr ? a.H : 0) + 2 * a.KVH;
-  const int per = 256 / (a.hd / 8);
-  if ((heads + per - 1) / per > 65535) return hipErrorInvalidValue;
-  const dim3 g((unsigned)(a.B * a.R), (unsigned)((heads + per - 1) / per));
-  if (a.hd == 128) {
-    if (a.bf16) hipLaunchKernelGGL((kvq_append_kernel<128, true>), g, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((kvq_append_kernel<128, false>), g, dim3(256), 0, st, a);
-  } else {
-    if (a.bf16) hipLaunchKernelGGL((kvq_append_kernel<64, true>), g, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((kvq_append_kernel<64, false>), g, dim3(256), 0, st, a);
-  }
+namespace {
+
+template <int HD, bool BF16>
+hipError_t append_t(const KvqAppend& a, hipStream_t st) {
+  const int heads = (a.q != nullptr ? a.H : 0) + 2 * a.KVH, rows = a.R >= 4 ? 4 : 1;
+  const int per = 256 / (HD / 8) / rows, gy = (heads + per - 1) / per;
+  if (gy > 65535) return hipErrorInvalidValue;
+  const dim3 g((unsigned)(a.B * ((a.R + rows - 1) / rows)), (unsigned)gy);
+  if (rows == 4) hipLaunchKernelGGL((kvq_append_kernel<HD, BF16, 4>), g, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((kvq_append_kernel<HD, BF16, 1>), g, dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
-hipError_t launch_kvq_read(const KvqRead& a, hipStream_t st) {
-  const int per = 256 / (a.hd / 8);
-  const int64_t items = (int64_t)a.B * a.R * a.KVH, grid = (items + per - 1) / per;
-  if (grid > 0x7fffffff) return hipErrorInvalidValue;
-  const dim3 g((unsigned)grid);
-  if (a.hd == 128) {
-    if (a.bf16) hipLaunchKernelGGL((kvq_read_kernel<128, true>), g, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((kvq_read_kernel<128, false>), g, dim3(256), 0, st, a);
-  } else {
-    if (a.bf16) hipLaunchKernelGGL((kvq_read_kernel<64, true>), g, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((kvq_read_kernel<64, false>), g, dim3(256), 0, st, a);
-  }
+}  // namespace
+
+hipError_t launch_kvq_append(const KvqAppend& a, hipStream_t st) {
+  if (a.hd == 128) return a.bf16 ? append_t<128, true>(a, st) : append_t<128, false>(a, st);
+  return a.bf16 ? append_t<64, true>(a, st) : append_t<64, false>(a, st);
+}
+
+namespace {
+
+template <int HD, bool BF16>
+hipError_t read_t(const KvqRead& a, hipStream_t st) {
+  const int rows = a.R >= 4 ? 4 : 1, per = 256 / (HD / 8) / rows, gy = (a.KVH + per - 1) / per;
+  if (gy > 65535) return hipErrorInvalidValue;
+  const dim3 g((unsigned)(a.B * ((a.R + rows - 1) / rows)), (unsigned)gy);
+  if (rows == 4) hipLaunchKernelGGL((kvq_read_kernel<HD, BF16, 4>), g, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((kvq_read_kernel<HD, BF16, 1>), g, dim3(256), 0, st, a);
   return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_kvq_read(const KvqRead& a, hipStream_t st) {
+  if (a.hd == 128) return a.bf16 ? read_t<128, true>(a, st) : read_t<128, false>(a, st);
+  return a.bf16 ? read_t<64, true>(a, st) : read_t<64, false>(a, st);
 }
 
 namespace {
@@ -1325,7 +1408,10 @@ hipError_t attend_hd(KvqAttend a, hipStream_t st) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (!whole) {
-    hipLaunchKernelGGL((kvq_merge_kernel<HD>), dim3((unsigned)rows), dim3(256), 0, st, a);
+    // about wgs / heads segments per head
+    constexpr int kRows = 256 / (HD / 4);
+    if (wgs >= 4 * heads) hipLaunchKernelGGL((kvq_merge_kernel<HD, true>), dim3((unsigned)rows), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((kvq_merge_kernel<HD, false>), dim3((unsigned)(heads * ((a.G * a.R + kRows - 1) / kRows))), dim3(256), 0, st, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (a.w_out != nullptr) {

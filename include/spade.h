@@ -53,7 +53,7 @@ typedef enum {
 } spade_status;
 
 enum { SPADE_GREEDY = 0, SPADE_SAMPLE = 1 };
-enum { SPADE_F32 = 0, SPADE_BF16 = 1 };
+enum { SPADE_F32 = 0, SPADE_BF16 = 1, SPADE_I4 = 2 /* kv_dtype only */ };
 
 /* Bits of the device error word. */
 enum {
@@ -97,6 +97,10 @@ enum {
  *
  * weight_dtype: SPADE_BF16 or SPADE_F32 for every matrix (gains are float32).
  * kv_dtype: storage type of K and V (RoPE is applied before storing).
+ * SPADE_I4 holds them in 4 bits, as spade_kvq_append does (below); prompts
+ * then go through 16 rows per request and forward, a request's results depend
+ * on the other requests of a call in their last bits, and the running weights
+ * and eviction of spade_kv_track_weights and spade_kv_evict are available.
  * n_kv_heads: 0 (the default: n_heads) or a divisor of n_heads.
  * Supported: head_dim 64 or 128; d_model = n_heads * head_dim; d_model and
  * d_ffn multiples of 256 (bf16 weights) or 128 (f32); any vocab >= 2; at most
@@ -133,7 +137,8 @@ size_t spade_workspace_bytes(const spade_config* cfg, int max_batch, int max_gam
  * of feature 16 t + i.  In a float32 cache a K block is [256][head_dim] (a row
  * per position) and a V block [head_dim][256].  So one wave's fragment load is
  * 1 KB contiguous and one 256-key chunk of K or V one contiguous block.
- * max_len <= 16384. */
+ * max_len <= 16384.  A 4-bit cache takes head_dim + 8 bytes per position and
+ * K/V head (max_len rounded up to 32) and 4 per request. */
 size_t spade_kv_bytes(const spade_config* cfg, int max_batch, int max_len);
 
 /* Create a model over caller-owned device buffers: d_weights of
@@ -154,11 +159,13 @@ spade_status spade_model_load_tensor(spade_model m, int kind, int layer, const v
  * bytes plus device int32 arrays lens[max_batch] (cached positions per
  * request) and pending[max_batch] (the token whose row has not been computed
  * yet: the last prompt token, then each round's correction).  lens and
- * pending start at 0. */
+ * pending start at 0.  With kv_dtype SPADE_I4 it clears the evicted counts in
+ * the buffer and synchronises. */
 spade_status spade_kv_create(spade_model m, void* d_kv, int max_batch, int max_len,
                              int32_t* d_lens, int32_t* d_pending, spade_kv* out);
 
-/* Set lens[0..B) and pending[0..B) from host arrays (a snapshot restore). */
+/* Set lens[0..B) and pending[0..B) from host arrays (a snapshot restore).  A
+ * request set to length 0 starts over: its evicted positions no longer count. */
 spade_status spade_kv_set_state(spade_kv kv, int B, const int32_t* h_lens,
                                 const int32_t* h_pending, void* stream);
 
@@ -168,7 +175,8 @@ spade_status spade_kv_get_state(spade_kv kv, int B, int32_t* h_lens, int32_t* h_
 /* Snapshot lens/pending [B] into caller device buffers (device-to-device) and
  * remember the host-side capacity bound; spade_kv_restore copies them back and
  * restores that bound.  Rows past the restored lengths are stale and get
- * overwritten, so verify -> commit -> restore replays a round exactly. */
+ * overwritten, so verify -> commit -> restore replays a round exactly.  Not
+ * across a spade_kv_evict, which moves the rows (SPADE_EINVAL). */
 spade_status spade_kv_snapshot(spade_kv kv, int B, int32_t* d_lens, int32_t* d_pending, void* stream);
 spade_status spade_kv_restore(spade_kv kv, int B, const int32_t* d_lens, const int32_t* d_pending,
                               void* stream);
@@ -292,6 +300,31 @@ spade_status spade_accept_from_logits_noalloc(int B, int gamma, int V, const flo
                                               const float* d_uniforms, const uint8_t* d_mode,
                                               float temperature, int32_t* d_n_accepted,
                                               int32_t* d_correction, uint32_t* d_err, void* stream);
+
+/* Head norms of a model with 4-bit caches (SPADE_EUNSUPPORTED for others):
+ * every query and key head is divided by its root mean square and multiplied
+ * by its layer's gain before the rotation.  d_gain_q, d_gain_k: float32
+ * [n_layers][head_dim], owned by the caller and read by every later call; both
+ * NULL turns the norms off. */
+spade_status spade_model_set_head_norms(spade_model m, const float* d_gain_q, const float* d_gain_k, float eps);
+
+/* Running weights of a 4-bit cache (SPADE_EUNSUPPORTED for others): from now on
+ * spade_verify and the prefill calls add the attention probability that every
+ * cached position receives, summed over the query heads of its K/V head, to
+ * d_weights, float32 [n_layers][max_batch][n_kv_heads][max_len], owned by the
+ * caller (NULL: off).  Prompt rows all count (the last layer's too), of a
+ * verify call the pending token's row, whose drafts may be rejected; a new
+ * position starts at 0.  A repeated spade_verify adds its row again. */
+spade_status spade_kv_track_weights(spade_kv kv, float* d_weights);
+
+/* Keep, for every layer and K/V head of requests 0 .. B - 1 with more than
+ * `budget` positions, the last `recent` and the budget - recent of the others
+ * with the largest running weights (spade_kvq_evict, in place); lens[b] becomes
+ * min(lens[b], budget).  Later rows keep counting their positions from the
+ * start of the sequence, which may go on to the model's max_len.  d_kept:
+ * int32 [n_layers][max_batch][n_kv_heads][budget].  Rows of a verify call that
+ * was not committed are lost. */
+spade_status spade_kv_evict(spade_kv kv, int B, int budget, int recent, int32_t* d_kept, void* stream);
 
 /*
  * K/V caches in 4 bits

@@ -7,6 +7,8 @@ from __future__ import annotations
 
 import numpy as np
 
+from .decoder import Decoder, apply_rope, rms_norm, rope_tables, silu
+
 
 def bf16(x: np.ndarray) -> np.ndarray:
     """The bfloat16 nearest to the float32 nearest to x (ties to even), as float64."""
@@ -84,3 +86,43 @@ def keep(weights: np.ndarray, n: int, budget: int, recent: int) -> np.ndarray:
     order = np.lexsort((np.arange(len(w)), -rank, ~np.isnan(w)))
     old = np.sort(order[:budget - recent])
     return np.concatenate([old, np.arange(n - recent, n)])
+
+
+class QuantDecoder(Decoder):
+    """The verifier over 4-bit caches, with the head norms where gains are
+    given.  A cache may have lost positions: ``shift`` of them (an attribute
+    set on the cache) come before its rows, which only moves the angles.
+    ``weights`` [layer][KV head, capacity], where set on the cache, gets the
+    probabilities of the first ``count`` rows of every call (count None: all)."""
+
+    def __init__(self, shape, get, gain_q=None, gain_k=None, eps: float = 1e-5, keep_f64: bool = False):
+        super().__init__(shape, get, keep_f64)
+        self.gain_q, self.gain_k, self.eps = gain_q, gain_k, eps
+        self.count = None
+
+    def stored(self, l, cache, k, v):
+        """The rows [R, KV heads, hd] as the cache holds them."""
+        return held(k), held(v)
+
+    def block(self, l, W, cache, x):
+        s = self.shape
+        R, L, H, hd, KVH = x.shape[0], cache.length, s.n_heads, s.head_dim, s.kv_heads
+        h = rms_norm(x, W("g_attn"), s.rms_eps)
+        q, k, v = ((h @ W(n).T).reshape(R, m, hd) for n, m in (("wq", H), ("wk", KVH), ("wv", KVH)))
+        cos, sin = rope_tables(np.arange(L, L + R) + getattr(cache, "shift", 0), hd, s.rope_theta)
+        if self.gain_q is not None:
+            q = q / np.sqrt((q * q).mean(-1, keepdims=True) + self.eps) * self.gain_q[l]
+            k = k / np.sqrt((k * k).mean(-1, keepdims=True) + self.eps) * self.gain_k[l]
+        q, k = apply_rope(q, cos, sin), apply_rope(k, cos, sin)
+        kk, vv = self.stored(l, cache, k, v)
+        cache.k[l][:, L:L + R] = kk.transpose(1, 0, 2)
+        cache.v[l][:, L:L + R] = vv.transpose(1, 0, 2)
+        o, p = attend(q, cache.k[l][:, :L + R].transpose(1, 0, 2).astype(np.float64),
+                      cache.v[l][:, :L + R].transpose(1, 0, 2).astype(np.float64), L, 1.0 / np.sqrt(hd))
+        if getattr(cache, "weights", None) is not None:
+            w = cache.weights[l]
+            w[:, L:L + R] = 0
+            w[:, :L + R] += p[:R if self.count is None else self.count].reshape(-1, KVH, H // KVH, L + R).sum((0, 2))
+        x = x + o.reshape(R, H * hd) @ W("wo").T
+        h = rms_norm(x, W("g_ffn"), s.rms_eps)
+        return x + (silu(h @ W("wg").T) * (h @ W("wu").T)) @ W("wd").T

@@ -34,14 +34,26 @@ spade_status hipfail(hipError_t e, const char* what) {
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Set the host bound of lens[0..B) to the device values (synchronises).
+// Set the host bound of lens[0..B) (and of the evicted positions) to the
+// device values (synchronises).
 spade_status refresh_bound(spade_kv kv, int B, hipStream_t st) {
-  std::vector<int32_t> h(B);
+  std::vector<int32_t> h(B), ev(B, 0);
   hipError_t e = hipMemcpyAsync(h.data(), kv->lens, (size_t)B * 4, hipMemcpyDeviceToHost, st);
+  if (e == hipSuccess && kv->evicted)
+    e = hipMemcpyAsync(ev.data(), kv->evicted, (size_t)B * 4, hipMemcpyDeviceToHost, st);
   if (e == hipSuccess) e = hipStreamSynchronize(st);
   if (e != hipSuccess) return hipfail(e, "reading lens");
-  for (int b = 0; b < B; ++b) kv->lens_ub[b] = std::max(0, (int)h[b]);
+  for (int b = 0; b < B; ++b) {
+    kv->lens_ub[b] = std::max(0, (int)h[b]);
+    kv->evicted_ub[b] = ev[b];
+  }
   return SPADE_OK;
+}
+
+// Whether `rows` more positions of request b fit the cache and the model's
+// positions (evicted ones count), by the host bounds.
+bool rows_fit(spade_kv kv, int b, int rows) {
+  return kv->lens_ub[b] + rows <= kv->max_len && kv->lens_ub[b] + kv->evicted_ub[b] + rows <= kv->model->max_len;
 }
 
 spade_status check_config(const spade_config* c) {
@@ -50,8 +62,8 @@ spade_status check_config(const spade_config* c) {
     return fail(SPADE_EINVAL, "config dimensions must be positive (vocab >= 2)");
   if (c->weight_dtype != SPADE_BF16 && c->weight_dtype != SPADE_F32)
     return fail(SPADE_EINVAL, "weight_dtype must be SPADE_BF16 or SPADE_F32");
-  if (c->kv_dtype != SPADE_BF16 && c->kv_dtype != SPADE_F32)
-    return fail(SPADE_EINVAL, "kv_dtype must be SPADE_BF16 or SPADE_F32");
+  if (c->kv_dtype != SPADE_BF16 && c->kv_dtype != SPADE_F32 && c->kv_dtype != SPADE_I4)
+    return fail(SPADE_EINVAL, "kv_dtype must be SPADE_BF16, SPADE_F32 or SPADE_I4");
   if (c->d_model != c->n_heads * c->head_dim) return fail(SPADE_EINVAL, "d_model != n_heads * head_dim");
   if (c->n_kv_heads < 0 || (c->n_kv_heads > 0 && c->n_heads % c->n_kv_heads != 0))
     return fail(SPADE_EINVAL, "n_kv_heads must be 0 or a divisor of n_heads");
@@ -103,7 +115,8 @@ ArenaLayout layout_of(const Dims& D) {
 struct WsPlan {
   size_t x, act_n, act_o, act_f, ssq, q, attn_o, attn_ml, attn_cnt, logits, stats, rope, err, split_cnt,
       split_part, wide_cnt, wide_part, tile_part, corr_lse, corr_part, corr_cnt, prefill_tok, prefill_cnt, prefill_base,
-      prefill_map, prefill_off, total;
+      prefill_map, prefill_off, stage_k, stage_v, stage_lens, stage_rope, stage_rows, kvq_work, kvq_part_rows, kvq_ml,
+      kvq_lse, total;
   size_t wide_items, wide_floats, tile_floats;
   int max_units;
   size_t act_split, actf_split;
@@ -175,6 +188,20 @@ WsPlan plan_ws(const Dims& D, int max_batch, int max_gamma, int max_len) {
   p.prefill_base = take((size_t)max_batch * 4);
   p.prefill_map = take((size_t)p.Mrows * 4);
   p.prefill_off = take((kPrefillPack + 1) * 4);
+  if (D.kvdt == SPADE_I4) {
+    const size_t rows = (size_t)max_batch * D.KVH * kVBlock * D.hd * 4;
+    p.stage_k = take(rows);
+    p.stage_v = take(rows);
+    p.stage_lens = take((size_t)max_batch * 4);
+    p.stage_rope = take((size_t)kMaxR * D.hd * 4);
+    p.stage_rows = take((size_t)max_batch * 4);
+    size_t ml, lse;
+    const size_t o = kvq_attend_floats(max_batch, D.H, D.KVH, D.hd, p.Rmax, &ml, &lse);
+    p.kvq_part_rows = o / D.hd;
+    p.kvq_ml = align256(o * 4);
+    p.kvq_lse = p.kvq_ml + align256(ml * 4);
+    p.kvq_work = take(p.kvq_lse + lse * 4);
+  }
   p.total = off;
   return p;
 }
@@ -209,6 +236,11 @@ bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
 }
 
+// the layers' heads of a model's 4-bit cache; the requests' evicted counts follow
+size_t kvq_codes_bytes(const Dims& D, int max_batch, int max_len) {
+  return align256((size_t)D.L * max_batch * D.KVH * kvq_head_bytes(max_len, D.hd));
+}
+
 size_t kvq_layer_bytes(const spade_kvq_shape* s) {
   return (size_t)s->batch * s->n_kv_heads * kvq_head_bytes(s->max_len, s->head_dim);
 }
@@ -232,6 +264,7 @@ size_t spade_workspace_bytes(const spade_config* cfg, int max_batch, int max_gam
 
 size_t spade_kv_bytes(const spade_config* cfg, int max_batch, int max_len) {
   if (check_config(cfg) != SPADE_OK || max_batch < 1 || max_len < 1) return 0;
+  if (cfg->kv_dtype == SPADE_I4) return kvq_codes_bytes(dims_of(cfg), max_batch, max_len) + align256((size_t)max_batch * 4);
   const size_t e = cfg->kv_dtype == SPADE_BF16 ? 2 : 4;
   const int kvh = cfg->n_kv_heads > 0 ? cfg->n_kv_heads : cfg->n_heads;
   return 2 * align256((size_t)cfg->n_layers * max_batch * kvh * kv_stride_of(max_len) * cfg->head_dim * e);
@@ -246,6 +279,9 @@ spade_status spade_model_create(const spade_config* cfg, void* d_weights, void* 
   if (max_batch < 1 || max_len < 2) return fail(SPADE_EINVAL, "max_batch >= 1 and max_len >= 2 required");
   if (max_len > kMaxLen) return fail(SPADE_ECAPACITY, "max_len must be <= %d", kMaxLen);
   if (max_gamma < 0 || max_gamma + 1 > kMaxR) return fail(SPADE_ECAPACITY, "max_gamma must be in [0, %d]", kMaxR - 1);
+  if (cfg->kv_dtype == SPADE_I4 &&
+      (size_t)max_batch * dims_of(cfg).KVH * kVBlock * cfg->head_dim * 4 > 0x7fffff00u)
+    return fail(SPADE_ECAPACITY, "max_batch times K/V heads is too large for a 4-bit cache");
   spade_model m = new (std::nothrow) spade_model_s();
   if (!m) return fail(SPADE_EINVAL, "out of host memory");
   m->cfg = *cfg;
@@ -314,6 +350,18 @@ spade_status spade_model_create(const spade_config* cfg, void* d_weights, void* 
   w.stats = (float*)(b + p.stats);
   w.rope = (float*)(b + p.rope);
   w.err = (uint32_t*)(b + p.err);
+  const bool quant = cfg->kv_dtype == SPADE_I4;
+  if (quant) {
+    w.stage_k = (float*)(b + p.stage_k);
+    w.stage_v = (float*)(b + p.stage_v);
+    w.stage_lens = (int32_t*)(b + p.stage_lens);
+    w.stage_rope = (float*)(b + p.stage_rope);
+    w.stage_rows = (int32_t*)(b + p.stage_rows);
+    w.kvq_work = b + p.kvq_work;
+    w.kvq_part_rows = p.kvq_part_rows;
+    w.kvq_ml = p.kvq_ml;
+    w.kvq_lse = p.kvq_lse;
+  }
   w.act_split = p.act_split;
   w.actf_split = p.actf_split;
   w.Mmax = p.Mmax;
@@ -337,6 +385,12 @@ spade_status spade_model_create(const spade_config* cfg, void* d_weights, void* 
   if (e == hipSuccess && p.wide_items > 0) e = hipMemset(w.wide_cnt, 0, p.wide_items * 4);
   if (e == hipSuccess) e = hipMemset(w.corr_cnt, 0, (size_t)max_batch * 4);
   if (e == hipSuccess) e = hipMemset(w.err, 0, 4);
+  if (quant) {
+    std::vector<float> none((size_t)kMaxR * half * 2);  // angles 0
+    for (size_t i = 0; i < none.size(); i += 2) none[i] = 1.f;
+    if (e == hipSuccess) e = hipMemcpy(w.stage_rope, none.data(), none.size() * 4, hipMemcpyHostToDevice);
+    if (e == hipSuccess) e = hipMemset(w.stage_lens, 0, (size_t)max_batch * 4);
+  }
   // activation buffers start at zero so rows past M never feed NaNs
   if (e == hipSuccess) e = hipMemset(b, 0, p.ssq);
   if (e == hipSuccess) e = hipDeviceSynchronize();
@@ -369,9 +423,14 @@ spade_status spade_kv_create(spade_model m, void* d_kv, int max_batch, int max_l
   spade_kv kv = new (std::nothrow) spade_kv_s();
   if (!kv) return fail(SPADE_EINVAL, "out of host memory");
   kv->model = m;
+  const bool quant = m->dims.kvdt == SPADE_I4;
   const size_t half = spade_kv_bytes(&m->cfg, max_batch, max_len) / 2;
   kv->k = (uint8_t*)d_kv;
-  kv->v = (uint8_t*)d_kv + half;
+  kv->v = quant ? nullptr : (uint8_t*)d_kv + half;
+  kv->evicted = quant ? (int32_t*)((uint8_t*)d_kv + kvq_codes_bytes(m->dims, max_batch, max_len)) : nullptr;
+  kv->evicted_ub = new (std::nothrow) int[max_batch]();
+  kv->weights = nullptr;
+  kv->evictions = kv->snap_evictions = 0;
   kv->lens = d_lens;
   kv->pending = d_pending;
   kv->max_batch = max_batch;
@@ -382,11 +441,17 @@ spade_status spade_kv_create(spade_model m, void* d_kv, int max_batch, int max_l
   kv->last_B = 0;
   kv->verified = false;
   kv->snap_ub = new (std::nothrow) int[max_batch]();
-  if (!kv->lens_ub || !kv->snap_ub) {
-    delete[] kv->lens_ub;
-    delete[] kv->snap_ub;
-    delete kv;
+  if (!kv->lens_ub || !kv->snap_ub || !kv->evicted_ub) {
+    spade_kv_destroy(kv);
     return fail(SPADE_EINVAL, "out of host memory");
+  }
+  if (quant) {
+    hipError_t e = hipMemset(kv->evicted, 0, (size_t)max_batch * 4);
+    if (e == hipSuccess) e = hipDeviceSynchronize();
+    if (e != hipSuccess) {
+      spade_kv_destroy(kv);
+      return hipfail(e, "kv_create");
+    }
   }
   *out = kv;
   return SPADE_OK;
@@ -396,6 +461,7 @@ void spade_kv_destroy(spade_kv kv) {
   if (!kv) return;
   delete[] kv->lens_ub;
   delete[] kv->snap_ub;
+  delete[] kv->evicted_ub;
   delete kv;
 }
 
@@ -409,9 +475,13 @@ spade_status spade_kv_set_state(spade_kv kv, int B, const int32_t* h_lens, const
   hipStream_t st = (hipStream_t)stream;
   hipError_t e = hipMemcpyAsync(kv->lens, h_lens, (size_t)B * 4, hipMemcpyHostToDevice, st);
   if (e == hipSuccess) e = hipMemcpyAsync(kv->pending, h_pending, (size_t)B * 4, hipMemcpyHostToDevice, st);
+  if (e == hipSuccess && kv->evicted) e = launch_kvq_restart(B, kv->lens, kv->evicted, st);
   if (e == hipSuccess) e = hipStreamSynchronize(st);
   if (e != hipSuccess) return hipfail(e, "kv_set_state");
-  for (int b = 0; b < B; ++b) kv->lens_ub[b] = h_lens[b];
+  for (int b = 0; b < B; ++b) {
+    kv->lens_ub[b] = h_lens[b];
+    if (h_lens[b] == 0) kv->evicted_ub[b] = 0;
+  }
   kv->verified = false;
   return SPADE_OK;
 }
@@ -435,12 +505,14 @@ spade_status spade_kv_snapshot(spade_kv kv, int B, int32_t* d_lens, int32_t* d_p
   hipError_t e = launch_copy_state(B, d_lens, d_pending, kv->lens, kv->pending, st);
   if (e != hipSuccess) return hipfail(e, "kv_snapshot");
   for (int b = 0; b < kv->max_batch; ++b) kv->snap_ub[b] = kv->lens_ub[b];
+  kv->snap_evictions = kv->evictions;
   return SPADE_OK;
 }
 
 spade_status spade_kv_restore(spade_kv kv, int B, const int32_t* d_lens, const int32_t* d_pending, void* stream) {
   if (!kv || !d_lens || !d_pending) return fail(SPADE_EINVAL, "null pointer");
   if (B < 1 || B > kv->max_batch) return fail(SPADE_ECAPACITY, "B out of range");
+  if (kv->evictions != kv->snap_evictions) return fail(SPADE_EINVAL, "positions were evicted since the snapshot");
   hipStream_t st = (hipStream_t)stream;
   hipError_t e = launch_copy_state(B, kv->lens, kv->pending, d_lens, d_pending, st);
   if (e != hipSuccess) return hipfail(e, "kv_restore");
@@ -455,7 +527,7 @@ spade_status spade_prefill(spade_model m, spade_kv kv, int b, const int32_t* d_t
   if (b < 0 || b >= kv->max_batch) return fail(SPADE_EINVAL, "request %d out of range", b);
   if (n_tokens < 1) return fail(SPADE_EINVAL, "n_tokens must be >= 1");
   const int n_cache = n_tokens - 1;
-  if (kv->lens_ub[b] + n_cache + 1 > kv->max_len)
+  if (!rows_fit(kv, b, n_cache + 1))
     return fail(SPADE_ECAPACITY, "prefill of %d tokens overflows max_len %d", n_tokens, kv->max_len);
   hipError_t e = launch_prefill_one(m, kv, b, d_tokens, n_cache, (hipStream_t)stream);
   if (e != hipSuccess) return hipfail(e, "prefill");
@@ -478,7 +550,7 @@ spade_status spade_verify(spade_model m, spade_kv kv, int B, int gamma, const in
   hipStream_t st = (hipStream_t)stream;
   bool refreshed = false;
   for (int b = 0; b < B; ++b)
-    if (kv->lens_ub[b] + gamma + 1 > kv->max_len) {
+    if (!rows_fit(kv, b, gamma + 1)) {
       // the host bound grows by gamma + 1 per commit while the lengths grow
       // by k + 1: read the device lengths once before giving up
       if (!refreshed) {
@@ -486,7 +558,7 @@ spade_status spade_verify(spade_model m, spade_kv kv, int B, int gamma, const in
         if (rs != SPADE_OK) return rs;
         refreshed = true;
       }
-      if (kv->lens_ub[b] + gamma + 1 > kv->max_len)
+      if (!rows_fit(kv, b, gamma + 1))
         return fail(SPADE_ECAPACITY, "request %d: %d cached + %d rows exceed max_len %d", b, kv->lens_ub[b],
                     gamma + 1, kv->max_len);
     }
@@ -604,7 +676,7 @@ spade_status spade_prefill_batch(spade_model m, spade_kv kv, int B, const int32_
   for (int b = 0; b < B; ++b) {
     if (h_n_tokens[b] < 1 || h_n_tokens[b] > ld) return fail(SPADE_EINVAL, "request %d: n_tokens must be in [1, ld]", b);
     n_cache[b] = h_n_tokens[b] - 1;
-    if (kv->lens_ub[b] + n_cache[b] + 1 > kv->max_len)
+    if (!rows_fit(kv, b, n_cache[b] + 1))
       return fail(SPADE_ECAPACITY, "request %d: %d cached + %d prompt tokens overflow max_len %d", b, kv->lens_ub[b],
                   h_n_tokens[b], kv->max_len);
   }
@@ -764,6 +836,62 @@ spade_status spade_tile_tiling(int kind, int rows, int n_units, int k, int n_cu,
   return SPADE_OK;
 }
 
+spade_status spade_model_set_head_norms(spade_model m, const float* d_gain_q, const float* d_gain_k, float eps) {
+  if (!m) return fail(SPADE_EINVAL, "null model");
+  if (m->dims.kvdt != SPADE_I4) return fail(SPADE_EUNSUPPORTED, "head norms need a 4-bit cache");
+  if (!d_gain_q != !d_gain_k) return fail(SPADE_EINVAL, "both gains or none");
+  if (!aligned16(d_gain_q) || !aligned16(d_gain_k)) return fail(SPADE_EINVAL, "gains must be 16-byte aligned");
+  if (!(eps >= 0.f && std::isfinite(eps))) return fail(SPADE_EINVAL, "eps must be finite and >= 0");
+  m->gain_q = d_gain_q;
+  m->gain_k = d_gain_k;
+  m->head_eps = eps;
+  return SPADE_OK;
+}
+
+spade_status spade_kv_track_weights(spade_kv kv, float* d_weights) {
+  if (!kv) return fail(SPADE_EINVAL, "null cache");
+  if (!kv->evicted) return fail(SPADE_EUNSUPPORTED, "running weights need a 4-bit cache");
+  kv->weights = d_weights;
+  return SPADE_OK;
+}
+
+spade_status spade_kv_evict(spade_kv kv, int B, int budget, int recent, int32_t* d_kept, void* stream) {
+  if (!kv || !d_kept) return fail(SPADE_EINVAL, "null pointer");
+  if (!kv->evicted) return fail(SPADE_EUNSUPPORTED, "eviction needs a 4-bit cache");
+  if (!kv->weights) return fail(SPADE_EINVAL, "eviction needs running weights (spade_kv_track_weights)");
+  if (B < 1 || B > kv->max_batch) return fail(SPADE_ECAPACITY, "B out of range");
+  if (budget < 1 || budget > kv->max_len) return fail(SPADE_ECAPACITY, "budget must be in [1, max_len]");
+  if (recent < 0 || recent > budget) return fail(SPADE_EINVAL, "recent must be in [0, budget]");
+  const Dims& D = kv->model->dims;
+  KvqEvict a{};
+  a.cache = kv->k;
+  a.out = kv->k;
+  a.head_bytes = a.out_head_bytes = kvq_head_bytes(kv->max_len, D.hd);
+  a.L = D.L;
+  a.batch = a.out_batch = kv->max_batch;
+  a.B = B;
+  a.KVH = D.KVH;
+  a.hd = D.hd;
+  a.max_len = a.out_max_len = kv->max_len;
+  a.budget = budget;
+  a.recent = recent;
+  a.w = kv->weights;
+  a.w_out = kv->weights;
+  a.lens = kv->lens;
+  a.lens_out = kv->lens;
+  a.kept = d_kept;
+  a.evicted = kv->evicted;
+  const hipError_t e = launch_kvq_evict(a, (hipStream_t)stream);
+  if (e != hipSuccess) return hipfail(e, "kv_evict");
+  for (int b = 0; b < B; ++b) {
+    kv->evicted_ub[b] += std::max(0, kv->lens_ub[b] - budget);
+    kv->lens_ub[b] = std::min(kv->lens_ub[b], budget);
+  }
+  kv->verified = false;
+  ++kv->evictions;
+  return SPADE_OK;
+}
+
 size_t spade_kvq_bytes(const spade_kvq_shape* s) {
   if (check_kvq(s) != SPADE_OK) return 0;
   return align256(s->n_layers * kvq_layer_bytes(s));
@@ -810,12 +938,10 @@ spade_status spade_kvq_append(const spade_kvq_shape* s, int layer, void* d_cache
   a.KVH = s->n_kv_heads;
   a.hd = hd;
   a.max_len = s->max_len;
-  a.q = d_q;
-  a.k = d_k;
-  a.v = d_v;
-  a.q_ld = q_ld;
-  a.k_ld = k_ld;
-  a.v_ld = v_ld;
+  a.q = KvqRows{d_q, R * q_ld, q_ld, hd};
+  a.k = KvqRows{d_k, R * k_ld, k_ld, hd};
+  a.v = KvqRows{d_v, R * v_ld, v_ld, hd};
+  a.v_feature = 1;
   a.bf16 = dtype == SPADE_BF16;
   a.gain_q = d_gain_q;
   a.gain_k = d_gain_k;

@@ -54,6 +54,7 @@
 #include "device_gemm.h"
 #include "device_gemm_split.h"
 #include "device_gemm_wide.h"
+#include "kvq.h"
 
 #include <float.h>
 #include <math.h>
@@ -1490,6 +1491,14 @@ hipError_t launch_layer_gemm(spade_model md, spade_kv kv, int kind, int layer, c
       g.q_out = W.q;
       g.kc = kv->k + (size_t)layer * kv_layer * kv_elt;
       g.vc = kv->v + (size_t)layer * kv_layer * kv_elt;
+      if (D.kvdt == SPADE_I4) {  // into the staged rows
+        g.kc = W.stage_k;
+        g.vc = W.stage_v;
+        g.kv_stride = kVBlock;
+        g.kv_bytes = (uint32_t)((size_t)md->max_batch * D.KVH * kVBlock * D.hd * 4);
+        g.lens = W.stage_lens;
+        g.rope = W.stage_rope;
+      }
       break;
     case GEMM_O:
       // O projection + residual; operand of gate/up = x * g_ffn
@@ -1536,8 +1545,8 @@ hipError_t launch_layer_gemm(spade_model md, spade_kv kv, int kind, int layer, c
   const int engine = gemm_engine(md, kind, M);
   if (kind == GEMM_QKV && fc.row_map != nullptr && engine != ENGINE_TILED) return hipErrorInvalidValue;
   if (engine == ENGINE_TILED) {
-    // the last layer of a prefill needs no query panels
-    if (kind == GEMM_QKV && fc.tokens != nullptr && !fc.want_logits && layer + 1 == D.L) {
+    // the last layer of a prefill needs no query panels (but for running weights)
+    if (kind == GEMM_QKV && fc.tokens != nullptr && !fc.want_logits && layer + 1 == D.L && kv->weights == nullptr) {
       g.unit0 = D.d / 16;
       wmat += (size_t)g.unit0 * (K / KBd) * kTileBytes;
       units -= g.unit0;
@@ -1593,6 +1602,78 @@ hipError_t launch_layer_gemm(spade_model md, spade_kv kv, int kind, int layer, c
   }
   return hipSuccess;
 }
+
+namespace {
+
+// Append and attention of one layer over a 4-bit cache: the staged rows of the
+// QKV projection into the cache, the queries normed and rotated where they
+// are, the attention's output as the O projection's operand.  Running weights
+// count every prompt row, but of a verify call only the pending token's row:
+// its drafts may be rejected.
+hipError_t launch_kvq_layer(spade_model md, spade_kv kv, int l, const ForwardCall& fc, int max_keys, bool last,
+                            hipStream_t st) {
+  const Dims& D = md->dims;
+  const Workspace& W = md->ws;
+  const size_t head = kvq_head_bytes(kv->max_len, D.hd), stage = (size_t)kVBlock * D.hd;
+  const size_t first = (size_t)fc.b0 * D.KVH, heads = (size_t)l * kv->max_batch * D.KVH + first;
+  float* weights = kv->weights != nullptr ? kv->weights + heads * kv->max_len : nullptr;
+  KvqAppend a{};
+  a.cache = kv->k + heads * head;
+  a.head_bytes = head;
+  a.B = fc.nb;
+  a.R = fc.R;
+  a.H = D.H;
+  a.KVH = D.KVH;
+  a.hd = D.hd;
+  a.max_len = kv->max_len;
+  if (!last || weights != nullptr) a.q = KvqRows{W.q, (int64_t)fc.R * D.d, D.d, D.hd};
+  a.k = KvqRows{W.stage_k + first * stage, (int64_t)(D.KVH * stage), D.hd, (int64_t)stage};
+  a.v = KvqRows{W.stage_v + first * stage, (int64_t)(D.KVH * stage), 1, (int64_t)stage};
+  a.v_feature = kVBlock;
+  a.gain_q = md->gain_q != nullptr ? md->gain_q + (size_t)l * D.hd : nullptr;
+  a.gain_k = md->gain_k != nullptr ? md->gain_k + (size_t)l * D.hd : nullptr;
+  a.eps = md->head_eps;
+  a.rope = W.rope;
+  a.rope_len = md->max_len;
+  a.shift = kv->evicted + fc.b0;
+  a.lens = kv->lens + fc.b0;
+  a.rows = fc.real_rows != nullptr ? fc.real_rows + fc.b0 : nullptr;
+  a.q_out = W.q;
+  a.qo_ld = D.d;
+  a.weights = weights;
+  a.err = W.err;
+  hipError_t e = launch_kvq_append(a, st);
+  if (e != hipSuccess || (last && weights == nullptr)) return e;
+  KvqAttend t{};
+  t.cache = a.cache;
+  t.head_bytes = head;
+  t.B = fc.nb;
+  t.R = fc.R;
+  t.H = D.H;
+  t.KVH = D.KVH;
+  t.G = D.H / D.KVH;
+  t.hd = D.hd;
+  t.max_len = kv->max_len;
+  t.q = W.q;
+  t.q_ld = D.d;
+  t.scale = 1.0f / sqrtf((float)D.hd);
+  t.lens = a.lens;
+  t.rows = a.rows;
+  t.max_keys = std::min(std::max(max_keys, fc.R), kv->max_len);
+  t.out = W.act_o;
+  t.out_ld = D.d;
+  t.split = D.wdt == SPADE_BF16 ? W.act_split : 0;
+  t.w_in = t.w_out = weights;
+  t.w_rows = fc.tokens != nullptr ? fc.R : 1;
+  t.part_o = (float*)W.kvq_work;
+  t.part_rows = W.kvq_part_rows;
+  t.part_ml = (float*)(W.kvq_work + W.kvq_ml);
+  t.lse = (float*)(W.kvq_work + W.kvq_lse);
+  t.err = W.err;
+  return launch_kvq_attend(t, st);
+}
+
+}  // namespace
 
 hipError_t launch_forward(spade_model md, spade_kv kv, const ForwardCall& fc, hipStream_t st) {
   const Dims& D = md->dims;
@@ -1659,7 +1740,16 @@ hipError_t launch_forward(spade_model md, spade_kv kv, const ForwardCall& fc, hi
   for (int l = 0; l < D.L; ++l) {
     if ((e = launch_layer_gemm(md, kv, GEMM_QKV, l, fc, st)) != hipSuccess) return e;
     // without logits only the last layer's K and V rows are used
-    if (!fc.want_logits && l + 1 == D.L) break;
+    const bool last = !fc.want_logits && l + 1 == D.L;
+    if (D.kvdt == SPADE_I4) {
+      if ((e = launch_kvq_layer(md, kv, l, fc, max_keys, last, st)) != hipSuccess) return e;
+      if (last) break;
+      if ((e = launch_layer_gemm(md, kv, GEMM_O, l, fc, st)) != hipSuccess) return e;
+      if ((e = launch_layer_gemm(md, kv, GEMM_GU, l, fc, st)) != hipSuccess) return e;
+      if ((e = launch_layer_gemm(md, kv, GEMM_DOWN, l, fc, st)) != hipSuccess) return e;
+      continue;
+    }
+    if (last) break;
     AttnParams ap{};
     ap.q = W.q;
     ap.kc = kv->k + (size_t)l * kv_layer * kv_elt;
@@ -2063,6 +2153,11 @@ hipError_t launch_prefill_batch(spade_model md, spade_kv kv, int B, const int32_
     fc.R = R;
     fc.tokens = W.prefill_tok;
     fc.want_logits = false;
+    if (md->dims.kvdt == SPADE_I4) {  // placeholder rows are not stored
+      e = launch_kvq_prefill_rows(b0, nb, R, W.prefill_cnt, W.prefill_base, kv->lens, W.stage_rows, st);
+      if (e != hipSuccess) return e;
+      fc.real_rows = W.stage_rows;
+    }
     e = launch_forward(md, kv, fc, st);
     if (e == hipSuccess) {
       hipLaunchKernelGGL(prefill_advance_kernel, dim3((nb + 63) / 64), dim3(64), 0, st, b0, nb, R, fc.row_off,

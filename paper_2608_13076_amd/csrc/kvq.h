@@ -36,22 +36,27 @@ inline size_t kvq_head_bytes(int max_len, int hd) {
 constexpr int kKvqMaxLen = 1 << 20;
 constexpr int kKvqMaxRows = 16;  // rows per request of one attention call
 
+// Rows of heads: element (request b, row i, head h, feature f) at b sb + i si +
+// h sh + f.
+struct KvqRows {
+  const void* p;
+  int64_t sb, si, sh;
+};
+
 struct KvqAppend {
   uint8_t* cache;  // the layer's [batch][KVH] heads
   size_t head_bytes;
   int B, R, H, KVH, hd, max_len;
-  // element (request b, row i, head h, feature f) of an input at (b R + i) ld + h hd + f
-  const void* q;
-  const void* k;
-  const void* v;
-  int64_t q_ld, k_ld, v_ld;
-  int bf16;  // inputs and q_out: bfloat16, else float32
+  KvqRows q, k, v;  // q.p NULL: no queries
+  int v_feature;    // distance of neighbouring features of v: 1, or float32 columns
+  int bf16;         // inputs and q_out: bfloat16, else float32
   const float* gain_q;
   const float* gain_k;
   float eps;
   const float* rope;
   int rope_len;
   const int32_t* pos;
+  const int32_t* shift;  // added to the position of every row, or NULL
   const int32_t* lens;
   const int32_t* rows;
   void* q_out;
@@ -85,6 +90,7 @@ struct KvqAttend {
   int max_keys;  // bound of lens + rows
   void* out;
   int64_t out_ld;
+  size_t split;  // 0, or float32 calls: out is the two bf16 terms of a GEMM operand, this many elements apart
   const float* w_in;
   float* w_out;  // the layer's [batch][KVH][max_len], or NULL
   int w_rows;
@@ -112,7 +118,14 @@ struct KvqEvict {
   const int32_t* lens;
   int32_t* lens_out;
   int32_t* kept;  // [L][batch][KVH][budget]
+  int32_t* evicted;  // [B] positions evicted so far, or NULL
 };
 hipError_t launch_kvq_evict(const KvqEvict& a, hipStream_t st);
+
+// counts of requests that start over: evicted[b] = 0 where lens[b] is 0
+hipError_t launch_kvq_restart(int B, const int32_t* lens, int32_t* evicted, hipStream_t st);
+// rows[b] of a prefill forward of R rows per request: the prompt tokens left, at most R
+hipError_t launch_kvq_prefill_rows(int b0, int nb, int R, const int32_t* n_cache, const int32_t* base,
+                                   const int32_t* lens, int32_t* rows, hipStream_t st);
 
 }  // namespace spade

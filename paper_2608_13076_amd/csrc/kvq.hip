@@ -206,7 +206,7 @@ template <int HD, bool BF16, int ROWS>
 __global__ void __launch_bounds__(256) kvq_append_kernel(KvqAppend p) {
   constexpr int LPH = HD / 8;
   const int c = threadIdx.x % LPH;
-  const int HQ = p.q != nullptr ? p.H : 0, heads = HQ + 2 * p.KVH;
+  const int HQ = p.q.p != nullptr ? p.H : 0, heads = HQ + 2 * p.KVH;
   int h = (int)blockIdx.y * (256 / LPH / ROWS) + threadIdx.x / LPH / ROWS;
   const int per = (p.R + ROWS - 1) / ROWS, b = (int)blockIdx.x / per;
   const int i = ((int)blockIdx.x - b * per) * ROWS + threadIdx.x / LPH % ROWS;
@@ -217,10 +217,18 @@ __global__ void __launch_bounds__(256) kvq_append_kernel(KvqAppend p) {
   if (!query) h -= key ? HQ : HQ + p.KVH;
   float x[8];
   {
-    const void* src = query ? p.q : key ? p.k : p.v;
-    const int64_t at = row * (query ? p.q_ld : key ? p.k_ld : p.v_ld) + h * HD;
-    load4<BF16>(src, at + f0, x);
-    load4<BF16>(src, at + f1, x + 4);
+    const KvqRows& in = query ? p.q : key ? p.k : p.v;
+    const int64_t at = b * in.sb + i * in.si + h * in.sh;
+    if (!BF16 && !query && !key && p.v_feature != 1) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        x[j] = ((const float*)in.p)[at + (int64_t)(f0 + j) * p.v_feature];
+        x[4 + j] = ((const float*)in.p)[at + (int64_t)(f1 + j) * p.v_feature];
+      }
+    } else {
+      load4<BF16>(in.p, at + f0, x);
+      load4<BF16>(in.p, at + f1, x + 4);
+    }
   }
   const int L = p.lens[b], n_rows = p.rows != nullptr ? min(p.rows[b], p.R) : p.R, t = L + i;
   if (i >= n_rows) {  // a row the request does not use
@@ -234,6 +242,7 @@ __global__ void __launch_bounds__(256) kvq_append_kernel(KvqAppend p) {
   const float* cs = nullptr;
   if (p.rope != nullptr) {
     int pos = (p.pos != nullptr ? p.pos[b] : L) + i;
+    if (p.shift != nullptr) pos += p.shift[b];
     if (pos < 0 || pos >= p.rope_len) {
       if (c == 0) flag_error(p.err, SPADE_DERR_CAPACITY);
       pos = pos < 0 ? 0 : p.rope_len - 1;
@@ -698,8 +707,17 @@ struct AttendSmem {
 __device__ __forceinline__ void store_out(const KvqAttend& p, int b, int kvh, int pr, int f, const float* x) {
   const int g = pr / p.R, i = pr - g * p.R;
   const int64_t at = ((int64_t)b * p.R + i) * p.out_ld + (kvh * p.G + g) * p.hd + f;
-  if (p.bf16) store4<true>(p.out, at, x);
-  else store4<false>(p.out, at, x);
+  if (p.bf16) {
+    store4<true>(p.out, at, x);
+  } else if (p.split != 0) {  // hi = rne(x), lo = rne(x - hi)
+    float lo[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) lo[k] = x[k] - bf2f(f2bf(x[k]));
+    store4<true>(p.out, at, x);
+    store4<true>(p.out, at + (int64_t)p.split, lo);
+  } else {
+    store4<false>(p.out, at, x);
+  }
 }
 
 template <int HD, bool QB>
@@ -1145,6 +1163,7 @@ __global__ void __launch_bounds__(kSelThreads) kvq_select_kernel(KvqEvict p) {
     }
     return;
   }
+  if (p.evicted != nullptr && l == 0 && h == 0 && tid == 0) p.evicted[b] += n - p.budget;
   const int cand = n - p.recent;
   uint32_t need = (uint32_t)(p.budget - p.recent), prefix = 0, mask = 0;
   if (need > 0) {
@@ -1333,13 +1352,20 @@ __global__ void __launch_bounds__(kMoveThreads) kvq_move_kernel(KvqEvict p, int 
   if (col == 2 && blockIdx.y == 0 && l == 0 && h == 0 && tid == 0) p.lens_out[b] = m;
 }
 
-}  // namespace
+__global__ void kvq_restart_kernel(int B, const int32_t* lens, int32_t* evicted) {
+  const int b = blockIdx.x * blockDim.x + threadIdx.x;
+  if (b < B && lens[b] == 0) evicted[b] = 0;
+}
 
-namespace {
+__global__ void kvq_prefill_rows_kernel(int b0, int nb, int R, const int32_t* n_cache, const int32_t* base,
+                                        const int32_t* lens, int32_t* rows) {
+  const int b = b0 + blockIdx.x * blockDim.x + threadIdx.x;
+  if (b < b0 + nb) rows[b] = max(0, min(n_cache[b] - (lens[b] - base[b]), R));
+}
 
 template <int HD, bool BF16>
 hipError_t append_t(const KvqAppend& a, hipStream_t st) {
-  const int heads = (a.q != nullptr ? a.H : 0) + 2 * a.KVH, rows = a.R >= 4 ? 4 : 1;
+  const int heads = (a.q.p != nullptr ? a.H : 0) + 2 * a.KVH, rows = a.R >= 4 ? 4 : 1;
   const int per = 256 / (HD / 8) / rows, gy = (heads + per - 1) / per;
   if (gy > 65535) return hipErrorInvalidValue;
   const dim3 g((unsigned)(a.B * ((a.R + rows - 1) / rows)), (unsigned)gy);
@@ -1448,6 +1474,17 @@ hipError_t launch_kvq_evict(const KvqEvict& a, hipStream_t st) {
   const dim3 g((unsigned)heads, in_place ? 1u : (unsigned)std::min((a.budget + 127) / 128, 64), 3);
   if (a.hd == 128) hipLaunchKernelGGL((kvq_move_kernel<128>), g, dim3(kMoveThreads), 0, st, a, in_place);
   else hipLaunchKernelGGL((kvq_move_kernel<64>), g, dim3(kMoveThreads), 0, st, a, in_place);
+  return hipGetLastError();
+}
+
+hipError_t launch_kvq_restart(int B, const int32_t* lens, int32_t* evicted, hipStream_t st) {
+  hipLaunchKernelGGL(kvq_restart_kernel, dim3((B + 63) / 64), dim3(64), 0, st, B, lens, evicted);
+  return hipGetLastError();
+}
+
+hipError_t launch_kvq_prefill_rows(int b0, int nb, int R, const int32_t* n_cache, const int32_t* base,
+                                   const int32_t* lens, int32_t* rows, hipStream_t st) {
+  hipLaunchKernelGGL(kvq_prefill_rows_kernel, dim3((nb + 63) / 64), dim3(64), 0, st, b0, nb, R, n_cache, base, lens, rows);
   return hipGetLastError();
 }
 

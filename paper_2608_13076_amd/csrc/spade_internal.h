@@ -146,6 +146,16 @@ struct Workspace {
   int32_t* prefill_map; // [Mrows] rows of a packed prefill forward: request of the range << 16 | row of the request
   int32_t* prefill_off; // [kPrefillPack + 1] first packed row of each request of the range
   int32_t* prefill_base; // [Bmax] each request's length when its batched prefill began
+  // 4-bit caches: the QKV projection stores a forward's rows unrotated into a
+  // float32 cache of one block per (request, K/V head) (positions 0 .. R - 1,
+  // angles 0), from where they are normed, rotated and quantised
+  float* stage_k;       // [Bmax][KVH][kVBlock][hd]
+  float* stage_v;       // [Bmax][KVH][hd][kVBlock]
+  int32_t* stage_lens;  // [Bmax] zeros
+  float* stage_rope;    // [kMaxR][hd/2][2] (1, 0)
+  int32_t* stage_rows;  // [Bmax] real rows of a batched prefill forward
+  uint8_t* kvq_work;    // workspace of the attention over a 4-bit cache
+  size_t kvq_part_rows, kvq_ml, kvq_lse;  // rows of its partials; byte offsets
   size_t act_split;   // elements between splits of act_n / act_o
   size_t actf_split;  // elements between splits of act_f
   int Mmax;   // rows of a verify call (logits, LM-head statistics)
@@ -178,6 +188,9 @@ struct spade_model_s {
   int mid_gemm;  // tiled GEMM of 17 to 144 rows: 0 chosen, 1 off, 2 every projection
   int mid_ks;    // its k-splits: 0 chosen per launch, 1..8 fixed
   int tile_rt, tile_p, tile_ks;  // tiled GEMM at any rows: tile and k-splits, 0 chosen per launch
+  const float* gain_q;  // [n_layers][hd] gains of the head norms (4-bit caches), or NULL
+  const float* gain_k;
+  float head_eps;
 };
 
 struct spade_kv_s {
@@ -193,6 +206,11 @@ struct spade_kv_s {
   int last_B;    // requests of that call
   bool verified; // a spade_verify ran since the last commit or state change
   int* snap_ub;  // lens_ub at the last snapshot
+  // 4-bit caches
+  int32_t* evicted;  // [max_batch] positions evicted so far (inside the caller's buffer)
+  int* evicted_ub;   // host upper bound of them
+  float* weights;    // the caller's running weights, or NULL
+  int evictions, snap_evictions;  // calls so far, at the last snapshot
 };
 
 namespace spade {
@@ -205,6 +223,7 @@ struct ForwardCall {
   const int32_t* row_off;
   const int32_t* tokens;   // prefill: [R] ids; verify: NULL
   const int32_t* drafts;   // verify: [nb][R-1]
+  const int32_t* real_rows;  // 4-bit cache, batched prefill: rows in use per request (device, absolute index), or NULL
   bool want_logits;
   float* logits_out;       // [nb*R][V] (user buffer or workspace)
   const uint8_t* mode;     // verify: [nb] modes (LM-head statistics use 1/T on sampling rows)

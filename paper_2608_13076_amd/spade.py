@@ -19,7 +19,7 @@ LIB_PATH = os.path.join(HERE, "libspade.so")
 
 SPADE_OK = 0
 GREEDY, SAMPLE = 0, 1
-F32, BF16 = 0, 1
+F32, BF16, I4 = 0, 1, 2
 KINDS = {"wq": 0, "wk": 1, "wv": 2, "wo": 3, "wg": 4, "wu": 5, "wd": 6,
          "g_attn": 7, "g_ffn": 8, "embed": 9, "g_final": 10, "lm_head": 11}
 GLOBAL_KINDS = ("embed", "g_final", "lm_head")
@@ -34,7 +34,7 @@ EXPORTED = (
     "spade_model_destroy", "spade_kv_destroy", "spade_softmax", "spade_prefill_batch",
     "spade_accept_from_logits_noalloc",
     "spade_kvq_bytes", "spade_kvq_workspace_bytes", "spade_kvq_append", "spade_kvq_read", "spade_kvq_attend",
-    "spade_kvq_evict",
+    "spade_kvq_evict", "spade_model_set_head_norms", "spade_kv_track_weights", "spade_kv_evict",
 )
 # include/spade_tuning.h: schedule controls and measurement hooks
 EXPORTED_TUNING = (
@@ -69,7 +69,7 @@ def config_from(shape) -> SpadeConfig:
     """spade_config from any object with the ModelShape attributes."""
     return SpadeConfig(shape.n_layers, shape.d_model, shape.n_heads, shape.head_dim, shape.d_ffn,
                        shape.vocab, BF16 if shape.weight_dtype == "bf16" else F32,
-                       BF16 if shape.kv_dtype == "bf16" else F32, shape.rms_eps, shape.rope_theta,
+                       {"bf16": BF16, "i4": I4}.get(shape.kv_dtype, F32), shape.rms_eps, shape.rope_theta,
                        getattr(shape, "n_kv_heads", 0))
 
 
@@ -121,6 +121,9 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "spade_wide_tiling": (I, [I, I, I, I, I, P, P, P]),
         "spade_tile_tiling": (I, [I, I, I, I, I, P, P, P]),
         "spade_model_gemm_engine": (I, [P, I, I, P]),
+        "spade_model_set_head_norms": (I, [P, P, P, F]),
+        "spade_kv_track_weights": (I, [P, P]),
+        "spade_kv_evict": (I, [P, I, I, I, P, P]),
         "spade_kvq_bytes": (SZ, [kvqp]),
         "spade_kvq_workspace_bytes": (SZ, [kvqp, I]),
         "spade_kvq_append": (I, [kvqp, I, P, I, I, I, P, L64, P, L64, P, L64, P, P, F, P, I, P, P, P, P, L64, P, P, P]),
@@ -258,6 +261,16 @@ class Model:
         in LDS: 0 chosen per launch, 2 or 4 fixed, -1 off."""
         _check(self.lib.spade_model_set_split_k(self.handle, int(splits)))
 
+    def set_head_norms(self, gain_q: Optional[torch.Tensor], gain_k: Optional[torch.Tensor], eps: float = 1e-5) -> None:
+        """RMSNorm of query and key heads (models with 4-bit caches): float32
+        gains [n_layers, head_dim] on the device, kept by the model; None: off."""
+        want = (self.shape.n_layers, self.shape.head_dim)
+        for t in (gain_q, gain_k):
+            if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != want or t.device != self.device):
+                raise ValueError(f"gains: expected float32 {want} on {self.device}")
+        _check(self.lib.spade_model_set_head_norms(self.handle, _ptr(gain_q), _ptr(gain_k), float(eps)))
+        self._head_gains = (gain_q, gain_k)
+
     def gemm_engine(self, kind: str, rows: int) -> int:
         """Engine of a projection launch of `rows` rows under the present
         settings: 0 skinny, 1 wide-row, 2 tiled."""
@@ -347,6 +360,28 @@ class KVCache:
         _check(self.lib.spade_prefill_batch(self.model.handle, self.handle, B, _ptr(t), ld,
                                             counts.ctypes.data_as(P), _stream()))
         torch.cuda.current_stream(self.model.device).synchronize()
+
+    def track_weights(self, on: bool = True) -> Optional[torch.Tensor]:
+        """Running attention weights of a 4-bit cache, float32 [n_layers,
+        max_batch, K/V heads, max_len] (self.weights), or off."""
+        w = None
+        if on:
+            s = self.model.shape
+            w = torch.zeros((s.n_layers, self.max_batch, getattr(s, "n_kv_heads", 0) or s.n_heads, self.max_len),
+                            dtype=torch.float32, device=self.model.device)
+        _check(self.lib.spade_kv_track_weights(self.handle, _ptr(w)))
+        self.weights = w
+        return w
+
+    def evict(self, B: int, budget: int, recent: int) -> torch.Tensor:
+        """Keep the last ``recent`` and the heaviest other positions of requests
+        0..B-1, ``budget`` in all (spade_kv_evict); returns the kept positions
+        int32 [n_layers, max_batch, K/V heads, budget]."""
+        s = self.model.shape
+        kept = torch.empty((s.n_layers, self.max_batch, getattr(s, "n_kv_heads", 0) or s.n_heads, max(int(budget), 0)),
+                           dtype=torch.int32, device=self.model.device)
+        _check(self.lib.spade_kv_evict(self.handle, B, int(budget), int(recent), _ptr(kept), _stream()))
+        return kept
 
     def commit(self, n: torch.Tensor, corr: torch.Tensor) -> None:
         _check(self.lib.spade_kv_commit(self.handle, n.numel(), _ptr(n), _ptr(corr), _stream()))

@@ -27,7 +27,7 @@ class ModelShape:
     d_ffn: int
     vocab: int
     weight_dtype: str = "bf16"  # "bf16" or "f32"
-    kv_dtype: str = "bf16"  # "bf16" or "f32"
+    kv_dtype: str = "bf16"  # "bf16", "f32" or "i4"
     rms_eps: float = 1e-5
     rope_theta: float = 10000.0
     init_std: float = 0.02

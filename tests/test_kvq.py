@@ -161,3 +161,22 @@ def test_oracle_keep():
     assert okvq.keep(w, 9, 4, 4).tolist() == [5, 6, 7, 8]
     assert okvq.keep(w, 9, 9, 1).tolist() == list(range(9))
     assert okvq.keep(np.zeros(6, np.float32), 6, 3, 0).tolist() == [0, 1, 2]
+
+
+def test_model_calls_refuse_null(lib):
+    assert lib.spade_model_set_head_norms(None, None, None, 1e-5) == EINVAL
+    assert lib.spade_kv_track_weights(None, None) == EINVAL
+    assert lib.spade_kv_evict(None, 1, 1, 0, PTR, None) == EINVAL
+
+
+def test_4_bit_model_buffers(lib):
+    from dataclasses import replace
+    from synth import workload
+    m = workload("gqa_8b_greedy").model
+    cfg, cfg4 = spade.config_from(m), spade.config_from(replace(m, kv_dtype="i4"))
+    assert cfg4.kv_dtype == spade.I4
+    n = lib.spade_kv_bytes(ctypes.byref(cfg4), 2, 1000)
+    assert n == (m.n_layers * 2 * 8 * 1024 * (128 + 8) + 255) // 256 * 256 + 256
+    assert n < 0.27 * lib.spade_kv_bytes(ctypes.byref(cfg), 2, 1024)
+    assert lib.spade_weight_bytes(ctypes.byref(cfg4)) == lib.spade_weight_bytes(ctypes.byref(cfg))
+    assert lib.spade_workspace_bytes(ctypes.byref(cfg4), 2, 8, 1000) > 0

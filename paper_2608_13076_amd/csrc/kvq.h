@@ -100,7 +100,8 @@ struct KvqAttend {
   size_t part_rows;  // rows that part_o holds
   uint32_t* err;
   // set by the launcher
-  int WG;  // ranges (0: a head per workgroup)
+  int WG;     // ranges
+  int parts;  // > 0: ranges are equal parts of a head, this many; 0: of the whole batch
   int TG;  // 16-row tiles of a K/V head's rows
 };
 size_t kvq_attend_floats(int B, int H, int KVH, int hd, int R, size_t* part_ml, size_t* lse);

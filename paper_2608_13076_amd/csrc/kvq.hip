@@ -584,6 +584,12 @@ struct Plan {
   }
 };
 
+// first block of part `part` of a head of nb blocks (parts may be empty)
+__device__ __forceinline__ int even_start(int nb, unsigned part, int parts) {
+  const unsigned q = (unsigned)nb / (unsigned)parts, r = (unsigned)nb - q * parts;
+  return (int)(part * q + min(part, r));
+}
+
 // blocks that request b brings per K/V head (ALL: also without rows in use)
 template <bool ALL>
 __device__ __forceinline__ uint32_t request_blocks(const RequestRows& rr) {
@@ -734,14 +740,16 @@ __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_e
   const int NR = p.G * p.R;
   const float sl = p.scale * kLog2e / kZScale;
   Segments<false> sg;
-  const bool whole = p.WG == 0;  // a head per workgroup
-  if (whole) {
-    if (range >= (unsigned)(p.B * p.KVH)) return;
-    sg.b = (int)(range / (unsigned)p.KVH);
-    sg.h = (int)(range - (unsigned)sg.b * p.KVH);
+  const bool even = p.parts > 0;  // every head in so many equal parts
+  if (even) {
+    const unsigned head = range / (unsigned)p.parts, part = range - head * p.parts;
+    if (head >= (unsigned)(p.B * p.KVH)) return;
+    sg.b = (int)(head / (unsigned)p.KVH);
+    sg.h = (int)(head - (unsigned)sg.b * p.KVH);
     sg.rr = request_rows(p, sg.b);
-    sg.lo = 0;
-    sg.nb = sg.hi = (int)request_blocks<false>(sg.rr);
+    sg.nb = (int)request_blocks<false>(sg.rr);
+    sg.lo = even_start(sg.nb, part, p.parts);
+    sg.hi = even_start(sg.nb, part + 1, p.parts);
   } else {
     if (range >= (unsigned)p.WG || !sg.init(p, lane, range)) return;
   }
@@ -776,7 +784,7 @@ __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_e
     const RequestRows rr = sg.rr;
     const int b = sg.b, kvh = sg.h, blk_hi = sg.hi;
     const unsigned bh = (unsigned)(b * p.KVH + kvh);
-    const bool all = sg.lo == 0 && sg.hi == sg.nb, ok = row_ok && i < rr.n;
+    const bool all = even ? p.parts == 1 : sg.lo == 0 && sg.hi == sg.nb, ok = row_ok && i < rr.n;
     const int vis = ok ? rr.L + i + 1 : 0;  // positions the lane's row sees
     Queries<HD, QB> Q;
     Q.convert(qx, ok);
@@ -896,7 +904,7 @@ __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_e
       sm.m[wave][c] = M;
       sm.l[wave][c] = lt;
     }
-    const bool more = !whole && sg.next(p);
+    const bool more = !even && sg.next(p);
     if (more) request();  // (in flight while this segment is put together)
     __syncthreads();
     for (int e = tid; e < 16 * (HD / 4); e += kWaves * 64) {
@@ -937,7 +945,7 @@ __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_e
 }
 
 // Merge of a head's segments, in order.  A head that lies in one range is
-// complete already; rows that are not in use get their zeros here.  ROWS = 1:
+// complete already (parts: there are several); rows that are not in use get their zeros here.  ROWS = 1:
 // a workgroup takes one row, its GR groups of HD / 4 lanes every GR-th segment,
 // and the groups are added in order (few rows of many segments); ROWS = GR: a
 // row per group (many rows of a few segments: 4608 of 2, 5 us, 10 with ROWS = 1).
@@ -951,12 +959,18 @@ __global__ void __launch_bounds__(256) kvq_merge_kernel(KvqAttend p) {
   const int pr = (int)(blockIdx.x - bh * per) * ROWS + (SPLIT ? 0 : g);
   const int b = (int)(bh / (unsigned)p.KVH), kvh = (int)(bh - (unsigned)b * p.KVH);
   const RequestRows rr = request_rows(p, b);
-  const uint32_t nb = request_blocks<false>(rr);
-  uint32_t before;
-  // the ranges of the head's first and last block
-  const Plan pl = find_request(p, tid & 63, b, &before);
-  before += (uint32_t)kvh * nb;
-  const uint32_t w0 = nb > 0 ? pl.range_of(before) : 0, w1 = nb > 0 ? pl.range_of(before + nb - 1) : 0;
+  uint32_t w0, w1;  // the head's first and last range
+  if (p.parts > 0) {
+    w0 = bh * (unsigned)p.parts;
+    w1 = w0 + p.parts - 1;
+  } else {
+    const uint32_t nb = request_blocks<false>(rr);
+    uint32_t before;
+    const Plan pl = find_request(p, tid & 63, b, &before);
+    before += (uint32_t)kvh * nb;
+    w0 = nb > 0 ? pl.range_of(before) : 0;
+    w1 = nb > 0 ? pl.range_of(before + nb - 1) : 0;
+  }
   const int i = pr - pr / p.R * p.R, nc = (int)(w1 - w0) + 1;
   if (pr < NR && i >= rr.n && (!SPLIT || g == 0)) {
     const float z[4] = {0.f, 0.f, 0.f, 0.f};
@@ -1409,11 +1423,12 @@ namespace {
 // 16384 positions, 8 K/V heads, one bf16 token took 104 us with 256 keys per
 // workgroup, 75 with 512 and 60 with 2048; and ranges of equal size beat chunks
 // of equal length where the requests' lengths differ (16 of 5000 to 16000: 40 us,
-// 55 with chunks).  Up to 256 keys a workgroup takes a whole head, without a
-// merge.
+// 55 with chunks).  Equal parts of every head never straddle two heads and need
+// no plan: they are taken for a single request, and where parts of two blocks per
+// wave all fit the round (6 rows over 1024 positions, 32 heads: 7.5 us, 11 as
+// ranges).  One part per head (up to 256 keys) needs no merge.
 constexpr int kAttendWgs = 512;
 constexpr int kWeightWgs = 1024;
-constexpr int kWholeKeys = 2 * kWaves * kKvqBlock;
 
 int64_t attend_blocks(const KvqAttend& a) { return (int64_t)a.B * a.KVH * ((a.max_keys + kKvqBlock - 1) / kKvqBlock); }
 
@@ -1421,19 +1436,22 @@ template <int HD>
 hipError_t attend_hd(KvqAttend a, hipStream_t st) {
   const int64_t heads = (int64_t)a.B * a.KVH, rows = heads * a.G * a.R;
   a.TG = (a.G * a.R + 15) / 16;
-  const bool whole = a.max_keys <= kWholeKeys;
+  const int blocks = (a.max_keys + kKvqBlock - 1) / kKvqBlock;
   const int64_t fill = (attend_blocks(a) + 2 * kWaves - 1) / (2 * kWaves);
   // (whole rounds of the eight XCDs)
-  const int64_t wgs = std::min<int64_t>(fill, std::max(8, kAttendWgs / 8 / a.TG * 8));
-  a.WG = whole ? 0 : (int)wgs;
-  const int64_t grid = 8 * a.TG * (((whole ? heads : wgs) + 7) / 8);
+  int64_t wgs = std::min<int64_t>(fill, std::max(8, kAttendWgs / 8 / a.TG * 8));
+  const int64_t pieces = (blocks + 2 * kWaves - 1) / (2 * kWaves), fit = kAttendWgs / a.TG / heads;
+  a.parts = a.B == 1 || pieces <= std::max<int64_t>(fit, 1) ? (int)std::max<int64_t>(1, std::min(pieces, fit)) : 0;
+  if (a.parts > 0) wgs = heads * a.parts;
+  a.WG = (int)wgs;
+  const int64_t grid = 8 * a.TG * ((wgs + 7) / 8);
   if (grid > 0x7fffffff || rows > 0x7fffffff || attend_blocks(a) > 0x7fffffff) return hipErrorInvalidValue;
-  if (!whole && (heads + wgs) * a.G * a.R > (int64_t)a.part_rows) return hipErrorInvalidValue;
+  if (a.parts != 1 && (heads + wgs) * a.G * a.R > (int64_t)a.part_rows) return hipErrorInvalidValue;
   if (a.bf16) hipLaunchKernelGGL((kvq_attend_kernel<HD, true>), dim3((unsigned)grid), dim3(kWaves * 64), 0, st, a);
   else hipLaunchKernelGGL((kvq_attend_kernel<HD, false>), dim3((unsigned)grid), dim3(kWaves * 64), 0, st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (!whole) {
+  if (a.parts != 1) {
     // about wgs / heads segments per head
     constexpr int kRows = 256 / (HD / 4);
     if (wgs >= 4 * heads) hipLaunchKernelGGL((kvq_merge_kernel<HD, true>), dim3((unsigned)rows), dim3(256), 0, st, a);

@@ -61,12 +61,14 @@ class QuantCache:
     def _call(self, fn, *args) -> None:
         """fn(shape, *args, stream) with the cache's device current, on its
         current stream."""
-        dev = self.device
-        if torch.cuda.current_device() == dev.index:
-            _check(fn(self._sp, *args, torch.cuda.current_stream(dev).cuda_stream))
+        i = self.device.index
+        # (the handle of torch.cuda.current_stream(i), without building the object)
+        stream = torch._C._cuda_getCurrentRawStream(i)
+        if torch.cuda.current_device() == i:
+            _check(fn(self._sp, *args, stream))
         else:
-            with torch.cuda.device(dev):
-                _check(fn(self._sp, *args, torch.cuda.current_stream(dev).cuda_stream))
+            with torch.cuda.device(i):
+                _check(fn(self._sp, *args, stream))
 
     def _arg(self, t: Optional[torch.Tensor], dtype, shape: tuple, name: str):
         """Address of a contiguous tensor of this dtype and shape on the cache's device."""

@@ -345,10 +345,11 @@ __global__ void __launch_bounds__(256) kvq_read_kernel(KvqRead p) {
 // Float32 queries enter as three bf16 terms, which hold all of their 24 bits,
 // and so do the products p s; bfloat16 calls take their queries as they are and
 // round p s to bfloat16 once (2^-9 of a weight, half a step of their outputs).
-// The matrix instructions cut the smaller of 32 products short, which for codes
-// of one sign adds up; float32 calls therefore take the values as c + (n - 8) s
-// and subtract eight times the sum of their weights, cut short alike, at the
-// end (error of the outputs about 3.5e-6, 8e-6 without).
+// The matrix instructions cut the smaller of 32 products short, and in bfloat16
+// calls p s is rounded; either adds up over codes of one sign.  The values are
+// therefore taken as c + (n - 8) s, c = m + 8 s: the sums of p s n lose eight
+// times the sum of the same p s, cut and rounded alike (error of the outputs
+// relative to their size: float32 about 3.5e-6, 8e-6 without).
 // ---------------------------------------------------------------------------
 constexpr int kWaves = 4;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -820,7 +821,7 @@ __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_e
         M = mn;
         l *= f;
         cs *= f;
-        if constexpr (!QB) p8 *= f;
+        p8 *= f;
 #pragma unroll
         for (int j = 0; j < FT; ++j) o[j] *= f;
       }
@@ -833,7 +834,7 @@ __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_e
           const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(z[u][r], sl, -base));
           const uint32_t pr = value_pair_of(cur.pr[u], r);
           l += e;
-          cs = __builtin_fmaf(e, QB ? hi_f(pr) : __builtin_fmaf(8.f, lo_f(pr), hi_f(pr)), cs);
+          cs = __builtin_fmaf(e, __builtin_fmaf(8.f, lo_f(pr), hi_f(pr)), cs);
           w[4 * u + r] = e * lo_f(pr);
         }
       ld.pairs(cur, nb);
@@ -865,11 +866,9 @@ __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_e
         }
       }
       ld.values(cur, nb);
-      if constexpr (!QB) {
-        const bf16x8 eight = op(0x00080008u, 0x00080008u, 0x00080008u, 0x00080008u);
+      const bf16x8 eight = op(0x00080008u, 0x00080008u, 0x00080008u, 0x00080008u);
 #pragma unroll
-        for (int n = 0; n < N; ++n) p8 = mfma(eight, P[n], p8);
-      }
+      for (int n = 0; n < N; ++n) p8 = mfma(eight, P[n], p8);
 #pragma unroll
       for (int jh = 0; jh < FT / 4; ++jh) {
         const uint32_t(&hf)[4] = half[jh];

@@ -33,6 +33,9 @@ namespace {
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t bf_bits(float f) { return (uint32_t)f2bf(f); }
 
+// lengths come from the caller's device memory: sums stop at the type's ends
+__device__ __forceinline__ int add_sat(int a, int b) { return __builtin_elementwise_add_sat(a, b); }
+
 // v of another lane of the wave's groups of 16: step 0 and 1 swap neighbours and
 // pairs, step 2 and 3 mirror eight and sixteen lanes (data-parallel moves, so a
 // reduction that does not care for its order needs no LDS traffic)
@@ -230,7 +233,7 @@ __global__ void __launch_bounds__(256) kvq_append_kernel(KvqAppend p) {
       load4<BF16>(in.p, at + f1, x + 4);
     }
   }
-  const int L = p.lens[b], n_rows = p.rows != nullptr ? min(p.rows[b], p.R) : p.R, t = L + i;
+  const int L = p.lens[b], n_rows = p.rows != nullptr ? min(p.rows[b], p.R) : p.R, t = add_sat(L, i);
   if (i >= n_rows) {  // a row the request does not use
     if (query) {
       const float z[4] = {0.f, 0.f, 0.f, 0.f};
@@ -241,8 +244,8 @@ __global__ void __launch_bounds__(256) kvq_append_kernel(KvqAppend p) {
   }
   const float* cs = nullptr;
   if (p.rope != nullptr) {
-    int pos = (p.pos != nullptr ? p.pos[b] : L) + i;
-    if (p.shift != nullptr) pos += p.shift[b];
+    int pos = add_sat(p.pos != nullptr ? p.pos[b] : L, i);
+    if (p.shift != nullptr) pos = add_sat(pos, p.shift[b]);
     if (pos < 0 || pos >= p.rope_len) {
       if (c == 0) flag_error(p.err, SPADE_DERR_CAPACITY);
       pos = pos < 0 ? 0 : p.rope_len - 1;
@@ -297,7 +300,7 @@ __global__ void __launch_bounds__(256) kvq_read_kernel(KvqRead p) {
   const int i = ((int)blockIdx.x - b * per) * ROWS + threadIdx.x / LPH % ROWS;
   if (h >= p.KVH || i >= p.R) return;
   const int n_rows = p.rows != nullptr ? min(p.rows[b], p.R) : p.R;
-  const int t = (p.start != nullptr ? p.start[b] : 0) + i;
+  const int t = add_sat(p.start != nullptr ? p.start[b] : 0, i);
   const bool live = i < n_rows && t >= 0 && t < p.max_len;
   float x[2][8] = {};
   if (live) {
@@ -563,9 +566,9 @@ __device__ __forceinline__ RequestRows request_rows(const KvqAttend& p, int b) {
   RequestRows r;
   r.n = p.rows != nullptr ? max(0, min(p.rows[b], p.R)) : p.R;
   r.L = p.lens[b];
-  if (r.L < 0 || r.L + r.n > p.max_keys) {
+  if (r.L < 0 || r.L > p.max_keys - r.n) {  // (n <= R <= max_keys)
     flag_error(p.err, SPADE_DERR_CAPACITY);
-    r.L = r.L < 0 ? 0 : max(0, p.max_keys - r.n);
+    r.L = r.L < 0 ? 0 : p.max_keys - r.n;
   }
   return r;
 }

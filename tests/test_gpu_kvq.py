@@ -345,6 +345,31 @@ def test_attend_longer_than_the_bound_is_cut_and_flagged():
     check_attend(q, k, v, [0, 78], [2, 2], out, 64 ** -0.5, "f32")
 
 
+def test_lengths_at_the_end_of_their_type():
+    """lens, pos and start near 2^31: their sums with row numbers stop at the
+    type's end, so rows are dropped, cut and flagged as at any other length."""
+    rng = np.random.default_rng(11)
+    big = 2**31 - 1
+    cache = kvq.QuantCache(1, 2, 2, 2, 64, 80, device=DEV)
+    k, v = rand(rng, 2, 80, 2, 64), rand(rng, 2, 80, 2, 64)
+    fill(cache, 0, k, v)
+    before = cache.buf.clone()
+    cache.lens.copy_(i32([big, big - 2]))
+    tab = kvq.rope_table(10, 64, 10000.0, DEV)
+    x = rand(rng, 2, 4, 2, 64)
+    q = cache.append(0, x, x, q=x, rope=tab)
+    assert cache.device_error() == spade.DERR_CAPACITY
+    assert torch.equal(cache.buf, before)
+    want = okvq.norm_rotate(f64(x).reshape(-1, 64), None, 0, f64(tab)[9]).reshape(x.shape)  # the table's last position
+    assert np.abs(f64(q) - want).max() <= 2.0 ** -20 * np.abs(want).max()
+    w = torch.zeros((2, 2, 80), device=DEV)
+    out = cache.attend(0, x, weights_out=w, weight_rows=1)
+    assert cache.device_error() == spade.DERR_CAPACITY
+    check_attend(x, k, v, [76, 76], [4, 4], out, 64 ** -0.5, "f32", None, w, 1)
+    for t in cache.read(0, 4, start=cache.lens):
+        assert not t.any()
+
+
 @pytest.mark.parametrize("n", [20000, 131072])
 def test_attend_long(n):
     rng = np.random.default_rng(9)

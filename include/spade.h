@@ -385,8 +385,9 @@ size_t spade_kvq_workspace_bytes(const spade_kvq_shape* shape, int max_rows);
  * flagged at max_len and beyond).  Keys are normed and rotated in double and
  * rounded once to float32 before they are quantised, so their codes do not
  * depend on the order of a sum.  d_q NULL: no queries (d_q_out is not used);
- * else d_q_out gets the queries in `dtype` (it may be d_q itself), zeros for
- * rows that a request does not use.  d_weights (NULL: none): the new
+ * else d_q_out gets the queries in `dtype` (it may be d_q itself with the same
+ * distance of rows; any other overlap with d_q, d_k or d_v is refused), zeros
+ * for rows that a request does not use.  d_weights (NULL: none): the new
  * positions' weights of this layer become 0.  R is any number of rows. */
 spade_status spade_kvq_append(const spade_kvq_shape* shape, int layer, void* d_cache, int B, int R, int dtype,
                               const void* d_q, int64_t q_ld, const void* d_k, int64_t k_ld, const void* d_v,
@@ -399,8 +400,8 @@ spade_status spade_kvq_append(const spade_kvq_shape* shape, int layer, void* d_c
  * which already holds those rows at positions lens[b] .. lens[b] + R - 1
  * (spade_kvq_append): row i sees positions 0 .. lens[b] + i,
  *   out = softmax(scale q . k) v   per query head,
- * d_q and d_out [B R] rows of n_heads heads in `dtype`; rows that a request
- * does not use give zeros.  max_keys: the host's bound of lens[b] + rows, in
+ * d_q and d_out [B R] rows of n_heads heads in `dtype` that do not overlap;
+ * rows that a request does not use give zeros.  max_keys: the host's bound of lens[b] + rows, in
  * [R, max_len], or 0 for max_len (a longer request is cut to it and flagged).
  * d_weights_out (NULL: none): out = in + sum of the probabilities that the
  * first weight_rows rows in use of request b gave a position, over the query

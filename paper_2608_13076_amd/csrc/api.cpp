@@ -235,6 +235,16 @@ bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
 }
+// Whether n rows of na bytes share one with n rows of nb bytes (sa, sb bytes
+// from row to row; rows of equal distance may be interleaved).
+bool rows_overlap(const void* a, int64_t na, int64_t sa, const void* b, int64_t nb, int64_t sb, int64_t n) {
+  const __int128 a0 = (uintptr_t)a, b0 = (uintptr_t)b;
+  if (a0 >= b0 + (__int128)(n - 1) * sb + nb || b0 >= a0 + (__int128)(n - 1) * sa + na) return false;
+  if (sa != sb || n == 1) return true;
+  int64_t d = ((int64_t)((uintptr_t)b - (uintptr_t)a)) % sa;  // of b's row behind the one of a before it
+  if (d < 0) d += sa;
+  return d < na || sa - d < nb;
+}
 
 // the layers' heads of a model's 4-bit cache; the requests' evicted counts follow
 size_t kvq_codes_bytes(const Dims& D, int max_batch, int max_len) {
@@ -929,6 +939,14 @@ spade_status spade_kvq_append(const spade_kvq_shape* s, int layer, void* d_cache
   if (d_rope && rope_len < 1) return fail(SPADE_EINVAL, "rope_len must be >= 1");
   if ((int64_t)B * R > (int64_t)0x7fffffff / (s->n_heads + 2 * s->n_kv_heads))
     return fail(SPADE_ECAPACITY, "too many rows");
+  if (d_q) {
+    const int64_t e = dtype == SPADE_F32 ? 4 : 2, n = (int64_t)B * R, nq = s->n_heads * hd * e, nk = s->n_kv_heads * hd * e;
+    const bool in_place = d_q_out == d_q && (q_out_ld == q_ld || n == 1);
+    if ((!in_place && rows_overlap(d_q_out, nq, q_out_ld * e, d_q, nq, q_ld * e, n)) ||
+        rows_overlap(d_q_out, nq, q_out_ld * e, d_k, nk, k_ld * e, n) ||
+        rows_overlap(d_q_out, nq, q_out_ld * e, d_v, nk, v_ld * e, n))
+      return fail(SPADE_EINVAL, "q_out overlaps other rows than q's own");
+  }
   KvqAppend a{};
   a.cache = (uint8_t*)d_cache + layer * kvq_layer_bytes(s);
   a.head_bytes = kvq_head_bytes(s->max_len, hd);
@@ -1015,6 +1033,8 @@ spade_status spade_kvq_attend(const spade_kvq_shape* s, int layer, const void* d
   const size_t o = kvq_attend_floats(B, s->n_heads, s->n_kv_heads, hd, R, &ml, &lse);
   if (align256(o * 4) + align256(ml * 4) + align256(lse * 4) > workspace_bytes)
     return fail(SPADE_ECAPACITY, "workspace of %zu bytes is too small", workspace_bytes);
+  const int64_t e = dtype == SPADE_F32 ? 4 : 2, nq = s->n_heads * hd * e;
+  if (rows_overlap(d_q, nq, q_ld * e, d_out, nq, out_ld * e, (int64_t)B * R)) return fail(SPADE_EINVAL, "q and out overlap");
   KvqAttend a{};
   a.cache = (const uint8_t*)d_cache + layer * kvq_layer_bytes(s);
   a.head_bytes = kvq_head_bytes(s->max_len, hd);
@@ -1042,8 +1062,8 @@ spade_status spade_kvq_attend(const spade_kvq_shape* s, int layer, const void* d
   a.part_ml = (float*)((uint8_t*)d_workspace + align256(o * 4));
   a.lse = (float*)((uint8_t*)d_workspace + align256(o * 4) + align256(ml * 4));
   a.err = d_err;
-  const hipError_t e = launch_kvq_attend(a, (hipStream_t)stream);
-  if (e != hipSuccess) return hipfail(e, "kvq_attend");
+  const hipError_t r2 = launch_kvq_attend(a, (hipStream_t)stream);
+  if (r2 != hipSuccess) return hipfail(r2, "kvq_attend");
   return SPADE_OK;
 }
 

@@ -102,6 +102,29 @@ def test_attend_refuses_a_small_workspace(lib):
     assert call_attend(lib, R=16, wsb=one) == ECAP
 
 
+FAR = dict(q=1 << 24, k=1 << 25, v=1 << 26, qo=1 << 27)  # 6 rows of 2048 or 512 bytes each, apart
+
+
+@pytest.mark.parametrize("kw", [
+    dict(qo=1 << 24, qo_ld=1536), dict(qo=(1 << 24) + 8), dict(qo=(1 << 24) + 5 * 2048), dict(qo=1 << 25),
+    dict(qo=(1 << 26) + 5 * 512 + 504), dict(q_ld=1536, qo_ld=1536, k_ld=1536, k=(1 << 24) + 2048, qo=(1 << 24) + 1024),
+    dict(q_ld=1536, qo_ld=1536, k_ld=1536, k=(1 << 24) + 2048, qo=(1 << 24) + 3072 - 8),
+])
+def test_append_refuses_overlapping_outputs(lib, kw):
+    assert call_append(lib, **{**FAR, **kw}) == EINVAL
+    assert "overlap" in lib.spade_last_error().decode()
+
+
+@pytest.mark.parametrize("kw", [
+    dict(out=1 << 24), dict(out=(1 << 24) + 2040), dict(out=(1 << 24) + 5 * 2048 + 2040), dict(out=(1 << 24) - 11 * 1024),
+    dict(q_ld=2048, out_ld=2048, out=(1 << 24) + 2040), dict(q_ld=2048, out_ld=2048, out=(1 << 24) + 4096 + 2056),
+    dict(B=1, R=1, out=1 << 24, out_ld=4096),
+])
+def test_attend_refuses_an_output_over_its_queries(lib, kw):
+    assert call_attend(lib, **{**dict(q=1 << 24, out=1 << 25), **kw}) == EINVAL
+    assert "overlap" in lib.spade_last_error().decode()
+
+
 def call_read(lib, **kw):
     d = dict(layer=0, cache=PTR, B=3, R=2, start=None, rows=None, dtype=0, k=PTR, v=PTR)
     d.update(kw)

@@ -165,7 +165,8 @@ spade_status spade_kv_create(spade_model m, void* d_kv, int max_batch, int max_l
                              int32_t* d_lens, int32_t* d_pending, spade_kv* out);
 
 /* Set lens[0..B) and pending[0..B) from host arrays (a snapshot restore).  A
- * request set to length 0 starts over: its evicted positions no longer count. */
+ * request set to length 0 starts over: its evicted positions no longer count.
+ * Lengths from before a spade_kv_evict do not fit the rows that it moved. */
 spade_status spade_kv_set_state(spade_kv kv, int B, const int32_t* h_lens,
                                 const int32_t* h_pending, void* stream);
 
@@ -176,7 +177,8 @@ spade_status spade_kv_get_state(spade_kv kv, int B, int32_t* h_lens, int32_t* h_
  * remember the host-side capacity bound; spade_kv_restore copies them back and
  * restores that bound.  Rows past the restored lengths are stale and get
  * overwritten, so verify -> commit -> restore replays a round exactly.  Not
- * across a spade_kv_evict, which moves the rows (SPADE_EINVAL). */
+ * across a spade_kv_evict, which moves the rows, nor across a spade_kv_set_state
+ * by which a request with evicted positions starts over (SPADE_EINVAL). */
 spade_status spade_kv_snapshot(spade_kv kv, int B, int32_t* d_lens, int32_t* d_pending, void* stream);
 spade_status spade_kv_restore(spade_kv kv, int B, const int32_t* d_lens, const int32_t* d_pending,
                               void* stream);
@@ -323,7 +325,8 @@ spade_status spade_kv_track_weights(spade_kv kv, float* d_weights);
  * min(lens[b], budget).  Later rows keep counting their positions from the
  * start of the sequence, which may go on to the model's max_len.  d_kept:
  * int32 [n_layers][max_batch][n_kv_heads][budget].  Rows of a verify call that
- * was not committed are lost. */
+ * was not committed are lost.  A captured call counts once for the host's
+ * bounds and snapshots, however often it is replayed. */
 spade_status spade_kv_evict(spade_kv kv, int B, int budget, int recent, int32_t* d_kept, void* stream);
 
 /*
@@ -409,7 +412,14 @@ spade_status spade_kvq_append(const spade_kvq_shape* shape, int layer, void* d_c
  * left as they were.  d_weights_in may be NULL (zeros) or d_weights_out.
  * Float32 calls keep their queries and the products of probabilities and
  * scales in 24 bits (three bfloat16 terms); bfloat16 calls round those products
- * to bfloat16 once.  Sums are float32. */
+ * to bfloat16 once.  Sums are float32, and the matrix instructions cut the
+ * smaller of 32 products short: outputs of float32 calls are good to about 4e-6
+ * of their size, probabilities to 1e-7.  Queries below 2^60 in size, values
+ * below 2^50 and spans max - m of a value row above 2^-40 keep that precision;
+ * smaller spans lose bits, larger numbers give infinities or NaN.  How the keys
+ * are divided among workgroups follows the lengths of all requests, so the
+ * last bits of a result do too; the same call gives the same bits.  scale: in
+ * (0, 2^50]. */
 spade_status spade_kvq_attend(const spade_kvq_shape* shape, int layer, const void* d_cache, int B, int R, int dtype,
                               const void* d_q, int64_t q_ld, float scale, const int32_t* d_lens,
                               const int32_t* d_rows, int max_keys, void* d_out, int64_t out_ld,

@@ -396,9 +396,12 @@ spade_status spade_model_create(const spade_config* cfg, void* d_weights, void* 
   if (e == hipSuccess) e = hipMemset(w.corr_cnt, 0, (size_t)max_batch * 4);
   if (e == hipSuccess) e = hipMemset(w.err, 0, 4);
   if (quant) {
-    std::vector<float> none((size_t)kMaxR * half * 2);  // angles 0
-    for (size_t i = 0; i < none.size(); i += 2) none[i] = 1.f;
-    if (e == hipSuccess) e = hipMemcpy(w.stage_rope, none.data(), none.size() * 4, hipMemcpyHostToDevice);
+    float none[kMaxR * 128];  // angles 0
+    for (int i = 0; i < kMaxR * 128; i += 2) {
+      none[i] = 1.f;
+      none[i + 1] = 0.f;
+    }
+    if (e == hipSuccess) e = hipMemcpy(w.stage_rope, none, (size_t)kMaxR * half * 2 * 4, hipMemcpyHostToDevice);
     if (e == hipSuccess) e = hipMemset(w.stage_lens, 0, (size_t)max_batch * 4);
   }
   // activation buffers start at zero so rows past M never feed NaNs
@@ -490,7 +493,10 @@ spade_status spade_kv_set_state(spade_kv kv, int B, const int32_t* h_lens, const
   if (e != hipSuccess) return hipfail(e, "kv_set_state");
   for (int b = 0; b < B; ++b) {
     kv->lens_ub[b] = h_lens[b];
-    if (h_lens[b] == 0) kv->evicted_ub[b] = 0;
+    if (h_lens[b] == 0 && kv->evicted_ub[b] > 0) {
+      kv->evicted_ub[b] = 0;
+      ++kv->evictions;  // a snapshot's rows counted them
+    }
   }
   kv->verified = false;
   return SPADE_OK;
@@ -1020,7 +1026,7 @@ spade_status spade_kvq_attend(const spade_kvq_shape* s, int layer, const void* d
     return fail(SPADE_EINVAL, "rows: alignment or leading dimension");
   if (((uintptr_t)d_cache | (uintptr_t)d_workspace) & 255)
     return fail(SPADE_EINVAL, "cache and workspace must be 256-byte aligned");
-  if (!(scale > 0.f && std::isfinite(scale))) return fail(SPADE_EINVAL, "scale must be finite and > 0");
+  if (!(scale > 0.f && scale <= 0x1p50f)) return fail(SPADE_EINVAL, "scale must be in (0, 2^50]");
   if (max_keys == 0) max_keys = s->max_len;
   if (max_keys < R || max_keys > s->max_len) return fail(SPADE_ECAPACITY, "max_keys must be in [R, max_len]");
   if (d_weights_out && (weight_rows < 0 || weight_rows > R)) return fail(SPADE_EINVAL, "weight_rows must be in [0, R]");

@@ -35,7 +35,8 @@ class QuantCache:
     ``lens`` (int32 [batch], on the device) counts the positions each request
     holds; ``append`` and ``attend`` leave it alone, so a program adds the rows
     it keeps itself (``cache.lens += n``).  ``max_rows``: most rows per request
-    of an ``attend`` call."""
+    of an ``attend`` call.  ``attend`` calls share one workspace, so those on
+    different streams have to be ordered by the program."""
 
     def __init__(self, n_layers: int, batch: int, n_heads: int, n_kv_heads: int, head_dim: int, max_len: int,
                  max_rows: int = 16, device="cuda:0"):

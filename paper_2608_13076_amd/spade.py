@@ -266,8 +266,9 @@ class Model:
         gains [n_layers, head_dim] on the device, kept by the model; None: off."""
         want = (self.shape.n_layers, self.shape.head_dim)
         for t in (gain_q, gain_k):
-            if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != want or t.device != self.device):
-                raise ValueError(f"gains: expected float32 {want} on {self.device}")
+            if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != want or t.device != self.device
+                                  or not t.is_contiguous()):
+                raise ValueError(f"gains: expected contiguous float32 {want} on {self.device}")
         _check(self.lib.spade_model_set_head_norms(self.handle, _ptr(gain_q), _ptr(gain_k), float(eps)))
         self._head_gains = (gain_q, gain_k)
 

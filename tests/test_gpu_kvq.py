@@ -291,6 +291,22 @@ def test_attend_scale_and_large_scores(dtype):
         check_attend(q, k, v, [297], [3], out, scale, dtype)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("qx,kx,vx", [(50, -50, 0), (-40, 40, 0), (60, -70, 40), (-30, 30, -37), (0, 0, 48)])
+def test_attend_keeps_its_precision_over_the_range(qx, kx, vx, dtype):
+    """Queries, keys and values of other magnitudes (by powers of two): the same
+    bounds, which are relative to the rows' scales."""
+    rng = np.random.default_rng(12)
+    cache = kvq.QuantCache(1, 2, 4, 1, 128, 400, device=DEV)
+    k, v = rand(rng, 2, 400, 1, 128, dtype=dtype) * 2.0 ** kx, rand(rng, 2, 400, 1, 128, dtype=dtype) * 2.0 ** vx
+    fill(cache, 0, k, v)
+    cache.lens.copy_(i32([395, 17]))
+    q = rand(rng, 2, 3, 4, 128, dtype=dtype) * 2.0 ** qx
+    scale = 2.0 ** (-qx - kx) / math.sqrt(128)
+    out = cache.attend(0, q, scale=scale)
+    check_attend(q, k, v, [395, 17], [3, 3], out, scale, dtype)
+
+
 def test_attend_hidden_positions_may_hold_anything():
     """Draft rows that are not finite, stale rows and empty space do not reach
     the rows that cannot see them; the rows that see them are NaN."""

@@ -284,6 +284,33 @@ def test_positions_and_snapshots_after_eviction():
     assert model.device_error() == 0
 
 
+def test_a_snapshot_does_not_survive_a_restart():
+    """A request with evicted positions that starts over forgets them, and its
+    snapshot's rows counted them."""
+    w = i4("mini_bf16_greedy")
+    model, _ = gpu_setup(w, max_len=200, max_batch=2)
+    kv = spade.KVCache(model, 2, 60)
+    kv.track_weights()
+    rng = np.random.default_rng(0)
+    for b in (0, 1):
+        kv.prefill(b, rng.integers(0, 4001, 41))
+    kv.evict(1, 20, 5)
+    snap = kv.snapshot(2)
+    kv.set_state([18, 0], [1, 1])
+    kv.restore(*snap)  # request 1 never lost a position
+    kv.set_state([0, 0], [0, 0])
+    with pytest.raises(spade.SpadeError) as e:
+        kv.restore(*snap)
+    assert e.value.status == -1
+
+
+def test_head_norms_refuse_strided_gains():
+    w, model, kv, _ = setup("mini_bf16_greedy")
+    g = torch.ones((w.model.n_layers, 2 * w.model.head_dim), device="cuda:0")[:, ::2]
+    with pytest.raises(ValueError):
+        model.set_head_norms(g, g.contiguous())
+
+
 def test_batched_prefill_stores_the_same_first_layer():
     """Ragged prompts at once or one by one: the first layer's rows do not see
     the attention, so they are the same bits; placeholder rows are not stored."""

@@ -102,6 +102,11 @@ def test_attend_refuses_a_small_workspace(lib):
     assert call_attend(lib, R=16, wsb=one) == ECAP
 
 
+@pytest.mark.parametrize("scale", [float("nan"), 2.0**51, 3e38])
+def test_attend_refuses_scales_beyond_its_range(lib, scale):
+    assert call_attend(lib, out=1 << 30, scale=scale) == EINVAL
+
+
 FAR = dict(q=1 << 24, k=1 << 25, v=1 << 26, qo=1 << 27)  # 6 rows of 2048 or 512 bytes each, apart
 
 

@@ -58,33 +58,41 @@ class QuantCache:
             self.lens = torch.zeros(batch, dtype=torch.int32, device=self.device)
             self.err = torch.zeros(1, dtype=torch.int32, device=self.device)
         self._wshape = (batch, n_kv_heads, max_len)
+        # (a call costs the host about as much as a short one costs the GPU)
+        self._index = self.device.index
+        self._at_buf, self._at_ws, self._at_err = self.buf.data_ptr(), self.workspace.data_ptr(), self.err.data_ptr()
+        self._ws_bytes, self._scale = ws, 1.0 / math.sqrt(head_dim)
 
     def _call(self, fn, *args) -> None:
         """fn(shape, *args, stream) with the cache's device current, on its
         current stream."""
-        i = self.device.index
+        i = self._index
         # (the handle of torch.cuda.current_stream(i), without building the object)
         stream = torch._C._cuda_getCurrentRawStream(i)
         if torch.cuda.current_device() == i:
-            _check(fn(self._sp, *args, stream))
+            status = fn(self._sp, *args, stream)
         else:
             with torch.cuda.device(i):
-                _check(fn(self._sp, *args, stream))
+                status = fn(self._sp, *args, stream)
+        if status:
+            _check(status)
 
     def _arg(self, t: Optional[torch.Tensor], dtype, shape: tuple, name: str):
         """Address of a contiguous tensor of this dtype and shape on the cache's device."""
         if t is None:
             return None
-        if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.device != self.device:
+        if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != self._index:
             raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {shape} on {self.device}")
         return t.data_ptr()
 
-    def _rows(self, t: torch.Tensor, B: int, R: int, heads: int, dtype, name: str):
+    def _rows(self, t: torch.Tensor, shape: tuple, dtype, name: str):
         """(address, ld) of rows [B, R, heads, head_dim]: contiguous heads, the
         rows of all requests one stride apart."""
-        hd = self.head_dim
-        if t.dtype is not dtype or t.shape != (B, R, heads, hd) or t.device != self.device:
-            raise ValueError(f"{name}: expected {dtype} [{B}, {R}, {heads}, {hd}] on {self.device}")
+        if t.dtype is not dtype or t.shape != shape or t.get_device() != self._index:
+            raise ValueError(f"{name}: expected {dtype} {list(shape)} on {self.device}")
+        B, R, heads, hd = shape
+        if t.is_contiguous():
+            return t.data_ptr(), heads * hd
         sb, sr, sh, sf = t.stride()
         ld = sr if R > 1 else (sb if B > 1 else heads * hd)
         if sf != 1 or (heads > 1 and sh != hd) or (R > 1 and B > 1 and sb != R * sr):
@@ -101,26 +109,28 @@ class QuantCache:
         (q_out where given), normed and rotated like the keys.  ``weights``: the
         layer's running weights [batch, n_kv_heads, max_len], zeroed for the new
         positions.  See spade_kvq_append."""
-        B, R = int(k.shape[0]), int(k.shape[1])
-        dt = k.dtype
-        if dt not in _DTYPES:
-            raise ValueError("k: float32 or bfloat16")
-        kp, kld = self._rows(k, B, R, self.n_kv_heads, dt, "k")
-        vp, vld = self._rows(v, B, R, self.n_kv_heads, dt, "v")
+        dt, shape, hd, arg = k.dtype, k.shape, self.head_dim, self._arg
+        if dt not in _DTYPES or len(shape) != 4:
+            raise ValueError("k: float32 or bfloat16 [B, R, n_kv_heads, head_dim]")
+        B, R = shape[0], shape[1]
+        shape = (B, R, self.n_kv_heads, hd)
+        kp, kld = self._rows(k, shape, dt, "k")
+        vp, vld = self._rows(v, shape, dt, "v")
         qp, qld, op, old = None, 0, None, 0
         if q is not None:
-            qp, qld = self._rows(q, B, R, self.n_heads, dt, "q")
+            shape = (B, R, self.n_heads, hd)
+            qp, qld = self._rows(q, shape, dt, "q")
             if q_out is None:
-                q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
-            op, old = self._rows(q_out, B, R, self.n_heads, dt, "q_out")
-        f32, i32, half = torch.float32, torch.int32, self.head_dim // 2
-        n_rope = 0 if rope is None else int(rope.shape[0])
+                q_out = q.new_empty(shape)
+            op, old = self._rows(q_out, shape, dt, "q_out")
+        f32, i32 = torch.float32, torch.int32
+        n_rope = 0 if rope is None else rope.shape[0]
         self._call(
-            self.lib.spade_kvq_append, layer, self.buf.data_ptr(), B, R, _DTYPES[dt], qp, qld, kp, kld, vp, vld,
-            self._arg(gain_q, f32, (self.head_dim,), "gain_q"), self._arg(gain_k, f32, (self.head_dim,), "gain_k"),
-            eps, self._arg(rope, f32, (n_rope, half, 2), "rope"), n_rope, self._arg(pos, i32, (B,), "pos"),
-            self._arg(self.lens, i32, (self.batch,), "lens"), self._arg(rows, i32, (B,), "rows"), op, old,
-            self._arg(weights, f32, self._wshape, "weights"), self.err.data_ptr())
+            self.lib.spade_kvq_append, layer, self._at_buf, B, R, _DTYPES[dt], qp, qld, kp, kld, vp, vld,
+            arg(gain_q, f32, (hd,), "gain_q"), arg(gain_k, f32, (hd,), "gain_k"), eps,
+            arg(rope, f32, (n_rope, hd // 2, 2), "rope"), n_rope, arg(pos, i32, (B,), "pos"),
+            arg(self.lens, i32, (self.batch,), "lens"), arg(rows, i32, (B,), "rows"), op, old,
+            arg(weights, f32, self._wshape, "weights"), self._at_err)
         return q_out
 
     def attend(self, layer: int, q: torch.Tensor, out: Optional[torch.Tensor] = None, scale: Optional[float] = None,
@@ -132,21 +142,21 @@ class QuantCache:
         rows (0: max_len).  weights_out = weights + the probabilities of the
         first weight_rows rows, both [batch, n_kv_heads, max_len] (may be one
         tensor).  See spade_kvq_attend."""
-        B, R = int(q.shape[0]), int(q.shape[1])
-        dt = q.dtype
-        if dt not in _DTYPES:
-            raise ValueError("q: float32 or bfloat16")
-        qp, qld = self._rows(q, B, R, self.n_heads, dt, "q")
+        dt, shape, arg = q.dtype, q.shape, self._arg
+        if dt not in _DTYPES or len(shape) != 4:
+            raise ValueError("q: float32 or bfloat16 [B, R, n_heads, head_dim]")
+        B, R = shape[0], shape[1]
+        shape = (B, R, self.n_heads, self.head_dim)
+        qp, qld = self._rows(q, shape, dt, "q")
         if out is None:
-            out = torch.empty_like(q, memory_format=torch.contiguous_format)
-        op, old = self._rows(out, B, R, self.n_heads, dt, "out")
+            out = q.new_empty(shape)
+        op, old = self._rows(out, shape, dt, "out")
         f32, i32 = torch.float32, torch.int32
         self._call(
-            self.lib.spade_kvq_attend, layer, self.buf.data_ptr(), B, R, _DTYPES[dt], qp, qld,
-            1.0 / math.sqrt(self.head_dim) if scale is None else scale,
-            self._arg(self.lens, i32, (self.batch,), "lens"), self._arg(rows, i32, (B,), "rows"), max_keys, op, old,
-            self._arg(weights, f32, self._wshape, "weights"), self._arg(weights_out, f32, self._wshape, "weights_out"),
-            weight_rows, self.workspace.data_ptr(), self.workspace.numel(), self.err.data_ptr())
+            self.lib.spade_kvq_attend, layer, self._at_buf, B, R, _DTYPES[dt], qp, qld,
+            self._scale if scale is None else scale, arg(self.lens, i32, (self.batch,), "lens"),
+            arg(rows, i32, (B,), "rows"), max_keys, op, old, arg(weights, f32, self._wshape, "weights"),
+            arg(weights_out, f32, self._wshape, "weights_out"), weight_rows, self._at_ws, self._ws_bytes, self._at_err)
         return out
 
     def read(self, layer: int, n: int, start: Optional[torch.Tensor] = None, rows: Optional[torch.Tensor] = None,
@@ -155,13 +165,13 @@ class QuantCache:
         (0) .. + n - 1 as they are held; zeros past rows[b].  See spade_kvq_read."""
         if dtype not in _DTYPES:
             raise ValueError("dtype: float32 or bfloat16")
-        k = torch.empty((self.batch, n, self.n_kv_heads, self.head_dim), dtype=dtype, device=self.device)
-        v = torch.empty_like(k)
-        i32 = torch.int32
+        shape = (self.batch, n, self.n_kv_heads, self.head_dim)
+        k = self.buf.new_empty(shape, dtype=dtype)
+        v = k.new_empty(shape)
+        i32, one = torch.int32, (self.batch,)
         self._call(
-            self.lib.spade_kvq_read, layer, self.buf.data_ptr(), self.batch, n,
-            self._arg(start, i32, (self.batch,), "start"), self._arg(rows, i32, (self.batch,), "rows"), _DTYPES[dtype],
-            k.data_ptr(), v.data_ptr())
+            self.lib.spade_kvq_read, layer, self._at_buf, self.batch, n, self._arg(start, i32, one, "start"),
+            self._arg(rows, i32, one, "rows"), _DTYPES[dtype], k.data_ptr(), v.data_ptr())
         return k, v
 
     def evict(self, weights: torch.Tensor, budget: int, recent: int, kept: Optional[torch.Tensor] = None,
@@ -180,7 +190,7 @@ class QuantCache:
         if kept is None:
             kept = torch.empty(tuple(max(int(x), 0) for x in kshape), dtype=i32, device=self.device)
         self._call(
-            self.lib.spade_kvq_evict, self.buf.data_ptr(), dst._sp, dst.buf.data_ptr(), self.batch, budget, recent,
+            self.lib.spade_kvq_evict, self._at_buf, dst._sp, dst._at_buf, self.batch, budget, recent,
             self._arg(weights, f32, (self.n_layers,) + self._wshape, "weights"),
             dst._arg(weights_out, f32, (dst.n_layers,) + dst._wshape, "weights_out"),
             self._arg(self.lens, i32, (self.batch,), "lens"), dst._arg(dst.lens, i32, (dst.batch,), "lens"),

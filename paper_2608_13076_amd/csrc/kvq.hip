@@ -339,10 +339,14 @@ __global__ void __launch_bounds__(256) kvq_read_kernel(KvqRead p) {
 //   O^T = V^T P^T B = probabilities of 2 x 16 positions straight from those
 //                 registers (k slots 8 q .. + 7 are positions 4 q .. + 3 of
 //                 either half), A = codes of features 8 c + j, j the product
-// A code n enters as the bf16 subnormal n 2^-133 (the matrix instructions keep
-// subnormal inputs, and these products come out exact), so one shift and one
-// mask make two operands of a code word.  Queries carry 2^60 and probabilities
-// 2^50 to keep the products in float32's normal range; with x = m + n s,
+// A code n enters as the bf16 number n 2^-133 or 16 n 2^-133: bits 0 .. 3 or 4 ..
+// 7 of a half word alone are just that, subnormal up to 127 and the first normal
+// numbers from there (the matrix instructions keep subnormal inputs, and these
+// products come out exact).  So a mask makes two operands of a code word, after
+// a shift by 8 for every other mask; queries of the features that enter sixteen
+// times as large are divided by 16, and so are their outputs.  Queries carry
+// 2^60 and probabilities 2^50 to keep the products in float32's normal range;
+// with x = m + n s,
 //   2^-73 q . x = s sum_f (2^60 q_f) (2^-133 n_f) + m 2^-73 sum_f q_f
 //   sum_t p_t x_t = 2^133 sum_t (p_t s_t) (2^-133 n_t) + sum_t p_t m_t.
 // Float32 queries enter as three bf16 terms, which hold all of their 24 bits,
@@ -351,8 +355,11 @@ __global__ void __launch_bounds__(256) kvq_read_kernel(KvqRead p) {
 // The matrix instructions cut the smaller of 32 products short, and in bfloat16
 // calls p s is rounded; either adds up over codes of one sign.  The values are
 // therefore taken as c + (n - 8) s, c = m + 8 s: the sums of p s n lose eight
-// times the sum of the same p s, cut and rounded alike (error of the outputs
-// relative to their size: float32 about 3.5e-6, 8e-6 without).
+// times the sum of the same p s, cut and rounded alike.  Where they are cut goes
+// by the inputs' exponents, which subnormal codes do not use up: float32 calls
+// take all value codes sixteen times as large (two shifts more a word; error of
+// the outputs relative to their size about 1.5e-6, 3.5e-6 with codes at bits 0,
+// 8e-6 without the eight taken off).
 // ---------------------------------------------------------------------------
 constexpr int kWaves = 4;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -369,8 +376,14 @@ __device__ __forceinline__ uint32_t pk_bf16(float a, float b) {
 __device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_f(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
-// codes j and j + 4 of a word as a bf16 pair
-__device__ __forceinline__ uint32_t code_pair(uint32_t w, int j) { return (w >> (4 * j)) & 0x000f000fu; }
+// codes j and j + 4 of a word as a bf16 pair, times 2^-133 / code_scale(j)
+template <bool SAME = false>  // all of them sixteen times as large, not only odd j
+__device__ __forceinline__ uint32_t code_pair(uint32_t w, int j) {
+  if (SAME) return (j == 0 ? w << 4 : w >> (4 * j - 4)) & 0x00f000f0u;
+  return (j < 2 ? w : w >> 8) & (j & 1 ? 0x00f000f0u : 0x000f000fu);
+}
+template <bool SAME = false>
+__device__ __forceinline__ float code_scale(int j) { return SAME || (j & 1) ? 0.0625f : 1.f; }
 
 __device__ __forceinline__ bf16x8 op(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   return __builtin_bit_cast(bf16x8, make_uint4(a, b, c, d));
@@ -457,7 +470,7 @@ struct Queries {
       for (int j = 0; j < 4; ++j) {
         const float a = ok ? x[j] : 0.f, b = ok ? x[j + 4] : 0.f;
         uint32_t e[N];
-        terms<N>(a * kQScale, b * kQScale, e);
+        terms<N>(a * (kQScale * code_scale(j)), b * (kQScale * code_scale(j)), e);
 #pragma unroll
         for (int n = 0; n < N; ++n) w[n][s][j] = e[n];
         t += a + b;
@@ -575,10 +588,16 @@ __device__ __forceinline__ RequestRows request_rows(const KvqAttend& p, int b) {
 
 // Work of an attention call: the blocks of 32 positions of request 0's first
 // K/V head, its second, .., request 1's, .., T in all, cut into WG ranges whose
-// sizes differ by one at most, whatever the requests' lengths.  Head bh's part
-// of range w (a segment) leaves its partial in slot w + bh: along the cut one of
-// the two moves on by one, so slots do not meet and a head's are contiguous.
-// The last bits of a row's result follow the cut, and so the batch.
+// sizes differ by one at most, whatever the requests' lengths.  Every head
+// counts kHeadCost blocks more, before its first: what its queries and its
+// partial cost, about three blocks of each wave (ranges over many short requests
+// took the longest without: 16 requests of 256 to 4096 positions, 9 rows, 40 us;
+// 37 with 4, 34 with 8 to 16).
+// Head bh's part of range w (a segment) leaves its partial in slot w + bh:
+// along the cut one of the two moves on by one, so slots do not meet and a
+// head's are contiguous.  The last bits of a row's result follow the cut, and
+// so the batch.
+constexpr int kHeadCost = 12;
 struct Plan {
   uint32_t T, q, r;  // the first r ranges hold q + 1 blocks, the others q
   __device__ __forceinline__ uint32_t start(uint32_t w) const { return w * q + min(w, r); }
@@ -599,12 +618,14 @@ template <bool ALL>
 __device__ __forceinline__ uint32_t request_blocks(const RequestRows& rr) {
   return !ALL && rr.n == 0 ? 0u : (uint32_t)(rr.L + rr.n + kKvqBlock - 1) / kKvqBlock;
 }
+// what they count in a plan
+__device__ __forceinline__ uint32_t planned_blocks(uint32_t nb) { return nb > 0 ? nb + kHeadCost : 0u; }
 
-// Blocks per K/V head of requests b0 .. b0 + 63, one per lane, and their
-// inclusive prefix.
+// Planned blocks per K/V head of requests b0 .. b0 + 63, one per lane, and
+// their inclusive prefix.
 template <bool ALL>
 __device__ __forceinline__ uint32_t scan_blocks(const KvqAttend& p, int b0, int lane, uint32_t* incl) {
-  const uint32_t n = b0 + lane < p.B ? request_blocks<ALL>(request_rows(p, b0 + lane)) : 0u;
+  const uint32_t n = b0 + lane < p.B ? planned_blocks(request_blocks<ALL>(request_rows(p, b0 + lane))) : 0u;
   uint32_t v = n;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -674,7 +695,7 @@ __device__ __forceinline__ Plan find_request(const KvqAttend& p, int lane, int b
 // of nb).
 template <bool ALL>
 struct Segments {
-  uint32_t left;  // blocks of the range still to go
+  uint32_t left;  // planned blocks of the range still to go
   int b, h, lo, hi, nb;
   RequestRows rr;
   __device__ __forceinline__ bool init(const KvqAttend& p, int lane, uint32_t w) {
@@ -685,13 +706,11 @@ struct Segments {
     if (b >= p.B || left == 0) return false;
     rr = request_rows(p, b);
     nb = (int)request_blocks<ALL>(rr);
-    h = (int)((s - before) / (uint32_t)nb);
-    lo = (int)(s - before) - h * nb;
-    hi = lo + (int)min((uint32_t)(nb - lo), left);
-    return true;
+    const uint32_t per = planned_blocks((uint32_t)nb);
+    h = (int)((s - before) / per);
+    return take(s - before - (uint32_t)h * per);
   }
   __device__ __forceinline__ bool next(const KvqAttend& p) {
-    left -= (uint32_t)(hi - lo);
     if (left == 0) return false;
     if (++h == p.KVH) {
       h = 0;
@@ -701,9 +720,16 @@ struct Segments {
         nb = (int)request_blocks<ALL>(rr);
       } while (nb == 0);
     }
-    lo = 0;
-    hi = (int)min((uint32_t)nb, left);
-    return true;
+    return take(0);
+  }
+  // the head's part from its planned block `at` on; false: the range ends
+  // before the head's first block
+  __device__ __forceinline__ bool take(uint32_t at) {
+    const uint32_t end = min(planned_blocks((uint32_t)nb), at + left);
+    left -= end - at;
+    lo = max((int)at - kHeadCost, 0);
+    hi = (int)end - kHeadCost;
+    return hi > lo;
   }
 };
 
@@ -869,7 +895,8 @@ __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_e
         }
       }
       ld.values(cur, nb);
-      const bf16x8 eight = op(0x00080008u, 0x00080008u, 0x00080008u, 0x00080008u);
+      constexpr uint32_t k8 = QB ? 0x00080008u : 0x00800080u;
+      const bf16x8 eight = op(k8, k8, k8, k8);
 #pragma unroll
       for (int n = 0; n < N; ++n) p8 = mfma(eight, P[n], p8);
 #pragma unroll
@@ -878,7 +905,7 @@ __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_e
         bf16x8 a[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          a[j] = op(code_pair(hf[0], j), code_pair(hf[1], j), code_pair(hf[2], j), code_pair(hf[3], j));
+          a[j] = op(code_pair<!QB>(hf[0], j), code_pair<!QB>(hf[1], j), code_pair<!QB>(hf[2], j), code_pair<!QB>(hf[3], j));
 #pragma unroll
         for (int n = 0; n < N; ++n)
 #pragma unroll
@@ -898,10 +925,12 @@ __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_e
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
-      for (int j = 0; j < FT; j += 4)
-        *(float4*)&sm.o[wave][c][q * (HD / 4) + r * FT + j] =
-            make_float4(code_sum(o[j][r] - p8[0]) + off, code_sum(o[j + 1][r] - p8[0]) + off,
-                        code_sum(o[j + 2][r] - p8[0]) + off, code_sum(o[j + 3][r] - p8[0]) + off);
+      for (int j = 0; j < FT; j += 4) {
+        float x[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = code_sum(o[j + k][r] * code_scale<!QB>(k) - p8[0] * code_scale<!QB>(0)) + off;
+        *(float4*)&sm.o[wave][c][q * (HD / 4) + r * FT + j] = make_float4(x[0], x[1], x[2], x[3]);
+      }
     if (q == 0) {
       sm.m[wave][c] = M;
       sm.l[wave][c] = lt;
@@ -969,7 +998,7 @@ __global__ void __launch_bounds__(256) kvq_merge_kernel(KvqAttend p) {
     const uint32_t nb = request_blocks<false>(rr);
     uint32_t before;
     const Plan pl = find_request(p, tid & 63, b, &before);
-    before += (uint32_t)kvh * nb;
+    before += (uint32_t)kvh * planned_blocks(nb) + kHeadCost;
     w0 = nb > 0 ? pl.range_of(before) : 0;
     w1 = nb > 0 ? pl.range_of(before + nb - 1) : 0;
   }
@@ -1432,7 +1461,9 @@ namespace {
 constexpr int kAttendWgs = 512;
 constexpr int kWeightWgs = 1024;
 
-int64_t attend_blocks(const KvqAttend& a) { return (int64_t)a.B * a.KVH * ((a.max_keys + kKvqBlock - 1) / kKvqBlock); }
+int64_t attend_blocks(const KvqAttend& a) {
+  return (int64_t)a.B * a.KVH * ((a.max_keys + kKvqBlock - 1) / kKvqBlock + kHeadCost);
+}
 
 template <int HD>
 hipError_t attend_hd(KvqAttend a, hipStream_t st) {

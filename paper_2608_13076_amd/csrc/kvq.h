@@ -63,6 +63,7 @@ struct KvqAppend {
   int64_t qo_ld;
   float* weights;  // the layer's [batch][KVH][max_len], or NULL
   uint32_t* err;
+  int run;  // set by the launcher: row groups of a workgroup
 };
 hipError_t launch_kvq_append(const KvqAppend& a, hipStream_t st);
 

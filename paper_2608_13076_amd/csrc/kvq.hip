@@ -21,8 +21,9 @@ namespace {
 // ---------------------------------------------------------------------------
 // Append.  A row is a request's position i; hd / 8 lanes hold one head of it,
 // lane c features 4 c .. + 3 and their rotary partners hd / 2 + 4 c .. + 3.  With
-// four rows or more per request (ROWS = 4) neighbouring lane groups take four
-// rows of one head, whose value words are 16-byte pieces; else heads of one row.
+// more than a few rows per request neighbouring lane groups take ROWS = 4 or 8
+// rows of one head (a wave), whose value words are 16-byte pieces; else heads of
+// one row.
 //
 // A key's codes have to be those of its definition, so that a cache does not
 // depend on how a sum was ordered: the norm and the rotation of keys run in
@@ -30,8 +31,16 @@ namespace {
 // s = bf16((max v - m) * (1 / 15)) the code is the integer nearest to (v - m) /
 // s, ties to even, clamped to 0..15.  The quotient comes from a reciprocal and is
 // corrected by its exact remainder.  Queries stay in float32.
+//
+// Bound by instructions, not by bytes: 2048 rows of 32 + 64 bf16 heads take 24 us
+// (76 MB, 3.2 TB/s) with the vector units and the scalar unit both three quarters
+// busy; one row of 48 heads takes 3.5 us, a launch and two memory latencies.
 // ---------------------------------------------------------------------------
-__device__ __forceinline__ uint32_t bf_bits(float f) { return (uint32_t)f2bf(f); }
+__device__ __forceinline__ uint32_t pk_bf16(float a, float b) {
+  typedef __attribute__((ext_vector_type(2))) float f2;
+  typedef __attribute__((ext_vector_type(2))) __bf16 b2;
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2){a, b}, b2));  // one v_cvt_pk_bf16_f32
+}
 
 // lengths come from the caller's device memory: sums stop at the type's ends
 __device__ __forceinline__ int add_sat(int a, int b) { return __builtin_elementwise_add_sat(a, b); }
@@ -53,21 +62,23 @@ __device__ __forceinline__ double lane_step(double v) {
   return __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
 }
 
-// over the LPH = 8 or 16 lanes of a head, in all of them
+// over the LPH = 8 or 16 lanes of a head, in all of them; NaN if one of them is
+__device__ __forceinline__ float min_nan(float a, float b) { return __builtin_elementwise_minimum(a, b); }
+__device__ __forceinline__ float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 template <int LPH>
 __device__ __forceinline__ float min_lanes(float v) {
-  v = fminf(v, lane_step<0>(v));
-  v = fminf(v, lane_step<1>(v));
-  v = fminf(v, lane_step<2>(v));
-  if constexpr (LPH == 16) v = fminf(v, lane_step<3>(v));
+  v = min_nan(v, lane_step<0>(v));
+  v = min_nan(v, lane_step<1>(v));
+  v = min_nan(v, lane_step<2>(v));
+  if constexpr (LPH == 16) v = min_nan(v, lane_step<3>(v));
   return v;
 }
 template <int LPH>
 __device__ __forceinline__ float max_lanes(float v) {
-  v = fmaxf(v, lane_step<0>(v));
-  v = fmaxf(v, lane_step<1>(v));
-  v = fmaxf(v, lane_step<2>(v));
-  if constexpr (LPH == 16) v = fmaxf(v, lane_step<3>(v));
+  v = max_nan(v, lane_step<0>(v));
+  v = max_nan(v, lane_step<1>(v));
+  v = max_nan(v, lane_step<2>(v));
+  if constexpr (LPH == 16) v = max_nan(v, lane_step<3>(v));
   return v;
 }
 template <int LPH, typename F>
@@ -104,10 +115,20 @@ __device__ __forceinline__ void load4(const void* base, int64_t at, float* x) {
 template <bool BF16>
 __device__ __forceinline__ void store4(void* base, int64_t at, const float* x) {
   if constexpr (BF16) {
-    *(uint2*)((uint16_t*)base + at) =
-        make_uint2(bf_bits(x[0]) | (bf_bits(x[1]) << 16), bf_bits(x[2]) | (bf_bits(x[3]) << 16));
+    *(uint2*)((uint16_t*)base + at) = make_uint2(pk_bf16(x[0], x[1]), pk_bf16(x[2], x[3]));
   } else {
     *(float4*)((float*)base + at) = make_float4(x[0], x[1], x[2], x[3]);
+  }
+}
+
+template <bool BF16>
+__device__ __forceinline__ void store8(void* base, int64_t at, const float* x) {
+  if constexpr (BF16) {
+    *(uint4*)((uint16_t*)base + at) =
+        make_uint4(pk_bf16(x[0], x[1]), pk_bf16(x[2], x[3]), pk_bf16(x[4], x[5]), pk_bf16(x[6], x[7]));
+  } else {
+    store4<false>(base, at, x);
+    store4<false>(base, at + 4, x + 4);
   }
 }
 
@@ -161,48 +182,64 @@ __device__ __noinline__ float exact_code(float v, float m, float s) {
 // the low half, those of the partners in the high half; pair = scale | minimum.
 template <int HD>
 __device__ __forceinline__ uint32_t quantise(const float (&v)[8], uint32_t* pair) {
-  float lo = fminf(fminf(fminf(v[0], v[1]), fminf(v[2], v[3])), fminf(fminf(v[4], v[5]), fminf(v[6], v[7])));
-  float hi = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
-  // NaN where a feature is not finite (min and max pass NaN over)
-  float bad = 0.f;
+  float lo = v[0], hi = v[0];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) bad += v[j] * 0.f;
+  for (int j = 1; j < 8; ++j) {
+    lo = min_nan(lo, v[j]);
+    hi = max_nan(hi, v[j]);
+  }
   lo = min_lanes<HD / 8>(lo);
   hi = max_lanes<HD / 8>(hi);
-  bad = sum_lanes<HD / 8>(bad);
   const uint16_t mb = f2bf(lo);
   const float m = bf2f(mb);
-  const float span = fmaxf(hi - m, 0.f);
-  bad += span * 0.f;  // a span beyond float32
+  const float span = max_nan(hi - m, 0.f);
+  const bool bad = !(span < INFINITY);  // a feature that is not finite, or a span beyond float32
   const uint16_t sb = f2bf(span * (1.0f / 15.0f));
   const float s = bf2f(sb);
   uint32_t code = 0;
-  if (bad == 0.f && s > 0.f) {
-    const float inv = 1.0f / s;
+  if (!bad && s > 0.f) {
+    // a reciprocal within 2^-23 and two roundings of a quotient below 16: within 4e-6
+    const float inv = __builtin_amdgcn_rcpf(s), h = 0.5f * s;
+    float n[8];
+    float far = s >= 0x1p-120f ? 0.f : 1.f;  // (1 / s may overflow)
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      // three roundings of 2^-24 of a quotient below 17: within 4e-6
-      const float d = v[j] - m, t = d * inv;
-      float n = rintf(t);
-      if (fabsf(fabsf(t - n) - 0.5f) < 1e-5f || !(t < 17.f)) {
-        // near a border (bfloat16 rows hit many exactly): by the remainder,
-        // which float32 holds exactly where it holds the difference
-        const float back = v[j] - d, lost = (v[j] - (d + back)) + (back - m);
-        const float e = __builtin_fmaf(-n, s, d), h = 0.5f * s;
-        if (lost == 0.f && t < 17.f) {
-          const bool odd = ((int)n) & 1;
-          if (e > h || (e == h && odd)) n += 1.f;
-          else if (e < -h || (e == -h && odd)) n -= 1.f;
+      const float t = (v[j] - m) * inv;
+      n[j] = rintf(t);
+      far = fmaxf(far, fabsf(t - n[j]));
+    }
+    if (far > 0.49999f) {
+      // next to a border (bfloat16 rows hit many exactly) n is at most one off and
+      // put right by its remainder e, which float32 holds exactly where it holds
+      // v - m
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float d = v[j] - m, back = v[j] - d, lost = (v[j] - (d + back)) + (back - m);
+        if (lost != 0.f || !(s >= 0x1p-120f)) {
+          n[j] = exact_code(v[j], m, s);
         } else {
-          n = exact_code(v[j], m, s);
+          const float e = __builtin_fmaf(-n[j], s, d), ae = fabsf(e);
+          const bool odd = (int)n[j] & 1;
+          n[j] += ae > h || (ae == h && odd) ? copysignf(1.f, e) : 0.f;
         }
       }
-      const int ni = (int)fminf(fmaxf(n, 0.f), 15.f);
-      code |= (uint32_t)ni << (j < 4 ? 4 * j : 16 + 4 * (j - 4));
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t ni = (uint32_t)__builtin_amdgcn_fmed3f(n[j], 0.f, 15.f);
+      code |= ni << (j < 4 ? 4 * j : 16 + 4 * (j - 4));
     }
   }
-  *pair = bad == 0.f ? ((uint32_t)sb | ((uint32_t)mb << 16)) : 0x7fc07fc0u;
+  *pair = bad ? 0x7fc07fc0u : (uint32_t)sb | ((uint32_t)mb << 16);
   return code;
+}
+
+// The head of a lane (LPH lanes a head, ROWS rows of it side by side); with rows
+// enough for a wave it is the wave's, and all that follows from it scalar.
+template <int LPH, int ROWS>
+__device__ __forceinline__ int head_of() {
+  const int h = (int)blockIdx.y * (256 / LPH / ROWS) + threadIdx.x / LPH / ROWS;
+  return LPH * ROWS == 64 ? __builtin_amdgcn_readfirstlane(h) : h;
 }
 
 template <int HD, bool BF16, int ROWS>
@@ -210,92 +247,99 @@ __global__ void __launch_bounds__(256) kvq_append_kernel(KvqAppend p) {
   constexpr int LPH = HD / 8;
   const int c = threadIdx.x % LPH;
   const int HQ = p.q.p != nullptr ? p.H : 0, heads = HQ + 2 * p.KVH;
-  int h = (int)blockIdx.y * (256 / LPH / ROWS) + threadIdx.x / LPH / ROWS;
-  const int per = (p.R + ROWS - 1) / ROWS, b = (int)blockIdx.x / per;
-  const int i = ((int)blockIdx.x - b * per) * ROWS + threadIdx.x / LPH % ROWS;
-  if (h >= heads || i >= p.R) return;  // whole groups of LPH lanes
-  const int64_t row = (int64_t)b * p.R + i;
-  const int f0 = 4 * c, f1 = HD / 2 + 4 * c;
+  int h = head_of<LPH, ROWS>();
+  const int step = ROWS * p.run, per = (p.R + step - 1) / step, b = (int)blockIdx.x / per;
+  const int first = ((int)blockIdx.x - b * per) * step;
+  if (h >= heads) return;  // whole groups of LPH lanes
+  const uint32_t f0 = 4 * c, f1 = HD / 2 + 4 * c;
   const bool query = h < HQ, key = !query && h < HQ + p.KVH;
   if (!query) h -= key ? HQ : HQ + p.KVH;
-  float x[8];
-  {
-    const KvqRows& in = query ? p.q : key ? p.k : p.v;
-    const int64_t at = b * in.sb + i * in.si + h * in.sh;
-    if (!BF16 && !query && !key && p.v_feature != 1) {
+  // (selected member by member: a reference would be a load of its own)
+  const void* in = query ? p.q.p : key ? p.k.p : p.v.p;
+  const int64_t sb = query ? p.q.sb : key ? p.k.sb : p.v.sb, si = query ? p.q.si : key ? p.k.si : p.v.si,
+                sh = query ? p.q.sh : key ? p.k.sh : p.v.sh;
+  const int L = p.lens[b], n_rows = p.rows != nullptr ? min(p.rows[b], p.R) : p.R;
+  const int pos0 = p.pos != nullptr ? p.pos[b] : L, shift = p.shift != nullptr ? p.shift[b] : 0;
+  // (a head has less than 2^31 bytes)
+  uint8_t* head = p.cache + (size_t)((int64_t)b * p.KVH + h) * p.head_bytes;
+  for (int i = first + threadIdx.x / LPH % ROWS, end = min(first + step, p.R); i < end; i += ROWS) {
+    const int64_t row = (int64_t)b * p.R + i;
+    const int t = add_sat(L, i);
+    float x[8];
+    {
+      const int64_t at = b * sb + i * si + h * sh;
+      if (!BF16 && !query && !key && p.v_feature != 1) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        x[j] = ((const float*)in.p)[at + (int64_t)(f0 + j) * p.v_feature];
-        x[4 + j] = ((const float*)in.p)[at + (int64_t)(f1 + j) * p.v_feature];
+        for (int j = 0; j < 4; ++j) {
+          x[j] = ((const float*)in)[at + (int64_t)(f0 + j) * p.v_feature];
+          x[4 + j] = ((const float*)in)[at + (int64_t)(f1 + j) * p.v_feature];
+        }
+      } else {
+        load4<BF16>(in, at + f0, x);
+        load4<BF16>(in, at + f1, x + 4);
       }
-    } else {
-      load4<BF16>(in.p, at + f0, x);
-      load4<BF16>(in.p, at + f1, x + 4);
     }
-  }
-  const int L = p.lens[b], n_rows = p.rows != nullptr ? min(p.rows[b], p.R) : p.R, t = add_sat(L, i);
-  if (i >= n_rows) {  // a row the request does not use
+    if (i >= n_rows) {  // a row the request does not use
+      if (query) {
+        const float z[4] = {0.f, 0.f, 0.f, 0.f};
+        store4<BF16>(p.q_out, row * p.qo_ld + h * HD + f0, z);
+        store4<BF16>(p.q_out, row * p.qo_ld + h * HD + f1, z);
+      }
+      continue;
+    }
+    const float* cs = nullptr;
+    if (p.rope != nullptr) {
+      int pos = add_sat(add_sat(pos0, i), shift);
+      if (pos < 0 || pos >= p.rope_len) {
+        if (c == 0) flag_error(p.err, SPADE_DERR_CAPACITY);
+        pos = pos < 0 ? 0 : p.rope_len - 1;
+      }
+      cs = p.rope + (size_t)pos * HD;
+    }
     if (query) {
-      const float z[4] = {0.f, 0.f, 0.f, 0.f};
-      store4<BF16>(p.q_out, row * p.qo_ld + h * HD + f0, z);
-      store4<BF16>(p.q_out, row * p.qo_ld + h * HD + f1, z);
+      norm_rotate<HD, float>(x, p.gain_q, p.eps, cs, c);
+      store4<BF16>(p.q_out, row * p.qo_ld + h * HD + f0, x);
+      store4<BF16>(p.q_out, row * p.qo_ld + h * HD + f1, x + 4);
+      continue;
     }
-    return;
-  }
-  const float* cs = nullptr;
-  if (p.rope != nullptr) {
-    int pos = add_sat(p.pos != nullptr ? p.pos[b] : L, i);
-    if (p.shift != nullptr) pos = add_sat(pos, p.shift[b]);
-    if (pos < 0 || pos >= p.rope_len) {
+    if (key && (p.gain_k != nullptr || cs != nullptr)) {
+      double y[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y[j] = x[j];
+      norm_rotate<HD, double>(y, p.gain_k, p.eps, cs, c);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = (float)y[j];
+    }
+    uint32_t pair;
+    const uint32_t code = quantise<HD>(x, &pair);
+    const uint32_t other = __float_as_uint(lane_step<0>(__uint_as_float(code)));
+    if (t < 0 || t >= p.max_len) {
       if (c == 0) flag_error(p.err, SPADE_DERR_CAPACITY);
-      pos = pos < 0 ? 0 : p.rope_len - 1;
+      continue;
     }
-    cs = p.rope + (size_t)pos * HD;
-  }
-  if (query) {
-    norm_rotate<HD, float>(x, p.gain_q, p.eps, cs, c);
-    store4<BF16>(p.q_out, row * p.qo_ld + h * HD + f0, x);
-    store4<BF16>(p.q_out, row * p.qo_ld + h * HD + f1, x + 4);
-    return;
-  }
-  if (key && (p.gain_k != nullptr || cs != nullptr)) {
-    double y[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) y[j] = x[j];
-    norm_rotate<HD, double>(y, p.gain_k, p.eps, cs, c);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = (float)y[j];
-  }
-  uint32_t pair;
-  const uint32_t code = quantise<HD>(x, &pair);
-  const uint32_t other = __float_as_uint(lane_step<0>(__uint_as_float(code)));
-  if (t < 0 || t >= p.max_len) {
-    if (c == 0) flag_error(p.err, SPADE_DERR_CAPACITY);
-    return;
-  }
-  // even lanes put the word of features 8 (c / 2) .. + 7 together, odd lanes
-  // that of their partners
-  const bool odd = c & 1;
-  const uint32_t word = odd ? ((other >> 16) | (code & 0xffff0000u)) : ((code & 0xffffu) | (other << 16));
-  const int w = (odd ? HD / 16 : 0) + c / 2;
-  uint8_t* blk = p.cache + (size_t)((int64_t)b * p.KVH + h) * p.head_bytes +
-                 (size_t)(t / kKvqBlock) * kvq_block_bytes(HD);
-  const int tb = t % kKvqBlock;
-  *(uint32_t*)(blk + (key ? kvq_k_word(tb, w, HD) : kvq_v_word(tb, w, HD))) = word;
-  if (c == 0) {
-    *(uint32_t*)(blk + kvq_pair(tb, HD) + (key ? 0 : 4)) = pair;
-    if (key && p.weights != nullptr) p.weights[((int64_t)b * p.KVH + h) * p.max_len + t] = 0.f;
+    // even lanes put the word of features 8 (c / 2) .. + 7 together, odd lanes
+    // that of their partners
+    const bool odd = c & 1;
+    const uint32_t word = odd ? ((other >> 16) | (code & 0xffff0000u)) : ((code & 0xffffu) | (other << 16));
+    const int w = (odd ? HD / 16 : 0) + c / 2;
+    uint8_t* blk = head + (uint32_t)t / kKvqBlock * kvq_block_bytes(HD);
+    const int tb = (uint32_t)t % kKvqBlock;
+    *(uint32_t*)(blk + (key ? kvq_k_word(tb, w, HD) : kvq_v_word(tb, w, HD))) = word;
+    if (c == 0) {
+      *(uint32_t*)(blk + kvq_pair(tb, HD) + (key ? 0 : 4)) = pair;
+      if (key && p.weights != nullptr) p.weights[((int64_t)b * p.KVH + h) * p.max_len + t] = 0.f;
+    }
   }
 }
 
 // ---------------------------------------------------------------------------
-// Read back: lanes as in the append.
+// Read back: lanes as in the append (2048 bf16 rows of 32 heads: 42 MB in 9.8 us).
 // ---------------------------------------------------------------------------
 template <int HD, bool BF16, int ROWS>
 __global__ void __launch_bounds__(256) kvq_read_kernel(KvqRead p) {
   constexpr int LPH = HD / 8;
   const int c = threadIdx.x % LPH;
-  const int h = (int)blockIdx.y * (256 / LPH / ROWS) + threadIdx.x / LPH / ROWS;
+  const int h = head_of<LPH, ROWS>();
   const int per = (p.R + ROWS - 1) / ROWS, b = (int)blockIdx.x / per;
   const int i = ((int)blockIdx.x - b * per) * ROWS + threadIdx.x / LPH % ROWS;
   if (h >= p.KVH || i >= p.R) return;
@@ -305,8 +349,8 @@ __global__ void __launch_bounds__(256) kvq_read_kernel(KvqRead p) {
   float x[2][8] = {};
   if (live) {
     const uint8_t* blk = p.cache + (size_t)((int64_t)b * p.KVH + h) * p.head_bytes +
-                         (size_t)(t / kKvqBlock) * kvq_block_bytes(HD);
-    const int tb = t % kKvqBlock;
+                         (uint32_t)t / kKvqBlock * kvq_block_bytes(HD);
+    const int tb = (uint32_t)t % kKvqBlock;
     const uint2 pr = *(const uint2*)(blk + kvq_pair(tb, HD));
     const uint32_t w[2] = {*(const uint32_t*)(blk + kvq_k_word(tb, c, HD)), *(const uint32_t*)(blk + kvq_v_word(tb, c, HD))};
 #pragma unroll
@@ -318,10 +362,8 @@ __global__ void __launch_bounds__(256) kvq_read_kernel(KvqRead p) {
     }
   }
   const int64_t at = (((int64_t)b * p.R + i) * p.KVH + h) * HD + 8 * c;
-  store4<BF16>(p.k, at, x[0]);
-  store4<BF16>(p.k, at + 4, x[0] + 4);
-  store4<BF16>(p.v, at, x[1]);
-  store4<BF16>(p.v, at + 4, x[1] + 4);
+  store8<BF16>(p.k, at, x[0]);
+  store8<BF16>(p.v, at, x[1]);
 }
 
 // ---------------------------------------------------------------------------
@@ -368,11 +410,6 @@ constexpr float kPLog = 50.f;                          // log2 of the probabilit
 // sums of p n as they come out, back in units of p
 __device__ __forceinline__ float code_sum(float x) { return x * 0x1p100f * 0x1p33f; }
 
-__device__ __forceinline__ uint32_t pk_bf16(float a, float b) {
-  typedef __attribute__((ext_vector_type(2))) float f2;
-  typedef __attribute__((ext_vector_type(2))) __bf16 b2;
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2){a, b}, b2));  // one v_cvt_pk_bf16_f32
-}
 __device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_f(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
@@ -1408,13 +1445,21 @@ __global__ void kvq_prefill_rows_kernel(int b0, int nb, int R, const int32_t* n_
   if (b < b0 + nb) rows[b] = max(0, min(n_cache[b] - (lens[b] - base[b]), R));
 }
 
+// Row groups of a wave of the append, where there are waves enough (as many as
+// the compute units hold): what a wave does once, some 170 instructions, is half
+// of a group's work (2048 rows of 96 heads: 24 us and 26 with one).
+constexpr int kAppendWaves = 8192, kAppendRun = 4;
+
 template <int HD, bool BF16>
-hipError_t append_t(const KvqAppend& a, hipStream_t st) {
-  const int heads = (a.q.p != nullptr ? a.H : 0) + 2 * a.KVH, rows = a.R >= 4 ? 4 : 1;
+hipError_t append_t(KvqAppend a, hipStream_t st) {
+  constexpr int kWaveRows = 64 / (HD / 8);
+  const int heads = (a.q.p != nullptr ? a.H : 0) + 2 * a.KVH, rows = a.R > kWaveRows / 2 ? kWaveRows : 1;
   const int per = 256 / (HD / 8) / rows, gy = (heads + per - 1) / per;
   if (gy > 65535) return hipErrorInvalidValue;
-  const dim3 g((unsigned)(a.B * ((a.R + rows - 1) / rows)), (unsigned)gy);
-  if (rows == 4) hipLaunchKernelGGL((kvq_append_kernel<HD, BF16, 4>), g, dim3(256), 0, st, a);
+  const int64_t groups = (int64_t)a.B * ((a.R + rows - 1) / rows), waves = groups * gy * 4;
+  a.run = (int)std::min<int64_t>(std::max<int64_t>(waves / kAppendWaves, 1), kAppendRun);
+  const dim3 g((unsigned)(a.B * ((a.R + rows * a.run - 1) / (rows * a.run))), (unsigned)gy);
+  if (rows > 1) hipLaunchKernelGGL((kvq_append_kernel<HD, BF16, kWaveRows>), g, dim3(256), 0, st, a);
   else hipLaunchKernelGGL((kvq_append_kernel<HD, BF16, 1>), g, dim3(256), 0, st, a);
   return hipGetLastError();
 }
@@ -1430,10 +1475,11 @@ namespace {
 
 template <int HD, bool BF16>
 hipError_t read_t(const KvqRead& a, hipStream_t st) {
-  const int rows = a.R >= 4 ? 4 : 1, per = 256 / (HD / 8) / rows, gy = (a.KVH + per - 1) / per;
+  constexpr int kWaveRows = 64 / (HD / 8);
+  const int rows = a.R > kWaveRows / 2 ? kWaveRows : 1, per = 256 / (HD / 8) / rows, gy = (a.KVH + per - 1) / per;
   if (gy > 65535) return hipErrorInvalidValue;
   const dim3 g((unsigned)(a.B * ((a.R + rows - 1) / rows)), (unsigned)gy);
-  if (rows == 4) hipLaunchKernelGGL((kvq_read_kernel<HD, BF16, 4>), g, dim3(256), 0, st, a);
+  if (rows > 1) hipLaunchKernelGGL((kvq_read_kernel<HD, BF16, kWaveRows>), g, dim3(256), 0, st, a);
   else hipLaunchKernelGGL((kvq_read_kernel<HD, BF16, 1>), g, dim3(256), 0, st, a);
   return hipGetLastError();
 }

@@ -32,6 +32,7 @@
 //                  K/V head in one workgroup (merged by attn_merge_kernel)
 //   attn_kernel / attn_combine_kernel  f32 cache or other head sizes:
 //                  128-key chunks, then the chunk-order merge
+//   (kvq.hip)      models with 4-bit caches: append, attention, eviction
 //   attn_prefill_kernel  prefill forwards of more than 16 rows per request:
 //                  one wave per 16-row tile, each tile computed as a verify
 //                  call of its own, K / V^T blocks shared through LDS

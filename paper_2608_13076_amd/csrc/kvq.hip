@@ -1,8 +1,8 @@
 // Kernels of the 4-bit K/V cache (layout in kvq.h):
 //   kvq_append_kernel   head norms, rotation and the 4-bit rows of new positions
 //   kvq_read_kernel     rows of the cache as the values they stand for
-//   kvq_attend_kernel   causal attention of a few rows per request, by chunks of keys
-//   kvq_merge_kernel    the chunks' partials in chunk order
+//   kvq_attend_kernel   causal attention of a few rows per request, by ranges of keys
+//   kvq_merge_kernel    the partials of a head's ranges, in order
 //   kvq_weights_kernel  the attention weight every position received
 //   kvq_select_kernel   the positions a cache keeps: the last and the heaviest
 //   kvq_move_kernel     closes the kept positions up
@@ -1101,6 +1101,10 @@ __global__ void __launch_bounds__(256) kvq_merge_kernel(KvqAttend p) {
 // a position's sum is three adds and two swaps.  A wave owns its blocks of 32
 // positions: nothing is added twice and the order of the sum is fixed.  The
 // cut is a plan of its own (requests without rows in use copy their weights).
+// Bound by the stream of keys and weights (80 bytes a position and head: 16
+// requests of 5000 to 16000 positions, 8 heads, 28 us, 4.1 TB/s).  Scores kept by
+// the attention would be read instead of the keys, 16 bytes a position for 4
+// query heads and one row, but need a workspace of rows x positions.
 template <int HD, bool QB>
 __global__ void __launch_bounds__(kWaves * 64) kvq_weights_kernel(KvqAttend p) {
   constexpr int S = HD / 32;
@@ -1212,7 +1216,8 @@ __global__ void __launch_bounds__(kWaves * 64) kvq_weights_kernel(KvqAttend p) {
 // positions the last `recent` stay, and of the others the budget - recent
 // heaviest, ties to the lower position.  The weight that decides is found by
 // four passes over 8 bits of an order-preserving key, then one pass takes the
-// positions in order.
+// positions in order.  A workgroup reads its weights five times, from the second
+// on from L2 (4 layers of 16 requests of 900 to 12000 positions, 8 heads: 31 us).
 // ---------------------------------------------------------------------------
 constexpr int kSelThreads = 1024;
 constexpr int kSelAhead = 4;  // weights a thread requests at once
@@ -1365,7 +1370,9 @@ __global__ void __launch_bounds__(kSelThreads) kvq_select_kernel(KvqEvict p) {
 // piece of four positions and eight features (from four places); column 2 the
 // pairs.  In place one workgroup goes through its column in order: a row moves
 // to a lower or the same position, and a round reads all of its rows before it
-// writes the first.
+// writes the first.  2048 kept positions of the 512 heads above: 142 MB out and at
+// least as many in, 92 us, 3.1 TB/s (a value piece holds four positions, so
+// scattered ones bring their neighbours along).
 constexpr int kMoveThreads = 512;
 
 template <int HD>
@@ -1496,14 +1503,22 @@ namespace {
 // Workgroups of the attention's ranges: two per compute unit (what their
 // registers allow) over all row tiles, one round; fewer where that left less
 // than two blocks per wave.  A workgroup costs about 5 us before and after its
-// stream, so one round of long ranges beats several of short ones: 16 requests of
-// 16384 positions, 8 K/V heads, one bf16 token took 104 us with 256 keys per
-// workgroup, 75 with 512 and 60 with 2048; and ranges of equal size beat chunks
-// of equal length where the requests' lengths differ (16 of 5000 to 16000: 40 us,
-// 55 with chunks).  Equal parts of every head never straddle two heads and need
-// no plan: they are taken for a single request, and where parts of two blocks per
-// wave all fit the round (6 rows over 1024 positions, 32 heads: 7.5 us, 11 as
-// ranges).  One part per head (up to 256 keys) needs no merge.
+// stream, so one round of long ranges beats several of short ones, and ranges of
+// equal size beat chunks of equal length where the requests' lengths differ (one
+// bf16 token, 8 K/V heads, 16 requests of 5000 to 16000 positions: 35 us, 40 to
+// 75 with chunks of 2048 to 256 keys).  Equal parts of every head never straddle
+// two heads and need no plan: they are taken for a single request, and where
+// parts of two blocks per wave all fit the round (6 float32 rows over 1024
+// positions, 32 heads: 7.3 us and 3.8 for the merge, 8.2 and 4.7 as ranges).  One
+// part per head (up to 256 keys) needs no merge (250 positions: 5.8 us, 6.5 and
+// 3.8 as ranges).
+//
+// What bounds it: long caches the stream (120 thousand positions, 130 MB, 24.7
+// us, 5.3 TB/s; the 16 requests above 5.6 TB/s, what a plain copy reaches); many
+// float32 rows over a few thousand positions the vector instructions (300 per
+// block and wave beside 51 matrix instructions: 16 requests of 256 to 4096
+// positions, 9 rows, 4 query heads a K/V head, 30 us); a short request the launch
+// and four dependent round trips to memory.
 constexpr int kAttendWgs = 512;
 constexpr int kWeightWgs = 1024;
 

@@ -413,7 +413,7 @@ spade_status spade_kvq_append(const spade_kvq_shape* shape, int layer, void* d_c
  * Float32 calls keep their queries and the products of probabilities and
  * scales in 24 bits (three bfloat16 terms); bfloat16 calls round those products
  * to bfloat16 once.  Sums are float32, and the matrix instructions cut the
- * smaller of 32 products short: outputs of float32 calls are good to about 2e-6
+ * smaller of 32 products short: outputs of float32 calls are good to about 1e-6
  * of their size, probabilities to 1e-7.  Queries below 2^60 in size, values
  * below 2^50 and spans max - m of a value row above 2^-40 keep that precision;
  * smaller spans lose bits, larger numbers give infinities or NaN.  How the keys

@@ -19,7 +19,11 @@ namespace spade {
 //           + (t % 4) 4: four positions of eight features are one 16-byte
 //           piece, so a lane's load holds four positions (the k index of O^T =
 //           V^T P^T) of its own eight features, and appending a position
-//           writes whole words.
+//           writes whole words.  A half word has features 4 i .. 4 i + 3, each
+//           as the sign of n - 7.5 and k = |n - 7.5| - 1/2 in 0 .. 7: the signs
+//           at bits 15, 11, 7 and 3, k at bits 4 .. 6, 0 .. 2, 12 .. 14 and
+//           8 .. 10, so that shifts by 0 and 4 of the half word and of its
+//           bytes swapped bring every one to bits 15 and 4 .. 6.
 //   pairs   8 bytes per position: scale and minimum (low and high half) of
 //           the keys, then of the values.
 constexpr int kKvqBlock = 32;

@@ -132,6 +132,22 @@ __device__ __forceinline__ void store8(void* base, int64_t at, const float* x) {
   }
 }
 
+// Codes 0 .. 15 in nibbles to value codes and back (kvq.h), for both halves of a
+// word: n is sign and magnitude of n - 7.5 in a nibble, then magnitudes of
+// neighbouring nibbles change places and the signs of a half reverse.
+__device__ __forceinline__ uint32_t sign_nibbles(uint32_t n) {
+  const uint32_t low = ~n & 0x88888888u;  // n < 8
+  return n ^ 0x88888888u ^ (low - (low >> 3));
+}
+__device__ __forceinline__ uint32_t nibbles_of_signs(uint32_t w) {
+  const uint32_t neg = w & 0x88888888u;
+  return w ^ 0x88888888u ^ (neg - (neg >> 3));
+}
+__device__ __forceinline__ uint32_t place_values(uint32_t w) {  // its own inverse
+  const uint32_t s = __builtin_amdgcn_perm(w, w, 0x02030001u);
+  return ((w & 0x07070707u) << 4) | ((w >> 4) & 0x07070707u) | ((s & 0x08080808u) << 4) | ((s >> 4) & 0x08080808u);
+}
+
 // x: a lane's features (0..3 and their partners 4..7) of one head; norm (gain
 // g != NULL) and rotation (rope row cs != NULL) in F.
 template <int HD, typename F>
@@ -324,7 +340,8 @@ __global__ void __launch_bounds__(256) kvq_append_kernel(KvqAppend p) {
     const int w = (odd ? HD / 16 : 0) + c / 2;
     uint8_t* blk = head + (uint32_t)t / kKvqBlock * kvq_block_bytes(HD);
     const int tb = (uint32_t)t % kKvqBlock;
-    *(uint32_t*)(blk + (key ? kvq_k_word(tb, w, HD) : kvq_v_word(tb, w, HD))) = word;
+    if (key) *(uint32_t*)(blk + kvq_k_word(tb, w, HD)) = word;
+    else *(uint32_t*)(blk + kvq_v_word(tb, w, HD)) = place_values(sign_nibbles(word));
     if (c == 0) {
       *(uint32_t*)(blk + kvq_pair(tb, HD) + (key ? 0 : 4)) = pair;
       if (key && p.weights != nullptr) p.weights[((int64_t)b * p.KVH + h) * p.max_len + t] = 0.f;
@@ -352,7 +369,8 @@ __global__ void __launch_bounds__(256) kvq_read_kernel(KvqRead p) {
                          (uint32_t)t / kKvqBlock * kvq_block_bytes(HD);
     const int tb = (uint32_t)t % kKvqBlock;
     const uint2 pr = *(const uint2*)(blk + kvq_pair(tb, HD));
-    const uint32_t w[2] = {*(const uint32_t*)(blk + kvq_k_word(tb, c, HD)), *(const uint32_t*)(blk + kvq_v_word(tb, c, HD))};
+    const uint32_t vw = place_values(*(const uint32_t*)(blk + kvq_v_word(tb, c, HD)));
+    const uint32_t w[2] = {*(const uint32_t*)(blk + kvq_k_word(tb, c, HD)), nibbles_of_signs(vw)};
 #pragma unroll
     for (int o = 0; o < 2; ++o) {
       const uint32_t pp = o ? pr.y : pr.x;
@@ -381,46 +399,50 @@ __global__ void __launch_bounds__(256) kvq_read_kernel(KvqRead p) {
 //   O^T = V^T P^T B = probabilities of 2 x 16 positions straight from those
 //                 registers (k slots 8 q .. + 7 are positions 4 q .. + 3 of
 //                 either half), A = codes of features 8 c + j, j the product
-// A code n enters as the bf16 number n 2^-133 or 16 n 2^-133: bits 0 .. 3 or 4 ..
-// 7 of a half word alone are just that, subnormal up to 127 and the first normal
-// numbers from there (the matrix instructions keep subnormal inputs, and these
-// products come out exact).  So a mask makes two operands of a code word, after
+// Bits 0 .. 7 of a half word alone are a bf16 number, their value times 2^-133:
+// subnormal up to 127, the first normal numbers from there (the matrix
+// instructions keep subnormal inputs, and these products come out exact).  So a
+// key code n in a nibble is the operand n 2^-133 or 16 n 2^-133 after a mask, and
 // a shift by 8 for every other mask; queries of the features that enter sixteen
-// times as large are divided by 16, and so are their outputs.  Queries carry
-// 2^60 and probabilities 2^50 to keep the products in float32's normal range;
-// with x = m + n s,
+// times as large are divided by 16.  Value codes are held as sign and magnitude
+// of n - 7.5 (kvq.h) so that a shift by 4, a swap of bytes and one and-or leave
+// them at bits 15 and 3 .. 6: 16 (n - 7.5) 2^-133.  Queries carry 2^60 and
+// probabilities 2^50 to keep the products in float32's normal range; with x = m +
+// n s,
 //   2^-73 q . x = s sum_f (2^60 q_f) (2^-133 n_f) + m 2^-73 sum_f q_f
-//   sum_t p_t x_t = 2^133 sum_t (p_t s_t) (2^-133 n_t) + sum_t p_t m_t.
+//   sum_t p_t x_t = 2^129 sum_t (p_t s_t) (2^-129 (n_t - 7.5)) + sum_t p_t (m_t + 7.5 s_t).
 // Float32 queries enter as three bf16 terms, which hold all of their 24 bits,
 // and so do the products p s; bfloat16 calls take their queries as they are and
 // round p s to bfloat16 once (2^-9 of a weight, half a step of their outputs).
-// The matrix instructions cut the smaller of 32 products short, and in bfloat16
-// calls p s is rounded; either adds up over codes of one sign.  The values are
-// therefore taken as c + (n - 8) s, c = m + 8 s: the sums of p s n lose eight
-// times the sum of the same p s, cut and rounded alike.  Where they are cut goes
-// by the inputs' exponents, which subnormal codes do not use up: float32 calls
-// take all value codes sixteen times as large (two shifts more a word; error of
-// the outputs relative to their size about 1.5e-6, 3.5e-6 with codes at bits 0,
-// 8e-6 without the eight taken off).
+// The matrix instructions cut the smaller of 32 products short by their operands'
+// exponents: codes of both signs keep that from adding up, scores take their
+// smallest terms first (error of float32 outputs relative to their size 4e-7 to
+// 8e-7; 3.5e-6 with codes of one sign, less eight times the sum of p s, and 1.1e-6
+// with the largest terms first).
 // ---------------------------------------------------------------------------
 constexpr int kWaves = 4;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kQScale = 0x1p60f, kZScale = 0x1p-73f;  // of queries; of the scores that come out
 constexpr float kPLog = 50.f;                          // log2 of the probabilities' scale
-// sums of p n as they come out, back in units of p
-__device__ __forceinline__ float code_sum(float x) { return x * 0x1p100f * 0x1p33f; }
+// sums of p (n - 7.5) as they come out, back in units of p
+__device__ __forceinline__ float code_sum(float x) { return x * 0x1p100f * 0x1p29f; }
 
 __device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_f(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
-// codes j and j + 4 of a word as a bf16 pair, times 2^-133 / code_scale(j)
-template <bool SAME = false>  // all of them sixteen times as large, not only odd j
+// key codes j and j + 4 of a word as a bf16 pair; odd j sixteen times as large
 __device__ __forceinline__ uint32_t code_pair(uint32_t w, int j) {
-  if (SAME) return (j == 0 ? w << 4 : w >> (4 * j - 4)) & 0x00f000f0u;
   return (j < 2 ? w : w >> 8) & (j & 1 ? 0x00f000f0u : 0x000f000fu);
 }
-template <bool SAME = false>
-__device__ __forceinline__ float code_scale(int j) { return SAME || (j & 1) ? 0.0625f : 1.f; }
+__device__ __forceinline__ float code_scale(int j) { return j & 1 ? 0.0625f : 1.f; }
+// value codes j of two half words, sixteen times n - 7.5 (swapped: the bytes of
+// both halves)
+__device__ __forceinline__ uint32_t value_pair(uint32_t w, uint32_t swapped, int j) {
+  const uint32_t v = j < 2 ? w : swapped;
+  uint32_t r;  // (one instruction, which takes one constant from a scalar register)
+  asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(j & 1 ? v << 4 : v), "s"(0x80708070u), "v"(0x00080008u));
+  return r;
+}
 
 __device__ __forceinline__ bf16x8 op(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   return __builtin_bit_cast(bf16x8, make_uint4(a, b, c, d));
@@ -443,9 +465,9 @@ __device__ __forceinline__ void terms(float a, float b, uint32_t (&w)[N]) {
 // lanes l, l ^ 16, l ^ 32, l ^ 48 combined in all of them
 __device__ __forceinline__ float max_q(float v) {
   const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  v = max_nan(__uint_as_float(r[0]), __uint_as_float(r[1]));
   const auto t = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(t[0]), __uint_as_float(t[1]));
+  return max_nan(__uint_as_float(t[0]), __uint_as_float(t[1]));
 }
 __device__ __forceinline__ float sum_q(float v) {
   const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -585,20 +607,18 @@ __device__ __forceinline__ uint32_t& value_pair_of(uint4 (&pr)[2], int r) {
 template <int HD, bool QB>
 __device__ __forceinline__ void scores(const Block<HD>& b, const Queries<HD, QB>& Q, float (&z)[2][4]) {
   floatx4 acc[2] = {};
+  bf16x8 a[HD / 32][2];
 #pragma unroll
-  for (int s = 0; s < HD / 32; ++s) {
-    bf16x8 a[2];
+  for (int n = Queries<HD, QB>::N - 1; n >= 0; --n)  // (smallest terms first)
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const uint32_t w = b.k[u][s];
-      a[u] = op(code_pair(w, 0), code_pair(w, 1), code_pair(w, 2), code_pair(w, 3));
+    for (int s = 0; s < HD / 32; ++s) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const uint32_t w = b.k[u][s];
+        if (n == Queries<HD, QB>::N - 1) a[s][u] = op(code_pair(w, 0), code_pair(w, 1), code_pair(w, 2), code_pair(w, 3));
+        acc[u] = mfma(a[s][u], op(Q.w[n][s][0], Q.w[n][s][1], Q.w[n][s][2], Q.w[n][s][3]), acc[u]);
+      }
     }
-#pragma unroll
-    for (int n = 0; n < Queries<HD, QB>::N; ++n)
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-        acc[u] = mfma(a[u], op(Q.w[n][s][0], Q.w[n][s][1], Q.w[n][s][2], Q.w[n][s][3]), acc[u]);
-  }
 #pragma unroll
   for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -856,7 +876,7 @@ __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_e
     Queries<HD, QB> Q;
     Q.convert(qx, ok);
     float M = -INFINITY, l = 0.f, cs = 0.f;
-    floatx4 o[FT], p8 = floatx4{0.f, 0.f, 0.f, 0.f};
+    floatx4 o[FT];
 #pragma unroll
     for (int j = 0; j < FT; ++j) o[j] = floatx4{0.f, 0.f, 0.f, 0.f};
 
@@ -878,8 +898,10 @@ __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_e
               value_pair_of(cur.pr[u], r) = 0;
             }
       }
-      float mx = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])),
-                       fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3])));
+      // (a row with a NaN is lost anyway: what becomes of its maximum is of no matter)
+      float mx = z[0][0];
+#pragma unroll
+      for (int k = 1; k < 8; ++k) mx = max_nan(mx, z[k >> 2][k & 3]);
       mx = max_q(mx) * sl;
       if (__any(mx > M)) {
         const float mn = fmaxf(M, mx);
@@ -887,7 +909,6 @@ __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_e
         M = mn;
         l *= f;
         cs *= f;
-        p8 *= f;
 #pragma unroll
         for (int j = 0; j < FT; ++j) o[j] *= f;
       }
@@ -900,7 +921,7 @@ __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_e
           const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(z[u][r], sl, -base));
           const uint32_t pr = value_pair_of(cur.pr[u], r);
           l += e;
-          cs = __builtin_fmaf(e, __builtin_fmaf(8.f, lo_f(pr), hi_f(pr)), cs);
+          cs = __builtin_fmaf(e, __builtin_fmaf(7.5f, lo_f(pr), hi_f(pr)), cs);
           w[4 * u + r] = e * lo_f(pr);
         }
       ld.pairs(cur, nb);
@@ -932,17 +953,17 @@ __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_e
         }
       }
       ld.values(cur, nb);
-      constexpr uint32_t k8 = QB ? 0x00080008u : 0x00800080u;
-      const bf16x8 eight = op(k8, k8, k8, k8);
-#pragma unroll
-      for (int n = 0; n < N; ++n) p8 = mfma(eight, P[n], p8);
 #pragma unroll
       for (int jh = 0; jh < FT / 4; ++jh) {
         const uint32_t(&hf)[4] = half[jh];
+        uint32_t sw[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sw[e] = __builtin_amdgcn_perm(hf[e], hf[e], 0x02030001u);
         bf16x8 a[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          a[j] = op(code_pair<!QB>(hf[0], j), code_pair<!QB>(hf[1], j), code_pair<!QB>(hf[2], j), code_pair<!QB>(hf[3], j));
+          a[j] = op(value_pair(hf[0], sw[0], j), value_pair(hf[1], sw[1], j), value_pair(hf[2], sw[2], j),
+                    value_pair(hf[3], sw[3], j));
 #pragma unroll
         for (int n = 0; n < N; ++n)
 #pragma unroll
@@ -962,12 +983,10 @@ __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_e
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
-      for (int j = 0; j < FT; j += 4) {
-        float x[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) x[k] = code_sum(o[j + k][r] * code_scale<!QB>(k) - p8[0] * code_scale<!QB>(0)) + off;
-        *(float4*)&sm.o[wave][c][q * (HD / 4) + r * FT + j] = make_float4(x[0], x[1], x[2], x[3]);
-      }
+      for (int j = 0; j < FT; j += 4)
+        *(float4*)&sm.o[wave][c][q * (HD / 4) + r * FT + j] =
+            make_float4(code_sum(o[j][r]) + off, code_sum(o[j + 1][r]) + off, code_sum(o[j + 2][r]) + off,
+                        code_sum(o[j + 3][r]) + off);
     if (q == 0) {
       sm.m[wave][c] = M;
       sm.l[wave][c] = lt;
@@ -1166,9 +1185,9 @@ __global__ void __launch_bounds__(kWaves * 64) kvq_weights_kernel(KvqAttend p) {
       auto block = [&](Part& cur, int blk) {
         floatx4 acc[2] = {};
 #pragma unroll
-        for (int s = 0; s < S; ++s)
+        for (int n = Queries<HD, QB>::N - 1; n >= 0; --n)  // (as in the attention)
 #pragma unroll
-          for (int n = 0; n < Queries<HD, QB>::N; ++n)
+          for (int s = 0; s < S; ++s)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
               const uint32_t w = cur.b.k[u][s];

@@ -32,8 +32,8 @@ namespace {
 // s, ties to even, clamped to 0..15.  The quotient comes from a reciprocal and is
 // corrected by its exact remainder.  Queries stay in float32.
 //
-// Bound by instructions, not by bytes: 2048 rows of 32 + 64 bf16 heads take 24 us
-// (76 MB, 3.2 TB/s) with the vector units and the scalar unit both three quarters
+// Bound by instructions, not by bytes: 2048 rows of 32 + 64 bf16 heads take 25 us
+// (76 MB, 3.0 TB/s) with the vector units and the scalar unit both three quarters
 // busy; one row of 48 heads takes 3.5 us, a launch and two memory latencies.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t pk_bf16(float a, float b) {
@@ -1473,7 +1473,7 @@ __global__ void kvq_prefill_rows_kernel(int b0, int nb, int R, const int32_t* n_
 
 // Row groups of a wave of the append, where there are waves enough (as many as
 // the compute units hold): what a wave does once, some 170 instructions, is half
-// of a group's work (2048 rows of 96 heads: 24 us and 26 with one).
+// of a group's work (2048 rows of 96 heads: 24 to 25 us, 26 with one).
 constexpr int kAppendWaves = 8192, kAppendRun = 4;
 
 template <int HD, bool BF16>

@@ -307,6 +307,22 @@ def test_attend_keeps_its_precision_over_the_range(qx, kx, vx, dtype):
     check_attend(q, k, v, [395, 17], [3, 3], out, scale, dtype)
 
 
+@pytest.mark.parametrize("hd,h,kvh,lens", [(128, 8, 2, [300, 2000]), (64, 6, 6, [40, 900])])
+def test_attend_precision_of_float32_calls(hd, h, kvh, lens):
+    """The header's figure, about 1e-6 of an output's size (2-norms), with a factor
+    of two for other inputs than it was measured on."""
+    rng = np.random.default_rng(13)
+    cache = kvq.QuantCache(1, 2, h, kvh, hd, max(lens) + 4, device=DEV)
+    k, v = rand(rng, 2, max(lens) + 4, kvh, hd), rand(rng, 2, max(lens) + 4, kvh, hd)
+    fill(cache, 0, k, v)
+    cache.lens.copy_(i32(lens))
+    q = rand(rng, 2, 4, h, hd, strong=False)
+    out = cache.attend(0, q)
+    for b, L in enumerate(lens):
+        want, _ = okvq.attend(f64(q[b]), okvq.held(f64(k[b, :L + 4])), okvq.held(f64(v[b, :L + 4])), L, hd ** -0.5)
+        assert np.linalg.norm(f64(out[b]) - want) <= 2e-6 * np.linalg.norm(want)
+
+
 def test_attend_hidden_positions_may_hold_anything():
     """Draft rows that are not finite, stale rows and empty space do not reach
     the rows that cannot see them; the rows that see them are NaN."""

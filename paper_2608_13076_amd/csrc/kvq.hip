@@ -1145,10 +1145,16 @@ __global__ void __launch_bounds__(kWaves * 64) kvq_weights_kernel(KvqAttend p) {
     struct Part {
       Block<HD> b;
       uint2 pr[2];  // key pair (and value pair) of positions 16 u + c
+      float w;      // weight so far of position lane % 32 (none: 0)
+    };
+    Rsrc from;
+    auto weights_from = [&](const float* w) {
+      from = make_rsrc(w + (w != nullptr ? bh * p.max_len : 0), w != nullptr ? (uint32_t)keys * 4 : 0u);
     };
     auto request = [&](Part& x, int blk) {
       blk = blk < hi ? blk : first;
       ld.keys(x.b, blk);
+      x.w = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(from, 4 * (blk * kKvqBlock + lane % kKvqBlock), 0, 0));
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const auto w = __builtin_amdgcn_raw_buffer_load_b64(ld.r, (int)kvq_pair(16 * u + c, HD),
@@ -1158,6 +1164,7 @@ __global__ void __launch_bounds__(kWaves * 64) kvq_weights_kernel(KvqAttend p) {
       __builtin_amdgcn_sched_barrier(0);
     };
     Part buf[2];
+    weights_from(p.w_in);
     request(buf[0], first);
     request(buf[1], first + kWaves);
     // sixteen counted rows at a time; the first tile (there is one even without
@@ -1181,7 +1188,6 @@ __global__ void __launch_bounds__(kWaves * 64) kvq_weights_kernel(KvqAttend p) {
         vis[r] = ok ? rr.L + i + 1 : 0;
         sq[r] = __shfl(Q.sum, 4 * q + r);
       }
-      const float* from = r0 == 0 ? p.w_in : p.w_out;
       auto block = [&](Part& cur, int blk) {
         floatx4 acc[2] = {};
 #pragma unroll
@@ -1195,6 +1201,7 @@ __global__ void __launch_bounds__(kWaves * 64) kvq_weights_kernel(KvqAttend p) {
                             op(code_pair(w, 0), code_pair(w, 1), code_pair(w, 2), code_pair(w, 3)), acc[u]);
             }
         const float s[2] = {lo_f(cur.pr[0].x), lo_f(cur.pr[1].x)}, m[2] = {hi_f(cur.pr[0].x), hi_f(cur.pr[1].x)};
+        const float before = cur.w;
         request(cur, blk + 2 * kWaves);
         float t[2];
 #pragma unroll
@@ -1212,7 +1219,7 @@ __global__ void __launch_bounds__(kWaves * 64) kvq_weights_kernel(KvqAttend p) {
         const int pos = blk * kKvqBlock + lane;
         if (lane < kKvqBlock && pos < keys) {
           const int64_t at = bh * p.max_len + pos;
-          p.w_out[at] = (from != nullptr ? from[at] : 0.f) + (q == 0 ? t[0] : t[1]);
+          p.w_out[at] = before + (q == 0 ? t[0] : t[1]);
         }
       };
       for (int blk = first; blk < hi; blk += 2 * kWaves) {
@@ -1221,6 +1228,7 @@ __global__ void __launch_bounds__(kWaves * 64) kvq_weights_kernel(KvqAttend p) {
         block(buf[1], blk + kWaves);
       }
       if (r0 + 16 < NW) {
+        weights_from(p.w_out);
         request(buf[0], first);
         request(buf[1], first + kWaves);
       }

@@ -548,8 +548,10 @@ struct Block {
   uint4 pr[2][2];  // (key pair, value pair) of positions 16 u + 4 q .. + 3
 };
 
-// Loads of block `blk` of a head (r: its region, nt policy: every block is read
-// by one workgroup or by the tile groups of one XCD).
+// Loads of block `blk` of a head (r: its region).  Values and pairs go by with
+// the nt policy; keys may stay, and are in the Infinity Cache when the weights
+// read them again (16 requests of 5000 to 16000 positions with weights: 62.0 us,
+// 66.2 with nt for the keys too, 68.4 with it for nothing).
 template <int HD>
 struct BlockLoader {
   Rsrc r;
@@ -560,21 +562,22 @@ struct BlockLoader {
     v = kvq_v_word(4 * q, HD == 128 ? c : c / 2, HD);
     pr = kvq_pair(4 * q, HD);
   }
+  template <int AUX = kAuxStream>
   __device__ __forceinline__ uint4 b128(uint32_t off, uint32_t so) const {
-    return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, (int)so, kAuxStream));
+    return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, (int)so, AUX));
   }
   __device__ __forceinline__ void keys(Block<HD>& b, int blk) const {
     const uint32_t so = (uint32_t)blk * kvq_block_bytes(HD);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       if constexpr (HD == 128) {
-        const uint4 w = b128(k + 16 * u * (HD / 2), so);
+        const uint4 w = b128<0>(k + 16 * u * (HD / 2), so);
         b.k[u][0] = w.x;
         b.k[u][1] = w.y;
         b.k[u][2] = w.z;
         b.k[u][3] = w.w;
       } else {
-        const auto w = __builtin_amdgcn_raw_buffer_load_b64(r, (int)(k + 16 * u * (HD / 2)), (int)so, kAuxStream);
+        const auto w = __builtin_amdgcn_raw_buffer_load_b64(r, (int)(k + 16 * u * (HD / 2)), (int)so, 0);
         b.k[u][0] = w[0];
         b.k[u][1] = w[1];
       }
@@ -1121,7 +1124,7 @@ __global__ void __launch_bounds__(256) kvq_merge_kernel(KvqAttend p) {
 // positions: nothing is added twice and the order of the sum is fixed.  The
 // cut is a plan of its own (requests without rows in use copy their weights).
 // Bound by the stream of keys and weights (80 bytes a position and head: 16
-// requests of 5000 to 16000 positions, 8 heads, 28 us, 4.1 TB/s).  Scores kept by
+// requests of 5000 to 16000 positions, 8 heads, 22 us, 5.3 TB/s).  Scores kept by
 // the attention would be read instead of the keys, 16 bytes a position for 4
 // query heads and one row, but need a workspace of rows x positions.
 template <int HD, bool QB>

@@ -389,9 +389,9 @@ __global__ void __launch_bounds__(256) kvq_read_kernel(KvqRead p) {
 //
 // Row i of request b (i < rows[b]) sees positions 0 .. lens[b] + i.  The G R
 // rows that share a K/V head are packed (row g R + i) into 16-row tiles; a
-// workgroup of W waves takes T tiles over a chunk of keys, wave w every W-th
+// workgroup of W waves takes one tile over a range of keys, wave w every W-th
 // block of 32 positions, with a running maximum, sum and output of its own
-// (one pass over the codes; the waves meet once, at the end of the chunk).
+// (one pass over the codes; the waves meet once, at the end of the range).
 //
 // Both products are transposed, so nothing crosses lanes between them:
 //   S^T = K Q^T   A = codes of 16 positions, B = queries; lane 16 q + c gets
@@ -793,10 +793,10 @@ struct Segments {
   }
 };
 
-template <int HD>
+template <int HD, int W>
 struct AttendSmem {
-  float o[kWaves][16][HD + 4];
-  float m[kWaves][16], l[kWaves][16];
+  float o[W][16][HD + 4];
+  float m[W][16], l[W][16];
 };
 
 // Output of (request b, packed row pr, features f .. + 3)
@@ -816,11 +816,12 @@ __device__ __forceinline__ void store_out(const KvqAttend& p, int b, int kvh, in
   }
 }
 
-template <int HD, bool QB>
-__global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2))) kvq_attend_kernel(KvqAttend p) {
+template <int HD, bool QB, int W>
+__global__ void __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(2))) kvq_attend_kernel(KvqAttend p) {
+  constexpr bool WHOLE = W != kWaves;  // a workgroup takes all of a head
   constexpr int FT = HD / 16;        // O^T products: features (HD / 16) c + j
   constexpr int N = QB ? 1 : 3;      // bf16 terms of p s
-  __shared__ AttendSmem<HD> sm;
+  __shared__ AttendSmem<HD, W> sm;
   const int tid = threadIdx.x, lane = tid & 63, q = lane >> 4, c = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // Workgroup i runs on XCD i % 8: the row tiles of one range follow each other
@@ -830,7 +831,7 @@ __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_e
   const int NR = p.G * p.R;
   const float sl = p.scale * kLog2e / kZScale;
   Segments<false> sg;
-  const bool even = p.parts > 0;  // every head in so many equal parts
+  const bool even = WHOLE || p.parts > 0;  // every head in so many equal parts
   if (even) {
     const unsigned head = range / (unsigned)p.parts, part = range - head * p.parts;
     if (head >= (unsigned)(p.B * p.KVH)) return;
@@ -859,7 +860,7 @@ __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_e
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
-      const int nb = max(min(sg.lo + wave + n * kWaves, sg.hi - 1), 0);
+      const int nb = max(min(sg.lo + wave + n * W, sg.hi - 1), 0);
       ld.keys(buf[n], nb);
       // (in the order of the loop, or its head would have to wait for more)
       asm volatile("" ::: "memory");
@@ -874,7 +875,7 @@ __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_e
     const RequestRows rr = sg.rr;
     const int b = sg.b, kvh = sg.h, blk_hi = sg.hi;
     const unsigned bh = (unsigned)(b * p.KVH + kvh);
-    const bool all = even ? p.parts == 1 : sg.lo == 0 && sg.hi == sg.nb, ok = row_ok && i < rr.n;
+    const bool all = WHOLE || (even ? p.parts == 1 : sg.lo == 0 && sg.hi == sg.nb), ok = row_ok && i < rr.n;
     const int vis = ok ? rr.L + i + 1 : 0;  // positions the lane's row sees
     Queries<HD, QB> Q;
     Q.convert(qx, ok);
@@ -884,7 +885,7 @@ __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_e
     for (int j = 0; j < FT; ++j) o[j] = floatx4{0.f, 0.f, 0.f, 0.f};
 
     auto block = [&](Block<HD>& cur, int blk) {
-      const int nb = min(blk + 2 * kWaves, blk_hi - 1);  // the buffer's next block
+      const int nb = min(blk + 2 * W, blk_hi - 1);  // the buffer's next block
       float z[2][4];
       scores<HD, QB>(cur, Q, z);
       ld.keys(cur, nb);
@@ -973,11 +974,11 @@ __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_e
           for (int j = 0; j < 4; ++j) o[4 * jh + j] = mfma(a[j], P[n], o[4 * jh + j]);
       }
     };
-    for (int blk = sg.lo + wave; blk < blk_hi; blk += 2 * kWaves) {
+    for (int blk = sg.lo + wave; blk < blk_hi; blk += 2 * W) {
       block(buf[0], blk);
       __builtin_amdgcn_sched_barrier(0);
-      if (blk + kWaves >= blk_hi) break;
-      block(buf[1], blk + kWaves);
+      if (blk + W >= blk_hi) break;
+      block(buf[1], blk + W);
       __builtin_amdgcn_sched_barrier(0);
     }
 
@@ -997,15 +998,15 @@ __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_e
     const bool more = !even && sg.next(p);
     if (more) request();  // (in flight while this segment is put together)
     __syncthreads();
-    for (int e = tid; e < 16 * (HD / 4); e += kWaves * 64) {
+    for (int e = tid; e < 16 * (HD / 4); e += W * 64) {
       const int row = e / (HD / 4), f = 4 * (e - row * (HD / 4)), pr = (int)tile * 16 + row;
       if (pr >= NR) continue;
       float mm = -INFINITY;
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) mm = fmaxf(mm, sm.m[w][row]);
+      for (int w = 0; w < W; ++w) mm = fmaxf(mm, sm.m[w][row]);
       float ll = 0.f, a[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
+      for (int w = 0; w < W; ++w) {
         const float mw = sm.m[w][row], lw = sm.l[w][row];
         // (a wave that saw nothing of this row holds zeros)
         const float s = mw == -INFINITY && lw == 0.f ? 0.f : __builtin_amdgcn_exp2f(mw - mm);
@@ -1543,6 +1544,15 @@ namespace {
 // part per head (up to 256 keys) needs no merge (250 positions: 5.8 us, 6.5 and
 // 3.8 as ranges).
 //
+// Workgroups of eight waves take whole heads where every compute unit gets one
+// at most and the heads are short for their number: it is the merge and its
+// launch against fewer workgroups.  Row tiles, blocks of keys each, us with
+// whole heads / without: 32 float32 tiles, 16 blocks 8.4 / 9.0, 24 9.8 / 9.7; 64,
+// 24 9.9 / 9.6; 96, 32 11.6 / 12.6, 64 17.5 / 17.5; 128, 40 13.2 / 17.0, 80 20.4 /
+// 21.5; 256, 40 13.8 / 21.2, 96 25.4 / 32.0; bf16, 8 tiles, 32 blocks 8.3 / 8.5;
+// 128, 40 10.2 / 14.2, 96 17.5 / 18.9.  The bound stays below what pays for equal
+// lengths, since a long request among short ones holds its workgroup alone.
+//
 // What bounds it: long caches the stream (120 thousand positions, 130 MB, 24.7
 // us, 5.3 TB/s; the 16 requests above 5.6 TB/s, what a plain copy reaches); many
 // float32 rows over a few thousand positions the vector instructions (300 per
@@ -1567,12 +1577,20 @@ hipError_t attend_hd(KvqAttend a, hipStream_t st) {
   const int64_t pieces = (blocks + 2 * kWaves - 1) / (2 * kWaves), fit = kAttendWgs / a.TG / heads;
   a.parts = a.B == 1 || pieces <= std::max<int64_t>(fit, 1) ? (int)std::max<int64_t>(1, std::min(pieces, fit)) : 0;
   if (a.parts > 0) wgs = heads * a.parts;
+  const int64_t tiles = heads * a.TG;
+  const bool whole = tiles <= kAttendWgs / 2 && blocks > 2 * kWaves && blocks <= std::max<int64_t>(a.bf16 ? 32 : 20, tiles * 3 / 8);
+  if (whole) {
+    a.parts = 1;
+    wgs = heads;
+  }
   a.WG = (int)wgs;
   const int64_t grid = 8 * a.TG * ((wgs + 7) / 8);
   if (grid > 0x7fffffff || rows > 0x7fffffff || attend_blocks(a) > 0x7fffffff) return hipErrorInvalidValue;
   if (a.parts != 1 && (heads + wgs) * a.G * a.R > (int64_t)a.part_rows) return hipErrorInvalidValue;
-  if (a.bf16) hipLaunchKernelGGL((kvq_attend_kernel<HD, true>), dim3((unsigned)grid), dim3(kWaves * 64), 0, st, a);
-  else hipLaunchKernelGGL((kvq_attend_kernel<HD, false>), dim3((unsigned)grid), dim3(kWaves * 64), 0, st, a);
+  auto launch = [&](auto kernel, int waves) { hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(waves * 64), 0, st, a); };
+  constexpr int W = kWaves, W2 = 2 * kWaves;
+  if (whole) launch(a.bf16 ? kvq_attend_kernel<HD, true, W2> : kvq_attend_kernel<HD, false, W2>, W2);
+  else launch(a.bf16 ? kvq_attend_kernel<HD, true, W> : kvq_attend_kernel<HD, false, W>, W);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (a.parts != 1) {

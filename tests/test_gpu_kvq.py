@@ -277,6 +277,36 @@ def test_attend(b, r, h, kvh, hd, lens, wr, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("b,r,h,kvh,hd,most", [
+    (16, 2, 16, 8, 128, 2500),  # ranges over the batch, several heads each
+    (70, 1, 4, 2, 64, 2300),    # more requests than a wave has lanes
+    (3, 16, 16, 2, 128, 2000),  # equal parts, tiles of 16 rows
+    (16, 3, 16, 8, 128, 1300),  # whole heads of a workgroup
+    (12, 16, 6, 1, 64, 700),
+    (1, 16, 1, 1, 128, 600),
+])
+def test_attend_cuts(b, r, h, kvh, hd, most, dtype):
+    """Batches of requests of all lengths, some without rows in use, whichever
+    way their heads are divided among workgroups; weights too."""
+    rng = np.random.default_rng(b + r)
+    lens = [int(x) for x in rng.integers(0, most, b)]
+    lens[-1] = most
+    rows = [int(x) for x in rng.integers(0, r + 1, b)]
+    rows[-1] = r
+    cache = kvq.QuantCache(1, b, h, kvh, hd, most + r, max_rows=r, device=DEV)
+    poison(cache)
+    k, v = rand(rng, b, most + r, kvh, hd, dtype=dtype), rand(rng, b, most + r, kvh, hd, dtype=dtype)
+    fill(cache, 0, k, v, rows=i32([a + c for a, c in zip(lens, rows)]))
+    cache.lens.copy_(i32(lens))
+    q = rand(rng, b, r, h, hd, dtype=dtype)
+    w = torch.zeros((b, kvh, cache.max_len), device=DEV)
+    out = cache.attend(0, q, rows=i32(rows), weights_out=w, weight_rows=1)
+    check_attend(q, k, v, lens, rows, out, hd ** -0.5, dtype, None, w, 1)
+    assert cache.device_error() == 0
+    assert torch.equal(cache.attend(0, q, rows=i32(rows)), out)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_attend_scale_and_large_scores(dtype):
     """Scores of some thousands (a softmax that is one position), and a scale
     of its own."""

@@ -1555,8 +1555,8 @@ namespace {
 //
 // What bounds it: long caches the stream (120 thousand positions, 130 MB, 24.7
 // us, 5.3 TB/s; the 16 requests above 5.6 TB/s, what a plain copy reaches); many
-// float32 rows over a few thousand positions the vector instructions (300 per
-// block and wave beside 51 matrix instructions: 16 requests of 256 to 4096
+// float32 rows over a few thousand positions the vector instructions (264 per
+// block and wave beside 48 matrix instructions: 16 requests of 256 to 4096
 // positions, 9 rows, 4 query heads a K/V head, 30 us); a short request the launch
 // and four dependent round trips to memory.
 constexpr int kAttendWgs = 512;

@@ -112,6 +112,38 @@ def test_append_holds_what_the_definition_gives(b, r, h, kvh, hd, lens, norm, ro
     assert cache.device_error() == 0
 
 
+@pytest.mark.parametrize("hd,r,h,kvh,dtype", [(128, 3001, 8, 4, "f32"), (64, 6011, 8, 4, "bf16"), (128, 9000, 2, 1, "bf16")])
+def test_append_long_prompts(hd, r, h, kvh, dtype):
+    """Prompts whose rows a workgroup takes in several rounds, the second
+    request's shorter than the call."""
+    rng = np.random.default_rng(r)
+    rows, lens = [r, r - 1234], [3, 0]
+    cache = kvq.QuantCache(1, 2, h, kvh, hd, r + 5, device=DEV)
+    poison(cache)
+    cache.lens.copy_(i32(lens))
+    q, k, v = (rand(rng, 2, r, n, hd, dtype=dtype) for n in (h, kvh, kvh))
+    gain = rand(rng, hd).abs()
+    tab = kvq.rope_table(r + 5, hd, 10000.0, DEV)
+    out = cache.append(0, k, v, q=q, gain_q=gain, gain_k=gain, rope=tab, rows=i32(rows))
+    assert cache.device_error() == 0
+    gk, gv = cache.read(0, r, start=cache.lens, rows=i32(rows))
+    for b in (0, 1):
+        n, ang = rows[b], f64(tab)[lens[b]:lens[b] + rows[b], None]
+        y = f64(k[b, :n])
+        y = y / np.sqrt((y * y).mean(-1, keepdims=True) + 1e-5) * f64(gain)
+        a, c = y[..., :hd // 2], y[..., hd // 2:]
+        y = np.concatenate([a * ang[..., 0] - c * ang[..., 1], c * ang[..., 0] + a * ang[..., 1]], -1)
+        np.testing.assert_array_equal(gk[b, :n].cpu().numpy(), okvq.held(y).astype(np.float32))
+        np.testing.assert_array_equal(gv[b, :n].cpu().numpy(), okvq.held(f64(v[b, :n])).astype(np.float32))
+        for i in (0, n // 2, n - 1):
+            want = okvq.norm_rotate(f64(q[b, i]), f64(gain), 1e-5, f64(tab)[lens[b] + i])
+            # roundings: as in test_append_holds_what_the_definition_gives
+            top = np.abs(want).max(-1, keepdims=True) * 2
+            tol = (hd / 8 + 16) * 2.0 ** -24 * top + (2.0 ** -8 * np.abs(want) if dtype == "bf16" else 0)
+            assert (np.abs(f64(out[b, i]) - want) <= tol).all()
+    assert not out[1, rows[1]:].any() and not gk[1, rows[1]:].any()
+
+
 def test_append_rows_at_borders():
     """Constant rows, zeros, halves of steps (ties to even), tiny and huge
     rows, rows that are not finite."""

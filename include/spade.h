@@ -404,8 +404,10 @@ spade_status spade_kvq_append(const spade_kvq_shape* shape, int layer, void* d_c
  * (spade_kvq_append): row i sees positions 0 .. lens[b] + i,
  *   out = softmax(scale q . k) v   per query head,
  * d_q and d_out [B R] rows of n_heads heads in `dtype` that do not overlap;
- * rows that a request does not use give zeros.  max_keys: the host's bound of lens[b] + rows, in
- * [R, max_len], or 0 for max_len (a longer request is cut to it and flagged).
+ * rows that a request does not use give zeros.  max_keys: the host's bound of
+ * lens[b] + the rows in use, in [1, max_len] ([R, max_len] without d_rows), or
+ * 0 for max_len.  A longer request is cut to it and flagged: its length, and of
+ * more than max_keys rows those behind count as not in use.
  * d_weights_out (NULL: none): out = in + sum of the probabilities that the
  * first weight_rows rows in use of request b gave a position, over the query
  * heads of its K/V head, for the positions below lens[b] + rows; the others are

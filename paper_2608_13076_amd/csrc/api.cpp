@@ -1028,7 +1028,10 @@ spade_status spade_kvq_attend(const spade_kvq_shape* s, int layer, const void* d
     return fail(SPADE_EINVAL, "cache and workspace must be 256-byte aligned");
   if (!(scale > 0.f && scale <= 0x1p50f)) return fail(SPADE_EINVAL, "scale must be in (0, 2^50]");
   if (max_keys == 0) max_keys = s->max_len;
-  if (max_keys < R || max_keys > s->max_len) return fail(SPADE_ECAPACITY, "max_keys must be in [R, max_len]");
+  // (a ragged batch of short contexts has a bound below its padded rows)
+  const int least = d_rows ? 1 : R;
+  if (max_keys < least || max_keys > s->max_len)
+    return fail(SPADE_ECAPACITY, "max_keys %d must be in [%d, %d]", max_keys, least, s->max_len);
   if (d_weights_out && (weight_rows < 0 || weight_rows > R)) return fail(SPADE_EINVAL, "weight_rows must be in [0, R]");
   if (d_weights_in && !d_weights_out) return fail(SPADE_EINVAL, "weights_in without weights_out");
   const size_t wb = (size_t)s->batch * s->n_kv_heads * s->max_len * 4;

@@ -92,7 +92,7 @@ struct KvqAttend {
   float scale;
   const int32_t* lens;
   const int32_t* rows;
-  int max_keys;  // bound of lens + rows
+  int max_keys;  // bound of lens + rows in use, in 1 .. max_len (may be below R)
   void* out;
   int64_t out_ld;
   size_t split;  // 0, or float32 calls: out is the two bf16 terms of a GEMM operand, this many elements apart

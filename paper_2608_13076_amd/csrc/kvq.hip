@@ -632,15 +632,16 @@ __device__ __forceinline__ void scores(const Block<HD>& b, const Queries<HD, QB>
 }
 
 struct RequestRows {
-  int L, n;  // cached positions before the rows, rows in use
+  int L, n;  // cached positions before the rows, rows in use: L, n >= 0, L + n <= max_keys
 };
 
 __device__ __forceinline__ RequestRows request_rows(const KvqAttend& p, int b) {
   RequestRows r;
   r.n = p.rows != nullptr ? max(0, min(p.rows[b], p.R)) : p.R;
   r.L = p.lens[b];
-  if (r.L < 0 || r.L > p.max_keys - r.n) {  // (n <= R <= max_keys)
+  if (r.L < 0 || r.L > p.max_keys - r.n) {  // (also where n > max_keys)
     flag_error(p.err, SPADE_DERR_CAPACITY);
+    r.n = min(r.n, p.max_keys);
     r.L = r.L < 0 ? 0 : p.max_keys - r.n;
   }
   return r;

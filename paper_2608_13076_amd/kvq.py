@@ -139,7 +139,7 @@ class QuantCache:
         """Causal attention of q [B, R, n_heads, head_dim], whose rows ``append``
         has stored, over the layer; returns out (same shape and dtype).  scale:
         1 / sqrt(head_dim) unless given.  max_keys: the host's bound of lens +
-        rows (0: max_len).  weights_out = weights + the probabilities of the
+        the rows in use (0: max_len; at least R without ``rows``).  weights_out = weights + the probabilities of the
         first weight_rows rows, both [batch, n_kv_heads, max_len] (may be one
         tensor).  See spade_kvq_attend."""
         dt, shape, arg = q.dtype, q.shape, self._arg

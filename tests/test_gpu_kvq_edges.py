@@ -1,0 +1,74 @@
+"""4-bit K/V caches at the ends of what their calls allow: bounds below the
+padded rows."""
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2608_13076_amd import kvq, spade
+from tests.test_gpu_kvq import DEV, check_attend, fill, i32, poison, rand
+
+pytestmark = pytest.mark.gpu
+
+
+# --- the bound of an attention call ---------------------------------------
+
+SHORT = [
+    # lens, rows, R, max_len, max_keys
+    ([4], [3], 8, 40, 7),
+    ([0, 1], [6, 1], 8, 40, 6),
+    ([3, 0], [2, 0], 5, 40, 5),
+    ([0, 0, 0], [1, 0, 2], 16, 40, 2),
+    ([0], [1], 16, 1, 0),          # a cache shorter than the padded rows
+    ([2, 5], [3, 0], 16, 5, 0),
+    ([0] * 20, [1 + i % 3 for i in range(20)], 9, 33, 3),
+]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("weights", [False, True])
+@pytest.mark.parametrize("hd,h,kvh", [(128, 8, 2), (64, 3, 3)])
+@pytest.mark.parametrize("lens,rows,R,max_len,max_keys", SHORT)
+def test_attend_bound_below_the_padded_rows(lens, rows, R, max_len, max_keys, hd, h, kvh, weights, dtype):
+    """max_keys bounds the rows in use: a ragged batch of short contexts has a
+    bound below R, and a cache may be shorter than R."""
+    rng = np.random.default_rng(R + max_len)
+    b = len(lens)
+    cache = kvq.QuantCache(1, b, h, kvh, hd, max_len, max_rows=R, device=DEV)
+    poison(cache)
+    n = max(a + c for a, c in zip(lens, rows))
+    k, v = rand(rng, b, n, kvh, hd, dtype=dtype), rand(rng, b, n, kvh, hd, dtype=dtype)
+    fill(cache, 0, k, v, rows=i32([a + c for a, c in zip(lens, rows)]))
+    cache.lens.copy_(i32(lens))
+    q = rand(rng, b, R, h, hd, dtype=dtype, strong=False)
+    kw, w, wo = {}, None, None
+    if weights:
+        w = rand(rng, b, kvh, max_len, strong=False).abs()
+        wo = torch.full_like(w, -3.0)
+        kw = dict(weights=w, weights_out=wo, weight_rows=R)
+    out = cache.attend(0, q, rows=i32(rows), max_keys=max_keys, **kw)
+    assert cache.device_error() == 0
+    check_attend(q, k, v, lens, rows, out, hd ** -0.5, dtype, w, wo, R, torch.full_like(wo, -3.0) if weights else None)
+
+
+def test_attend_rows_beyond_the_bound_are_cut_and_flagged():
+    """More rows in use than the bound: the first max_keys of them over the
+    empty cache, zeros behind; with a length, the length is cut first."""
+    rng = np.random.default_rng(4)
+    cache = kvq.QuantCache(1, 3, 4, 2, 128, 30, max_rows=8, device=DEV)
+    k, v = rand(rng, 3, 30, 2, 128), rand(rng, 3, 30, 2, 128)
+    fill(cache, 0, k, v)
+    q = rand(rng, 3, 8, 4, 128, strong=False)
+    for lens in ([0, 9, -2], [2, 0, 2**31 - 1]):
+        cache.lens.copy_(i32(lens))
+        w = torch.zeros((3, 2, 30), device=DEV)
+        out = cache.attend(0, q, rows=i32([8, 7, 8]), max_keys=5, weights_out=w, weight_rows=8)
+        assert cache.device_error() == spade.DERR_CAPACITY
+        check_attend(q, k, v, [0, 0, 0], [5, 5, 5], out, 128 ** -0.5, "f32", None, w, 8)
+        assert not w[:, :, 5:].any()
+    with pytest.raises(spade.SpadeError):  # without rows all R are in use
+        cache.attend(0, q, max_keys=5)
+    with pytest.raises(spade.SpadeError):
+        cache.attend(0, q, rows=i32([1, 1, 1]), max_keys=31)
+    with pytest.raises(spade.SpadeError):
+        cache.attend(0, q, rows=i32([1, 1, 1]), max_keys=-1)

@@ -230,6 +230,10 @@ spade_status spade_prefill(spade_model m, spade_kv kv, int b, const int32_t* d_t
  * bound alone fails), and B <= max_batch, gamma <= max_gamma.  A device
  * length the bound did not cover (lens written outside the library) is
  * clamped on the device and flagged SPADE_DERR_CAPACITY.
+ * A captured call covers lens[b] + gamma + 1 up to the largest bound at the
+ * capture, rounded up to whole chunks of 256 positions (bf16 cache of head_dim
+ * 128) or 128 (others) and at most max_len; a longer request is clamped and
+ * flagged likewise.
  */
 spade_status spade_verify(spade_model m, spade_kv kv, int B, int gamma,
                           const int32_t* d_draft_tokens, const float* d_draft_probs,

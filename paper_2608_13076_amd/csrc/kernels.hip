@@ -1610,8 +1610,9 @@ namespace {
 // QKV projection into the cache, the queries normed and rotated where they
 // are, the attention's output as the O projection's operand.  Running weights
 // count every prompt row, but of a verify call only the pending token's row:
-// its drafts may be rejected.
-hipError_t launch_kvq_layer(spade_model md, spade_kv kv, int l, const ForwardCall& fc, int max_keys, bool last,
+// its drafts may be rejected.  len_limit bounds lens + R on the device
+// (embed_kernel), also where a captured call is replayed over longer requests.
+hipError_t launch_kvq_layer(spade_model md, spade_kv kv, int l, const ForwardCall& fc, int len_limit, bool last,
                             hipStream_t st) {
   const Dims& D = md->dims;
   const Workspace& W = md->ws;
@@ -1660,7 +1661,7 @@ hipError_t launch_kvq_layer(spade_model md, spade_kv kv, int l, const ForwardCal
   t.scale = 1.0f / sqrtf((float)D.hd);
   t.lens = a.lens;
   t.rows = a.rows;
-  t.max_keys = std::min(std::max(max_keys, fc.R), kv->max_len);
+  t.max_keys = len_limit;
   t.out = W.act_o;
   t.out_ld = D.d;
   t.split = D.wdt == SPADE_BF16 ? W.act_split : 0;
@@ -1743,7 +1744,7 @@ hipError_t launch_forward(spade_model md, spade_kv kv, const ForwardCall& fc, hi
     // without logits only the last layer's K and V rows are used
     const bool last = !fc.want_logits && l + 1 == D.L;
     if (D.kvdt == SPADE_I4) {
-      if ((e = launch_kvq_layer(md, kv, l, fc, max_keys, last, st)) != hipSuccess) return e;
+      if ((e = launch_kvq_layer(md, kv, l, fc, ep.len_limit, last, st)) != hipSuccess) return e;
       if (last) break;
       if ((e = launch_layer_gemm(md, kv, GEMM_O, l, fc, st)) != hipSuccess) return e;
       if ((e = launch_layer_gemm(md, kv, GEMM_GU, l, fc, st)) != hipSuccess) return e;

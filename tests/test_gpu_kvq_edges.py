@@ -1,12 +1,15 @@
 """4-bit K/V caches at the ends of what their calls allow: bounds below the
-padded rows."""
+padded rows, captured calls over growing lengths."""
 
 import numpy as np
 import pytest
 import torch
 
 from paper_2608_13076_amd import kvq, spade
+from synth import make_inputs
+from tests.helpers import gpu_setup
 from tests.test_gpu_kvq import DEV, check_attend, fill, i32, poison, rand
+from tests.test_gpu_kvq_model import i4
 
 pytestmark = pytest.mark.gpu
 
@@ -72,3 +75,44 @@ def test_attend_rows_beyond_the_bound_are_cut_and_flagged():
         cache.attend(0, q, rows=i32([1, 1, 1]), max_keys=31)
     with pytest.raises(spade.SpadeError):
         cache.attend(0, q, rows=i32([1, 1, 1]), max_keys=-1)
+
+
+# --- captured verify calls ------------------------------------------------
+
+
+@pytest.mark.parametrize("name", ["mini_bf16_mixed", "mini_gqa_mixed_b5", "mini_f32_greedy"])
+def test_captured_verify_covers_growing_lengths(name):
+    """One graph of a verify call, replayed after commits that move the lengths
+    on: every replay equals the eager call at the same lengths (contexts of one
+    attention part per head, whose bits do not depend on the bound)."""
+    w = i4(name)
+    model, kv = gpu_setup(w, max_len=200)
+    W = kv.track_weights()
+    rng = np.random.default_rng(2)
+    kv.prefill_batch([rng.integers(0, w.model.vocab, 40 + 3 * b).astype(np.int32) for b in range(w.batch)])
+    inp = make_inputs(w)
+    buf = spade.VerifyBuffers(model, inp.drafts, inp.draft_probs, inp.uniforms, inp.modes, True)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(s):
+        with torch.cuda.graph(graph, stream=s):
+            spade.verify(model, kv, buf, inp.temperature)
+    torch.cuda.synchronize()
+    R = w.gamma + 1
+    n = torch.full((w.batch,), w.gamma, dtype=torch.int32, device=DEV)
+    top = 39 + 3 * (w.batch - 1)
+    while top + R <= 128:
+        before = W.clone()
+        graph.replay()
+        torch.cuda.synchronize()
+        got, got_w = buf.logits.clone(), W.clone()
+        W.copy_(before)
+        buf.logits.zero_()
+        spade.verify(model, kv, buf, inp.temperature)
+        torch.cuda.synchronize()
+        assert torch.equal(got, buf.logits), top
+        assert torch.equal(got_w, W), top
+        kv.commit(n, buf.corr)
+        top += R
+    assert model.device_error() == 0

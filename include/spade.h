@@ -253,7 +253,8 @@ spade_status spade_verify(spade_model m, spade_kv kv, int B, int gamma,
  * weights too and more than 32 rows holds each request's own number of rows;
  * in others a request whose prompt runs out contributes placeholder rows,
  * written past its length and only where the cache has room.  Needs lens + h_n_tokens[b] <=
- * max_len (else SPADE_ECAPACITY).  Counts are read from host memory
+ * max_len (else SPADE_ECAPACITY; checked as by spade_verify, and so by
+ * spade_prefill).  Counts are read from host memory
  * (h_n_tokens) before the call returns. */
 spade_status spade_prefill_batch(spade_model m, spade_kv kv, int B, const int32_t* d_tokens, int ld,
                                  const int32_t* h_n_tokens, void* stream);
@@ -327,7 +328,8 @@ spade_status spade_kv_track_weights(spade_kv kv, float* d_weights);
  * `budget` positions, the last `recent` and the budget - recent of the others
  * with the largest running weights (spade_kvq_evict, in place); lens[b] becomes
  * min(lens[b], budget).  Later rows keep counting their positions from the
- * start of the sequence, which may go on to the model's max_len.  d_kept:
+ * start of the sequence, which may go on to the model's max_len: where it ends
+ * before the cache is full, spade_verify and the prefill calls refuse too.  d_kept:
  * int32 [n_layers][max_batch][n_kv_heads][budget].  Rows of a verify call that
  * was not committed are lost.  A captured call counts once for the host's
  * bounds and snapshots, however often it is replayed. */

@@ -53,7 +53,39 @@ spade_status refresh_bound(spade_kv kv, int B, hipStream_t st) {
 // Whether `rows` more positions of request b fit the cache and the model's
 // positions (evicted ones count), by the host bounds.
 bool rows_fit(spade_kv kv, int b, int rows) {
-  return kv->lens_ub[b] + rows <= kv->max_len && kv->lens_ub[b] + kv->evicted_ub[b] + rows <= kv->model->max_len;
+  const int64_t end = (int64_t)kv->lens_ub[b] + rows;
+  return end <= kv->max_len && end + kv->evicted_ub[b] <= kv->model->max_len;
+}
+
+bool capturing(hipStream_t st) {
+  hipStreamCaptureStatus c;
+  if (hipStreamIsCapturing(st, &c) == hipSuccess) return c != hipStreamCaptureStatusNone;
+  (void)hipGetLastError();  // (the default stream beside a capture)
+  return true;
+}
+
+// Whether rows(b) more positions of every request b0 <= b < B fit.  The host
+// bound grows by gamma + 1 per commit (an eviction moves that on to the evicted
+// positions) while the lengths grow by k + 1: where it does not allow the rows,
+// the device's counts are read once before giving up (a capture cannot wait for
+// them).
+template <typename Rows>
+spade_status make_fit(spade_kv kv, int b0, int B, Rows rows, hipStream_t st) {
+  bool refreshed = false;
+  for (int b = b0; b < B; ++b) {
+    const int n = rows(b);
+    if (!rows_fit(kv, b, n) && !refreshed && !capturing(st)) {
+      const spade_status rs = refresh_bound(kv, B, st);
+      if (rs != SPADE_OK) return rs;
+      refreshed = true;
+    }
+    if (rows_fit(kv, b, n)) continue;
+    if ((int64_t)kv->lens_ub[b] + n > kv->max_len)
+      return fail(SPADE_ECAPACITY, "request %d: %d cached + %d positions exceed max_len %d", b, kv->lens_ub[b], n, kv->max_len);
+    return fail(SPADE_ECAPACITY, "request %d: %d cached, %d evicted + %d exceed the model's %d positions", b, kv->lens_ub[b],
+                kv->evicted_ub[b], n, kv->model->max_len);
+  }
+  return SPADE_OK;
 }
 
 spade_status check_config(const spade_config* c) {
@@ -508,6 +540,8 @@ spade_status spade_kv_get_state(spade_kv kv, int B, int32_t* h_lens, int32_t* h_
   hipStream_t st = (hipStream_t)stream;
   hipError_t e = hipMemcpyAsync(h_lens, kv->lens, (size_t)B * 4, hipMemcpyDeviceToHost, st);
   if (e == hipSuccess) e = hipMemcpyAsync(h_pending, kv->pending, (size_t)B * 4, hipMemcpyDeviceToHost, st);
+  if (e == hipSuccess && kv->evicted)
+    e = hipMemcpyAsync(kv->evicted_ub, kv->evicted, (size_t)B * 4, hipMemcpyDeviceToHost, st);
   if (e == hipSuccess) e = hipStreamSynchronize(st);
   if (e != hipSuccess) return hipfail(e, "kv_get_state");
   for (int b = 0; b < B; ++b) kv->lens_ub[b] = h_lens[b];
@@ -543,8 +577,8 @@ spade_status spade_prefill(spade_model m, spade_kv kv, int b, const int32_t* d_t
   if (b < 0 || b >= kv->max_batch) return fail(SPADE_EINVAL, "request %d out of range", b);
   if (n_tokens < 1) return fail(SPADE_EINVAL, "n_tokens must be >= 1");
   const int n_cache = n_tokens - 1;
-  if (!rows_fit(kv, b, n_cache + 1))
-    return fail(SPADE_ECAPACITY, "prefill of %d tokens overflows max_len %d", n_tokens, kv->max_len);
+  const spade_status fit = make_fit(kv, b, b + 1, [&](int) { return n_tokens; }, (hipStream_t)stream);
+  if (fit != SPADE_OK) return fit;
   hipError_t e = launch_prefill_one(m, kv, b, d_tokens, n_cache, (hipStream_t)stream);
   if (e != hipSuccess) return hipfail(e, "prefill");
   kv->verified = false;
@@ -564,20 +598,8 @@ spade_status spade_verify(spade_model m, spade_kv kv, int B, int gamma, const in
   if (!(temperature > 0.f && std::isfinite(temperature)))
     return fail(SPADE_EINVAL, "temperature must be finite and > 0");
   hipStream_t st = (hipStream_t)stream;
-  bool refreshed = false;
-  for (int b = 0; b < B; ++b)
-    if (!rows_fit(kv, b, gamma + 1)) {
-      // the host bound grows by gamma + 1 per commit while the lengths grow
-      // by k + 1: read the device lengths once before giving up
-      if (!refreshed) {
-        spade_status rs = refresh_bound(kv, B, st);
-        if (rs != SPADE_OK) return rs;
-        refreshed = true;
-      }
-      if (!rows_fit(kv, b, gamma + 1))
-        return fail(SPADE_ECAPACITY, "request %d: %d cached + %d rows exceed max_len %d", b, kv->lens_ub[b],
-                    gamma + 1, kv->max_len);
-    }
+  const spade_status fit = make_fit(kv, 0, B, [&](int) { return gamma + 1; }, st);
+  if (fit != SPADE_OK) return fit;
   kv->last_rows = gamma + 1;
   kv->last_B = B;
   kv->verified = true;
@@ -692,10 +714,9 @@ spade_status spade_prefill_batch(spade_model m, spade_kv kv, int B, const int32_
   for (int b = 0; b < B; ++b) {
     if (h_n_tokens[b] < 1 || h_n_tokens[b] > ld) return fail(SPADE_EINVAL, "request %d: n_tokens must be in [1, ld]", b);
     n_cache[b] = h_n_tokens[b] - 1;
-    if (!rows_fit(kv, b, n_cache[b] + 1))
-      return fail(SPADE_ECAPACITY, "request %d: %d cached + %d prompt tokens overflow max_len %d", b, kv->lens_ub[b],
-                  h_n_tokens[b], kv->max_len);
   }
+  const spade_status fit = make_fit(kv, 0, B, [&](int b) { return h_n_tokens[b]; }, (hipStream_t)stream);
+  if (fit != SPADE_OK) return fit;
   hipError_t e = launch_prefill_batch(m, kv, B, d_tokens, ld, n_cache.data(), (hipStream_t)stream);
   if (e != hipSuccess) return hipfail(e, "prefill_batch");
   kv->verified = false;

@@ -1,5 +1,5 @@
 """4-bit K/V caches at the ends of what their calls allow: bounds below the
-padded rows, captured calls over growing lengths."""
+padded rows, captured calls over growing lengths, host bounds after evictions."""
 
 import numpy as np
 import pytest
@@ -116,3 +116,58 @@ def test_captured_verify_covers_growing_lengths(name):
         kv.commit(n, buf.corr)
         top += R
     assert model.device_error() == 0
+
+
+# --- host bounds after evictions ------------------------------------------
+
+
+def drifted():
+    """A model of 200 positions over a cache of 60: 30 rounds of verify, commit
+    of no draft and eviction, whose host bound counts five positions each where
+    one was evicted."""
+    model, _ = gpu_setup(i4("mini_bf16_greedy"), max_len=200)
+    kv = spade.KVCache(model, 1, 60)
+    kv.track_weights()
+    rng = np.random.default_rng(0)
+    kv.prefill(0, rng.integers(0, 4001, 41).astype(np.int32))
+    none = torch.zeros(1, dtype=torch.int32, device=DEV)
+    for _ in range(30):
+        buf = spade.VerifyBuffers(model, np.zeros((1, 4), np.int32), None, None, np.zeros(1, np.uint8), False)
+        spade.verify(model, kv, buf)
+        kv.commit(none, none)
+        kv.evict(1, 40, 5)
+    return model, kv, rng.integers(0, 4001, 131).astype(np.int32)
+
+
+@pytest.mark.parametrize("how", ["prefill", "get_state and prefill", "batch"])
+def test_prompts_after_evictions_fit_where_there_is_room(how):
+    model, kv, ids = drifted()
+    if how == "get_state and prefill":
+        assert kv.get_state(1)[0].tolist() == [40]
+    if how == "batch":
+        kv.prefill_batch([ids[:15]])
+    else:
+        kv.prefill(0, ids[:15])
+    assert kv.get_state(1)[0].tolist() == [54]
+    assert model.device_error() == 0
+
+
+def test_refusals_name_what_ran_out():
+    model, kv, ids = drifted()
+    for call in (lambda: kv.prefill(0, ids[:30]), lambda: kv.prefill_batch([ids[:30]])):
+        with pytest.raises(spade.SpadeError) as e:
+            call()
+        assert e.value.status == -2 and "60" in str(e.value)  # the cache
+    big = spade.KVCache(model, 1, 190)
+    big.track_weights()
+    big.prefill(0, ids)
+    big.evict(1, 10, 2)  # 120 of 130 positions
+    for call in (lambda: big.prefill(0, ids[:71]), lambda: big.prefill_batch([ids[:71]])):
+        with pytest.raises(spade.SpadeError) as e:
+            call()
+        assert e.value.status == -2 and "200 positions" in str(e.value)
+    big.prefill(0, ids[:70])
+    buf = spade.VerifyBuffers(model, np.zeros((1, 4), np.int32), None, None, np.zeros(1, np.uint8), False)
+    with pytest.raises(spade.SpadeError) as e:
+        spade.verify(model, big, buf)
+    assert e.value.status == -2 and "200 positions" in str(e.value)

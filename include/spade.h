@@ -343,10 +343,10 @@ spade_status spade_kv_evict(spade_kv kv, int B, int budget, int recent, int32_t*
  * projections itself.  Every position and K/V head holds a key and a value of
  * head_dim features as codes n of 4 bits, with one scale s and one minimum m
  * (bfloat16) each:
- *   m = bf16(min_f x_f), s = bf16((max_f x_f - m) * (1 / 15))  (in float32)
+ *   m = bf16(min_f x_f), s = bf16(max(max_f x_f - m, 0) * (1 / 15))  (in float32)
  *   n_f = clamp((x_f - m) / s to the nearest integer, ties to even, 0, 15)
  *   (0 where s = 0), and the cache stands for x_f ~ m + n_f s.
- * A row with a feature that is not finite, or whose span max - m is not, is
+ * A row with a feature that is not finite, or whose m or max - m is not, is
  * held as NaN.  head_dim bytes and 8 more per position and K/V head (bfloat16
  * takes 4 head_dim).
  *

@@ -21,15 +21,16 @@ def bf16(x: np.ndarray) -> np.ndarray:
 
 def codes(x: np.ndarray):
     """(n, s, m) of rows x [..., hd]; rows that are not finite, or whose span
-    is beyond float32: s = m = NaN."""
+    max - m is not: s = m = NaN."""
     x = np.asarray(x, dtype=np.float32).astype(np.float64)
     bad = ~np.isfinite(x).all(-1, keepdims=True)
     x = np.where(bad, 0.0, x)
     m = bf16(x.min(-1, keepdims=True))
     with np.errstate(over="ignore"):
-        d = np.maximum((x.max(-1, keepdims=True) - m).astype(np.float32), np.float32(0))
+        d = (x.max(-1, keepdims=True) - m).astype(np.float32)
     bad = bad | ~np.isfinite(d)
-    d = np.where(bad, np.float32(0), d)
+    d = np.where(bad, np.float32(0), np.maximum(d, np.float32(0)))
+    m = np.where(bad, 0.0, m)
     s = bf16(d * np.float32(1 / 15))
     with np.errstate(divide="ignore", invalid="ignore"):
         n = np.where(s > 0, np.clip(np.rint((x - m) / np.where(s > 0, s, 1.0)), 0, 15), 0.0)

@@ -208,8 +208,8 @@ __device__ __forceinline__ uint32_t quantise(const float (&v)[8], uint32_t* pair
   hi = max_lanes<HD / 8>(hi);
   const uint16_t mb = f2bf(lo);
   const float m = bf2f(mb);
+  const bool bad = !(fabsf(hi - m) < INFINITY);  // a feature, the minimum as bfloat16 or the span is not finite
   const float span = max_nan(hi - m, 0.f);
-  const bool bad = !(span < INFINITY);  // a feature that is not finite, or a span beyond float32
   const uint16_t sb = f2bf(span * (1.0f / 15.0f));
   const float s = bf2f(sb);
   uint32_t code = 0;

@@ -1,10 +1,12 @@
 """4-bit K/V caches at the ends of what their calls allow: bounds below the
-padded rows, captured calls over growing lengths, host bounds after evictions."""
+padded rows, captured calls over growing lengths, host bounds after evictions,
+rows near the end of float32."""
 
 import numpy as np
 import pytest
 import torch
 
+from oracle import kvq as okvq
 from paper_2608_13076_amd import kvq, spade
 from synth import make_inputs
 from tests.helpers import gpu_setup
@@ -171,3 +173,25 @@ def test_refusals_name_what_ran_out():
     with pytest.raises(spade.SpadeError) as e:
         spade.verify(model, big, buf)
     assert e.value.status == -2 and "200 positions" in str(e.value)
+
+
+# --- ends of float32 ------------------------------------------------------
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_rows_whose_minimum_is_beyond_bfloat16_are_nan(hd):
+    """max - m of a row above the largest bfloat16 is not finite: NaN, as the
+    header says; next to it, rows that bfloat16 holds."""
+    x = np.full((4, 1, hd), 3.4e38, np.float32)
+    x[1, 0, ::2] = 3.398e38
+    x[2] = 3.389e38
+    x[3] = -3.4e38
+    t = torch.from_numpy(x)[None].to(DEV)
+    cache = kvq.QuantCache(1, 1, 1, 1, hd, 4, device=DEV)
+    cache.append(0, t, t)
+    for got in cache.read(0, 4):
+        got = got[0].cpu().numpy()
+        assert np.isnan(got[[0, 1, 3]]).all()
+        np.testing.assert_array_equal(got[2], okvq.held(x[2]).astype(np.float32))
+    want = okvq.held(x)
+    assert np.isnan(want[[0, 1, 3]]).all() and np.isfinite(want[2]).all()

@@ -208,3 +208,12 @@ def test_4_bit_model_buffers(lib):
     assert n < 0.27 * lib.spade_kv_bytes(ctypes.byref(cfg), 2, 1024)
     assert lib.spade_weight_bytes(ctypes.byref(cfg4)) == lib.spade_weight_bytes(ctypes.byref(cfg))
     assert lib.spade_workspace_bytes(ctypes.byref(cfg4), 2, 8, 1000) > 0
+
+
+def test_oracle_holds_minima_beyond_bfloat16_as_nan():
+    """A minimum that rounds to infinity in bfloat16 leaves no finite max - m."""
+    x = np.full((3, 64), 3.4e38, np.float32)
+    x[1] = -3.4e38
+    x[2] = 3.389e38
+    n, s, m = okvq.codes(x)
+    assert np.isnan(s[:2]).all() and np.isnan(m[:2]).all() and np.isfinite(okvq.held(x)[2]).all()

@@ -1,6 +1,6 @@
 """4-bit K/V caches at the ends of what their calls allow: bounds below the
 padded rows, captured calls over growing lengths, host bounds after evictions,
-rows near the end of float32."""
+rows and queries near the ends of float32."""
 
 import numpy as np
 import pytest
@@ -10,7 +10,7 @@ from oracle import kvq as okvq
 from paper_2608_13076_amd import kvq, spade
 from synth import make_inputs
 from tests.helpers import gpu_setup
-from tests.test_gpu_kvq import DEV, check_attend, fill, i32, poison, rand
+from tests.test_gpu_kvq import DEV, check_attend, f64, fill, i32, poison, rand
 from tests.test_gpu_kvq_model import i4
 
 pytestmark = pytest.mark.gpu
@@ -195,3 +195,28 @@ def test_rows_whose_minimum_is_beyond_bfloat16_are_nan(hd):
         np.testing.assert_array_equal(got[2], okvq.held(x[2]).astype(np.float32))
     want = okvq.held(x)
     assert np.isnan(want[[0, 1, 3]]).all() and np.isfinite(want[2]).all()
+
+
+# --- norms of queries -----------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("eps", [0.0, 1e-6])
+@pytest.mark.parametrize("e", [-110, -70, 0, 64, 100, 120])
+def test_queries_are_normed_over_the_range_of_float32(e, eps, dtype):
+    """Squares of 2^70 leave float32, the norm does not.  The result is rounded
+    once: half a step of its type."""
+    rng = np.random.default_rng(e + 200)
+    hd = 128
+    cache = kvq.QuantCache(1, 2, 4, 2, hd, 20, device=DEV)
+    q, k = rand(rng, 2, 5, 4, hd, dtype=dtype) * 2.0 ** e, rand(rng, 2, 5, 2, hd, dtype=dtype)
+    g, tab = rand(rng, hd), kvq.rope_table(20, hd, 10000.0, DEV)
+    out = f64(cache.append(0, k, k, q=q, gain_q=g, gain_k=g, eps=eps, rope=tab))
+    eps = float(np.float32(eps))
+    for b in (0, 1):
+        for i in range(5):
+            want = okvq.norm_rotate(f64(q[b, i]), f64(g), eps, f64(tab)[i])
+            # (a result rounded to float32 first: 2^-24 more)
+            half = 2.0 ** -24 if dtype == "f32" else 2.0 ** -8 + 2.0 ** -23
+            tol = half * np.abs(want) + 2.0 ** -40 * np.abs(want).max() + (2.0 ** -149 if dtype == "f32" else 2.0 ** -133)
+            assert (np.abs(out[b, i] - want) <= tol).all(), (e, eps)

@@ -420,12 +420,14 @@ spade_status spade_kvq_append(const spade_kvq_shape* shape, int layer, void* d_c
  * left as they were.  d_weights_in may be NULL (zeros) or d_weights_out.
  * Float32 calls keep their queries and the products of probabilities and
  * scales in 24 bits (three bfloat16 terms); bfloat16 calls round those products
- * to bfloat16 once.  Sums are float32, and the matrix instructions cut the
- * smaller of 32 products short: outputs of float32 calls are good to about 1e-6
- * of their size, probabilities to 1e-7.  Queries below 2^60 in size, values
- * below 2^50 and spans max - m of a value row above 2^-40 keep that precision;
- * smaller spans lose bits, larger numbers give infinities or NaN.  How the keys
- * are divided among workgroups follows the lengths of all requests, so the
+ * to bfloat16 once.  Sums and scores are float32, and the matrix instructions cut
+ * the smaller of 32 products short: where no score scale q . k, nor its part scale
+ * m sum_f q_f, exceeds 11 in size, outputs of float32 calls and probabilities
+ * (also as weights) are good to 1e-6 of their size, beyond that to 1e-6 + 2^-22
+ * of the largest.  Queries below 2^60 in size, values below 2^50 and spans max - m
+ * of a value row above 2^-40 keep that precision; smaller spans lose bits, larger
+ * numbers give infinities or NaN.  How the keys are divided among workgroups
+ * follows the lengths of all requests, so the
  * last bits of a result do too; the same call gives the same bits.  scale: in
  * (0, 2^50]. */
 spade_status spade_kvq_attend(const spade_kvq_shape* shape, int layer, const void* d_cache, int B, int R, int dtype,

@@ -1,6 +1,16 @@
 """4-bit K/V caches at the ends of what their calls allow: bounds below the
 padded rows, captured calls over growing lengths, host bounds after evictions,
-rows and queries near the ends of float32."""
+rows and queries near the ends of float32, and the precision of outputs and
+running weights.
+
+Precision.  Errors are taken as 2-norms over a request's rows in use.  With
+scores of at most 16 (in units of log2) a float32 evaluation of the formulas is
+off by: the exponent's argument and the log-sum-exp, half a step of numbers up
+to 16 each, 2^-21 ln 2 = 3.3e-7; a score of 128 products in three terms, some
+roundings of 2^-24 of sums below 16, 3e-7 in all as they have either sign; the
+exponential and the quotient, 2^-23 each.  Together below 1e-6 of an output's
+size, and of the size of a head's weights.
+"""
 
 import numpy as np
 import pytest
@@ -14,6 +24,27 @@ from tests.test_gpu_kvq import DEV, check_attend, f64, fill, i32, poison, rand
 from tests.test_gpu_kvq_model import i4
 
 pytestmark = pytest.mark.gpu
+
+
+def check(q, k, v, lens, rows, out, weights=None, w_out=None, wr=0):
+    """Outputs and weights of the requests against the oracle over the held
+    rows, to the bounds above; rows that are not in use are zeros."""
+    b, R, H, hd = q.shape
+    KVH = k.shape[2]
+    for i in range(b):
+        n, end = rows[i], lens[i] + rows[i]
+        assert not out[i, n:].any()
+        want_w = f64(weights[i, :, :end]) if weights is not None else np.zeros((KVH, end))
+        if n:
+            kk, vv = okvq.held(f64(k[i, :end])), okvq.held(f64(v[i, :end]))
+            o, p = okvq.attend(f64(q[i, :n]), kk, vv, lens[i], hd ** -0.5)
+            err = f64(out[i, :n]) - o
+            assert np.linalg.norm(err) <= 1e-6 * np.linalg.norm(o), (i, np.linalg.norm(err) / np.linalg.norm(o))
+            want_w = want_w + p[:min(wr, n)].sum(0).reshape(KVH, H // KVH, end).sum(1)
+        if w_out is not None:
+            d = f64(w_out[i, :, :end]) - want_w
+            # (and half a step of the running weights themselves)
+            assert np.linalg.norm(d) <= (1e-6 + 2.0 ** -24) * np.linalg.norm(want_w), (i, np.linalg.norm(d) / np.linalg.norm(want_w))
 
 
 # --- the bound of an attention call ---------------------------------------
@@ -220,3 +251,61 @@ def test_queries_are_normed_over_the_range_of_float32(e, eps, dtype):
             half = 2.0 ** -24 if dtype == "f32" else 2.0 ** -8 + 2.0 ** -23
             tol = half * np.abs(want) + 2.0 ** -40 * np.abs(want).max() + (2.0 ** -149 if dtype == "f32" else 2.0 ** -133)
             assert (np.abs(out[b, i] - want) <= tol).all(), (e, eps)
+
+
+# --- precision ------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", ["f32"])
+@pytest.mark.parametrize("b,r,h,kvh,hd,most", [
+    (16, 2, 16, 8, 128, 2500),  # ranges over the batch, several heads each
+    (70, 1, 4, 2, 64, 2300),    # more requests than a wave has lanes
+    (3, 16, 16, 2, 128, 2000),  # equal parts, tiles of 16 rows
+    (16, 3, 16, 8, 128, 1300),  # whole heads of a workgroup
+    (12, 16, 6, 1, 64, 700),
+    (1, 16, 1, 1, 128, 600),
+    (1, 2, 8, 2, 128, 30000),   # a long request
+    (2, 9, 8, 2, 128, 200),     # one part per head
+])
+def test_outputs_and_weights_are_as_precise_as_float32(b, r, h, kvh, hd, most, dtype):
+    """Whichever way the heads are divided; every row counted into the weights."""
+    rng = np.random.default_rng(b + r + most)
+    lens = [int(x) for x in rng.integers(most // 8, most, b)]
+    lens[-1] = most
+    rows = [int(x) for x in rng.integers(0, r + 1, b)]
+    rows[-1] = r
+    cache = kvq.QuantCache(1, b, h, kvh, hd, most + r, max_rows=r, device=DEV)
+    k, v = rand(rng, b, most + r, kvh, hd, dtype=dtype), rand(rng, b, most + r, kvh, hd, dtype=dtype)
+    fill(cache, 0, k, v, rows=i32([a + c for a, c in zip(lens, rows)]))
+    cache.lens.copy_(i32(lens))
+    q = rand(rng, b, r, h, hd, dtype=dtype, strong=False)
+    w = rand(rng, b, kvh, cache.max_len, strong=False).abs() * 1e-3
+    wo = torch.empty_like(w)
+    out = cache.attend(0, q, rows=i32(rows), weights=w, weights_out=wo, weight_rows=r)
+    assert cache.device_error() == 0
+    check(q, k, v, lens, rows, out, w, wo, r)
+
+
+@pytest.mark.parametrize("mul", [4, 32, 256])
+def test_precision_of_large_scores(mul):
+    """Float32 scores beyond 11: the products' sum, the minimum's term, the sum of
+    both and the scale are half a step of the largest score each, 2^-22 of it
+    together, which is what a probability moves by."""
+    rng = np.random.default_rng(mul)
+    n, hd = 1500, 128
+    cache = kvq.QuantCache(1, 2, 8, 2, hd, n + 3, max_rows=3, device=DEV)
+    k, v = rand(rng, 2, n + 3, 2, hd), rand(rng, 2, n + 3, 2, hd)
+    fill(cache, 0, k, v)
+    cache.lens.fill_(n)
+    q = rand(rng, 2, 3, 8, hd, strong=False) * mul
+    w = torch.zeros((2, 2, n + 3), device=DEV)
+    out = cache.attend(0, q, weights_out=w, weight_rows=3)
+    for b in (0, 1):
+        kk, vv = okvq.held(f64(k[b])), okvq.held(f64(v[b]))
+        o, p = okvq.attend(f64(q[b]), kk, vv, n, hd ** -0.5)
+        top = max(np.abs(kk[:, h // 4] @ f64(q[b, i, h])).max() for i in range(3) for h in range(8)) * hd ** -0.5
+        assert top > 11
+        tol = 1e-6 + 2.0 ** -22 * top
+        pw = p.sum(0).reshape(2, 4, n + 3).sum(1)
+        assert np.linalg.norm(f64(out[b]) - o) <= tol * np.linalg.norm(o)
+        assert np.linalg.norm(f64(w[b]) - pw) <= tol * np.linalg.norm(pw)

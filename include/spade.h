@@ -419,8 +419,8 @@ spade_status spade_kvq_append(const spade_kvq_shape* shape, int layer, void* d_c
  * heads of its K/V head, for the positions below lens[b] + rows; the others are
  * left as they were.  d_weights_in may be NULL (zeros) or d_weights_out.
  * Float32 calls keep their queries and the products of probabilities and
- * scales in 24 bits (three bfloat16 terms); bfloat16 calls round those products
- * to bfloat16 once.  Sums and scores are float32, and the matrix instructions cut
+ * scales in 24 bits (three bfloat16 terms), bfloat16 calls those products in 16.
+ * Sums and scores are float32, and the matrix instructions cut
  * the smaller of 32 products short: where no score scale q . k, nor its part scale
  * m sum_f q_f, exceeds 11 in size, outputs of float32 calls and probabilities
  * (also as weights) are good to 1e-6 of their size, beyond that to 1e-6 + 2^-22

@@ -9,7 +9,9 @@ off by: the exponent's argument and the log-sum-exp, half a step of numbers up
 to 16 each, 2^-21 ln 2 = 3.3e-7; a score of 128 products in three terms, some
 roundings of 2^-24 of sums below 16, 3e-7 in all as they have either sign; the
 exponential and the quotient, 2^-23 each.  Together below 1e-6 of an output's
-size, and of the size of a head's weights.
+size, and of the size of a head's weights.  bfloat16 outputs add their own half
+step, 2^-8 of the element; the probabilities times scales enter in 16 bits, half
+a step 2^-17 of a term |n - 7.5| s <= 7.5 s_max.
 """
 
 import numpy as np
@@ -26,7 +28,7 @@ from tests.test_gpu_kvq_model import i4
 pytestmark = pytest.mark.gpu
 
 
-def check(q, k, v, lens, rows, out, weights=None, w_out=None, wr=0):
+def check(q, k, v, lens, rows, out, dtype, weights=None, w_out=None, wr=0):
     """Outputs and weights of the requests against the oracle over the held
     rows, to the bounds above; rows that are not in use are zeros."""
     b, R, H, hd = q.shape
@@ -39,7 +41,12 @@ def check(q, k, v, lens, rows, out, weights=None, w_out=None, wr=0):
             kk, vv = okvq.held(f64(k[i, :end])), okvq.held(f64(v[i, :end]))
             o, p = okvq.attend(f64(q[i, :n]), kk, vv, lens[i], hd ** -0.5)
             err = f64(out[i, :n]) - o
-            assert np.linalg.norm(err) <= 1e-6 * np.linalg.norm(o), (i, np.linalg.norm(err) / np.linalg.norm(o))
+            if dtype == "f32":
+                assert np.linalg.norm(err) <= 1e-6 * np.linalg.norm(o), (i, np.linalg.norm(err) / np.linalg.norm(o))
+            else:
+                _, s, _ = okvq.codes(f64(v[i, :end]))
+                inner = 7.5 * s.max() * 2.0 ** -17 + 4e-6 * np.abs(vv).max()
+                assert (np.abs(err) <= 2.0 ** -8 * (np.abs(o) + inner) + inner).all(), (i, np.abs(err).max())
             want_w = want_w + p[:min(wr, n)].sum(0).reshape(KVH, H // KVH, end).sum(1)
         if w_out is not None:
             d = f64(w_out[i, :, :end]) - want_w
@@ -256,7 +263,7 @@ def test_queries_are_normed_over_the_range_of_float32(e, eps, dtype):
 # --- precision ------------------------------------------------------------
 
 
-@pytest.mark.parametrize("dtype", ["f32"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("b,r,h,kvh,hd,most", [
     (16, 2, 16, 8, 128, 2500),  # ranges over the batch, several heads each
     (70, 1, 4, 2, 64, 2300),    # more requests than a wave has lanes
@@ -283,7 +290,7 @@ def test_outputs_and_weights_are_as_precise_as_float32(b, r, h, kvh, hd, most, d
     wo = torch.empty_like(w)
     out = cache.attend(0, q, rows=i32(rows), weights=w, weights_out=wo, weight_rows=r)
     assert cache.device_error() == 0
-    check(q, k, v, lens, rows, out, w, wo, r)
+    check(q, k, v, lens, rows, out, dtype, w, wo, r)
 
 
 @pytest.mark.parametrize("mul", [4, 32, 256])

@@ -1558,12 +1558,16 @@ namespace {
 //
 // Workgroups of eight waves take whole heads where every compute unit gets one
 // at most and the heads are short for their number: it is the merge and its
-// launch against fewer workgroups.  Row tiles, blocks of keys each, us with
-// whole heads / without: 32 float32 tiles, 16 blocks 8.4 / 9.0, 24 9.8 / 9.7; 64,
-// 24 9.9 / 9.6; 96, 32 11.6 / 12.6, 64 17.5 / 17.5; 128, 40 13.2 / 17.0, 80 20.4 /
-// 21.5; 256, 40 13.8 / 21.2, 96 25.4 / 32.0; bf16, 8 tiles, 32 blocks 8.3 / 8.5;
-// 128, 40 10.2 / 14.2, 96 17.5 / 18.9.  The bound stays below what pays for equal
-// lengths, since a long request among short ones holds its workgroup alone.
+// launch against fewer workgroups.  While parts of two blocks per wave leave a
+// workgroup per compute unit, that pays up to 20 blocks of keys (28 for bfloat16),
+// where they do not, longer.  Row tiles, blocks, us with whole heads / without: 32
+// float32 tiles, 20 blocks 8.9 / 9.6, 22 9.8 / 9.5; 64, 20 9.1 / 9.8, 24 10.1 / 9.8;
+// 80, 24 10.1 / 10.0, 28 10.7 / 12.3, 40 13.1 / 12.6; 96, 36 12.3 / 12.9, 64 17.7 /
+// 17.7; 128, 48 14.8 / 18.0, 80 20.8 / 21.2; 256, 96 25.4 / 32.5; bfloat16, 8 tiles,
+// 28 blocks 8.2 / 8.4, 32 9.0 / 8.5; 64, 28 8.7 / 9.0, 32 9.5 / 9.0; 96, 36 10.1 /
+// 11.2; 128, 48 12.1 / 15.5, 96 19.3 / 20.1; 256, 96 22.5 / 28.4.  The bound for many
+// tiles stays below what pays for equal lengths, since a long request among short
+// ones holds its workgroup alone.
 //
 // What bounds it: long caches the stream (120 thousand positions, 130 MB, 24.7
 // us, 5.3 TB/s; the 16 requests above 5.6 TB/s, what a plain copy reaches); many
@@ -1590,7 +1594,8 @@ hipError_t attend_hd(KvqAttend a, hipStream_t st) {
   a.parts = a.B == 1 || pieces <= std::max<int64_t>(fit, 1) ? (int)std::max<int64_t>(1, std::min(pieces, fit)) : 0;
   if (a.parts > 0) wgs = heads * a.parts;
   const int64_t tiles = heads * a.TG;
-  const bool whole = tiles <= kAttendWgs / 2 && blocks > 2 * kWaves && blocks <= std::max<int64_t>(a.bf16 ? 32 : 20, tiles * 3 / 8);
+  const int64_t most = std::max<int64_t>(a.bf16 ? 28 : 20, tiles * pieces > kAttendWgs / 2 ? tiles * 3 / 8 : 0);
+  const bool whole = tiles <= kAttendWgs / 2 && blocks > 2 * kWaves && blocks <= most;
   if (whole) {
     a.parts = 1;
     wgs = heads;

@@ -36,7 +36,8 @@ class QuantCache:
     holds; ``append`` and ``attend`` leave it alone, so a program adds the rows
     it keeps itself (``cache.lens += n``).  ``max_rows``: most rows per request
     of an ``attend`` call.  ``attend`` calls share one workspace, so those on
-    different streams have to be ordered by the program."""
+    different streams have to be ordered by the program.  No call records a
+    gradient: outputs do not require one, whatever the inputs do."""
 
     def __init__(self, n_layers: int, batch: int, n_heads: int, n_kv_heads: int, head_dim: int, max_len: int,
                  max_rows: int = 16, device="cuda:0"):
@@ -123,6 +124,8 @@ class QuantCache:
             if q_out is None:
                 q_out = q.new_empty(shape)
             op, old = self._rows(q_out, shape, dt, "q_out")
+        elif q_out is not None:
+            raise ValueError("q_out without q")
         f32, i32 = torch.float32, torch.int32
         n_rope = 0 if rope is None else rope.shape[0]
         self._call(

@@ -316,3 +316,13 @@ def test_precision_of_large_scores(mul):
         pw = p.sum(0).reshape(2, 4, n + 3).sum(1)
         assert np.linalg.norm(f64(out[b]) - o) <= tol * np.linalg.norm(o)
         assert np.linalg.norm(f64(w[b]) - pw) <= tol * np.linalg.norm(pw)
+
+
+# --- the binding ----------------------------------------------------------
+
+
+def test_append_refuses_an_output_without_queries():
+    cache = kvq.QuantCache(1, 1, 4, 2, 64, 8, device=DEV)
+    x = torch.zeros((1, 2, 2, 64), device=DEV)
+    with pytest.raises(ValueError):
+        cache.append(0, x, x, q_out=torch.zeros((1, 2, 4, 64), device=DEV))

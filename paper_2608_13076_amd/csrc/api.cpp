@@ -34,18 +34,19 @@ spade_status hipfail(hipError_t e, const char* what) {
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Set the host bound of lens[0..B) (and of the evicted positions) to the
+// Set the host bound of lens[b0..B) (and of the evicted positions) to the
 // device values (synchronises).
-spade_status refresh_bound(spade_kv kv, int B, hipStream_t st) {
-  std::vector<int32_t> h(B), ev(B, 0);
-  hipError_t e = hipMemcpyAsync(h.data(), kv->lens, (size_t)B * 4, hipMemcpyDeviceToHost, st);
+spade_status refresh_bound(spade_kv kv, int b0, int B, hipStream_t st) {
+  const size_t n = (size_t)(B - b0);
+  std::vector<int32_t> h(n), ev(n, 0);
+  hipError_t e = hipMemcpyAsync(h.data(), kv->lens + b0, n * 4, hipMemcpyDeviceToHost, st);
   if (e == hipSuccess && kv->evicted)
-    e = hipMemcpyAsync(ev.data(), kv->evicted, (size_t)B * 4, hipMemcpyDeviceToHost, st);
+    e = hipMemcpyAsync(ev.data(), kv->evicted + b0, n * 4, hipMemcpyDeviceToHost, st);
   if (e == hipSuccess) e = hipStreamSynchronize(st);
   if (e != hipSuccess) return hipfail(e, "reading lens");
-  for (int b = 0; b < B; ++b) {
-    kv->lens_ub[b] = std::max(0, (int)h[b]);
-    kv->evicted_ub[b] = ev[b];
+  for (size_t i = 0; i < n; ++i) {
+    kv->lens_ub[b0 + i] = std::max(0, (int)h[i]);
+    kv->evicted_ub[b0 + i] = ev[i];
   }
   return SPADE_OK;
 }
@@ -75,7 +76,7 @@ spade_status make_fit(spade_kv kv, int b0, int B, Rows rows, hipStream_t st) {
   for (int b = b0; b < B; ++b) {
     const int n = rows(b);
     if (!rows_fit(kv, b, n) && !refreshed && !capturing(st)) {
-      const spade_status rs = refresh_bound(kv, B, st);
+      const spade_status rs = refresh_bound(kv, b0, B, st);
       if (rs != SPADE_OK) return rs;
       refreshed = true;
     }

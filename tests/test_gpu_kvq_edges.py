@@ -20,10 +20,10 @@ import torch
 
 from oracle import kvq as okvq
 from paper_2608_13076_amd import kvq, spade
-from synth import make_inputs
-from tests.helpers import gpu_setup
+from synth import ModelWeights, make_inputs
+from tests.helpers import LOGIT_TOL, gpu_setup
 from tests.test_gpu_kvq import DEV, check_attend, f64, fill, i32, poison, rand
-from tests.test_gpu_kvq_model import i4
+from tests.test_gpu_kvq_model import Given, caches_of, device_rows, i4
 
 pytestmark = pytest.mark.gpu
 
@@ -316,6 +316,41 @@ def test_precision_of_large_scores(mul):
         pw = p.sum(0).reshape(2, 4, n + 3).sum(1)
         assert np.linalg.norm(f64(out[b]) - o) <= tol * np.linalg.norm(o)
         assert np.linalg.norm(f64(w[b]) - pw) <= tol * np.linalg.norm(pw)
+
+
+# --- long contexts in a model ---------------------------------------------
+
+
+@pytest.mark.parametrize("name,ctx", [("mini_gqa_greedy", (2300, 2300)), ("mini_bf16_mixed", (40, 1500)),
+                                      ("mini_f32_greedy", (1000, 1200))])
+def test_verify_over_long_contexts(name, ctx):
+    """A model's prompts of a thousand positions and more, where the attention's
+    heads are divided: logits and the prompts' running weights against the oracle
+    over the rows that the device stored.  Weights: scores of size 10 at most
+    whose queries are 2^-14 off, 2e-3 of a probability."""
+    w = i4(name).with_(ctx=ctx)
+    weights = ModelWeights(w.model, w.seed)
+    model, kv = gpu_setup(w, weights)
+    dec = Given(w.model, weights.get, keep_f64=True)
+    W = kv.track_weights()
+    inp = make_inputs(w)
+    kv.prefill_batch([np.asarray(p) for p in inp.prompts])
+    caches = caches_of(w, dec, inp, kv, weights=True)
+    rng = np.random.default_rng(3)
+    drafts = rng.integers(0, w.model.vocab, (w.batch, w.gamma)).astype(np.int32)
+    buf = spade.VerifyBuffers(model, drafts, None, None, np.zeros(w.batch, np.uint8), True)
+    spade.verify(model, kv, buf)
+    lg = buf.logits.cpu().numpy()
+    dec.rows = device_rows(kv, kv.max_len)
+    dec.count = 1
+    for b, c in enumerate(caches):
+        L = c.length
+        want = dec.forward(c, [int(inp.pending[b])] + drafts[b].tolist())
+        assert np.abs(lg[b] - want).max() <= LOGIT_TOL[w.model.weight_dtype], b
+        for l in range(w.model.n_layers):
+            got, ww = W[l, b, :, :L + 1].cpu().numpy(), c.weights[l][:, :L + 1]
+            assert (np.abs(got - ww) <= 2e-3 * ww + 1e-6).all(), (l, b)
+    assert model.device_error() == 0
 
 
 # --- the binding ----------------------------------------------------------

@@ -322,6 +322,7 @@ class KVCache:
                                         _ptr(self.pending), ctypes.byref(h)))
         self.handle = h
         self.max_batch, self.max_len = max_batch, max_len
+        self.weights: Optional[torch.Tensor] = None  # (track_weights)
 
     def set_state(self, lens, pending) -> None:
         l = np.ascontiguousarray(lens, dtype=np.int32)
@@ -377,10 +378,11 @@ class KVCache:
     def evict(self, B: int, budget: int, recent: int) -> torch.Tensor:
         """Keep the last ``recent`` and the heaviest other positions of requests
         0..B-1, ``budget`` in all (spade_kv_evict); returns the kept positions
-        int32 [n_layers, max_batch, K/V heads, budget]."""
+        int32 [n_layers, max_batch, K/V heads, budget], -1 behind the last and
+        for other requests."""
         s = self.model.shape
-        kept = torch.empty((s.n_layers, self.max_batch, getattr(s, "n_kv_heads", 0) or s.n_heads, max(int(budget), 0)),
-                           dtype=torch.int32, device=self.model.device)
+        kept = torch.full((s.n_layers, self.max_batch, getattr(s, "n_kv_heads", 0) or s.n_heads, max(int(budget), 0)),
+                          -1, dtype=torch.int32, device=self.model.device)
         _check(self.lib.spade_kv_evict(self.handle, B, int(budget), int(recent), _ptr(kept), _stream()))
         return kept
 

@@ -361,3 +361,17 @@ def test_append_refuses_an_output_without_queries():
     x = torch.zeros((1, 2, 2, 64), device=DEV)
     with pytest.raises(ValueError):
         cache.append(0, x, x, q_out=torch.zeros((1, 2, 4, 64), device=DEV))
+
+
+def test_evict_of_some_requests_says_so():
+    """kept holds -1 for the requests that an eviction of the first B leaves alone."""
+    w = i4("mini_gqa_mixed_b5")
+    model, kv = gpu_setup(w, max_len=200)
+    assert kv.weights is None
+    assert kv.track_weights() is kv.weights
+    rng = np.random.default_rng(5)
+    kv.prefill_batch([rng.integers(0, w.model.vocab, 60).astype(np.int32) for _ in range(5)])
+    torch.full((1 << 16,), 77, dtype=torch.int32, device=DEV)  # (freed memory that an allocation may find)
+    kept = kv.evict(2, 40, 5)
+    assert (kept[:, :2] >= 0).all() and (kept[:, 2:] == -1).all()
+    assert kv.get_state(5)[0].tolist() == [40, 40, 59, 59, 59]

@@ -33,9 +33,11 @@ namespace {
 // corrected by its exact remainder.  Queries are normed in double too, whose squares
 // stay in range; those that are only rotated stay in float32.
 //
-// Bound by instructions, not by bytes: 2048 rows of 32 + 64 bf16 heads take 25 us
-// (76 MB, 3.0 TB/s) with the vector units and the scalar unit both three quarters
-// busy; one row of 48 heads takes 3.5 us, a launch and two memory latencies.
+// 2048 rows of 32 + 64 bf16 heads take 26 us (76 MB, 2.9 TB/s; 25 with the inputs in
+// the caches): by counters the vector units issue in 0.71 and the scalar unit in 0.47
+// of the cycles, and waves wait for memory for 0.45 of theirs.  The same in float32
+// 28 us (143 MB, 5.1 TB/s); one row of 48 heads 4 us, a launch and two memory
+// latencies.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t pk_bf16(float a, float b) {
   typedef __attribute__((ext_vector_type(2))) float f2;
@@ -1414,7 +1416,7 @@ __global__ void __launch_bounds__(kSelThreads) kvq_select_kernel(KvqEvict p) {
 // pairs.  In place one workgroup goes through its column in order: a row moves
 // to a lower or the same position, and a round reads all of its rows before it
 // writes the first.  2048 kept positions of the 512 heads above: 142 MB out and at
-// least as many in, 92 us, 3.1 TB/s (a value piece holds four positions, so
+// least as many in, 94 us, 3.0 TB/s (a value piece holds four positions, so
 // scattered ones bring their neighbours along).
 constexpr int kMoveThreads = 512;
 
@@ -1569,12 +1571,13 @@ namespace {
 // tiles stays below what pays for equal lengths, since a long request among short
 // ones holds its workgroup alone.
 //
-// What bounds it: long caches the stream (120 thousand positions, 130 MB, 24.7
-// us, 5.3 TB/s; the 16 requests above 5.6 TB/s, what a plain copy reaches); many
-// float32 rows over a few thousand positions the vector instructions (264 per
-// block and wave beside 48 matrix instructions: 16 requests of 256 to 4096
-// positions, 9 rows, 4 query heads a K/V head, 30 us); a short request the launch
-// and four dependent round trips to memory.
+// What bounds it: long caches the stream (bf16 calls: 120 thousand positions, 130
+// MB, 26.7 us, 4.9 TB/s; the 16 requests above 38 us, 5.2 TB/s; a plain copy of 512
+// MB reaches 5.3); float32 calls the vector instructions beside it (three terms: 43
+// us for the 120 thousand positions, and of 16 requests of 256 to 4096 positions, 9
+// rows, 4 query heads a K/V head, 30 us, with vector issue in 0.58 and the matrix
+// units busy in 0.25 of the cycles); a short request the launch and four dependent
+// round trips to memory.
 constexpr int kAttendWgs = 512;
 constexpr int kWeightWgs = 1024;
 

@@ -14,16 +14,18 @@ step, 2^-8 of the element; the probabilities times scales enter in 16 bits, half
 a step 2^-17 of a term |n - 7.5| s <= 7.5 s_max.
 """
 
+from dataclasses import replace
+
 import numpy as np
 import pytest
 import torch
 
 from oracle import kvq as okvq
 from paper_2608_13076_amd import kvq, spade
-from synth import ModelWeights, make_inputs
+from synth import ModelWeights, make_inputs, workload
 from tests.helpers import LOGIT_TOL, gpu_setup
 from tests.test_gpu_kvq import DEV, check_attend, f64, fill, i32, poison, rand
-from tests.test_gpu_kvq_model import Given, caches_of, device_rows, i4
+from tests.test_gpu_kvq_model import Given, caches_of, device_rows, gains, i4
 
 pytestmark = pytest.mark.gpu
 
@@ -350,6 +352,31 @@ def test_verify_over_long_contexts(name, ctx):
         for l in range(w.model.n_layers):
             got, ww = W[l, b, :, :L + 1].cpu().numpy(), c.weights[l][:, :L + 1]
             assert (np.abs(got - ww) <= 2e-3 * ww + 1e-6).all(), (l, b)
+    assert model.device_error() == 0
+
+
+@pytest.mark.parametrize("name", ["c2_7b_greedy", "gqa_8b_greedy"])
+def test_verify_of_full_size_layers(name):
+    """Two layers of the 7B and the grouped-query 8B shape (a short vocabulary),
+    300 cached positions, head norms on: logits against the oracle over the
+    device's rows."""
+    w = workload(name).with_(ctx=(300, 300))
+    w = w.with_(model=replace(w.model, n_layers=2, vocab=8011, kv_dtype="i4"))
+    weights = ModelWeights(w.model, w.seed)
+    model, kv = gpu_setup(w, weights)
+    gq, gk = gains(w, True)
+    model.set_head_norms(torch.from_numpy(gq).cuda(), torch.from_numpy(gk).cuda(), 1e-6)
+    dec = Given(w.model, weights.get, gq, gk, 1e-6)
+    inp = make_inputs(w)
+    kv.prefill_batch([np.asarray(p) for p in inp.prompts])
+    c = caches_of(w, dec, inp, kv)[0]
+    drafts = np.random.default_rng(3).integers(0, w.model.vocab, (1, w.gamma)).astype(np.int32)
+    buf = spade.VerifyBuffers(model, drafts, None, None, np.zeros(1, np.uint8), True)
+    spade.verify(model, kv, buf)
+    lg = buf.logits.cpu().numpy()
+    dec.rows = device_rows(kv, kv.max_len)
+    want = dec.forward(c, [int(inp.pending[0])] + drafts[0].tolist())
+    assert np.abs(lg[0] - want).max() <= LOGIT_TOL["bf16"]
     assert model.device_error() == 0
 
 

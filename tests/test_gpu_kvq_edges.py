@@ -194,6 +194,37 @@ def test_prompts_after_evictions_fit_where_there_is_room(how):
     assert model.device_error() == 0
 
 
+def test_a_refusal_leaves_a_capture_as_it_is():
+    """A capture cannot wait for the device's counts: the call is refused by the
+    host's bound, the capture goes on, and outside of it the call fits."""
+    model, kv, ids = drifted()
+    none = torch.zeros(1, dtype=torch.int32, device=DEV)
+    buf = spade.VerifyBuffers(model, np.zeros((1, 4), np.int32), None, None, np.zeros(1, np.uint8), False)
+    spade.verify(model, kv, buf)
+    kv.commit(none, none)
+    kv.evict(1, 40, 5)  # the bound: 40 cached, 155 evicted
+    wide = spade.VerifyBuffers(model, np.zeros((1, 5), np.int32), None, None, np.zeros(1, np.uint8), False)
+    x = torch.zeros(8, device=DEV)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(s):
+        with torch.cuda.graph(graph, stream=s):
+            x.add_(1)
+            with pytest.raises(spade.SpadeError) as e:
+                spade.verify(model, kv, wide)
+            x.add_(1)
+    torch.cuda.synchronize()
+    assert e.value.status == -2
+    for i in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert (x == 2 * (i + 1)).all()
+    spade.verify(model, kv, wide)
+    torch.cuda.synchronize()
+    assert model.device_error() == 0
+
+
 def test_refusals_name_what_ran_out():
     model, kv, ids = drifted()
     for call in (lambda: kv.prefill(0, ids[:30]), lambda: kv.prefill_batch([ids[:30]])):

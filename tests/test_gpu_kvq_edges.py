@@ -225,6 +225,33 @@ def test_a_refusal_leaves_a_capture_as_it_is():
     assert model.device_error() == 0
 
 
+def test_get_state_brings_both_bounds_in_line():
+    """After it a call needs no refresh: it fits in a capture too."""
+    model, kv, ids = drifted()
+    none = torch.zeros(1, dtype=torch.int32, device=DEV)
+    buf = spade.VerifyBuffers(model, np.zeros((1, 4), np.int32), None, None, np.zeros(1, np.uint8), False)
+    spade.verify(model, kv, buf)
+    kv.commit(none, none)
+    kv.evict(1, 40, 5)
+    wide = spade.VerifyBuffers(model, np.zeros((1, 5), np.int32), None, None, np.zeros(1, np.uint8), True)
+    assert kv.get_state(1)[0].tolist() == [40]
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(s):
+        with torch.cuda.graph(graph, stream=s):
+            spade.verify(model, kv, wide)
+    torch.cuda.synchronize()
+    spade.verify(model, kv, wide)
+    want = wide.logits.clone()
+    for _ in range(3):
+        wide.logits.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(wide.logits, want)
+    assert model.device_error() == 0
+
+
 def test_refusals_name_what_ran_out():
     model, kv, ids = drifted()
     for call in (lambda: kv.prefill(0, ids[:30]), lambda: kv.prefill_batch([ids[:30]])):

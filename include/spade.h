@@ -64,8 +64,9 @@ enum {
   SPADE_DERR_CAPACITY = 16u, /* a request's length left fewer than gamma + 1 free
                                 positions (lens written outside the library's
                                 calls); clamped, that call's outputs are invalid */
-  SPADE_DERR_COMMIT = 32u   /* spade_kv_commit read an n_accepted outside
+  SPADE_DERR_COMMIT = 32u,  /* spade_kv_commit read an n_accepted outside
                                [0, gamma] of the last verify call; clamped      */
+  SPADE_DERR_TREE = 64u     /* a parent was outside [-1, i); taken as -1        */
 };
 
 /* Weight tensors, row-major [out_features, in_features] unless noted. */
@@ -461,6 +462,153 @@ spade_status spade_kvq_evict(const spade_kvq_shape* shape, const void* d_cache, 
                              void* d_cache_out, int B, int budget, int recent, const float* d_weights,
                              float* d_weights_out, const int32_t* d_lens, int32_t* d_lens_out, int32_t* d_kept,
                              void* stream);
+
+/*
+ * Trees of drafts
+ * ---------------
+ * Verification of a tree instead of a chain, for a program that computes its
+ * projections itself: R rows (nodes) per request, row i with a parent before it
+ * (d_parents int32 [B][R], in [-1, i); -1: none; NULL: i - 1, a chain), row 0 the
+ * root (the pending token).  The rows of a layer are appended to the cache behind
+ * the lens[b] positions that it holds, attend to the context, to their ancestors
+ * and to themselves, and a walk over the next tokens that the program has drawn
+ * for every row (spade_sample) keeps the path that they follow.  So every kept
+ * token is drawn from its own row's distribution, whatever the drafts are.
+ *
+ * The calls share a shape, given by value of its fields at every call:
+ *   n_layers, batch    layers and requests of the cache
+ *   n_heads            query heads, a multiple of n_kv_heads (grouped-query:
+ *                      query head h reads K/V head h / (n_heads / n_kv_heads))
+ *   head_dim           64 or 128
+ *   max_len            positions per request, at most 1048576
+ * A cache is laid out as a model's bfloat16 cache of these sizes (spade_kv_bytes),
+ * so the buffer of one can be used: spade_prefill fills it.  Rows, their ld and
+ * alignment, d_rows (int32 [B], rows in use, clamped to [0, R]; NULL: all) and
+ * d_err as for spade_kvq_*; lens (int32 [B]) is changed by spade_tree_commit
+ * alone.  All calls are asynchronous, allocate nothing and can be captured.
+ */
+typedef struct {
+  int32_t n_layers, batch, n_heads, n_kv_heads, head_dim, max_len;
+} spade_tree_shape;
+
+/* Bytes of a cache (256-byte aligned; needs no initial contents). */
+size_t spade_tree_bytes(const spade_tree_shape* shape);
+
+/* Bytes of the workspace of spade_tree_attend calls of up to max_rows rows (1 to
+ * 64) per request.  Calls that may overlap need a workspace each; it needs no
+ * initial contents and keeps nothing between calls. */
+size_t spade_tree_workspace_bytes(const spade_tree_shape* shape, int max_rows);
+
+/* Rotation of queries and keys: the first rot_dim features of a head (a multiple
+ * of 8, at most head_dim) are pairs j = 0 .. rot_dim / 2 - 1, features j and j +
+ * rot_dim / 2, or 2 j and 2 j + 1 where interleaved is not 0.  At position p, pair
+ * (x, y) becomes amplitude (x cos a - y sin a, y cos a + x sin a), a = p freq[j] in
+ * double; the other features stay.  d_freq: device, float64 [rot_dim / 2], 8-byte
+ * aligned (theta^(-2 j / rot_dim), or scaled for long contexts). */
+typedef struct {
+  const double* d_freq;
+  int32_t rot_dim, interleaved;
+  float amplitude;
+} spade_rotary;
+
+/* New rows of one layer: row i of request b is stored as position lens[b] + i of
+ * the cache (dropped and flagged outside [0, max_len)), keys and values rounded
+ * to bfloat16.  Queries and keys are rotated first (rotary NULL: not) by position
+ * (d_pos ? d_pos[b] : lens[b]) + (d_depth ? d_depth[b R + i] : i): d_depth int32
+ * [B][R], of a tree the number of ancestors.  d_q NULL: no queries (d_q_out is not
+ * used); else d_q_out gets them in `dtype`, zeros for rows that a request does not
+ * use (it may be d_q itself with the same distance of rows; any other overlap with
+ * d_q, d_k or d_v is refused).  R is any number of rows. */
+spade_status spade_tree_append(const spade_tree_shape* shape, int layer, void* d_cache, int B, int R, int dtype,
+                               const void* d_q, int64_t q_ld, const void* d_k, int64_t k_ld, const void* d_v,
+                               int64_t v_ld, const spade_rotary* rotary, const int32_t* d_pos, const int32_t* d_depth,
+                               const int32_t* d_lens, const int32_t* d_rows, void* d_q_out, int64_t q_out_ld,
+                               uint32_t* d_err, void* stream);
+
+/* Attention of R rows per request (1 to 64) over one layer of the cache, which
+ * already holds them at positions lens[b] .. lens[b] + R - 1: row i sees positions
+ * 0 .. lens[b] - 1, its ancestors and itself,
+ *   out = softmax(scale q . k) v   per query head.
+ * d_q and d_out: [B R] rows of n_heads heads in `dtype` that do not overlap; rows
+ * that a request does not use give zeros.  What a row does not see has no part in
+ * its output, infinities and NaN among it; a value that is not finite gives NaN in
+ * the rows that see it.  max_keys: the host's bound of lens[b] + the rows in use, in
+ * [1, max_len] ([R, max_len] without d_rows), or 0 for max_len; a longer request is
+ * cut to it and flagged, as by spade_kvq_attend.  scale: in [2^-50, 2^50].  Float32
+ * calls keep queries and probabilities in 24 bits, bfloat16 calls the
+ * probabilities in 16; scores and sums are float32.  The last bits of a result
+ * depend on B, R and max_keys, not on other requests; the same call gives the
+ * same bits. */
+spade_status spade_tree_attend(const spade_tree_shape* shape, int layer, const void* d_cache, int B, int R, int dtype,
+                               const void* d_q, int64_t q_ld, float scale, const int32_t* d_parents,
+                               const int32_t* d_lens, const int32_t* d_rows, int max_keys, void* d_out, int64_t out_ld,
+                               void* d_workspace, size_t workspace_bytes, uint32_t* d_err, void* stream);
+
+/* Rows of one layer: positions start[b] + i (NULL: i), i < R, as [B][R][n_kv_heads]
+ * [head_dim] in `dtype`; zeros for rows past d_rows[b] and for positions outside
+ * [0, max_len). */
+spade_status spade_tree_read(const spade_tree_shape* shape, int layer, const void* d_cache, int B, int R,
+                             const int32_t* d_start, const int32_t* d_rows, int dtype, void* d_k, void* d_v,
+                             void* stream);
+
+/* Keep the path that the drawn tokens follow, in all layers.  From row 0 on, the
+ * walk goes to the lowest row i in use whose parent is the present row and whose
+ * token d_tokens[b R + i] is d_next[b R + present], until there is none.
+ *   n_accepted[b]  rows behind row 0 on the path (-1: the request uses no rows)
+ *   path[b R + j]  the path's rows, 0 first; -1 behind the last
+ *   correction[b]  d_next of the last of them: the new pending token (-1: no rows)
+ * The path's rows become positions lens[b] .. lens[b] + n_accepted[b] of every
+ * layer and head, lens_out[b] = lens[b] + n_accepted[b] + 1 (d_lens_out may be
+ * d_lens).  The other rows are left where they were, as far as they are not
+ * written over.  R: 1 to 64; all arrays int32. */
+spade_status spade_tree_commit(const spade_tree_shape* shape, void* d_cache, int B, int R, const int32_t* d_tokens,
+                               const int32_t* d_parents, const int32_t* d_next, const int32_t* d_rows,
+                               const int32_t* d_lens, int32_t* d_lens_out, int32_t* d_n_accepted, int32_t* d_path,
+                               int32_t* d_correction, uint32_t* d_err, void* stream);
+
+/* Sampling
+ * --------
+ * One token per row of logits, and the distribution it was drawn from.  In double,
+ * with l a token's logit, T its row's temperature and d = (max l - l) / T, weight
+ * exp(-d), the tokens in the order of their logits (equal ones by id) are kept
+ * while
+ *   d <= 32;
+ *   the token is among the first top_k of those (top_k <= 0: no limit);
+ *   the weight before it is below (top_p - 2^-40) of theirs (top_p >= 1: no limit;
+ *     the first token always stays);
+ *   exp(-d) >= min(min_p, 1).
+ * The token is argmax (-d + G) over the kept ones (ties: the lowest id), G_v the
+ * noise of spade_verify's draws, seeded with the bits of the row's uniform; its
+ * probability among them goes to d_chosen, all of them (0 for the others) to
+ * d_probs.  T not above 0: the largest logit (ties: the lowest id), probability 1.
+ * A NaN logit counts as -infinity and is flagged (SPADE_DERR_NAN), +infinity as the
+ * largest finite number; of a row without a logit above -infinity (flagged too) the
+ * token is 0, all probabilities are 0. */
+typedef struct {
+  float temperature;
+  int32_t top_k;
+  float top_p, min_p;
+} spade_sampling;
+
+/* Bytes of the workspace of spade_sample calls of up to `rows` rows of V tokens
+ * (0: refused).  Calls that may overlap need a workspace each; it needs no initial
+ * contents and keeps nothing between calls. */
+size_t spade_sample_workspace_bytes(int rows, int V);
+
+/* d_logits: [rows] of V numbers of `dtype` (SPADE_F32 or SPADE_BF16), ld elements
+ * from one row to the next.  Request r has rows r rows_per_request .. ; its values
+ * are those of d_temperature, d_top_k, d_top_p and d_min_p ([requests] on the
+ * device; the last request may have fewer rows), where one is NULL the one in
+ * `all` (NULL: 1, 0, 1, 0).  d_uniforms float32 [rows]; d_tokens int32 [rows];
+ * d_chosen float32 [rows] or NULL; d_probs float32 [rows][V] or NULL (it may be
+ * float32 logits with ld = V; any other overlap is refused).  2 <= V <= 1048576.
+ * Asynchronous, allocates nothing, can be captured; the same call gives the same
+ * bits. */
+spade_status spade_sample(int rows, int V, int dtype, const void* d_logits, int64_t ld, int rows_per_request,
+                          const spade_sampling* all, const float* d_temperature, const int32_t* d_top_k,
+                          const float* d_top_p, const float* d_min_p, const float* d_uniforms, int32_t* d_tokens,
+                          float* d_chosen, float* d_probs, void* d_workspace, size_t workspace_bytes,
+                          uint32_t* d_err, void* stream);
 
 /* Read and clear the device error word.  Synchronises the stream. */
 spade_status spade_get_device_error(spade_model m, uint32_t* h_flags, void* stream);

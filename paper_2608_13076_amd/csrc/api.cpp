@@ -12,7 +12,9 @@
 #include <vector>
 
 #include "kvq.h"
+#include "sample.h"
 #include "spade_internal.h"
+#include "tree.h"
 
 using namespace spade;
 
@@ -282,6 +284,41 @@ bool rows_overlap(const void* a, int64_t na, int64_t sa, const void* b, int64_t 
 // the layers' heads of a model's 4-bit cache; the requests' evicted counts follow
 size_t kvq_codes_bytes(const Dims& D, int max_batch, int max_len) {
   return align256((size_t)D.L * max_batch * D.KVH * kvq_head_bytes(max_len, D.hd));
+}
+
+spade_status check_tree(const spade_tree_shape* s) {
+  if (!s) return fail(SPADE_EINVAL, "null shape");
+  if (s->n_layers < 1 || s->batch < 1 || s->n_kv_heads < 1 || s->n_heads < 1 || s->n_heads % s->n_kv_heads != 0)
+    return fail(SPADE_EINVAL, "shape: layers, batch and heads must be positive, n_heads a multiple of n_kv_heads");
+  if (s->head_dim != 64 && s->head_dim != 128) return fail(SPADE_EUNSUPPORTED, "head_dim must be 64 or 128");
+  if (s->max_len < 1 || s->max_len > kTreeMaxLen) return fail(SPADE_ECAPACITY, "max_len must be in [1, %d]", kTreeMaxLen);
+  // every count of heads fits 31 bits, also times the rows of a tree
+  if ((int64_t)s->n_layers * s->batch > 0x7fffffff / s->n_heads / kTreeMaxRows)
+    return fail(SPADE_ECAPACITY, "too many layers, requests and heads");
+  return SPADE_OK;
+}
+
+spade_status check_tree_call(const spade_tree_shape* s, int layer, int B, int dtype) {
+  const spade_status r = check_tree(s);
+  if (r != SPADE_OK) return r;
+  if (layer < 0 || layer >= s->n_layers) return fail(SPADE_EINVAL, "layer %d out of range", layer);
+  if (B < 1 || B > s->batch) return fail(SPADE_ECAPACITY, "B=%d out of range", B);
+  if (dtype != SPADE_F32 && dtype != SPADE_BF16) return fail(SPADE_EINVAL, "dtype must be SPADE_F32 or SPADE_BF16");
+  return SPADE_OK;
+}
+
+int64_t tree_layer_elems(const spade_tree_shape* s) {
+  return (int64_t)s->batch * s->n_kv_heads * kv_stride_of(s->max_len) * s->head_dim;
+}
+// the layer's heads in a cache of the model's layout
+TreeCache tree_cache(const spade_tree_shape* s, const void* d_cache, int layer) {
+  const int64_t n = tree_layer_elems(s);
+  uint16_t* k = (uint16_t*)const_cast<void*>(d_cache);
+  return TreeCache{k + layer * n, k + s->n_layers * n + layer * n, (int64_t)kv_stride_of(s->max_len) * s->head_dim};
+}
+size_t tree_workspace(int G, int hd, int max_rows) {
+  const size_t rows = tree_part_rows(G, max_rows);
+  return align256(rows * hd * 4) + align256(rows * 2 * 4);
 }
 
 size_t kvq_layer_bytes(const spade_kvq_shape* s) {
@@ -1149,6 +1186,268 @@ spade_status spade_kvq_evict(const spade_kvq_shape* s, const void* d_cache, cons
   a.kept = d_kept;
   const hipError_t e = launch_kvq_evict(a, (hipStream_t)stream);
   if (e != hipSuccess) return hipfail(e, "kvq_evict");
+  return SPADE_OK;
+}
+
+size_t spade_tree_bytes(const spade_tree_shape* s) {
+  if (check_tree(s) != SPADE_OK) return 0;
+  return 2 * align256((size_t)s->n_layers * tree_layer_elems(s) * 2);
+}
+
+size_t spade_tree_workspace_bytes(const spade_tree_shape* s, int max_rows) {
+  if (check_tree(s) != SPADE_OK) return 0;
+  if (max_rows < 1 || max_rows > kTreeMaxRows) {
+    fail(SPADE_ECAPACITY, "max_rows must be in [1, %d]", kTreeMaxRows);
+    return 0;
+  }
+  return tree_workspace(s->n_heads / s->n_kv_heads, s->head_dim, max_rows);
+}
+
+spade_status spade_tree_append(const spade_tree_shape* s, int layer, void* d_cache, int B, int R, int dtype,
+                               const void* d_q, int64_t q_ld, const void* d_k, int64_t k_ld, const void* d_v,
+                               int64_t v_ld, const spade_rotary* rotary, const int32_t* d_pos, const int32_t* d_depth,
+                               const int32_t* d_lens, const int32_t* d_rows, void* d_q_out, int64_t q_out_ld,
+                               uint32_t* d_err, void* stream) {
+  const spade_status r = check_tree_call(s, layer, B, dtype);
+  if (r != SPADE_OK) return r;
+  if (!d_cache || !d_k || !d_v || !d_lens || (d_q && !d_q_out)) return fail(SPADE_EINVAL, "null pointer");
+  if (R < 1) return fail(SPADE_EINVAL, "R must be >= 1");
+  const int hd = s->head_dim;
+  if (!kvq_rows_ok(d_k, k_ld, s->n_kv_heads, hd, dtype) || !kvq_rows_ok(d_v, v_ld, s->n_kv_heads, hd, dtype) ||
+      (d_q && (!kvq_rows_ok(d_q, q_ld, s->n_heads, hd, dtype) || !kvq_rows_ok(d_q_out, q_out_ld, s->n_heads, hd, dtype))))
+    return fail(SPADE_EINVAL, "rows: alignment or leading dimension");
+  if ((uintptr_t)d_cache & 255) return fail(SPADE_EINVAL, "the cache must be 256-byte aligned");
+  if (rotary) {
+    if (rotary->rot_dim < 8 || rotary->rot_dim > hd || rotary->rot_dim % 8 != 0)
+      return fail(SPADE_EINVAL, "rot_dim must be a multiple of 8 in [8, head_dim]");
+    if (!rotary->d_freq || ((uintptr_t)rotary->d_freq & 7)) return fail(SPADE_EINVAL, "frequencies: null or not 8-byte aligned");
+    if (!std::isfinite(rotary->amplitude)) return fail(SPADE_EINVAL, "amplitude must be finite");
+  }
+  if ((int64_t)B * R > (int64_t)0x7fffffff / (s->n_heads + 2 * s->n_kv_heads))
+    return fail(SPADE_ECAPACITY, "too many rows");
+  if (d_q) {
+    const int64_t e = dtype == SPADE_F32 ? 4 : 2, n = (int64_t)B * R, nq = s->n_heads * hd * e, nk = s->n_kv_heads * hd * e;
+    const bool in_place = d_q_out == d_q && (q_out_ld == q_ld || n == 1);
+    if ((!in_place && rows_overlap(d_q_out, nq, q_out_ld * e, d_q, nq, q_ld * e, n)) ||
+        rows_overlap(d_q_out, nq, q_out_ld * e, d_k, nk, k_ld * e, n) ||
+        rows_overlap(d_q_out, nq, q_out_ld * e, d_v, nk, v_ld * e, n))
+      return fail(SPADE_EINVAL, "q_out overlaps other rows than q's own");
+  }
+  TreeAppend a{};
+  a.cache = tree_cache(s, d_cache, layer);
+  a.B = B;
+  a.R = R;
+  a.H = s->n_heads;
+  a.KVH = s->n_kv_heads;
+  a.hd = hd;
+  a.max_len = s->max_len;
+  a.q = d_q;
+  a.k = d_k;
+  a.v = d_v;
+  a.q_ld = q_ld;
+  a.k_ld = k_ld;
+  a.v_ld = v_ld;
+  a.bf16 = dtype == SPADE_BF16;
+  if (rotary) {
+    a.freq = rotary->d_freq;
+    a.pairs = rotary->rot_dim / 2;
+    a.interleaved = rotary->interleaved != 0;
+    a.amplitude = rotary->amplitude;
+  }
+  a.pos = d_pos;
+  a.depth = d_depth;
+  a.lens = d_lens;
+  a.rows = d_rows;
+  a.q_out = d_q_out;
+  a.qo_ld = q_out_ld;
+  a.err = d_err;
+  const hipError_t e = launch_tree_append(a, (hipStream_t)stream);
+  if (e != hipSuccess) return hipfail(e, "tree_append");
+  return SPADE_OK;
+}
+
+spade_status spade_tree_read(const spade_tree_shape* s, int layer, const void* d_cache, int B, int R,
+                             const int32_t* d_start, const int32_t* d_rows, int dtype, void* d_k, void* d_v,
+                             void* stream) {
+  const spade_status r = check_tree_call(s, layer, B, dtype);
+  if (r != SPADE_OK) return r;
+  if (!d_cache || !d_k || !d_v) return fail(SPADE_EINVAL, "null pointer");
+  if (R < 1) return fail(SPADE_EINVAL, "R must be >= 1");
+  if ((uintptr_t)d_cache & 255) return fail(SPADE_EINVAL, "the cache must be 256-byte aligned");
+  if (!aligned16(d_k) || !aligned16(d_v)) return fail(SPADE_EINVAL, "outputs must be 16-byte aligned");
+  if ((int64_t)B * R > (int64_t)0x7fffffff / s->n_kv_heads) return fail(SPADE_ECAPACITY, "too many rows");
+  TreeRead a{};
+  a.cache = tree_cache(s, d_cache, layer);
+  a.B = B;
+  a.R = R;
+  a.KVH = s->n_kv_heads;
+  a.hd = s->head_dim;
+  a.max_len = s->max_len;
+  a.bf16 = dtype == SPADE_BF16;
+  a.start = d_start;
+  a.rows = d_rows;
+  a.k = d_k;
+  a.v = d_v;
+  const hipError_t e = launch_tree_read(a, (hipStream_t)stream);
+  if (e != hipSuccess) return hipfail(e, "tree_read");
+  return SPADE_OK;
+}
+
+spade_status spade_tree_attend(const spade_tree_shape* s, int layer, const void* d_cache, int B, int R, int dtype,
+                               const void* d_q, int64_t q_ld, float scale, const int32_t* d_parents,
+                               const int32_t* d_lens, const int32_t* d_rows, int max_keys, void* d_out, int64_t out_ld,
+                               void* d_workspace, size_t workspace_bytes, uint32_t* d_err, void* stream) {
+  const spade_status r = check_tree_call(s, layer, B, dtype);
+  if (r != SPADE_OK) return r;
+  if (!d_cache || !d_q || !d_out || !d_lens || !d_workspace) return fail(SPADE_EINVAL, "null pointer");
+  if (R < 1 || R > kTreeMaxRows) return fail(SPADE_ECAPACITY, "R must be in [1, %d]", kTreeMaxRows);
+  const int hd = s->head_dim;
+  if (!kvq_rows_ok(d_q, q_ld, s->n_heads, hd, dtype) || !kvq_rows_ok(d_out, out_ld, s->n_heads, hd, dtype))
+    return fail(SPADE_EINVAL, "rows: alignment or leading dimension");
+  if (((uintptr_t)d_cache | (uintptr_t)d_workspace) & 255)
+    return fail(SPADE_EINVAL, "cache and workspace must be 256-byte aligned");
+  if (!(scale >= 0x1p-50f && scale <= 0x1p50f)) return fail(SPADE_EINVAL, "scale must be in [2^-50, 2^50]");
+  if (max_keys == 0) max_keys = s->max_len;
+  // (a ragged batch of short contexts has a bound below its padded rows)
+  const int least = d_rows ? 1 : R;
+  if (max_keys < least || max_keys > s->max_len)
+    return fail(SPADE_ECAPACITY, "max_keys %d must be in [%d, %d]", max_keys, least, s->max_len);
+  const int G = s->n_heads / s->n_kv_heads;
+  if (tree_workspace(G, hd, R) > workspace_bytes)
+    return fail(SPADE_ECAPACITY, "workspace of %zu bytes is too small", workspace_bytes);
+  const int64_t e = dtype == SPADE_F32 ? 4 : 2, nq = s->n_heads * hd * e;
+  if (rows_overlap(d_q, nq, q_ld * e, d_out, nq, out_ld * e, (int64_t)B * R)) return fail(SPADE_EINVAL, "q and out overlap");
+  TreeAttend a{};
+  a.cache = tree_cache(s, d_cache, layer);
+  a.B = B;
+  a.R = R;
+  a.H = s->n_heads;
+  a.KVH = s->n_kv_heads;
+  a.G = G;
+  a.hd = hd;
+  a.q = d_q;
+  a.q_ld = q_ld;
+  a.bf16 = dtype == SPADE_BF16;
+  a.scale = scale;
+  a.parents = d_parents;
+  a.lens = d_lens;
+  a.rows = d_rows;
+  a.max_keys = max_keys;
+  a.out = d_out;
+  a.out_ld = out_ld;
+  a.part_rows = tree_part_rows(G, R);
+  a.part_o = (float*)d_workspace;
+  a.part_ml = (float*)((uint8_t*)d_workspace + align256(a.part_rows * hd * 4));
+  a.err = d_err;
+  const hipError_t r2 = launch_tree_attend(a, (hipStream_t)stream);
+  if (r2 != hipSuccess) return hipfail(r2, "tree_attend");
+  return SPADE_OK;
+}
+
+spade_status spade_tree_commit(const spade_tree_shape* s, void* d_cache, int B, int R, const int32_t* d_tokens,
+                               const int32_t* d_parents, const int32_t* d_next, const int32_t* d_rows,
+                               const int32_t* d_lens, int32_t* d_lens_out, int32_t* d_n_accepted, int32_t* d_path,
+                               int32_t* d_correction, uint32_t* d_err, void* stream) {
+  const spade_status r = check_tree_call(s, 0, B, SPADE_BF16);
+  if (r != SPADE_OK) return r;
+  if (!d_cache || !d_tokens || !d_next || !d_lens || !d_lens_out || !d_n_accepted || !d_path || !d_correction)
+    return fail(SPADE_EINVAL, "null pointer");
+  if (R < 1 || R > kTreeMaxRows) return fail(SPADE_ECAPACITY, "R must be in [1, %d]", kTreeMaxRows);
+  if ((uintptr_t)d_cache & 255) return fail(SPADE_EINVAL, "the cache must be 256-byte aligned");
+  // outputs apart from the inputs and from each other (lens_out may be lens)
+  const size_t nb = (size_t)B * 4, nr = (size_t)B * R * 4;
+  const struct { const void* p; size_t n; } out[4] = {{d_lens_out, nb}, {d_n_accepted, nb}, {d_path, nr}, {d_correction, nb}},
+      in[5] = {{d_tokens, nr}, {d_parents, nr}, {d_next, nr}, {d_rows, nb}, {d_lens, nb}};
+  for (int i = 0; i < 4; ++i) {
+    for (int j = i + 1; j < 4; ++j)
+      if (overlap(out[i].p, out[i].n, out[j].p, out[j].n)) return fail(SPADE_EINVAL, "outputs overlap");
+    for (int j = 0; j < 5; ++j)
+      if (in[j].p && !(i == 0 && j == 4 && d_lens_out == d_lens) && overlap(out[i].p, out[i].n, in[j].p, in[j].n))
+        return fail(SPADE_EINVAL, "an output overlaps an input");
+  }
+  TreeCommit a{};
+  a.cache = tree_cache(s, d_cache, 0);
+  a.layer_elems = tree_layer_elems(s);
+  a.L = s->n_layers;
+  a.B = B;
+  a.R = R;
+  a.KVH = s->n_kv_heads;
+  a.hd = s->head_dim;
+  a.max_len = s->max_len;
+  a.tokens = d_tokens;
+  a.parents = d_parents;
+  a.next = d_next;
+  a.rows = d_rows;
+  a.lens = d_lens;
+  a.lens_out = d_lens_out;
+  a.n_accepted = d_n_accepted;
+  a.path = d_path;
+  a.correction = d_correction;
+  a.err = d_err;
+  const hipError_t e = launch_tree_commit(a, (hipStream_t)stream);
+  if (e != hipSuccess) return hipfail(e, "tree_commit");
+  return SPADE_OK;
+}
+
+size_t spade_sample_workspace_bytes(int rows, int V) {
+  if (rows < 1 || V < 2 || V > kSampleMaxVocab || rows > 0x7fffffff / 256) {
+    fail(SPADE_EINVAL, "rows must be in [1, %d], V in [2, %d]", 0x7fffffff / 256, kSampleMaxVocab);
+    return 0;
+  }
+  return sample_workspace(rows, V, nullptr, nullptr);
+}
+
+spade_status spade_sample(int rows, int V, int dtype, const void* d_logits, int64_t ld, int rows_per_request,
+                          const spade_sampling* all, const float* d_temperature, const int32_t* d_top_k,
+                          const float* d_top_p, const float* d_min_p, const float* d_uniforms, int32_t* d_tokens,
+                          float* d_chosen, float* d_probs, void* d_workspace, size_t workspace_bytes,
+                          uint32_t* d_err, void* stream) {
+  const size_t need = spade_sample_workspace_bytes(rows, V);
+  if (need == 0) return SPADE_EINVAL;
+  if (dtype != SPADE_F32 && dtype != SPADE_BF16) return fail(SPADE_EINVAL, "dtype must be SPADE_F32 or SPADE_BF16");
+  if (!d_logits || !d_uniforms || !d_tokens || !d_workspace) return fail(SPADE_EINVAL, "null pointer");
+  if (rows_per_request < 1) return fail(SPADE_EINVAL, "rows_per_request must be >= 1");
+  const int64_t e = dtype == SPADE_F32 ? 4 : 2;
+  if (ld < V || ld > (int64_t)1 << 40) return fail(SPADE_EINVAL, "ld must be at least V");
+  if (((uintptr_t)d_logits & (e - 1)) || ((uintptr_t)d_probs & 3)) return fail(SPADE_EINVAL, "logits or probs: alignment");
+  if ((uintptr_t)d_workspace & 255) return fail(SPADE_EINVAL, "the workspace must be 256-byte aligned");
+  if (need > workspace_bytes) return fail(SPADE_ECAPACITY, "workspace of %zu bytes is too small", workspace_bytes);
+  const size_t lb = ((size_t)(rows - 1) * ld + V) * e, nr = (size_t)rows * 4, pb = (size_t)rows * V * 4;
+  if (d_probs && !((const void*)d_probs == d_logits && dtype == SPADE_F32 && ld == V) && overlap(d_probs, pb, d_logits, lb))
+    return fail(SPADE_EINVAL, "probs and logits overlap");
+  const size_t nq = ((size_t)(rows - 1) / rows_per_request + 1) * 4;
+  const struct { const void* p; size_t n; } out[3] = {{d_tokens, nr}, {d_chosen, nr}, {d_probs, pb}},
+      in[6] = {{d_logits, lb}, {d_uniforms, nr}, {d_temperature, nq}, {d_top_k, nq}, {d_top_p, nq}, {d_min_p, nq}};
+  for (int i = 0; i < 3; ++i) {
+    if (!out[i].p) continue;
+    for (int j = i + 1; j < 3; ++j)
+      if (out[j].p && overlap(out[i].p, out[i].n, out[j].p, out[j].n)) return fail(SPADE_EINVAL, "outputs overlap");
+    for (int j = i == 2 ? 1 : 0; j < 6; ++j)
+      if (in[j].p && overlap(out[i].p, out[i].n, in[j].p, in[j].n)) return fail(SPADE_EINVAL, "an output overlaps an input");
+  }
+  SampleArgs a{};
+  sample_workspace(rows, V, &a, (uint8_t*)d_workspace);
+  a.rows = rows;
+  a.V = V;
+  a.bf16 = dtype == SPADE_BF16;
+  a.logits = d_logits;
+  a.ld = ld;
+  a.per = rows_per_request;
+  a.temperature = all ? all->temperature : 1.f;
+  a.top_k = all ? all->top_k : 0;
+  a.top_p = all ? all->top_p : 1.f;
+  a.min_p = all ? all->min_p : 0.f;
+  a.d_temperature = d_temperature;
+  a.d_top_k = d_top_k;
+  a.d_top_p = d_top_p;
+  a.d_min_p = d_min_p;
+  a.u = d_uniforms;
+  a.tokens = d_tokens;
+  a.chosen = d_chosen;
+  a.probs = d_probs;
+  a.err = d_err;
+  const hipError_t r = launch_sample(a, (hipStream_t)stream);
+  if (r != hipSuccess) return hipfail(r, "sample");
   return SPADE_OK;
 }
 

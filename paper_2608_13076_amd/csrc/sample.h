@@ -1,0 +1,58 @@
+// Internal declarations of the filtered sampler: the launcher of its kernels
+// (sample.hip), used by the C ABI (api.cpp).
+#pragma once
+
+#include "spade_internal.h"
+
+namespace spade {
+
+constexpr int kSampleMaxVocab = 1 << 20;
+constexpr int kSampleSlice = 4096;  // tokens of a workgroup of the first pass: 16 per thread
+constexpr int kSampleBins = 128;    // of a slice's weights
+constexpr int kSampleList = 4096;   // candidates of a row kept apart
+constexpr int kSampleParts = 32;    // most workgroups of a row in the second pass
+
+// What the passes of a row hand on.
+struct SampleRow {
+  double mass;    // of the tokens above bin `lo`, over the largest weight
+  double total;   // of all
+  float max;
+  int lo, hi;     // bins whose tokens are listed (below the top bin)
+  int above;      // tokens above bin lo
+  int k_in;       // whether the first top_k end in the list
+  double inv_T, cut, inv_sum;  // probabilities: exp(-d) inv_sum where d <= cut
+  uint32_t key, id;            // and the token comes no later than this one
+};
+
+struct SampleArgs {
+  int rows, V, bf16;
+  const void* logits;
+  int64_t ld;
+  int per;  // rows of a request
+  float temperature, top_p, min_p;
+  int top_k;
+  const float* d_temperature;  // [requests], or NULL: the value above
+  const int32_t* d_top_k;
+  const float* d_top_p;
+  const float* d_min_p;
+  const float* u;
+  int32_t* tokens;
+  float* chosen;  // or NULL
+  float* probs;   // or NULL
+  uint32_t* err;
+  // workspace
+  float* smax;          // [rows][NS] largest logit of a slice
+  int32_t* sarg;        // ... its lowest token (greedy rows)
+  uint64_t* hist;       // [rows][NS][kSampleBins] count and weight
+  double* best;         // [rows][kSampleParts] best score of a part, its token, the weight of its kept tokens
+  int32_t* best_id;
+  double* sum;
+  SampleRow* row;       // [rows]
+  uint32_t* count;      // [rows] listed tokens
+  uint2* list;          // [rows][kSampleList] token and logit
+  int NS, NW, spw;      // slices, parts, slices of a part
+};
+size_t sample_workspace(int rows, int V, SampleArgs* a, uint8_t* base);
+hipError_t launch_sample(const SampleArgs& a, hipStream_t st);
+
+}  // namespace spade

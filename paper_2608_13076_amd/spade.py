@@ -24,8 +24,9 @@ KINDS = {"wq": 0, "wk": 1, "wv": 2, "wo": 3, "wg": 4, "wu": 5, "wd": 6,
          "g_attn": 7, "g_ffn": 8, "embed": 9, "g_final": 10, "lm_head": 11}
 GLOBAL_KINDS = ("embed", "g_final", "lm_head")
 DERR_TOKEN, DERR_NAN, DERR_RESIDUAL, DERR_NOQ, DERR_CAPACITY, DERR_COMMIT = 1, 2, 4, 8, 16, 32
+DERR_TREE = 64
 
-# include/spade.h: the calls of the method and of 4-bit caches
+# include/spade.h: the calls of the method, of 4-bit caches, of trees of drafts and of sampling
 EXPORTED = (
     "spade_weight_bytes", "spade_workspace_bytes", "spade_kv_bytes", "spade_model_create",
     "spade_model_load_tensor", "spade_kv_create", "spade_kv_set_state", "spade_kv_get_state",
@@ -35,6 +36,8 @@ EXPORTED = (
     "spade_accept_from_logits_noalloc",
     "spade_kvq_bytes", "spade_kvq_workspace_bytes", "spade_kvq_append", "spade_kvq_read", "spade_kvq_attend",
     "spade_kvq_evict", "spade_model_set_head_norms", "spade_kv_track_weights", "spade_kv_evict",
+    "spade_tree_bytes", "spade_tree_workspace_bytes", "spade_tree_append", "spade_tree_read", "spade_tree_attend",
+    "spade_tree_commit", "spade_sample_workspace_bytes", "spade_sample",
 )
 # include/spade_tuning.h: schedule controls and measurement hooks
 EXPORTED_TUNING = (
@@ -65,6 +68,20 @@ class KVQShape(ctypes.Structure):
                 ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("max_len", ctypes.c_int32)]
 
 
+class TreeShape(ctypes.Structure):
+    _fields_ = KVQShape._fields_
+
+
+class RotaryArgs(ctypes.Structure):
+    _fields_ = [("d_freq", ctypes.c_void_p), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("amplitude", ctypes.c_float)]
+
+
+class SamplingArgs(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_float), ("top_k", ctypes.c_int32), ("top_p", ctypes.c_float),
+                ("min_p", ctypes.c_float)]
+
+
 def config_from(shape) -> SpadeConfig:
     """spade_config from any object with the ModelShape attributes."""
     return SpadeConfig(shape.n_layers, shape.d_model, shape.n_heads, shape.head_dim, shape.d_ffn,
@@ -88,6 +105,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib = ctypes.CDLL(path)
     cfgp = ctypes.POINTER(SpadeConfig)
     kvqp = ctypes.POINTER(KVQShape)
+    treep, rotp, samp = ctypes.POINTER(TreeShape), ctypes.POINTER(RotaryArgs), ctypes.POINTER(SamplingArgs)
     sig = {
         "spade_weight_bytes": (SZ, [cfgp]),
         "spade_workspace_bytes": (SZ, [cfgp, I, I, I]),
@@ -130,6 +148,14 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "spade_kvq_read": (I, [kvqp, I, P, I, I, P, P, I, P, P, P]),
         "spade_kvq_attend": (I, [kvqp, I, P, I, I, I, P, L64, F, P, P, I, P, L64, P, P, I, P, SZ, P, P]),
         "spade_kvq_evict": (I, [kvqp, P, kvqp, P, I, I, I, P, P, P, P, P, P]),
+        "spade_tree_bytes": (SZ, [treep]),
+        "spade_tree_workspace_bytes": (SZ, [treep, I]),
+        "spade_tree_append": (I, [treep, I, P, I, I, I, P, L64, P, L64, P, L64, rotp, P, P, P, P, P, L64, P, P]),
+        "spade_tree_read": (I, [treep, I, P, I, I, P, P, I, P, P, P]),
+        "spade_tree_attend": (I, [treep, I, P, I, I, I, P, L64, F, P, P, P, I, P, L64, P, SZ, P, P]),
+        "spade_tree_commit": (I, [treep, P, I, I, P, P, P, P, P, P, P, P, P, P, P]),
+        "spade_sample_workspace_bytes": (SZ, [I, I]),
+        "spade_sample": (I, [I, I, I, P, L64, I, samp, P, P, P, P, P, P, P, P, P, SZ, P, P]),
         "spade_last_error": (ctypes.c_char_p, []),
         "spade_model_destroy": (None, [P]),
         "spade_kv_destroy": (None, [P]),

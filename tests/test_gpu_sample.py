@@ -1,0 +1,243 @@
+"""Filtered sampling on the GPU against the float64 oracle (oracle/tree.py).
+
+Tokens are compared for equality: the oracle's borders and draws are decided in 64
+bits, the kernels' to 2^-34 or better, and the inputs are seeded, so a row whose
+border or draw is closer than that would show in the first run.  A probability is a
+quotient in double rounded once to float32: 2^-24 of it, with weights and sums good
+to 2^-33: 2^-23 in all.
+"""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import tree as otree
+from paper_2608_13076_amd import sampling, spade
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TD = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def check(logits, u, probs, tokens, chosen, per, **kw):
+    """Rows against the oracle; kw: lists of one value per request."""
+    l = logits.float().cpu().numpy().astype(np.float64)
+    got_p = None if probs is None else probs.cpu().numpy().astype(np.float64)
+    for row in range(len(l)):
+        one = {k: v[row // per] for k, v in kw.items()}
+        t, p = otree.sample(l[row], float(u[row]), **one)
+        assert int(tokens[row]) == t, (row, one, int(tokens[row]), t, p[int(tokens[row])], p[t])
+        assert abs(float(chosen[row]) - p[t]) <= 2.0 ** -23 * p[t], (row, one)
+        if got_p is not None:
+            assert ((got_p[row] > 0) == (p > 0)).all() or (np.abs(got_p[row] - p) <= 1e-38).all(), (row, one)
+            assert (np.abs(got_p[row] - p) <= 2.0 ** -23 * p + 1e-38).all(), (row, one)
+
+
+def settings(rng, n):
+    t = np.where(rng.random(n) < 0.15, 0.0, rng.uniform(0.3, 1.5, n)).astype(np.float32)
+    k = np.where(rng.random(n) < 0.5, 0, np.exp(rng.uniform(0, 8, n))).astype(np.int32)
+    p = np.where(rng.random(n) < 0.4, 1.0, rng.uniform(0.05, 0.999, n)).astype(np.float32)
+    m = np.where(rng.random(n) < 0.6, 0.0, rng.uniform(0.0, 0.3, n)).astype(np.float32)
+    return {"temperature": t, "top_k": k, "top_p": p, "min_p": m}
+
+
+def run(logits, u, kw, per=1, probs=True, sampler=None):
+    rows, V = logits.shape
+    s = sampler or sampling.Sampler(rows, V, device=DEV)
+    pr = torch.full((rows, V), 7.0, device=DEV) if probs else None
+    args = {k: (torch.from_numpy(np.ascontiguousarray(v)).to(DEV) if isinstance(v, np.ndarray) else v) for k, v in kw.items()}
+    tok, ch = s.draw(logits, u, probs=pr, **args)
+    return tok, ch, pr, s
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,per,V,scale", [(40, 1, 2, 1.0), (40, 1, 7, 3.0), (30, 2, 100, 2.0), (24, 1, 4095, 2.0),
+                                           (24, 1, 4097, 5.0), (16, 3, 32000, 2.5), (8, 1, 128256, 2.0), (6, 1, 128256, 6.0),
+                                           (3, 1, 300001, 0.5)])
+def test_sample(n, per, V, scale, dtype):
+    rng = np.random.default_rng(V + n)
+    x = rng.normal(size=(n * per, V)).astype(np.float32) * scale
+    x[:, rng.integers(0, V, 8)] += rng.uniform(0, 8, 8).astype(np.float32)
+    logits = torch.from_numpy(x).to(DEV).to(TD[dtype])
+    u = torch.from_numpy(rng.random(n * per, np.float32)).to(DEV)
+    kw = settings(rng, n)
+    tok, ch, pr, s = run(logits, u, kw, per)
+    check(logits, u, pr, tok, ch, per, **kw)
+    assert s.device_error() == 0
+    # the same call gives the same bits, also without the distribution
+    tok2, ch2, _, _ = run(logits, u, kw, per, probs=False, sampler=s)
+    assert torch.equal(tok, tok2) and torch.equal(ch, ch2)
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(temperature=0.0), dict(temperature=0.7), dict(top_k=1), dict(top_k=50),
+                                dict(top_p=0.9), dict(top_p=1e-9), dict(top_p=0.0), dict(top_p=-1.0), dict(min_p=0.1),
+                                dict(min_p=1.0), dict(min_p=7.0), dict(top_k=50, top_p=0.5, min_p=0.05),
+                                dict(top_k=100000), dict(temperature=-3.0), dict(top_k=-5),
+                                dict(top_p=float(np.nextafter(np.float32(1), np.float32(0))))])
+@pytest.mark.parametrize("V", [1000, 20000])
+def test_one_setting_for_all(kw, V):
+    rng = np.random.default_rng(V)
+    logits = torch.from_numpy(rng.normal(size=(12, V)).astype(np.float32) * 3).to(DEV)
+    u = torch.from_numpy(rng.random(12, np.float32)).to(DEV)
+    tok, ch, pr, _ = run(logits, u, kw)
+    check(logits, u, pr, tok, ch, 12, **{k: [v] for k, v in kw.items()})
+
+
+def ties(V, kind, rng):
+    if kind == "equal":
+        return np.zeros(V, np.float32)
+    if kind == "levels":
+        return rng.integers(0, 4, V).astype(np.float32)
+    if kind == "signed zeros":
+        return np.where(rng.random(V) < 0.5, 0.0, -0.0).astype(np.float32)
+    return np.repeat(rng.normal(size=(V + 6) // 7), 7)[:V].astype(np.float32)
+
+
+@pytest.mark.parametrize("kind", ["equal", "levels", "signed zeros", "runs"])
+@pytest.mark.parametrize("V", [16, 5000, 70000])
+def test_ties_go_to_the_lowest_ids(kind, V):
+    rng = np.random.default_rng(V)
+    sets = [dict(top_k=k) for k in (1, 3, V // 2, V - 1)] + [dict(top_p=p) for p in (0.25, 0.5, 0.75, 0.9)]
+    sets += [dict(top_k=V // 2, top_p=0.5), dict(min_p=1.0), dict(temperature=0.0)]
+    row = ties(V, kind, rng)
+    logits = torch.from_numpy(np.stack([row] * len(sets))).to(DEV)
+    u = torch.from_numpy(rng.random(len(sets), np.float32)).to(DEV)
+    base = dict(temperature=1.0, top_k=0, top_p=1.0, min_p=0.0)
+    cols = {k: np.array([{**base, **s}[k] for s in sets], np.int32 if k == "top_k" else np.float32) for k in base}
+    tok, ch, pr, _ = run(logits, u, cols)
+    check(logits, u, pr, tok, ch, 1, **cols)
+
+
+@pytest.mark.parametrize("V", [50, 9000])
+def test_masked_and_extreme_logits(V):
+    """-infinity, the lowest number, +infinity and NaN among the logits, tiny and
+    huge temperatures, rows with nothing left."""
+    rng = np.random.default_rng(V)
+    base = rng.normal(size=V).astype(np.float32) * 4
+    rows, sets = [], []
+    for fill in (-np.inf, np.finfo(np.float32).min, -1e30):
+        for s in (dict(), dict(top_k=20), dict(top_p=0.8), dict(temperature=0.0), dict(top_k=V - 2, top_p=0.99)):
+            r = base.copy()
+            r[rng.random(V) < 0.9] = fill
+            r[rng.integers(0, V)] = 1.0
+            rows.append(r)
+            sets.append(s)
+    for s in (dict(), dict(top_k=5), dict(top_p=0.5), dict(temperature=0.0)):
+        r = base.copy()
+        r[[3, V - 1]] = np.inf
+        rows.append(r)
+        sets.append(s)
+        r = np.full(V, -np.inf, np.float32)
+        r[V // 2] = -1e38
+        rows.append(r)
+        sets.append(s)
+    for t in (1e-45, 1e-30, 1e-6, 1e-3, 50.0, 1e30, np.inf):
+        for s in (dict(), dict(top_k=9), dict(top_p=0.7), dict(min_p=0.2)):
+            rows.append(base if t > 1e-20 else base * np.float32(1e20))
+            sets.append(dict(s, temperature=t))
+    for s in (dict(temperature=1e-20), dict(temperature=1e-3, top_k=7), dict(temperature=1e30, top_p=0.5)):
+        r = base * np.float32(1e30)
+        r[rng.integers(0, V, 9)] = r.max()
+        rows.append(r)
+        sets.append(s)
+    logits = torch.from_numpy(np.stack(rows)).to(DEV)
+    u = torch.from_numpy(rng.random(len(rows), np.float32)).to(DEV)
+    d = dict(temperature=1.0, top_k=0, top_p=1.0, min_p=0.0)
+    cols = {k: np.array([{**d, **s}[k] for s in sets], np.int32 if k == "top_k" else np.float32) for k in d}
+    tok, ch, pr, sm = run(logits, u, cols)
+    check(logits, u, pr, tok, ch, 1, **cols)
+    assert sm.device_error() == 0
+    # NaN counts as -infinity and is flagged; rows of nothing give token 0 and no probability
+    bad = logits[:4].clone()
+    bad[0, ::2] = float("nan")
+    bad[1] = float("nan")
+    bad[2] = float("-inf")
+    bad[3, :] = float("-inf")
+    bad[3, V - 1] = float("nan")
+    kw = dict(temperature=np.array([1, 1, 0.5, 0], np.float32), top_k=np.array([0, 5, 0, 0], np.int32))
+    tok, ch, pr, sm = run(bad, u[:4].contiguous(), kw)
+    assert sm.device_error() == spade.DERR_NAN and sm.device_error() == 0
+    assert tok.tolist()[1:] == [0, 0, 0] and ch.tolist()[1:] == [0.0] * 3 and not pr[1:].any()
+    check(bad[:1], u[:1], pr[:1], tok[:1], ch[:1], 1, temperature=[1.0])
+
+
+def test_parameters_that_are_not_numbers():
+    """NaN turns a filter off, of a temperature makes the row greedy."""
+    rng = np.random.default_rng(1)
+    logits = torch.from_numpy(rng.normal(size=(4, 600)).astype(np.float32)).to(DEV)
+    u = torch.rand(4, device=DEV)
+    nan = float("nan")
+    kw = dict(temperature=np.array([1, nan, 1, 1], np.float32), top_p=np.array([nan, 0.5, 0.5, 1], np.float32),
+              min_p=np.array([0, 0, nan, nan], np.float32))
+    tok, ch, pr, _ = run(logits, u, kw)
+    check(logits, u, pr, tok, ch, 1, temperature=[1, 0, 1, 1], top_p=[1, 1, 0.5, 1], min_p=[0] * 4)
+
+
+def test_strides_in_place_and_reuse():
+    """Rows of a wider buffer at odd addresses; the distribution over the logits;
+    one sampler for smaller calls."""
+    rng = np.random.default_rng(2)
+    s = sampling.Sampler(9, 5003, device=DEV)
+    for dtype in ("f32", "bf16"):
+        wide = torch.from_numpy(rng.normal(size=(6, 5011)).astype(np.float32) * 3).to(DEV).to(TD[dtype])
+        u = torch.from_numpy(rng.random(6, np.float32)).to(DEV)
+        for off, V in ((0, 5003), (3, 5001), (1, 77)):
+            logits = wide[:, off:off + V]
+            tok, ch, pr, _ = run(logits, u, dict(top_p=0.7), sampler=s)
+            check(logits, u, pr, tok, ch, 6, top_p=[0.7])
+    logits = wide[:, :1999].float().contiguous()
+    want = run(logits, u, dict(top_k=30, temperature=0.6), sampler=s)
+    tok, ch = s.draw(logits, u, top_k=30, temperature=0.6, probs=logits)
+    assert torch.equal(tok, want[0]) and torch.equal(ch, want[1]) and torch.equal(logits, want[2])
+
+
+def test_the_same_draws_as_the_verifier():
+    """Without filters and at one temperature the draw is spade_softmax's
+    distribution and the verifier's bonus token of the same uniform."""
+    rng = np.random.default_rng(3)
+    V, B = 8011, 12
+    logits = torch.from_numpy(rng.normal(size=(B, V)).astype(np.float32) * 2).to(DEV)
+    u = torch.from_numpy(rng.random(B, np.float32)).to(DEV)
+    n, corr, err = (torch.zeros(x, dtype=torch.int32, device=DEV) for x in (B, B, 1))
+    modes = torch.ones(B, dtype=torch.uint8, device=DEV)
+    spade.accept_from_logits_noalloc(logits[:, None].contiguous(), None, None, u, modes, 0.75, n, corr, err)
+    tok, ch, pr, _ = run(logits, u, dict(temperature=0.75))
+    assert torch.equal(tok, corr)
+    sm = torch.empty_like(logits)
+    spade.softmax_into(logits, sm, 0.75)
+    assert ((pr - sm).abs() <= 1e-5 * sm + 1e-12).all()  # (spade_softmax is float32: exponents up to 22 rounded at 2^-20)
+
+
+def test_distribution_of_the_draw():
+    """Many uniforms over one row: chi-squared against the filtered distribution."""
+    rng = np.random.default_rng(4)
+    row = torch.from_numpy(rng.normal(size=50).astype(np.float32) * 1.5).to(DEV)
+    N = 20000
+    logits = row[None].expand(N, 50).contiguous()
+    u = torch.from_numpy(rng.random(N, np.float32)).to(DEV)
+    tok, _, _, _ = run(logits, u, dict(top_p=0.9), probs=False)
+    _, p = otree.sample(row.cpu().numpy(), 0.5, top_p=0.9)
+    got = np.bincount(tok.cpu().numpy(), minlength=50)
+    ok = p > 0
+    assert got[~ok].sum() == 0
+    chi = ((got - N * p)[ok] ** 2 / (N * p[ok])).sum()
+    k = ok.sum() - 1
+    assert chi < k + 3.3 * np.sqrt(2 * k) + 6  # (0.1%)
+
+
+def test_draw_refuses():
+    s = sampling.Sampler(4, 100, device=DEV)
+    x, u = torch.zeros(4, 100, device=DEV), torch.zeros(4, device=DEV)
+    for bad in (lambda: s.draw(x.half(), u), lambda: s.draw(x.cpu(), u), lambda: s.draw(x[0], u),
+                lambda: s.draw(torch.zeros(5, 100, device=DEV), torch.zeros(5, device=DEV)),
+                lambda: s.draw(torch.zeros(4, 101, device=DEV), u), lambda: s.draw(x, u[:3]),
+                lambda: s.draw(x, u.double()), lambda: s.draw(x, u, top_k=torch.zeros(2, device=DEV)),
+                lambda: s.draw(x, u, temperature=torch.zeros(3, device=DEV)),
+                lambda: s.draw(x, u, temperature=torch.ones(2, device=DEV), top_p=torch.ones(4, device=DEV)),
+                lambda: s.draw(x.t(), u), lambda: s.draw(x, u, probs=torch.zeros(4, 99, device=DEV))):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(spade.SpadeError):
+        s.draw(x[:0], u[:0])
+    with pytest.raises(spade.SpadeError):
+        sampling.Sampler(1, 1, device=DEV)

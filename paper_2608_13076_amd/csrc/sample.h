@@ -9,7 +9,7 @@ namespace spade {
 constexpr int kSampleMaxVocab = 1 << 20;
 constexpr int kSampleSlice = 4096;  // tokens of a workgroup of the first pass: 16 per thread
 constexpr int kSampleBins = 128;    // of a slice's weights
-constexpr int kSampleList = 4096;   // candidates of a row kept apart
+constexpr int kSampleList = 8192;   // candidates of a row kept apart
 constexpr int kSampleParts = 32;    // most workgroups of a row in the second pass
 
 // What the passes of a row hand on.
@@ -44,7 +44,7 @@ struct SampleArgs {
   float* smax;          // [rows][NS] largest logit of a slice
   int32_t* sarg;        // ... its lowest token (greedy rows)
   uint64_t* hist;       // [rows][NS][kSampleBins] count and weight
-  double* best;         // [rows][kSampleParts] best score of a part, its token, the weight of its kept tokens
+  double* best;         // [rows][NS] best score of a part (or slice), its token, the weight of its kept tokens
   int32_t* best_id;
   double* sum;
   SampleRow* row;       // [rows]

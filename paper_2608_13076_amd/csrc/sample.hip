@@ -36,6 +36,9 @@ struct Request {
   int top_k;
   bool greedy, use_k, use_p;
   __device__ __forceinline__ bool listed() const { return use_k || use_p; }
+  // neither borders nor the row's maximum matter to a slice's draw: tokens that the other slices'
+  // maxima leave out could not win (32 below them; the noise spans 19.5), and weigh 2^-46
+  __device__ __forceinline__ bool plain() const { return !greedy && !listed() && min_d >= kSpan; }
 };
 
 __device__ __forceinline__ Request request_of(const SampleArgs& a, int row) {
@@ -62,24 +65,78 @@ __device__ __forceinline__ double row_inv_T(double inv_T, float m) {
   return fmin(inv_T, most);
 }
 
-// Bins of l / T on a grid that all slices share, and their upper edges.
-__device__ __forceinline__ double bin_of(float l, double inv_T) { return floor((double)l * inv_T * kBinsPerUnit); }
-__device__ __forceinline__ double edge_of(double bin) { return (bin + 1.0) * kBin; }
+// Bins of l / T on a grid that all slices of a row share, each cut into steps: l c is
+// the number of a token's step.  A step's weight comes from a table, the rest of the
+// step from a short series (below 2^-10: 2^-34 of the weight; float32's exponential
+// would leave the border of a fine distribution to its rounding).
+constexpr double kStep = kBin / kSteps;
+struct Grid {
+  double c;
+  double top;   // the largest logit's bin
+  double at;    // and its place in it, in steps
+  int top_i;
+  bool wide;    // step numbers beyond 31 bits: only the difference from the bin is exact then
+  __device__ __forceinline__ Grid(double inv_T, float m) {
+    c = inv_T * (kSteps * kBinsPerUnit);
+    top = floor((double)m * c * (1.0 / kSteps));
+    at = fmin(fmax(__builtin_fma((double)m, c, -top * kSteps), 0.0), kSteps - 0x1p-20);
+    wide = !(fabs(top) < 0x1p22);
+    top_i = (int)top;
+  }
+  // bins below the top (below 0 or beyond the bins: not of the row's window), the
+  // step in its bin and the rest of a step
+  __device__ __forceinline__ int place(float l, int& step, float& rest) const {
+    const double z = (double)l * c;
+    if (wide) {
+      const double bin = floor(z * (1.0 / kSteps));
+      const double t = fmin(fmax(__builtin_fma((double)l, c, -bin * kSteps), 0.0), kSteps - 0x1p-20);
+      step = (int)t;
+      rest = (float)(t - (double)step);
+      return (int)fmin(top - bin, 1e6);
+    }
+    const double q = floor(z);
+    const int i = (int)q;
+    rest = (float)(z - q);
+    step = i & (kSteps - 1);
+    return top_i - (i >> 8);
+  }
+};
 
-// exp(x) for x in a bin below its edge: a table's step and a short series of the
-// rest (|r| < 0.001: 2^-34 of the value; float32's exponential would leave the
-// border of a fine distribution to its rounding).
-__device__ __forceinline__ double bin_weight(const double* table, double x) {
-  constexpr float scale = (float)(kSteps / kBin);
-  const int i = min(max((int)((float)x * -scale), 0), kSteps - 1);
-  const float r = (float)__builtin_fma((double)i, kBin / kSteps, x);
+// exp of what the tables hold: by its series at x / 64
+constexpr double const_exp(double x) {
+  double t = 1.0, s = 1.0;
+  for (int i = 1; i < 24; ++i) {
+    t *= x / 64.0 / i;
+    s += t;
+  }
+  for (int i = 0; i < 6; ++i) s *= s;
+  return s;
+}
+struct Tables {
+  double step[kSteps];       // weight of a step over its bin's upper edge's
+  double edge[kSampleBins];  // weight of the upper edge of the bin j below the first over that bin's lower edge's
+};
+constexpr Tables make_tables() {
+  Tables t{};
+  for (int i = 0; i < kSteps; ++i) t.step[i] = const_exp((i - kSteps) * kStep);
+  for (int j = 0; j < kSampleBins; ++j) t.edge[j] = const_exp((1 - j) * kBin);
+  return t;
+}
+__device__ const Tables kTables = make_tables();
+// weight of a place over its bin's upper edge's
+__device__ __forceinline__ double place_weight(const double* table, int step, float rest) {
+  const float r = rest * (float)kStep;
   const float e = r * __builtin_fmaf(r, __builtin_fmaf(r, 1.f / 6.f, 0.5f), 1.f);
-  const double t = table[i];
+  const double t = table[step];
   return __builtin_fma(t, (double)e, t);
 }
-__device__ __forceinline__ void fill_table(double* table, int tid) {
-  static_assert(kSteps == kThreads, "a step per thread");
-  table[tid] = exp(-(double)tid * (kBin / kSteps));
+static_assert(kSteps == kThreads && kSteps == 256, "a step per thread, 8 bits");
+// The lower edge of the top bin over the largest logit, whose weight is 1.
+__device__ __forceinline__ double top_scale(const Grid& g, const double* table, float m) {
+  int step;
+  float rest;
+  g.place(m, step, rest);
+  return 1.0 / (place_weight(table, step, rest) * const_exp(kBin));
 }
 
 // w 2^n as an integer, w 2^n < 2^51
@@ -87,6 +144,7 @@ template <int N>
 __device__ __forceinline__ uint64_t fixed(double w) {
   return (uint64_t)__double_as_longlong(__builtin_fma(w, (double)(1ull << N), 0x1p52)) & 0xfffffffffffffull;
 }
+constexpr int kCopies = 4;     // of a slice's bins, by lane: neighbouring lanes often meet in a bin
 constexpr int kMassBits = 38;  // of a slice's bins: 4096 weights up to 1 below the count at bit 51
 
 // Order-preserving integer of a float.
@@ -153,46 +211,164 @@ __device__ __forceinline__ float load1(const SampleArgs& a, int row, int v) {
   return x != x ? -INFINITY : fminf(x, FLT_MAX);
 }
 
+// Values of other lanes by data-parallel moves, which cost an instruction where a
+// shuffle goes through the LDS.  After the six steps of a reduction (or inclusive
+// prefix: 1, 2, 4 and 8 lanes down within a row of sixteen, then a row's last lane to
+// the next row, lane 31 to the upper half) the last lane has the whole.
+template <int STEP>
+__device__ __forceinline__ uint32_t lane_step(uint32_t v, uint32_t none) {
+  constexpr int ctrl = STEP < 4 ? 0x110 + (1 << STEP) : STEP == 4 ? 0x142 : 0x143;
+  constexpr int rows = STEP < 4 ? 0xf : STEP == 4 ? 0xa : 0xc;
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)v, ctrl, rows, 0xf, false);
+}
+template <int STEP>
+__device__ __forceinline__ uint64_t lane_step(uint64_t v, uint64_t none) {
+  return (uint64_t)lane_step<STEP>((uint32_t)(v >> 32), (uint32_t)(none >> 32)) << 32 | lane_step<STEP>((uint32_t)v, (uint32_t)none);
+}
+template <int STEP>
+__device__ __forceinline__ double lane_step(double v, double none) {
+  return __longlong_as_double((long long)lane_step<STEP>((uint64_t)__double_as_longlong(v), (uint64_t)__double_as_longlong(none)));
+}
+template <int STEP>
+__device__ __forceinline__ float lane_step(float v, float none) {
+  return __uint_as_float(lane_step<STEP>(__float_as_uint(v), __float_as_uint(none)));
+}
+template <int STEP>
+__device__ __forceinline__ int lane_step(int v, int none) {
+  return (int)lane_step<STEP>((uint32_t)v, (uint32_t)none);
+}
+// v of lane l, the same for all
+__device__ __forceinline__ uint32_t lane_of(uint32_t v, int l) { return (uint32_t)__builtin_amdgcn_readlane((int)v, l); }
+__device__ __forceinline__ int lane_of(int v, int l) { return __builtin_amdgcn_readlane(v, l); }
+__device__ __forceinline__ float lane_of(float v, int l) { return __uint_as_float(lane_of(__float_as_uint(v), l)); }
+__device__ __forceinline__ uint64_t lane_of(uint64_t v, int l) {
+  return (uint64_t)lane_of((uint32_t)(v >> 32), l) << 32 | lane_of((uint32_t)v, l);
+}
+__device__ __forceinline__ double lane_of(double v, int l) {
+  return __longlong_as_double((long long)lane_of((uint64_t)__double_as_longlong(v), l));
+}
+template <typename T, typename F>
+__device__ __forceinline__ T all_steps(T v, F f) {
+  v = f(v, lane_step<0>(v, v));
+  v = f(v, lane_step<1>(v, v));
+  v = f(v, lane_step<2>(v, v));
+  v = f(v, lane_step<3>(v, v));
+  v = f(v, lane_step<4>(v, v));
+  return f(v, lane_step<5>(v, v));
+}
 __device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
-  return v;
+  return lane_of(all_steps(v, [](float x, float y) { return fmaxf(x, y); }), 63);
 }
 __device__ __forceinline__ int wave_min(int v) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v = min(v, __shfl_xor(v, o));
-  return v;
+  return lane_of(all_steps(v, [](int x, int y) { return min(x, y); }), 63);
 }
-__device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o);
-  return v;
+// inclusive prefix sums
+template <typename T>
+__device__ __forceinline__ T wave_prefix(T v) {
+  v += lane_step<0>(v, (T)0);
+  v += lane_step<1>(v, (T)0);
+  v += lane_step<2>(v, (T)0);
+  v += lane_step<3>(v, (T)0);
+  v += lane_step<4>(v, (T)0);
+  return v + lane_step<5>(v, (T)0);
 }
+__device__ __forceinline__ double wave_sum(double v) { return lane_of(wave_prefix(v), 63); }
 
 struct Draw {
   double s;
   int id;
 };
 __device__ __forceinline__ Draw better_draw(Draw x, Draw y) { return y.s > x.s || (y.s == x.s && y.id < x.id) ? y : x; }
+template <int STEP>
+__device__ __forceinline__ Draw lane_step(Draw v, Draw) {
+  return Draw{lane_step<STEP>(v.s, v.s), lane_step<STEP>(v.id, v.id)};
+}
 __device__ __forceinline__ Draw wave_draw(Draw v) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v = better_draw(v, Draw{__shfl_xor(v.s, o), __shfl_xor(v.id, o)});
-  return v;
+  v = all_steps(v, [](Draw x, Draw y) { return better_draw(x, y); });
+  return Draw{lane_of(v.s, 63), lane_of(v.id, 63)};
 }
 
-// Token `id` at distance d takes part in the draw.  It wins with U above
-// exp(-exp(-(best + d))) only, so 1 - U below exp(-(best + d)): most tokens end
-// there, without a logarithm, and those that no noise could lift (1 - U is at
-// least 2^-24) without their hash.
-__device__ __forceinline__ void draw(Draw& best, float& bestf, uint64_t seed, int id, double d) {
-  const float t = __builtin_amdgcn_exp2f(-(bestf + (float)d) * 1.44269504f) * 1.001f;
-  if (t < 0x1p-24f) return;
-  const uint32_t x = (uint32_t)(splitmix64_at(seed, (uint64_t)id) >> 41);
-  if (((float)(0x7fffffu - x) + 0.5f) * 0x1p-23f > t) return;
+// The draw as a race: argmax(G - d) is the token with the least e = -log(U) exp(d).
+// A token is read with 1 - U <= -log(U) first, so most end without a logarithm, and
+// those that no noise could bring ahead (1 - U is at least 2^-24) without their hash.
+// e is good to 2^-17 in float32: tokens closer than that are told apart in double.
+__device__ __noinline__ double score_of(uint32_t x, double d) {
   const double U = ((double)x + 0.5) * 0x1p-23;
-  const Draw n{-log(-log(U)) - d, id};
-  best = better_draw(best, n);
-  bestf = (float)best.s;
+  return -log(-log(U)) - d;
+}
+constexpr float kNear = 0x1p-15f;
+constexpr uint64_t kGolden = 0x9E3779B97F4A7C15ull;  // of SplitMix64's state
+struct Race {
+  float bound = INFINITY;  // nothing above it can win
+  float e = INFINITY;      // the lane's best
+  uint32_t x = 0;
+  int id = 0x7fffffff;
+  double d = INFINITY;
+  // Token n, whose weight is w: the hash of output n of the stream z0 + (n + 1)
+  // golden (z: that sum), of which 23 bits count: the product's upper word
+  __device__ __forceinline__ void enter(uint64_t z, int n, float w, const double& max, const float& l, const double& inv_T) {
+    const float f = __builtin_amdgcn_rcpf(w);
+    if (f * 0x1p-24f > bound) return;
+    z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
+    z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;  // (z ^ z >> 31 leaves the upper 23 bits alone)
+    const uint32_t xn = (uint32_t)(z >> 32) >> 9;
+    const float y = ((float)(0x7fffffu - xn) + 0.5f) * 0x1p-23f;  // 1 - U, exact
+    if (y * f > bound) return;
+    // -log(1 - y): a series below 1/8
+    float g = __builtin_fmaf(y, 1.f / 6.f, 0.2f);
+    g = __builtin_fmaf(y, g, 0.25f);
+    g = __builtin_fmaf(y, g, 1.f / 3.f);
+    g = __builtin_fmaf(y, g, 0.5f);
+    g = __builtin_fmaf(y, g, 1.f) * y;
+    if (y >= 0.125f) g = __builtin_amdgcn_logf(1.f - y) * -0.69314718f;
+    const float en = g * f;
+    const double dn = (max - (double)l) * inv_T;
+    bool first = en < e;
+    if (en >= e * (1.f - kNear) && en <= e * (1.f + kNear)) {
+      const double a = score_of(xn, dn), b = score_of(x, d);
+      first = a > b || (a == b && n < id);
+    }
+    if (first) {
+      e = en;
+      x = xn;
+      id = n;
+      d = dn;
+      bound = fminf(bound, e * (1.f + 4.f * kNear));
+    }
+  }
+  // the lanes' bounds to all (all lanes of the wave call it)
+  __device__ __forceinline__ void share() {
+    bound = lane_of(all_steps(bound, [](float a, float b) { return fminf(a, b); }), 63);
+  }
+  // the wave's token
+  __device__ __forceinline__ Draw best() {
+    share();
+    Draw r{-INFINITY, 0x7fffffff};
+    if (e <= bound) r = Draw{score_of(x, d), id};
+    return wave_draw(r);
+  }
+};
+
+// A workgroup's draws and weights to one place.
+template <int W>
+__device__ __forceinline__ void store_draw(const SampleArgs& a, int64_t at, Race& race, double sum, Draw* wd, double* ws, int tid) {
+  Draw best = race.best();
+  sum = wave_sum(sum);
+  if ((tid & 63) == 0) {
+    wd[tid >> 6] = best;
+    ws[tid >> 6] = sum;
+  }
+  __syncthreads();
+  if (tid == 0) {
+#pragma unroll
+    for (int w = 1; w < W; ++w) {
+      best = better_draw(best, wd[w]);
+      sum += ws[w];
+    }
+    a.best[at] = best.s;
+    a.best_id[at] = best.id;
+    a.sum[at] = sum;
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -200,17 +376,19 @@ template <bool BF16>
 __global__ void __launch_bounds__(kThreads) sample_slice_kernel(SampleArgs a) {
   __shared__ float wm[4];
   __shared__ int wi[4];
-  __shared__ double table[kSteps];
-  __shared__ uint64_t bins[kSampleBins];
+  __shared__ double table[kSteps], edge[kSampleBins];
+  __shared__ uint64_t bins[kSampleBins * kCopies];
+  __shared__ Draw wd[4];
+  __shared__ double ws[4];
   const int row = blockIdx.x / a.NS, s = blockIdx.x - row * a.NS, tid = threadIdx.x, wave = tid >> 6;
-  const Request q = request_of(a, row);
   float x[16];
   const bool nan = load16<BF16>(a, row, s * kSampleSlice, tid, x);
+  const Request q = request_of(a, row);
   if (nan) flag_error(a.err, SPADE_DERR_NAN);
-  if (q.listed()) {
-    fill_table(table, tid);
-    if (tid < kSampleBins) bins[tid] = 0;
-  }
+  table[tid] = kTables.step[tid];
+  if (tid < kSampleBins) edge[tid] = kTables.edge[tid];
+#pragma unroll
+  for (int c = 0; c < kSampleBins * kCopies; c += kThreads) bins[c + tid] = 0;
   float m = x[0];
 #pragma unroll
   for (int k = 1; k < 16; ++k) m = fmaxf(m, x[k]);
@@ -234,25 +412,53 @@ __global__ void __launch_bounds__(kThreads) sample_slice_kernel(SampleArgs a) {
     if (tid == 0) a.sarg[at] = min(min(wi[0], wi[1]), min(wi[2], wi[3]));
     return;
   }
+  const double inv_T = row_inv_T(q.inv_T, m);
+  const Grid grid(inv_T, m);
+  if (q.plain()) {
+    const int base = token_of<BF16>(s * kSampleSlice, tid, 0);
+    const uint64_t z0 = (uint64_t)__float_as_uint(a.u[row]) + (uint64_t)(base + 1) * kGolden;
+    Race race;
+    double sum = 0.0;
+    const double scale = top_scale(grid, table, m);
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      int step;
+      float rest;
+      const int j = grid.place(x[k], step, rest);
+      if (x[k] > -INFINITY && j < kSampleBins) {
+        const double w = place_weight(table, step, rest) * (edge[j] * scale);
+        sum += w;
+        const int off = token_of<BF16>(0, 0, k);
+        race.enter(z0 + (uint64_t)off * kGolden, base + off, (float)w, (double)m, x[k], inv_T);
+      }
+      if (k == 0 || k == 4) race.share();
+    }
+    store_draw<4>(a, (int64_t)row * a.NS + s, race, sum, wd, ws, tid);
+    return;
+  }
   if (!q.listed()) return;
-  const double inv_T = row_inv_T(q.inv_T, m), top = bin_of(m, inv_T);
 #pragma unroll
   for (int k = 0; k < 16; ++k) {
-    const double bin = bin_of(x[k], inv_T), j = top - bin;
-    if (x[k] > -INFINITY && j < (double)kSampleBins) {
-      const double w = bin_weight(table, __builtin_fma((double)x[k], inv_T, -edge_of(bin)));
-      atomicAdd((unsigned long long*)&bins[(int)j], (unsigned long long)(fixed<kMassBits>(w) | 1ull << 51));
-    }
+    int step;
+    float rest;
+    const int j = grid.place(x[k], step, rest);
+    if (x[k] > -INFINITY && j < kSampleBins)
+      atomicAdd((unsigned long long*)&bins[j * kCopies + (tid & (kCopies - 1))], (unsigned long long)(fixed<kMassBits>(place_weight(table, step, rest)) | 1ull << 51));
   }
   __syncthreads();
-  if (tid < kSampleBins) a.hist[at * kSampleBins + tid] = bins[tid];
+  if (tid < kSampleBins) {
+    uint64_t w = 0;
+#pragma unroll
+    for (int c = 0; c < kCopies; ++c) w += bins[tid * kCopies + c];
+    a.hist[at * kSampleBins + tid] = w;
+  }
 }
 
 // ---------------------------------------------------------------------------
 // Inclusive prefix of two values per lane over 128 bins.
 struct ScanSmem {
   double table[kSteps];
-  double factor[kSampleBins];  // weight of a bin's edge over the largest weight
+  double factor[kSampleBins];  // weight of a bin's upper edge over the largest weight
   uint64_t mass[2][kSampleBins];
   uint32_t cnt[2][kSampleBins];
   int off[256];  // bins between a slice's top and the row's (1000: out of reach)
@@ -267,19 +473,23 @@ __global__ void __launch_bounds__(kThreads) sample_scan_kernel(SampleArgs a) {
   __shared__ ScanSmem sm;
   const int row = blockIdx.x / a.NW, part = blockIdx.x - row * a.NW, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const Request q = request_of(a, row);
-  if (q.greedy) return;
+  if (q.greedy || q.plain()) return;
   const float ms = tid < a.NS ? a.smax[(int64_t)row * a.NS + tid] : -INFINITY;  // (at most 256 slices)
   const float m0 = wave_max(ms);
   if (lane == 0) sm.wm[wave] = m0;
-  fill_table(sm.table, tid);
+  sm.table[tid] = kTables.step[tid];
+  const double ej = kTables.edge[tid & (kSampleBins - 1)];
   __syncthreads();
   const float M = fmaxf(fmaxf(sm.wm[0], sm.wm[1]), fmaxf(sm.wm[2], sm.wm[3]));
   if (M == -INFINITY) return;
-  const double inv_T = row_inv_T(q.inv_T, M), top = bin_of(M, inv_T);
+  const double inv_T = row_inv_T(q.inv_T, M);
+  const Grid grid(inv_T, M);
   {
+    int step;
+    float rest;
     const double d = ((double)M - (double)ms) * inv_T;
-    sm.off[tid] = ms > -INFINITY && d <= kSpan ? (int)(top - bin_of(ms, inv_T)) : 1000;
-    if (tid < kSampleBins) sm.factor[tid] = exp(__builtin_fma(-(double)M, inv_T, edge_of(top - tid)));
+    sm.off[tid] = ms > -INFINITY && d <= kSpan ? grid.place(ms, step, rest) : 1000;
+    if (tid < kSampleBins) sm.factor[tid] = ej * top_scale(grid, sm.table, M);
   }
   __syncthreads();
   int lo = kSampleBins, hi = kSampleBins;
@@ -288,12 +498,18 @@ __global__ void __launch_bounds__(kThreads) sample_scan_kernel(SampleArgs a) {
     uint64_t mass = 0;
     uint32_t cnt = 0;
     const uint64_t* h = a.hist + (int64_t)row * a.NS * kSampleBins;
-#pragma unroll 4
-    for (int s = half; s < a.NS; s += 2) {
-      const int jj = j - sm.off[s];
-      const uint64_t w = jj >= 0 ? h[s * kSampleBins + jj] : 0ull;
-      mass += w & 0x7ffffffffffffull;
-      cnt += (uint32_t)(w >> 51);
+    for (int s0 = half; s0 < a.NS; s0 += 32) {  // (sixteen loads in flight)
+      uint64_t w[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int s = s0 + 2 * e, jj = s < a.NS ? j - sm.off[s] : -1;
+        w[e] = jj >= 0 ? h[s * kSampleBins + jj] : 0ull;
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        mass += w[e] & 0x7ffffffffffffull;
+        cnt += (uint32_t)(w[e] >> 51);
+      }
     }
     sm.mass[half][j] = mass;
     sm.cnt[half][j] = cnt;
@@ -307,37 +523,27 @@ __global__ void __launch_bounds__(kThreads) sample_scan_kernel(SampleArgs a) {
         w[e] = (double)(sm.mass[0][b] + sm.mass[1][b]) * 0x1p-38 * sm.factor[b];
         c[e] = (int)(sm.cnt[0][b] + sm.cnt[1][b]);
       }
-      double sw = w[0] + w[1];
-      int sc = c[0] + c[1];
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const double tw = __shfl_up(sw, o);
-        const int tc = __shfl_up(sc, o);
-        if (lane >= o) {
-          sw += tw;
-          sc += tc;
-        }
-      }
+      const double sw = wave_prefix(w[0] + w[1]);
+      const int sc = wave_prefix(c[0] + c[1]);
       wi[1] = sw;
       wi[0] = sw - w[1];
       ci[1] = sc;
       ci[0] = sc - c[1];
-      const double total = __shfl(sw, 63);
+      const double total = lane_of(sw, 63);
       // the first bin with f, and the counts and weights before it
       auto first = [&](bool f0, bool f1) {
         const uint64_t hit = __ballot(f0 || f1);
         if (hit == 0) return kSampleBins - 1;
         const int l = __ffsll((unsigned long long)hit) - 1;
-        return 2 * l + (__shfl((int)f0, l) ? 0 : 1);
+        return 2 * l + (lane_of((int)f0, l) ? 0 : 1);
       };
       int k_bin = kSampleBins - 1, k_in = 0;
       double least = total, most = total;  // of the weight that top_p refers to
-      if (q.use_k && __shfl(ci[1], 63) > q.top_k) {  // (else all are among the first top_k)
+      if (q.use_k && lane_of(ci[1], 63) > q.top_k) {  // (else all are among the first top_k)
         k_in = 1;
         k_bin = first(ci[0] >= q.top_k, ci[1] >= q.top_k);
-        const double in = __shfl(k_bin & 1 ? wi[1] : wi[0], k_bin >> 1);
-        most = in;
-        least = in - __shfl(k_bin & 1 ? w[1] : w[0], k_bin >> 1);
+        most = lane_of(k_bin & 1 ? wi[1] : wi[0], k_bin >> 1);
+        least = most - lane_of(k_bin & 1 ? w[1] : w[0], k_bin >> 1);
       }
       lo = hi = k_bin;
       if (q.use_p) {
@@ -347,8 +553,8 @@ __global__ void __launch_bounds__(kThreads) sample_scan_kernel(SampleArgs a) {
         hi = min(hi, first(wi[0] >= t1, wi[1] >= t1));
         if (k_in) hi = k_bin;  // the first top_k tokens' weight ends there
       }
-      const double in = __shfl(lo & 1 ? wi[1] : wi[0], lo >> 1), ex = in - __shfl(lo & 1 ? w[1] : w[0], lo >> 1);
-      const int above = __shfl(lo & 1 ? ci[1] : ci[0], lo >> 1) - __shfl(lo & 1 ? c[1] : c[0], lo >> 1);
+      const double in = lane_of(lo & 1 ? wi[1] : wi[0], lo >> 1), ex = in - lane_of(lo & 1 ? w[1] : w[0], lo >> 1);
+      const int above = lane_of(lo & 1 ? ci[1] : ci[0], lo >> 1) - lane_of(lo & 1 ? c[1] : c[0], lo >> 1);
       if (lane == 0) {
         sm.row.mass = lo == 0 ? 0.0 : ex;
         sm.row.total = total;
@@ -373,142 +579,165 @@ __global__ void __launch_bounds__(kThreads) sample_scan_kernel(SampleArgs a) {
     r.inv_T = inv_T;
     a.row[row] = r;
   }
-  const uint64_t seed = (uint64_t)__float_as_uint(a.u[row]);
-  Draw best{-INFINITY, 0x7fffffff};
-  float bestf = -INFINITY;
+  // a logit that no token of the bins up to hi is below (with room for its rounding)
+  float least = -INFINITY;
+  if (inv_T > 0.0) {
+    const double l = hi < kSampleBins ? (grid.top - hi) * kSteps / grid.c : (double)M - q.min_d / inv_T;
+    least = (float)fmax(l - fabs(l) * 0x1p-20 - fabs((double)M) * 0x1p-40, -3e38);
+  }
+  const uint64_t z0 = (uint64_t)__float_as_uint(a.u[row]);
+  Race race;
   double sum = 0.0;
-  const int s1 = min(a.NS, (part + 1) * a.spw);
-  for (int s = part * a.spw; s < s1; ++s) {
-    if (sm.off[s] > min(hi, kSampleBins - 1)) continue;
+  const int s1 = min(a.NS, (part + 1) * a.spw), reach = min(hi, kSampleBins - 1);
+  // the slices that reach these bins, one ahead
+  auto after = [&](int s) {
+    while (s < s1 && sm.off[s] > reach) ++s;
+    return s;
+  };
+  float next[16];
+  int s = after(part * a.spw);
+  if (s < s1) load16<BF16>(a, row, s * kSampleSlice, tid, next);
+  while (s < s1) {
     float x[16];
-    load16<BF16>(a, row, s * kSampleSlice, tid, x);
+#pragma unroll
+    for (int k = 0; k < 16; ++k) x[k] = next[k];
+    const int here = s;
+    s = after(s + 1);
+    if (s < s1) load16<BF16>(a, row, s * kSampleSlice, tid, next);
     uint32_t listed = 0;
 #pragma unroll
     for (int k = 0; k < 16; ++k) {
+      if (x[k] < least) continue;
       const double d = ((double)M - (double)x[k]) * inv_T;
       if (!(x[k] > -INFINITY && d <= kSpan)) continue;
-      const double bin = bin_of(x[k], inv_T);
-      const int j = min((int)(top - bin), kSampleBins - 1);
+      int step;
+      float rest;
+      const int j = min(grid.place(x[k], step, rest), kSampleBins - 1);
       if (j > hi) continue;
       if (j >= lo) {
         listed |= 1u << k;
       } else if (d <= q.min_d) {
-        sum += bin_weight(sm.table, __builtin_fma((double)x[k], inv_T, -edge_of(bin))) * sm.factor[j];
-        draw(best, bestf, seed, token_of<BF16>(s * kSampleSlice, tid, k), d);
+        const double w = place_weight(sm.table, step, rest) * sm.factor[j];
+        sum += w;
+        const int id = token_of<BF16>(here * kSampleSlice, tid, k);
+        race.enter(z0 + (uint64_t)(id + 1) * kGolden, id, (float)w, (double)M, x[k], inv_T);
       }
     }
-    bestf = wave_max(bestf);  // (a bound for the other lanes' tokens, not their best)
+    race.share();
     if (__any(listed != 0)) {
       const int n = __popc(listed);
-      int in = n;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const int t = __shfl_up(in, o);
-        if (lane >= o) in += t;
-      }
+      const int in = wave_prefix(n);
       uint32_t at = 0;
       if (lane == 63) at = atomicAdd(a.count + row, (uint32_t)in);
-      at = (uint32_t)__shfl((int)at, 63) + (uint32_t)(in - n);
+      at = lane_of(at, 63) + (uint32_t)(in - n);
 #pragma unroll
       for (int k = 0; k < 16; ++k)
         if (listed >> k & 1u) {
           if (at < kSampleList)
-            a.list[(int64_t)row * kSampleList + at] = make_uint2((uint32_t)token_of<BF16>(s * kSampleSlice, tid, k), __float_as_uint(x[k]));
+            a.list[(int64_t)row * kSampleList + at] = make_uint2((uint32_t)token_of<BF16>(here * kSampleSlice, tid, k), __float_as_uint(x[k]));
           ++at;
         }
     }
   }
-  best = wave_draw(best);
-  sum = wave_sum(sum);
-  if (lane == 0) {
-    sm.wd[wave] = best;
-    sm.ws[wave] = sum;
-  }
-  __syncthreads();
-  if (tid == 0) {
-    for (int w = 1; w < 4; ++w) {
-      best = better_draw(best, sm.wd[w]);
-      sum += sm.ws[w];
-    }
-    const int64_t at = (int64_t)row * kSampleParts + part;
-    a.best[at] = best.s;
-    a.best_id[at] = best.id;
-    a.sum[at] = sum;
-  }
+  store_draw<4>(a, (int64_t)row * a.NS + part, race, sum, sm.wd, sm.ws, tid);
 }
 
 // ---------------------------------------------------------------------------
+constexpr int kFinish = 1024;                     // threads of a row's last workgroup
+constexpr int kStaged = kSampleList;               // listed tokens kept in LDS
+constexpr int kListBits = 40;  // of a listed weight: 2^20 of them stay below 2^61
+
 struct FinishSmem {
-  uint2 list[2048];
-  uint64_t mass[256];
-  uint32_t cnt[256];
-  Draw wd[4];
-  double ws[4];
-  float wm[4];
-  int wi[4];
+  uint2 list[kStaged];
+  double table[kSteps];
+  double factor[kSampleBins];  // weight of a bin's edge over that of the list's first
+  uint64_t mass[2][256];  // of this digit and, cleared meanwhile, of the next
+  uint32_t cnt[2][256];
+  Draw wd[kFinish / 64];
+  double ws[kFinish / 64];
+  float wm[kFinish / 64];
+  int wi[kFinish / 64];
+  uint32_t key_lo, key_hi;
   // of a selection
   int digit;
   uint32_t cnt_in;
   uint64_t before, total;
 };
 
-// The listed tokens of a row: in LDS, in the list, or, where there are more, all
-// tokens of the row again.
+// The listed tokens of a row: in LDS, from the list, or, where that was too short
+// for them, all tokens of the row again.
 template <bool BF16>
-struct Listed {
+struct Tokens {
   const SampleArgs& a;
   FinishSmem& sm;
   int row, tid;
   uint32_t n;
-  double top, inv_T, M;
+  double M, inv_T;
+  Grid grid;
   int lo, hi;
   __device__ __forceinline__ void stage() {
-    if (n <= 2048) {
-      for (uint32_t i = tid; i < n; i += kThreads) sm.list[i] = a.list[(int64_t)row * kSampleList + i];
-    }
+    if (tid < kSteps) sm.table[tid] = kTables.step[tid];
+    // (bin j's over bin 0's: the same steps down, from 1)
+    if (tid < kSampleBins) sm.factor[tid] = tid == 0 ? 1.0 : kTables.edge[tid] / kTables.edge[0];
+    if (n <= kStaged)
+      for (uint32_t i = tid; i < n; i += kFinish) sm.list[i] = a.list[(int64_t)row * kSampleList + i];
     __syncthreads();
+  }
+  // a listed token's weight over that of the first listed bin's edge
+  __device__ __forceinline__ uint64_t weight(float l) const {
+    int step;
+    float rest;
+    const int j = min(max(grid.place(l, step, rest) - lo, 0), kSampleBins - 1);
+    // (in the bins' own steps first, so that equal weights add up to exactly what the bins hold)
+    const double w = (double)fixed<kMassBits>(place_weight(sm.table, step, rest)) * 0x1p-38;
+    return fixed<kListBits>(w * sm.factor[j]);
   }
   template <typename F>
   __device__ __forceinline__ void each(F f) const {
-    if (n <= 2048) {
-      for (uint32_t i = tid; i < n; i += kThreads) f((int)sm.list[i].x, __uint_as_float(sm.list[i].y));
-    } else if (n <= kSampleList) {
-      for (uint32_t i = tid; i < n; i += kThreads) {
-        const uint2 e = a.list[(int64_t)row * kSampleList + i];
-        f((int)e.x, __uint_as_float(e.y));
-      }
-    } else {
-      for (int v = tid; v < a.V; v += kThreads) {
-        const float l = load1<BF16>(a, row, v);
+    const uint32_t count = n <= kSampleList ? n : (uint32_t)a.V;
+#pragma unroll 1
+    for (uint32_t i = tid; i < count; i += kFinish) {
+      uint2 e;
+      if (n <= kStaged) {
+        e = sm.list[i];
+      } else if (n <= kSampleList) {
+        e = a.list[(int64_t)row * kSampleList + i];
+      } else {
+        const float l = load1<BF16>(a, row, (int)i);
         if (!(l > -INFINITY && (M - (double)l) * inv_T <= kSpan)) continue;
-        const int j = min((int)(top - bin_of(l, inv_T)), kSampleBins - 1);
-        if (j >= lo && j <= hi) f(v, l);
+        int step;
+        float rest;
+        const int j = min(grid.place(l, step, rest), kSampleBins - 1);
+        if (j < lo || j > hi) continue;
+        e = make_uint2(i, __float_as_uint(l));
       }
+      const float l = __uint_as_float(e.y);
+      f((int)e.x, key_of(l), l);
     }
   }
 };
 
-constexpr int kListBits = 40;  // of a listed weight: 2^20 of them stay below 2^61
-
 // The digit at which `target` (a count, or a weight) is reached, from the highest
 // down (UP: from the lowest up), with what comes before it.  False: never.
 template <bool MASS, bool UP>
-__device__ __forceinline__ bool find_digit(FinishSmem& sm, int tid, uint64_t target) {
+__device__ __forceinline__ bool find_digit(FinishSmem& sm, int tid, int& turn, uint64_t target) {
   __syncthreads();
+  const int now = turn;
+  turn ^= 1;
+  if (tid >= 64)
+    for (int i = tid - 64; i < 256; i += kFinish - 64) {
+      sm.cnt[turn][i] = 0;
+      sm.mass[turn][i] = 0;
+    }
   if (tid < 64) {
     uint64_t v[4], s = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int b = UP ? 4 * tid + e : 255 - 4 * tid - e;
-      v[e] = MASS ? sm.mass[b] : (uint64_t)sm.cnt[b];
+      v[e] = MASS ? sm.mass[now][b] : (uint64_t)sm.cnt[now][b];
       s += v[e];
     }
-    uint64_t in = s;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const uint64_t t = __shfl_up((unsigned long long)in, o);
-      if (tid >= o) in += t;
-    }
+    const uint64_t in = wave_prefix(s);
     const uint64_t hit = __ballot(in >= target);
     if (hit == 0) {
       if (tid == 0) sm.digit = -1;
@@ -524,7 +753,7 @@ __device__ __forceinline__ bool find_digit(FinishSmem& sm, int tid, uint64_t tar
       const int b = UP ? 4 * tid + e : 255 - 4 * tid - e;
       sm.digit = b;
       sm.before = before;
-      sm.cnt_in = sm.cnt[b];
+      sm.cnt_in = sm.cnt[now][b];
     }
   }
   __syncthreads();
@@ -532,76 +761,155 @@ __device__ __forceinline__ bool find_digit(FinishSmem& sm, int tid, uint64_t tar
 }
 
 // Among the listed tokens that `in` allows, the key at which the target is reached
-// in descending order: the key, what is before it and how many tokens have it.
+// in descending order: the key, what is before it and how many tokens have it.  The
+// keys' differences from the lowest are cut into digits of 8 bits, the highest first
+// (the keys of a bin agree in their upper bits: digits of the keys themselves would
+// count all tokens in one place).
 struct Border {
   uint32_t key, ties;
   uint64_t before;
   bool found;
 };
 template <bool MASS, typename L, typename In>
-__device__ __forceinline__ Border find_key(const L& ls, FinishSmem& sm, int tid, uint64_t target, double ref, In in) {
+__device__ __forceinline__ Border find_key(const L& ls, FinishSmem& sm, int tid, int& turn, uint64_t target, In in) {
   Border b{0u, 0u, 0u, true};
+  const uint32_t base = sm.key_lo, span = sm.key_hi - base;
+  int shift = max(0, 32 - __clz((int)span) - 8), last = 32;
 #pragma unroll 1
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    sm.cnt[tid] = 0;
-    sm.mass[tid] = 0;
-    __syncthreads();
-    ls.each([&](int id, float l) {
-      const uint32_t key = key_of(l);
-      if (!in(id, key) || (shift < 24 && (key ^ b.key) >> (shift + 8) != 0)) return;
-      const uint32_t dg = key >> shift & 255u;
-      atomicAdd(&sm.cnt[dg], 1u);
-      if (MASS)
-        atomicAdd((unsigned long long*)&sm.mass[dg], (unsigned long long)fixed<kListBits>(exp(__builtin_fma((double)l, ls.inv_T, -ref))));
+  for (;;) {
+    ls.each([&](int id, uint32_t key, float l) {
+      const uint32_t v = key - base;
+      if (!in(id, key) || (last < 32 && v >> last != b.key)) return;
+      const uint32_t dg = last < 32 ? v >> shift & ((1u << (last - shift)) - 1) : v >> shift;
+      atomicAdd(&sm.cnt[turn][dg], 1u);
+      if (MASS) atomicAdd((unsigned long long*)&sm.mass[turn][dg], (unsigned long long)ls.weight(l));
     });
-    if (!find_digit<MASS, false>(sm, tid, target)) {
+    if (!find_digit<MASS, false>(sm, tid, turn, target)) {
       b.found = false;
-      __syncthreads();
       return b;
     }
-    b.key |= (uint32_t)sm.digit << shift;
+    b.key = last < 32 ? b.key << (last - shift) | (uint32_t)sm.digit : (uint32_t)sm.digit;
     b.before += sm.before;
     target -= sm.before;
     b.ties = sm.cnt_in;
-    __syncthreads();
+    if (shift == 0) break;
+    last = shift;
+    shift = max(0, shift - 8);
   }
+  b.key += base;
   return b;
 }
 
 // The n-th lowest id (from 1) of the listed tokens with this key.
 template <typename L>
-__device__ __forceinline__ uint32_t find_id(const L& ls, FinishSmem& sm, int tid, uint32_t key, uint32_t n) {
+__device__ __forceinline__ uint32_t find_id(const L& ls, FinishSmem& sm, int tid, int& turn, uint32_t key, uint32_t n) {
   uint32_t found = 0;
   uint64_t target = n;
 #pragma unroll 1
   for (int shift = 16; shift >= 0; shift -= 8) {
-    sm.cnt[tid] = 0;
-    __syncthreads();
-    ls.each([&](int id, float l) {
-      if (key_of(l) == key && (shift == 16 || ((uint32_t)id ^ found) >> (shift + 8) == 0)) atomicAdd(&sm.cnt[(uint32_t)id >> shift & 255u], 1u);
+    ls.each([&](int id, uint32_t k, float) {
+      if (k == key && (shift == 16 || ((uint32_t)id ^ found) >> (shift + 8) == 0)) atomicAdd(&sm.cnt[turn][(uint32_t)id >> shift & 255u], 1u);
     });
-    if (!find_digit<false, true>(sm, tid, target)) {
-      __syncthreads();
-      return 0xffffffffu;
-    }
+    if (!find_digit<false, true>(sm, tid, turn, target)) return 0xffffffffu;
     found |= (uint32_t)sm.digit << shift;
     target -= sm.before;
-    __syncthreads();
   }
   return found;
 }
 
+// a key's logit
+__device__ __forceinline__ float logit_of(uint32_t key) {
+  return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
+}
+
+// The row's border (key, id) among its listed tokens, and their part in the draw.
+template <typename L>
+__device__ __forceinline__ void finish_list(const L& ls, FinishSmem& sm, int tid, const Request& q, const SampleRow& r,
+                                            uint64_t z0, uint32_t& key, uint32_t& id_to, Race& race, double& sum) {
+  const double factor = kTables.edge[min(r.lo, kSampleBins - 1)] * top_scale(ls.grid, sm.table, r.max);
+  uint32_t lo = 0xffffffffu, hi = 0u;
+  ls.each([&](int, uint32_t k, float) {
+    lo = min(lo, k);
+    hi = max(hi, k);
+  });
+  if (tid == 0) {
+    sm.key_lo = 0xffffffffu;
+    sm.key_hi = 0;
+    sm.total = 0;
+  }
+  int turn = 0;
+  if (tid < 256) {
+    sm.cnt[0][tid] = 0;
+    sm.mass[0][tid] = 0;
+  }
+  __syncthreads();
+  lo = lane_of(all_steps(lo, [](uint32_t x, uint32_t y) { return min(x, y); }), 63);
+  hi = lane_of(all_steps(hi, [](uint32_t x, uint32_t y) { return max(x, y); }), 63);
+  if ((tid & 63) == 0 && lo <= hi) {
+    atomicMin(&sm.key_lo, lo);
+    atomicMax(&sm.key_hi, hi);
+  }
+  __syncthreads();
+  if (sm.key_lo > sm.key_hi) return;  // nothing listed
+  double total = r.total;
+  if (r.k_in) {
+    const uint32_t n = (uint32_t)(q.top_k - r.above);
+    const Border b = find_key<false>(ls, sm, tid, turn, n, [](int, uint32_t) { return true; });
+    if (b.found) {
+      key = b.key;
+      if (n - (uint32_t)b.before < b.ties) id_to = find_id(ls, sm, tid, turn, key, n - (uint32_t)b.before);
+    }
+    if (q.use_p) {  // the weight of the first top_k
+      uint64_t mine = 0;
+      ls.each([&](int id, uint32_t k, float l) {
+        if (k > key || (k == key && (uint32_t)id <= id_to)) mine += ls.weight(l);
+      });
+      atomicAdd((unsigned long long*)&sm.total, (unsigned long long)mine);
+      __syncthreads();
+      total = r.mass + (double)sm.total * 0x1p-40 * factor;
+    }
+  }
+  if (q.use_p) {
+    const uint64_t target = (uint64_t)fmax(ceil(((q.top_p - kSlack) * total - r.mass) / factor * 0x1p40), 1.0);
+    const uint32_t k_key = key, k_id = id_to;
+    const Border b = find_key<true>(ls, sm, tid, turn, target, [&](int id, uint32_t k) {
+      return k > k_key || (k == k_key && (uint32_t)id <= k_id);
+    });
+    if (b.found) {
+      key = b.key;
+      // as many of the equal tokens as it takes, in their order
+      const uint64_t w = ls.weight(logit_of(key));
+      const uint64_t need = w > 0 ? (target - b.before + w - 1) / w : b.ties;
+      const uint32_t n = (uint32_t)(need < 1 ? 1 : need > b.ties ? b.ties : need);
+      if (b.key != k_key) id_to = 0xffffffffu;
+      if (n < b.ties) id_to = find_id(ls, sm, tid, turn, key, n);
+    }
+  }
+  ls.each([&](int id, uint32_t k, float l) {
+    if (!(k > key || (k == key && (uint32_t)id <= id_to))) return;
+    const double d = ((double)r.max - (double)l) * r.inv_T;
+    if (d > q.min_d) return;
+    const double w = (double)ls.weight(l) * 0x1p-40 * factor;
+    sum += w;
+    race.enter(z0 + (uint64_t)(id + 1) * kGolden, id, fmaxf((float)w, 1e-14f), (double)r.max, l, r.inv_T);
+  });
+}
+
 template <bool BF16>
-__global__ void __launch_bounds__(kThreads) sample_finish_kernel(SampleArgs a) {
+__global__ void __launch_bounds__(kFinish) sample_finish_kernel(SampleArgs a) {
   __shared__ FinishSmem sm;
+  constexpr int W = kFinish / 64;
   const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const Request q = request_of(a, row);
+  const SampleRow r0 = a.row[row];
+  const uint32_t n = a.count[row];
   // the row's maximum
   const float ms = tid < a.NS ? a.smax[(int64_t)row * a.NS + tid] : -INFINITY;
   const float m0 = wave_max(ms);
   if (lane == 0) sm.wm[wave] = m0;
   __syncthreads();
-  const float M = fmaxf(fmaxf(sm.wm[0], sm.wm[1]), fmaxf(sm.wm[2], sm.wm[3]));
+  float M = sm.wm[0];
+  for (int w = 1; w < W; ++w) M = fmaxf(M, sm.wm[w]);
   if (M == -INFINITY || q.greedy) {
     int id = 0x7fffffff;
     if (q.greedy && ms == M && tid < a.NS) id = a.sarg[(int64_t)row * a.NS + tid];
@@ -609,7 +917,7 @@ __global__ void __launch_bounds__(kThreads) sample_finish_kernel(SampleArgs a) {
     if (lane == 0) sm.wi[wave] = id;
     __syncthreads();
     if (tid == 0) {
-      id = min(min(sm.wi[0], sm.wi[1]), min(sm.wi[2], sm.wi[3]));
+      for (int w = 0; w < W; ++w) id = min(id, sm.wi[w]);
       const bool none = M == -INFINITY;
       if (none) {
         flag_error(a.err, SPADE_DERR_NAN);
@@ -628,69 +936,34 @@ __global__ void __launch_bounds__(kThreads) sample_finish_kernel(SampleArgs a) {
     }
     return;
   }
-  SampleRow r = a.row[row];
-  const uint64_t seed = (uint64_t)__float_as_uint(a.u[row]);
-  Draw best{-INFINITY, 0x7fffffff};
+  SampleRow r = r0;
+  const uint64_t z0 = (uint64_t)__float_as_uint(a.u[row]);
+  Race race;
+  Draw best{-INFINITY, 0x7fffffff};  // of the earlier passes
   double sum = 0.0;
-  if (tid < a.NW) {
-    const int64_t at = (int64_t)row * kSampleParts + tid;
-    best = Draw{a.best[at], a.best_id[at]};
-    sum = a.sum[at];
-  }
   uint32_t key = 0, id_to = 0xffffffffu;
   if (q.listed()) {
-    Listed<BF16> ls{a, sm, row, tid, a.count[row], bin_of(M, r.inv_T), r.inv_T, (double)M, r.lo, r.hi};
+    Tokens<BF16> ls{a, sm, row, tid, n, (double)M, r.inv_T, Grid(r.inv_T, M), r.lo, r.hi};
     ls.stage();
-    const double ref = edge_of(ls.top - r.lo), factor = exp(__builtin_fma(-(double)M, r.inv_T, ref));
-    double total = r.total;
-    uint32_t ties_k = 0xffffffffu;
-    if (r.k_in) {
-      const Border b = find_key<false>(ls, sm, tid, (uint64_t)(q.top_k - r.above), ref, [](int, uint32_t) { return true; });
-      if (b.found) {
-        key = b.key;
-        ties_k = (uint32_t)(q.top_k - r.above) - (uint32_t)b.before;
-        if (ties_k < b.ties) id_to = find_id(ls, sm, tid, key, ties_k);
-      }
-      // the weight of the first top_k
-      if (tid == 0) sm.total = 0;
-      __syncthreads();
-      uint64_t mine = 0;
-      ls.each([&](int id, float l) {
-        const uint32_t k = key_of(l);
-        if (k > key || (k == key && (uint32_t)id <= id_to)) mine += fixed<kListBits>(exp(__builtin_fma((double)l, r.inv_T, -ref)));
-      });
-      atomicAdd((unsigned long long*)&sm.total, (unsigned long long)mine);
-      __syncthreads();
-      total = r.mass + (double)sm.total * 0x1p-40 * factor;
-      __syncthreads();
-    }
-    if (q.use_p) {
-      const uint64_t target = (uint64_t)fmax(ceil(((q.top_p - kSlack) * total - r.mass) / factor * 0x1p40), 1.0);
-      const uint32_t k_key = key, k_id = id_to;
-      const Border b = find_key<true>(ls, sm, tid, target, ref, [&](int id, uint32_t k) {
-        return k > k_key || (k == k_key && (uint32_t)id <= k_id);
-      });
-      if (b.found) {
-        key = b.key;
-        // as many of the equal tokens as it takes, in their order
-        const uint32_t bits = key & 0x80000000u ? key ^ 0x80000000u : ~key;
-        const uint64_t w = fixed<kListBits>(exp(__builtin_fma((double)__uint_as_float(bits), r.inv_T, -ref)));
-        const uint64_t need = w > 0 ? (target - b.before + w - 1) / w : b.ties;
-        const uint32_t n = (uint32_t)(need < 1 ? 1 : need > b.ties ? b.ties : need);
-        id_to = n < b.ties || b.key == k_key ? find_id(ls, sm, tid, key, n) : 0xffffffffu;
-      }
-    }
-    float bestf = -INFINITY;
-    ls.each([&](int id, float l) {
-      const uint32_t k = key_of(l);
-      if (!(k > key || (k == key && (uint32_t)id <= id_to))) return;
-      const double d = ((double)M - (double)l) * r.inv_T;
-      if (d > q.min_d) return;
-      sum += exp(-d);
-      draw(best, bestf, seed, id, d);
-    });
+    finish_list(ls, sm, tid, q, r, z0, key, id_to, race, sum);
   }
-  best = wave_draw(best);
+  if (q.plain()) {
+    // the slices' own draws, relative to their maxima
+    r = SampleRow{};
+    r.max = M;
+    r.inv_T = row_inv_T(q.inv_T, M);
+    const double d = ((double)M - (double)ms) * r.inv_T;
+    if (tid < a.NS && ms > -INFINITY && d <= kSpan) {
+      const int64_t at = (int64_t)row * a.NS + tid;
+      best = Draw{a.best[at] - d, a.best_id[at]};
+      sum = a.sum[at] * exp(-d);
+    }
+  } else if (tid * a.spw < a.NS) {  // the second pass's
+    const int64_t at = (int64_t)row * a.NS + tid;
+    best = Draw{a.best[at], a.best_id[at]};
+    sum += a.sum[at];
+  }
+  best = better_draw(wave_draw(best), race.best());
   sum = wave_sum(sum);
   if (lane == 0) {
     sm.wd[wave] = best;
@@ -698,7 +971,7 @@ __global__ void __launch_bounds__(kThreads) sample_finish_kernel(SampleArgs a) {
   }
   __syncthreads();
   if (tid == 0) {
-    for (int w = 1; w < 4; ++w) {
+    for (int w = 1; w < W; ++w) {
       best = better_draw(best, sm.wd[w]);
       sum += sm.ws[w];
     }
@@ -758,7 +1031,7 @@ hipError_t sample_t(const SampleArgs& a, hipStream_t st) {
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((sample_scan_kernel<BF16>), dim3((unsigned)parts), dim3(kThreads), 0, st, a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  hipLaunchKernelGGL((sample_finish_kernel<BF16>), dim3((unsigned)a.rows), dim3(kThreads), 0, st, a);
+  hipLaunchKernelGGL((sample_finish_kernel<BF16>), dim3((unsigned)a.rows), dim3(kFinish), 0, st, a);
   if ((e = hipGetLastError()) != hipSuccess || a.probs == nullptr) return e;
   hipLaunchKernelGGL((sample_probs_kernel<BF16>), dim3((unsigned)slices), dim3(kThreads), 0, st, a);
   return hipGetLastError();
@@ -777,9 +1050,9 @@ size_t sample_workspace(int rows, int V, SampleArgs* a, uint8_t* base) {
   uint8_t* smax = take(R * NS * 4);
   uint8_t* sarg = take(R * NS * 4);
   uint8_t* hist = take(R * NS * kSampleBins * 8);
-  uint8_t* best = take(R * kSampleParts * 8);
-  uint8_t* best_id = take(R * kSampleParts * 4);
-  uint8_t* sum = take(R * kSampleParts * 8);
+  uint8_t* best = take(R * NS * 8);
+  uint8_t* best_id = take(R * NS * 4);
+  uint8_t* sum = take(R * NS * 8);
   uint8_t* row = take(R * sizeof(SampleRow));
   uint8_t* count = take(R * 4);
   uint8_t* list = take(R * kSampleList * 8);
@@ -801,7 +1074,7 @@ hipError_t launch_sample(const SampleArgs& in, hipStream_t st) {
   SampleArgs a = in;
   a.NS = (a.V + kSampleSlice - 1) / kSampleSlice;
   // every part reads the row's bins (1 KB a slice): few rows take many parts, many rows few
-  const int parts = std::max(1, std::min({kSampleParts, a.NS, 2048 / a.rows}));
+  const int parts = std::max(1, std::min({kSampleParts, a.NS, 4096 / a.rows}));
   a.spw = (a.NS + parts - 1) / parts;
   a.NW = (a.NS + a.spw - 1) / a.spw;
   return a.bf16 ? sample_t<true>(a, st) : sample_t<false>(a, st);

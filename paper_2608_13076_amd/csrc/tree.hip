@@ -12,6 +12,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "device_util.h"
 
@@ -340,41 +341,6 @@ __device__ __forceinline__ void swap_words(uint32_t a, uint32_t b, uint32_t& w0,
   w2 = t[1];
 }
 
-// One block of 32 positions: two 16-position groups of keys, HD / 16 tiles of values.
-template <int HD>
-struct KvBlock {
-  uint4 k[2][HD / 32];
-  uint4 v[HD / 16];
-};
-
-template <int HD>
-struct KvLoader {
-  Rsrc k, v;
-  uint32_t lane16;
-  __device__ __forceinline__ void init(const TreeCache& c, int64_t head, int lane) {
-    // (a head has at most 2^28 bytes)
-    k = make_rsrc(c.k + head * c.head_elems, (uint32_t)(c.head_elems * 2));
-    v = make_rsrc(c.v + head * c.head_elems, (uint32_t)(c.head_elems * 2));
-    lane16 = 16u * lane;
-  }
-  // blk at or past `end`: nothing is read
-  __device__ __forceinline__ void keys(KvBlock<HD>& b, int blk, int end) const {
-    const uint32_t so = blk < end ? (uint32_t)blk * (64 * HD) : 0u, vo = blk < end ? lane16 : kOob;
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int s = 0; s < HD / 32; ++s)
-        b.k[u][s] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(
-                                                  k, (int)vo, (int)(so + (u * (HD / 32) + s) * 1024), 0));
-  }
-  __device__ __forceinline__ void values(KvBlock<HD>& b, int blk, int end) const {
-    const uint32_t so = blk < end ? (uint32_t)(blk >> 3) * (512 * HD) + (uint32_t)(blk & 7) * 1024 : 0u, vo = blk < end ? lane16 : kOob;
-#pragma unroll
-    for (int t = 0; t < HD / 16; ++t)
-      b.v[t] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(v, (int)vo, (int)(so + t * 8192), 0));
-  }
-};
-
 // the bf16 terms of two floats, largest first
 template <int N>
 __device__ __forceinline__ void terms(float a, float b, uint32_t (&w)[N]) {
@@ -422,179 +388,159 @@ __device__ __forceinline__ void zero_rows(const TreeAttend& p, int b, int kvh, i
   }
 }
 
-template <int HD, int RT>
-struct TreeSmem {
-  float o[kWaves][RT * 16][HD + 4];
-  float m[kWaves][RT * 16], l[kWaves][RT * 16];
+// Which part of the call a workgroup has.  Workgroup i runs on XCD i % 8: those
+// that read the same keys for other rows follow each other there and share its L2.
+struct Part {
+  unsigned unit, head;
+  int b, kvh, rb, L, n, rows, nb, lo, hi;
+  __device__ __forceinline__ bool init(const TreeAttend& p, int tid) {
+    const unsigned xcd = blockIdx.x & 7, jj = blockIdx.x >> 3, tt = jj / (unsigned)p.RB;
+    rb = (int)(jj - tt * p.RB);
+    unit = 8 * tt + xcd;
+    if (unit >= (unsigned)(p.B * p.KVH * p.NS)) return false;
+    head = unit / (unsigned)p.NS;
+    const int split = (int)(unit - head * p.NS);
+    b = (int)(head / (unsigned)p.KVH);
+    kvh = (int)(head - (unsigned)b * p.KVH);
+    const TreeRows rr = tree_rows(p, b, split == 0 && rb == 0 && kvh == 0 && tid == 0);
+    L = rr.L;
+    n = rr.n;
+    rows = p.G * n;
+    nb = (L + n + 31) / 32;
+    lo = split * p.CB;
+    hi = min(nb, lo + p.CB);
+    return true;
+  }
 };
 
-template <int HD, bool QB, int RT>
-__global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(RT == 1 ? 2 : 1)))
-tree_attend_kernel(TreeAttend p) {
-  constexpr int FT = HD / 16, S = HD / 32;
-  constexpr int NQ = QB ? 1 : 3, NP = QB ? 2 : 3;  // bf16 terms of queries and of probabilities
-  extern __shared__ __align__(16) uint8_t smem_raw[];
-  TreeSmem<HD, RT>& sm = *reinterpret_cast<TreeSmem<HD, RT>*>(smem_raw);
-  const int tid = threadIdx.x, lane = tid & 63, q = lane >> 4, c = lane & 15;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // Workgroup i runs on XCD i % 8: those that read the same keys for other rows
-  // follow each other there and share its L2.
-  const unsigned xcd = blockIdx.x & 7, jj = blockIdx.x >> 3;
-  const unsigned tt = jj / (unsigned)p.RB, rb = jj - tt * p.RB, unit = 8 * tt + xcd;
-  if (unit >= (unsigned)(p.B * p.KVH * p.NS)) return;
-  const unsigned head = unit / (unsigned)p.NS, split = unit - head * p.NS;
-  const int b = (int)(head / (unsigned)p.KVH), kvh = (int)(head - (unsigned)b * p.KVH);
-  const bool first = split == 0 && rb == 0;
-  const TreeRows rr = tree_rows(p, b, first && kvh == 0 && tid == 0);
-  const int L = rr.L, n = rr.n, total = L + n, rows = p.G * n, r0 = (int)rb * RT * 16;
-  if (p.NS == 1 && rb == 0 && n < p.R) zero_rows<HD, QB>(p, b, kvh, n, tid, kWaves * 64);
-  const int nb = (total + 31) / 32, lo = (int)split * p.CB, hi = min(nb, lo + p.CB);
-  if (r0 >= rows || lo >= hi) return;
+// One head's keys and values: fragments of 1 KB, a lane's 16 bytes at 16 lane.
+template <int HD>
+struct KvLoader {
+  Rsrc k, v;
+  __device__ __forceinline__ void init(const TreeCache& c, int64_t head) {
+    // (a head has at most 2^28 bytes)
+    k = make_rsrc(c.k + head * c.head_elems, (uint32_t)(c.head_elems * 2));
+    v = make_rsrc(c.v + head * c.head_elems, (uint32_t)(c.head_elems * 2));
+  }
+  // fragment f of a block of 32 positions; nothing is read where `there` is false
+  __device__ __forceinline__ uint4 key(int blk, int f, int lane, bool there) const {
+    const uint32_t so = there ? (uint32_t)blk * (64 * HD) : 0u;
+    return __builtin_bit_cast(
+        uint4, __builtin_amdgcn_raw_buffer_load_b128(k, (int)(there ? 16u * lane : kOob), (int)(so + f * 1024), 0));
+  }
+  __device__ __forceinline__ uint4 value(int blk, int f, int lane, bool there) const {
+    const uint32_t so = there ? (uint32_t)(blk >> 3) * (512 * HD) + (uint32_t)(blk & 7) * 1024 : 0u;
+    return __builtin_bit_cast(
+        uint4, __builtin_amdgcn_raw_buffer_load_b128(v, (int)(there ? 16u * lane : kOob), (int)(so + f * 8192), 0));
+  }
+};
 
-  KvLoader<HD> ld;
-  ld.init(p.cache, (int64_t)head, lane);
-  KvBlock<HD> buf[2];
+// Masks of a lane's eight positions, the first d from the tree's first row: up to the
+// last row; the tree's rows.
+__device__ __forceinline__ void tail_masks(int d0, int n, uint32_t (&keep)[4], uint32_t (&own)[4]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    keep[j] = own[j] = 0;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int d = d0 + 2 * j + e;
+      const uint32_t half = 0xffffu << (16 * e);
+      if (d < n) keep[j] |= half;
+      if (d >= 0 && d < n) own[j] |= half;
+    }
+  }
+}
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) {
+  return ((w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+}
+
+// The rows of a wave: RT tiles of 16, a lane with row c of each.
+template <int HD, bool QB, int RT>
+struct Rows {
+  static constexpr int FT = HD / 16, S = HD / 32;
+  static constexpr int NQ = QB ? 1 : 3, NP = QB ? 2 : 3;  // bf16 terms of queries and of probabilities
   bf16x8 Q[RT][NQ][S];
-  int node[RT];
-  // queries first: the blocks' loads are waited for in order
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    const int m = r0 + rt * 16 + c, g = m / n, i = m - g * n;
-    const bool ok = m < rows;
-    node[rt] = ok ? i : -1;
-    const int64_t at = ((int64_t)b * p.R + (ok ? i : 0)) * p.q_ld + ((int64_t)kvh * p.G + (ok ? g : 0)) * HD + 8 * q;
-#pragma unroll
-    for (int s = 0; s < S; ++s) {
-      float x[8];
-      load4<QB>(p.q, at + 32 * s, x);
-      load4<QB>(p.q, at + 32 * s + 4, x + 4);
-      uint32_t w[NQ][4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        uint32_t e[NQ];
-        terms<NQ>(ok ? x[2 * j] : 0.f, ok ? x[2 * j + 1] : 0.f, e);
-#pragma unroll
-        for (int k = 0; k < NQ; ++k) w[k][j] = e[k];
-      }
-#pragma unroll
-      for (int k = 0; k < NQ; ++k) Q[rt][k][s] = op(w[k][0], w[k][1], w[k][2], w[k][3]);
-    }
-  }
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    ld.keys(buf[k], lo + wave + k * kWaves, hi);
-    ld.values(buf[k], lo + wave + k * kWaves, hi);
-  }
-  uint64_t anc[RT] = {};
-  if (32 * hi > L) {
-    const uint64_t all = ancestors(p, b, n, lane, kvh == 0 && rb == 0 && hi == nb);
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      const int from = max(node[rt], 0);
-      const uint64_t w = (uint64_t)(uint32_t)__shfl((uint32_t)(all >> 32), from) << 32 | (uint32_t)__shfl((uint32_t)all, from);
-      anc[rt] = node[rt] >= 0 ? w : 0ull;
-    }
-  }
-  const float sl = p.scale * kLog2e;
+  uint64_t anc[RT];
   float M[RT], l[RT];
   floatx4 o[RT][FT];
+  bool broken;  // a value of the tree's own rows was not finite, and cleared
+
+  __device__ __forceinline__ void load(const TreeAttend& p, const Part& w, int r0, int lane) {
+    const int q = lane >> 4, c = lane & 15;
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    M[rt] = -INFINITY;
-    l[rt] = 0.f;
+    for (int rt = 0; rt < RT; ++rt) {
+      const int m = r0 + rt * 16 + c, g = m / w.n, i = m - g * w.n;
+      const bool ok = m < w.rows;
+      const int64_t at =
+          ((int64_t)w.b * p.R + (ok ? i : 0)) * p.q_ld + ((int64_t)w.kvh * p.G + (ok ? g : 0)) * HD + 8 * q;
 #pragma unroll
-    for (int t = 0; t < FT; ++t) o[rt][t] = floatx4{0.f, 0.f, 0.f, 0.f};
+      for (int s = 0; s < S; ++s) {
+        float x[8];
+        load4<QB>(p.q, at + 32 * s, x);
+        load4<QB>(p.q, at + 32 * s + 4, x + 4);
+        uint32_t e[NQ][4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          uint32_t t[NQ];
+          terms<NQ>(ok ? x[2 * j] : 0.f, ok ? x[2 * j + 1] : 0.f, t);
+#pragma unroll
+          for (int k = 0; k < NQ; ++k) e[k][j] = t[k];
+        }
+#pragma unroll
+        for (int k = 0; k < NQ; ++k) Q[rt][k][s] = op(e[k][0], e[k][1], e[k][2], e[k][3]);
+      }
+      anc[rt] = 0;
+      M[rt] = -INFINITY;
+      l[rt] = 0.f;
+#pragma unroll
+      for (int t = 0; t < FT; ++t) o[rt][t] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+    broken = false;
+  }
+  __device__ __forceinline__ void load_ancestors(const TreeAttend& p, const Part& w, int r0, int lane, bool flag) {
+    const uint64_t all = ancestors(p, w.b, w.n, lane, flag);
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const int m = r0 + rt * 16 + (lane & 15), i = m - m / w.n * w.n;
+      const uint64_t x = (uint64_t)__shfl((uint32_t)(all >> 32), i) << 32 | __shfl((uint32_t)all, i);
+      anc[rt] = m < w.rows ? x : 0ull;
+    }
   }
 
-  auto step = [&](KvBlock<HD>& cur, int blk) {
-    const int p0 = 32 * blk, nxt = blk + 2 * kWaves;
-    const bool tail = p0 + 32 > L;
+  // Block blk: key fragment (u, s) and value fragment t from K and V.  TAIL: some
+  // row does not see all of it.
+  template <bool TAIL, typename KF, typename VF>
+  __device__ __forceinline__ void step(int blk, const Part& w, float sl, int lane, KF K, VF V) {
+    const int q = lane >> 4, d0 = 32 * blk - w.L;  // distance of the first position from the tree's first row
     floatx4 z[RT][2];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        z[rt][u] = floatx4{0.f, 0.f, 0.f, 0.f};
+      for (int u = 0; u < 2; ++u) z[rt][u] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int k = NQ - 1; k >= 0; --k)  // (smallest terms first)
+    for (int u = 0; u < 2; ++u) {
+      uint4 kf[S];
 #pragma unroll
-          for (int s = 0; s < S; ++s) z[rt][u] = mfma(cur.k[u][s], Q[rt][k][s], z[rt][u]);
-      }
-    ld.keys(cur, nxt, hi);
-    if (tail) {
-      // A hidden position may hold anything, NaN among it: its score is replaced,
-      // and values behind the last row are cleared.  A value of the tree's own rows
-      // that is not finite must not reach the rows that do not see it: it is cleared
-      // too, and the rows that see it get NaN at its feature.
+      for (int s = 0; s < S; ++s) kf[s] = K(u, s);
+#pragma unroll
+      for (int k = NQ - 1; k >= 0; --k)  // (smallest terms first)
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) z[rt][u] = mfma(kf[s], Q[rt][k][s], z[rt][u]);
+    }
+    if constexpr (TAIL) {
+      // (a hidden position may hold anything, NaN among it)
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const int d = p0 + 16 * u + 4 * q + r - L;
-            const bool sees = d < 0 || (d < n && (anc[rt] >> (d & 63) & 1ull));
+            const int d = d0 + 16 * u + 4 * q + r;
+            const bool sees = d < 0 || (d < w.n && (anc[rt] >> (d & 63) & 1ull));
             if (!sees) z[rt][u][r] = -INFINITY;
           }
-      uint32_t keep[4], own[4], any = 0;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        keep[j] = own[j] = 0;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int d = p0 + 8 * q + 2 * j + e - L;
-          const uint32_t half = 0xffffu << (16 * e);
-          if (d < n) keep[j] |= half;
-          if (d >= 0 && d < n) own[j] |= half;
-        }
-      }
-      auto broken = [&](uint32_t w, int j) {
-        uint32_t m = 0;
-        if ((w & 0x7f80u) == 0x7f80u) m |= 0xffffu;
-        if ((w & 0x7f800000u) == 0x7f800000u) m |= 0xffff0000u;
-        return m & own[j];
-      };
-#pragma unroll
-      for (int t = 0; t < FT; ++t) {
-        uint32_t* w = (uint32_t*)&cur.v[t];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          w[j] &= keep[j];
-          any |= broken(w[j], j);
-        }
-      }
-      if (__any(any != 0)) {
-        bf16x8 sees[RT];
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-          uint32_t w[4] = {};
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int d = p0 + 8 * q + e - L;
-            if (d >= 0 && d < n && (anc[rt] >> (d & 63) & 1ull)) w[e >> 1] |= 0x3f80u << (16 * (e & 1));
-          }
-          sees[rt] = op(w[0], w[1], w[2], w[3]);
-        }
-#pragma unroll
-        for (int t = 0; t < FT; ++t) {
-          uint32_t* w = (uint32_t*)&cur.v[t];
-          uint32_t one[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint32_t m = broken(w[j], j);
-            one[j] = m & 0x3f803f80u;
-            w[j] &= ~m;
-          }
-          const uint4 a = make_uint4(one[0], one[1], one[2], one[3]);
-#pragma unroll
-          for (int rt = 0; rt < RT; ++rt) {
-            const floatx4 hit = mfma(a, sees[rt], floatx4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (hit[r] > 0.f) o[rt][t][r] = __uint_as_float(0x7fc00000u);
-          }
-        }
-      }
     }
     bf16x8 P[RT][NP];
 #pragma unroll
@@ -629,78 +575,509 @@ tree_attend_kernel(TreeAttend p) {
       }
 #pragma unroll
       for (int k = 0; k < NP; ++k) {
-        uint32_t w[4];
-        swap_words(pw[0][0][k], pw[1][0][k], w[0], w[2]);
-        swap_words(pw[0][1][k], pw[1][1][k], w[1], w[3]);
-        P[rt][k] = op(w[0], w[1], w[2], w[3]);
+        uint32_t x[4];
+        swap_words(pw[0][0][k], pw[1][0][k], x[0], x[2]);
+        swap_words(pw[0][1][k], pw[1][1][k], x[1], x[3]);
+        P[rt][k] = op(x[0], x[1], x[2], x[3]);
       }
     }
+    uint32_t keep[4], own[4];
+    if constexpr (TAIL) tail_masks(d0 + 8 * q, w.n, keep, own);
 #pragma unroll
-    for (int t = 0; t < FT; ++t)
+    for (int t = 0; t < FT; ++t) {
+      uint4 vf = V(t);
+      if constexpr (TAIL) {
+        // Values behind the last row are cleared, and those of the tree's own rows that are not
+        // finite, which must not reach the rows that do not see them (mend puts NaN where they do).
+        uint32_t x[4] = {vf.x, vf.y, vf.z, vf.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          x[j] &= keep[j];
+          const uint32_t bad = not_finite(x[j]) & own[j];
+          x[j] &= ~bad;
+          broken |= bad != 0;
+        }
+        vf = make_uint4(x[0], x[1], x[2], x[3]);
+      }
 #pragma unroll
       for (int k = NP - 1; k >= 0; --k)
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) o[rt][t] = mfma(cur.v[t], P[rt][k], o[rt][t]);
-    ld.values(cur, nxt, hi);
-  };
-
-  for (int blk = lo + wave; blk < hi; blk += 2 * kWaves) {
-    step(buf[0], blk);
-    if (blk + kWaves >= hi) break;
-    step(buf[1], blk + kWaves);
-  }
-
-  // the waves' parts
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    const float s = sum_q(l[rt]);
-    if (q == 0) {
-      sm.m[wave][rt * 16 + c] = M[rt];
-      sm.l[wave][rt * 16 + c] = s;
+        for (int rt = 0; rt < RT; ++rt) o[rt][t] = mfma(vf, P[rt][k], o[rt][t]);
     }
   }
-  __syncthreads();
+
+  // A block whose values were cleared: NaN at their features in the rows that see them
+  // (a product of marks counts them).
+  __device__ __forceinline__ void mend(const KvLoader<HD>& ld, int blk, const Part& w, int lane) {
+    const int q = lane >> 4, d0 = 32 * blk - w.L;
+    uint32_t keep[4], own[4];
+    tail_masks(d0 + 8 * q, w.n, keep, own);
+    bf16x8 sees[RT];
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    float m = sm.m[0][rt * 16 + c];
+    for (int rt = 0; rt < RT; ++rt) {
+      uint32_t x[4] = {};
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) m = fmaxf(m, sm.m[w][rt * 16 + c]);
-    const float f = M[rt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M[rt] - m);
+      for (int e = 0; e < 8; ++e) {
+        const int d = d0 + 8 * q + e;
+        if (d >= 0 && d < w.n && (anc[rt] >> (d & 63) & 1ull)) x[e >> 1] |= 0x3f80u << (16 * (e & 1));
+      }
+      sees[rt] = op(x[0], x[1], x[2], x[3]);
+    }
 #pragma unroll
     for (int t = 0; t < FT; ++t) {
-      const floatx4 x = o[rt][t] * f;
-      *(floatx4*)&sm.o[wave][rt * 16 + c][16 * t + 4 * q] = x;
-    }
-  }
-  __syncthreads();
-  constexpr int LPR = HD / 4;  // lanes a row
-  for (int k = tid; k < RT * 16 * LPR; k += kWaves * 64) {
-    const int r = k / LPR, f = (k - r * LPR) * 4, m = r0 + r;
-    if (m >= rows) break;
-    float mx = sm.m[0][r];
+      const uint4 vf = ld.value(blk, t, lane, true);
+      const uint4 one = make_uint4(not_finite(vf.x) & own[0] & 0x3f803f80u, not_finite(vf.y) & own[1] & 0x3f803f80u,
+                                   not_finite(vf.z) & own[2] & 0x3f803f80u, not_finite(vf.w) & own[3] & 0x3f803f80u);
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) mx = fmaxf(mx, sm.m[w][r]);
-    float s = 0.f;
-    floatx4 x = {0.f, 0.f, 0.f, 0.f};
+      for (int rt = 0; rt < RT; ++rt) {
+        const floatx4 hit = mfma(one, sees[rt], floatx4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const float mw = sm.m[w][r];
-      s += mw == -INFINITY ? sm.l[w][r] : sm.l[w][r] * __builtin_amdgcn_exp2f(mw - mx);
-      x += *(const floatx4*)&sm.o[w][r][f];
-    }
-    if (p.NS == 1) {
-      const int g = m / n, i = m - g * n;
-      const float y[4] = {x[0] / s, x[1] / s, x[2] / s, x[3] / s};
-      store4<QB>(p.out, ((int64_t)b * p.R + i) * p.out_ld + ((int64_t)kvh * p.G + g) * HD + f, y);
-    } else {
-      const int64_t at = (int64_t)unit * p.G * p.R + m;
-      *(floatx4*)(p.part_o + at * HD + f) = x;
-      if (f == 0) {
-        p.part_ml[2 * at] = mx;
-        p.part_ml[2 * at + 1] = s;
+        for (int r = 0; r < 4; ++r)
+          if (hit[r] > 0.f) o[rt][t][r] = __uint_as_float(0x7fc00000u);
       }
     }
   }
+};
+
+// An output, or a split's part of it: x of packed row m at features f .. + 3, its
+// reference mx and sum s.
+template <int HD, bool QB>
+__device__ __forceinline__ void put(const TreeAttend& p, const Part& w, int m, int f, floatx4 x, float mx, float s) {
+  if (p.NS == 1) {
+    const int g = m / w.n, i = m - g * w.n;
+    const float y[4] = {x[0] / s, x[1] / s, x[2] / s, x[3] / s};
+    store4<QB>(p.out, ((int64_t)w.b * p.R + i) * p.out_ld + ((int64_t)w.kvh * p.G + g) * HD + f, y);
+  } else {
+    const int64_t at = (int64_t)w.unit * p.G * p.R + m;
+    *(floatx4*)(p.part_o + at * HD + f) = x;
+    if (f == 0) {
+      p.part_ml[2 * at] = mx;
+      p.part_ml[2 * at + 1] = s;
+    }
+  }
+}
+
+// KW waves of the same rows put their parts together; wave kw of rows rw writes to
+// o[kw RW + rw].
+template <int HD, int RT, int WAVES>
+struct JoinSmem {
+  float o[WAVES][RT * 16][HD + 4];
+  float m[WAVES][RT * 16], l[WAVES][RT * 16];
+};
+template <int HD, bool QB, int RT, int RW, int KW>
+__device__ __forceinline__ void join_rows(const TreeAttend& p, const Part& w, const JoinSmem<HD, RT, RW * KW>& sm, int tid) {
+  constexpr int LPR = HD / 4;  // lanes a row
+  for (int k = tid; k < RW * RT * 16 * LPR; k += RW * KW * 64) {
+    const int r = k / LPR, f = (k - r * LPR) * 4, m = w.rb * RW * RT * 16 + r, v = r / (RT * 16), e = r - v * (RT * 16);
+    if (m >= w.rows) break;
+    float mx = sm.m[v][e];
+#pragma unroll
+    for (int j = 1; j < KW; ++j) mx = fmaxf(mx, sm.m[j * RW + v][e]);
+    float s = 0.f;
+    floatx4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < KW; ++j) {
+      const float mw = sm.m[j * RW + v][e], lw = sm.l[j * RW + v][e];
+      // (a part that is NaN stays so whatever its reference)
+      s += mw == -INFINITY ? lw : lw * __builtin_amdgcn_exp2f(mw - mx);
+      x += *(const floatx4*)&sm.o[j * RW + v][e][f];
+    }
+    put<HD, QB>(p, w, m, f, x, mx, s);
+  }
+}
+template <int HD, bool QB, int RT, int RW, int KW>
+__device__ __forceinline__ void join(const TreeAttend& p, const Part& w, Rows<HD, QB, RT>& R, JoinSmem<HD, RT, RW * KW>& sm,
+                                     int rw, int kw, int tid) {
+  const int lane = tid & 63, q = lane >> 4, c = lane & 15, me = kw * RW + rw;
+  if constexpr (KW == 1) {
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const int m = (w.rb * RW + rw) * RT * 16 + rt * 16 + c;
+      const float s = sum_q(R.l[rt]);
+      if (m < w.rows)
+#pragma unroll
+        for (int t = 0; t < HD / 16; ++t) put<HD, QB>(p, w, m, 16 * t + 4 * q, R.o[rt][t], R.M[rt], s);
+    }
+    return;
+  }
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const float s = sum_q(R.l[rt]);
+    if (q == 0) {
+      sm.m[me][rt * 16 + c] = R.M[rt];
+      sm.l[me][rt * 16 + c] = s;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    float m = sm.m[rw][rt * 16 + c];
+#pragma unroll
+    for (int k = 1; k < KW; ++k) m = fmaxf(m, sm.m[k * RW + rw][rt * 16 + c]);
+    const float f = R.M[rt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(R.M[rt] - m);
+#pragma unroll
+    for (int t = 0; t < HD / 16; ++t) {
+      const floatx4 x = R.o[rt][t] * f;
+      *(floatx4*)&sm.o[me][rt * 16 + c][16 * t + 4 * q] = x;
+    }
+  }
+  __syncthreads();
+  join_rows<HD, QB, RT, RW, KW>(p, w, sm, tid);
+}
+
+// Few rows: four waves with the same RT tiles, wave w every fourth block, two blocks
+// in flight in registers.
+template <int HD, bool QB, int RT>
+__global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(RT == 1 ? 2 : 1)))
+tree_attend_kernel(TreeAttend p) {
+  constexpr int FT = HD / 16, S = HD / 32;
+  extern __shared__ __align__(16) uint8_t smem_raw[];
+  auto& sm = *reinterpret_cast<JoinSmem<HD, RT, kWaves>*>(smem_raw);
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  Part w;
+  if (!w.init(p, tid)) return;
+  if (p.NS == 1 && w.rb == 0 && w.n < p.R) zero_rows<HD, QB>(p, w.b, w.kvh, w.n, tid, kWaves * 64);
+  const int r0 = w.rb * RT * 16;
+  if (r0 >= w.rows || w.lo >= w.hi) return;
+  KvLoader<HD> ld;
+  ld.init(p.cache, (int64_t)w.head);
+  Rows<HD, QB, RT> R;
+  R.load(p, w, r0, lane);  // (first: the blocks' loads are waited for in order)
+  uint4 kb[2][2 * S], vb[2][FT];
+  auto request = [&](int e, int blk) {
+#pragma unroll
+    for (int f = 0; f < 2 * S; ++f) kb[e][f] = ld.key(blk, f, lane, blk < w.hi);
+#pragma unroll
+    for (int t = 0; t < FT; ++t) vb[e][t] = ld.value(blk, t, lane, blk < w.hi);
+  };
+  request(0, w.lo + wave);
+  request(1, w.lo + wave + kWaves);
+  const int full = min(w.hi, w.L / 32);  // blocks that every row sees
+  if (full < w.hi) R.load_ancestors(p, w, r0, lane, w.kvh == 0 && w.rb == 0 && w.hi == w.nb);
+  const float sl = p.scale * kLog2e;
+  auto step = [&](auto tail, int e, int blk) {
+    R.template step<decltype(tail)::value>(
+        blk, w, sl, lane, [&](int u, int s) { return kb[e][u * S + s]; }, [&](int t) { return vb[e][t]; });
+  };
+  int blk = w.lo + wave;
+  for (; blk + kWaves < full; blk += 2 * kWaves) {
+    step(std::false_type{}, 0, blk);
+    request(0, blk + 2 * kWaves);
+    step(std::false_type{}, 1, blk + kWaves);
+    request(1, blk + 3 * kWaves);
+  }
+  // what is left: at most one full block, and the tree's
+  const int first = blk;
+  for (; blk < w.hi; blk += 2 * kWaves) {
+    step(std::true_type{}, 0, blk);
+    if (blk + kWaves >= w.hi) break;
+    request(0, blk + 2 * kWaves);
+    step(std::true_type{}, 1, blk + kWaves);
+    request(1, blk + 3 * kWaves);
+  }
+  if (__any(R.broken))
+    for (int e = first; e < w.hi; e += kWaves) R.mend(ld, e, w, lane);
+  join<HD, QB, RT, 1, kWaves>(p, w, R, sm, 0, wave, tid);
+}
+
+// Many rows: eight waves, RW of them with 32 rows (float32: 16) each over the same
+// keys, KW = 8 / RW blocks at a time, which pass through LDS: every byte enters the
+// compute unit once for RW waves.  Loads run D rounds ahead in registers.
+//
+// bfloat16 calls use the 32 x 32 products, whose tile is a block's 32 positions by a
+// wave's 32 rows: lane 32 h + c has the scores of row c at positions 8 g + 4 h .. + 3,
+// and one swap of lane halves per pair of words makes them the next operand.
+typedef __attribute__((ext_vector_type(16))) float floatx16;
+__device__ __forceinline__ floatx16 mfma32(uint4 a, bf16x8 b, floatx16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), b, c, 0, 0, 0);
+}
+__device__ __forceinline__ float half_max(float v) {
+  const auto t = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return max_nan(__uint_as_float(t[0]), __uint_as_float(t[1]));
+}
+__device__ __forceinline__ float half_sum(float v) {
+  const auto t = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(t[0]) + __uint_as_float(t[1]);
+}
+// a pair's second terms: what its first terms w leave
+__device__ __forceinline__ uint32_t second_terms(float a, float b, uint32_t w) {
+  return pk_bf16(a - lo_f(w), b - hi_f(w));
+}
+
+template <int HD>
+struct Rows32 {
+  static constexpr int FT = HD / 32, E = HD / 16, S = HD / 32;
+  bf16x8 Q[E];
+  uint64_t anc;
+  float M, l;  // reference; the lane's part of the sum
+  floatx16 o[FT];
+  bool broken;
+
+  __device__ __forceinline__ void load(const TreeAttend& p, const Part& w, int r0, int lane) {
+    const int h = lane >> 5, m = r0 + (lane & 31), g = m / w.n, i = m - g * w.n;
+    const bool ok = m < w.rows;
+    const int64_t at = ((int64_t)w.b * p.R + (ok ? i : 0)) * p.q_ld + ((int64_t)w.kvh * p.G + (ok ? g : 0)) * HD + 8 * h;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {  // (rows are aligned to 8 bytes)
+      const uint2 a = *(const uint2*)((const uint16_t*)p.q + at + 16 * e), b = *(const uint2*)((const uint16_t*)p.q + at + 16 * e + 4);
+      Q[e] = ok ? op(a.x, a.y, b.x, b.y) : op(0, 0, 0, 0);
+    }
+    anc = 0;
+    M = -INFINITY;
+    l = 0.f;
+    broken = false;
+#pragma unroll
+    for (int t = 0; t < FT; ++t) o[t] = floatx16{};
+  }
+  __device__ __forceinline__ void load_ancestors(const TreeAttend& p, const Part& w, int r0, int lane, bool flag) {
+    const uint64_t all = ancestors(p, w.b, w.n, lane, flag);
+    const int m = r0 + (lane & 31), i = m - m / w.n * w.n;
+    const uint64_t x = (uint64_t)__shfl((uint32_t)(all >> 32), i) << 32 | __shfl((uint32_t)all, i);
+    anc = m < w.rows ? x : 0ull;
+  }
+  __device__ __forceinline__ bool sees(int d, int n) const { return d < 0 || (d < n && (anc >> (d & 63) & 1ull)); }
+
+  // A block at `at` in LDS, fragments of 16 positions by 32 features, then of 16
+  // features by 32 positions: the pieces of a 32 x 16 operand lie in two of them.
+  template <bool TAIL>
+  __device__ __forceinline__ void step(int blk, const Part& w, float sl, int lane, const uint4* at) {
+    const int h = lane >> 5, d0 = 32 * blk - w.L;
+    const uint4* kp = at + (lane >> 4 & 1) * (S * 64) + 16 * h + (lane & 15);
+    const uint4* vp = at + 2 * S * 64 + (lane >> 4 & 1) * 64 + 16 * h + (lane & 15);
+    uint4 kf[E], vf[FT][2];
+#pragma unroll
+    for (int e = 0; e < E; ++e) kf[e] = kp[(e >> 1) * 64 + (e & 1) * 32];
+    floatx16 z = mfma32(kf[0], Q[0], floatx16{});
+#pragma unroll
+    for (int e = 1; e < E; ++e) z = mfma32(kf[e], Q[e], z);
+#pragma unroll
+    for (int t = 0; t < FT; ++t)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) vf[t][s] = vp[t * 128 + s * 32];
+    if constexpr (TAIL) {
+#pragma unroll
+      for (int k = 0; k < 16; ++k)
+        if (!sees(d0 + 8 * (k >> 2) + 4 * h + (k & 3), w.n)) z[k] = -INFINITY;
+    }
+    // A row keeps its reference as long as its sum stays in range (it starts with the first
+    // maximum): no maximum in most blocks, and a row's bits do not depend on the others.
+    float e[16], s = l, base = M == -INFINITY ? 0.f : M;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      e[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[k], sl, -base));
+      s += e[k];
+    }
+    const uint64_t out = __ballot(M == -INFINITY || !(s <= 0x1p60f));
+    if (out != 0) {
+      float mx = z[0];
+#pragma unroll
+      for (int k = 1; k < 16; ++k) mx = max_nan(mx, z[k]);
+      mx = half_max(mx) * sl;
+      const bool up = (out | out >> 32) >> (lane & 31) & 1u;
+      const float mn = up ? fmaxf(M, mx) : M;
+      const float f = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - mn);
+      M = mn;
+      base = M == -INFINITY ? 0.f : M;
+      s = l * f;
+#pragma unroll
+      for (int t = 0; t < FT; ++t) o[t] *= f;
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        e[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[k], sl, -base));
+        s += e[k];
+      }
+    }
+    l = s;
+    bf16x8 P[2][2];  // [16 positions][term]
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2) {
+      uint32_t a[2][4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float x = e[8 * s2 + 2 * j], y = e[8 * s2 + 2 * j + 1];
+        a[0][j] = pk_bf16(x, y);
+        a[1][j] = second_terms(x, y, a[0][j]);
+      }
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const auto r0 = __builtin_amdgcn_permlane32_swap(a[k][0], a[k][2], false, false);
+        const auto r1 = __builtin_amdgcn_permlane32_swap(a[k][1], a[k][3], false, false);
+        P[s2][k] = op(r0[0], r1[0], r0[1], r1[1]);
+      }
+    }
+    if constexpr (TAIL) {
+#pragma unroll
+      for (int s2 = 0; s2 < 2; ++s2) {
+        uint32_t keep[4], own[4];
+        tail_masks(d0 + 16 * s2 + 8 * h, w.n, keep, own);
+#pragma unroll
+        for (int t = 0; t < FT; ++t) {
+          uint32_t x[4] = {vf[t][s2].x, vf[t][s2].y, vf[t][s2].z, vf[t][s2].w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            x[j] &= keep[j];
+            const uint32_t bad = not_finite(x[j]) & own[j];
+            x[j] &= ~bad;
+            broken |= bad != 0;
+          }
+          vf[t][s2] = make_uint4(x[0], x[1], x[2], x[3]);
+        }
+      }
+    }
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+      for (int k = 1; k >= 0; --k)
+#pragma unroll
+        for (int t = 0; t < FT; ++t) o[t] = mfma32(vf[t][s2], P[s2][k], o[t]);
+  }
+  __device__ __forceinline__ void mend(const KvLoader<HD>& ld, int blk, const Part& w, int lane) {
+    const int h = lane >> 5, d0 = 32 * blk - w.L;
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2) {
+      uint32_t keep[4], own[4], x[4] = {};
+      tail_masks(d0 + 16 * s2 + 8 * h, w.n, keep, own);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int d = d0 + 16 * s2 + 8 * h + e;
+        if (d >= 0 && d < w.n && (anc >> (d & 63) & 1ull)) x[e >> 1] |= 0x3f80u << (16 * (e & 1));
+      }
+      const bf16x8 see = op(x[0], x[1], x[2], x[3]);
+#pragma unroll
+      for (int t = 0; t < FT; ++t) {
+        // (fragment 2 t or 2 t + 1, its lane 16 (2 s2 + h) + feature)
+        const uint4 a = ld.value(blk, 2 * t, 32 * s2 + 16 * h + (lane & 15), true);
+        const uint4 b = ld.value(blk, 2 * t + 1, 32 * s2 + 16 * h + (lane & 15), true);
+        const uint4 vf = lane & 16 ? b : a;
+        const uint4 one = make_uint4(not_finite(vf.x) & own[0] & 0x3f803f80u, not_finite(vf.y) & own[1] & 0x3f803f80u,
+                                     not_finite(vf.z) & own[2] & 0x3f803f80u, not_finite(vf.w) & own[3] & 0x3f803f80u);
+        const floatx16 hit = mfma32(one, see, floatx16{});
+#pragma unroll
+        for (int k = 0; k < 16; ++k)
+          if (hit[k] > 0.f) o[t][k] = __uint_as_float(0x7fc00000u);
+      }
+    }
+  }
+};
+
+// KW groups of RW waves put their parts together; wave kw RW + rw has rows rw.
+template <int HD, int WAVES>
+using JoinSmem32 = JoinSmem<HD, 2, WAVES>;
+template <int HD, int RW, int KW>
+__device__ __forceinline__ void join32(const TreeAttend& p, const Part& w, Rows32<HD>& R, JoinSmem32<HD, RW * KW>& sm, int rw,
+                                       int kw, int tid) {
+  const int lane = tid & 63, h = lane >> 5, c = lane & 31, me = kw * RW + rw;
+  const float s = half_sum(R.l);
+  if constexpr (KW == 1) {
+    const int m = (w.rb * RW + rw) * 32 + c;
+    if (m < w.rows)
+#pragma unroll
+      for (int t = 0; t < HD / 32; ++t)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          put<HD, true>(p, w, m, 32 * t + 8 * g + 4 * h,
+                        floatx4{R.o[t][4 * g], R.o[t][4 * g + 1], R.o[t][4 * g + 2], R.o[t][4 * g + 3]}, R.M, s);
+  } else {
+    if (h == 0) {
+      sm.m[me][c] = R.M;
+      sm.l[me][c] = s;
+    }
+    __syncthreads();
+    float m = sm.m[rw][c];
+#pragma unroll
+    for (int k = 1; k < KW; ++k) m = fmaxf(m, sm.m[k * RW + rw][c]);
+    const float f = R.M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(R.M - m);
+#pragma unroll
+    for (int t = 0; t < HD / 32; ++t)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *(floatx4*)&sm.o[me][c][32 * t + 8 * g + 4 * h] =
+            floatx4{R.o[t][4 * g] * f, R.o[t][4 * g + 1] * f, R.o[t][4 * g + 2] * f, R.o[t][4 * g + 3] * f};
+    __syncthreads();
+    join_rows<HD, true, 2, RW, KW>(p, w, sm, tid);
+  }
+}
+
+template <int HD, bool QB, int RW>
+struct Wide {
+  static constexpr int KW = 8 / RW, RT = QB ? 2 : 1, D = KW == 1 ? 3 : KW == 2 ? 2 : 1;
+  static constexpr int kRows = RW * RT * 16;
+  static constexpr int kPieces = 8 * HD;                    // 16-byte pieces of a block, keys first
+  static constexpr int kLoads = KW * kPieces / 512;         // of a thread and round
+  static constexpr size_t kRing = 2 * KW * kPieces * 16, kJoin = KW == 1 ? 0 : sizeof(JoinSmem<HD, RT, 8>);
+  static constexpr size_t kSmem = kRing > kJoin ? kRing : kJoin;
+};
+
+template <int HD, bool QB, int RW>
+__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) tree_attend_wide_kernel(TreeAttend p) {
+  using C = Wide<HD, QB, RW>;
+  constexpr int S = HD / 32, RT = C::RT, KW = C::KW, D = C::D, N = C::kLoads;
+  extern __shared__ __align__(16) uint8_t smem_raw[];
+  uint4* ring = reinterpret_cast<uint4*>(smem_raw);  // [2][KW][kPieces]
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), rw = wave % RW, kw = wave / RW;
+  Part w;
+  if (!w.init(p, tid)) return;
+  if (p.NS == 1 && w.rb == 0 && w.n < p.R) zero_rows<HD, QB>(p, w.b, w.kvh, w.n, tid, 512);
+  if (w.rb * C::kRows >= w.rows || w.lo >= w.hi) return;
+  const int r0 = (w.rb * RW + rw) * RT * 16;
+  const bool work = r0 < w.rows;
+  KvLoader<HD> ld;
+  ld.init(p.cache, (int64_t)w.head);
+  std::conditional_t<QB, Rows32<HD>, Rows<HD, QB, RT>> R;
+  R.load(p, w, r0, lane);
+  // piece x of a round: block x / kPieces of it, keys before values
+  auto load = [&](int round, int e) {
+    const int x = e * 512 + wave * 64, blk = w.lo + round * KW + x / C::kPieces, f = x % C::kPieces / 64;
+    return f < 2 * S ? ld.key(blk, f, lane, blk < w.hi) : ld.value(blk, f - 2 * S, lane, blk < w.hi);
+  };
+  uint4 reg[D][N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) ring[e * 512 + tid] = load(0, e);
+#pragma unroll
+  for (int d = 0; d < D; ++d)
+#pragma unroll
+    for (int e = 0; e < N; ++e) reg[d][e] = load(1 + d, e);
+  if (32 * w.hi > w.L && work) R.load_ancestors(p, w, r0, lane, w.kvh == 0 && r0 == 0 && kw == 0 && w.hi == w.nb);
+  const float sl = p.scale * kLog2e;
+  const int rounds = (w.hi - w.lo + KW - 1) / KW;
+  auto round = [&](auto tail, int it, uint4 (&next_regs)[N]) {
+    uint4* next = ring + ((it + 1) & 1) * (KW * C::kPieces);
+#pragma unroll
+    for (int e = 0; e < N; ++e) next[e * 512 + tid] = next_regs[e];
+#pragma unroll
+    for (int e = 0; e < N; ++e) next_regs[e] = load(it + 1 + D, e);
+    const int blk = w.lo + it * KW + kw;
+    if (blk < w.hi && work) {
+      const uint4* here = ring + (it & 1) * (KW * C::kPieces) + kw * C::kPieces;
+      if constexpr (QB) {
+        R.template step<decltype(tail)::value>(blk, w, sl, lane, here);
+      } else {
+        R.template step<decltype(tail)::value>(
+            blk, w, sl, lane, [&](int u, int s) { return here[(u * S + s) * 64 + lane]; },
+            [&](int t) { return here[(2 * S + t) * 64 + lane]; });
+      }
+    }
+    __syncthreads();
+  };
+  __syncthreads();
+  // rounds whose blocks every row sees, D at a time (the registers' turn); the rest with the masks
+  const int full = min(max((w.L / 32 - w.lo) / KW, 0), rounds) / D * D;
+  for (int it = 0; it < full; it += D)
+#pragma unroll
+    for (int d = 0; d < D; ++d) round(std::false_type{}, it + d, reg[d]);
+  for (int it = full; it < rounds; it += D)
+#pragma unroll
+    for (int d = 0; d < D; ++d) {
+      if (it + d >= rounds) break;
+      round(std::true_type{}, it + d, reg[d]);
+    }
+  if (__any(R.broken))
+    for (int e = w.lo + kw; e < w.hi; e += KW)
+      if (32 * e + 32 > w.L) R.mend(ld, e, w, lane);
+  if constexpr (QB) join32<HD, RW, KW>(p, w, R, *reinterpret_cast<JoinSmem32<HD, 8>*>(smem_raw), rw, kw, tid);
+  else join<HD, QB, RT, RW, KW>(p, w, R, *reinterpret_cast<JoinSmem<HD, RT, 8>*>(smem_raw), rw, kw, tid);
 }
 
 // The splits of a row, in order: GR groups of HD / 4 lanes take every GR-th one.
@@ -887,51 +1264,69 @@ hipError_t read_t(TreeRead a, hipStream_t st) {
   return hipGetLastError();
 }
 
-constexpr int kTreeWgs = 1024;  // most workgroups of a call whose keys are split
+// LDS beyond 64 KB has to be asked for, once for every device.
+template <auto KERNEL>
+hipError_t allow_lds(size_t bytes) {
+  if (bytes <= 65536) return hipSuccess;
+  static std::atomic<uint64_t> done{0};
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  const uint64_t bit = 1ull << (dev & 63);
+  if (!(done.load() & bit)) {
+    e = hipFuncSetAttribute(reinterpret_cast<const void*>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e != hipSuccess) return e;
+    done.fetch_or(bit);
+  }
+  return hipSuccess;
+}
 
-template <int HD, bool QB, int RT>
-hipError_t attend_rt(TreeAttend a, hipStream_t st) {
-  const int tiles = (a.G * a.R + 15) / 16;
-  a.RB = (tiles + RT - 1) / RT;
+// rows: packed rows of a workgroup; want: workgroups of one round; step: blocks that a
+// workgroup takes at once
+template <int HD, bool QB, auto KERNEL>
+hipError_t attend_with(TreeAttend a, int rows, int want, int step, int threads, size_t lds, hipStream_t st) {
+  a.RB = (a.G * a.R + rows - 1) / rows;
   const int blocks = (a.max_keys + 31) / 32;
   const int64_t items = (int64_t)a.B * a.KVH * a.RB;
-  const int64_t want = RT == 1 ? 512 : 256;
-  int64_t ns = std::min<int64_t>((a.B > 1 ? 2 : 1) * want / items, (blocks + 2 * kWaves - 1) / (2 * kWaves));
+  int64_t ns = std::min<int64_t>((a.B > 1 ? 2 : 1) * want / items, (blocks + 2 * step - 1) / (2 * step));
   ns = std::max<int64_t>(ns, 1);
   a.CB = (int)((blocks + ns - 1) / ns);
   a.NS = (blocks + a.CB - 1) / a.CB;
   const int64_t units = (int64_t)a.B * a.KVH * a.NS, grid = 8 * a.RB * ((units + 7) / 8);
   if (grid > 0x7fffffff) return hipErrorInvalidValue;
   if (a.NS > 1 && units * a.G * a.R > (int64_t)a.part_rows) return hipErrorInvalidValue;
-  const void* fn = reinterpret_cast<const void*>(&tree_attend_kernel<HD, QB, RT>);
-  constexpr int lds = (int)sizeof(TreeSmem<HD, RT>);
-  if (lds > 65536) {  // once for every device
-    static std::atomic<uint64_t> done{0};
-    int dev = 0;
-    hipError_t e = hipGetDevice(&dev);
-    if (e != hipSuccess) return e;
-    const uint64_t bit = 1ull << (dev & 63);
-    if (!(done.load() & bit)) {
-      if ((e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds)) != hipSuccess) return e;
-      done.fetch_or(bit);
-    }
-  }
-  hipLaunchKernelGGL((tree_attend_kernel<HD, QB, RT>), dim3((unsigned)grid), dim3(kWaves * 64), lds, st, a);
-  const hipError_t e = hipGetLastError();
+  hipError_t e = allow_lds<KERNEL>(lds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(KERNEL, dim3((unsigned)grid), dim3(threads), lds, st, a);
+  e = hipGetLastError();
   if (e != hipSuccess || a.NS == 1) return e;
   constexpr int LPR = HD / 4, per = 256 / LPR;
-  const int64_t rows = (int64_t)a.B * a.H * a.R;
-  if (a.NS >= 8) hipLaunchKernelGGL((tree_merge_kernel<HD, QB, per>), dim3((unsigned)rows), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((tree_merge_kernel<HD, QB, 1>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, st, a);
+  const int64_t out = (int64_t)a.B * a.H * a.R;
+  if (a.NS >= 8) hipLaunchKernelGGL((tree_merge_kernel<HD, QB, per>), dim3((unsigned)out), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((tree_merge_kernel<HD, QB, 1>), dim3((unsigned)((out + per - 1) / per)), dim3(256), 0, st, a);
   return hipGetLastError();
+}
+
+template <int HD, bool QB, int RT>
+hipError_t attend_few(const TreeAttend& a, hipStream_t st) {
+  return attend_with<HD, QB, tree_attend_kernel<HD, QB, RT>>(a, RT * 16, RT == 1 ? 512 : 256, kWaves, kWaves * 64,
+                                                            sizeof(JoinSmem<HD, RT, kWaves>), st);
+}
+template <int HD, bool QB, int RW>
+hipError_t attend_wide(const TreeAttend& a, hipStream_t st) {
+  using C = Wide<HD, QB, RW>;
+  return attend_with<HD, QB, tree_attend_wide_kernel<HD, QB, RW>>(a, C::kRows, 256, C::KW, 512, C::kSmem, st);
 }
 
 template <int HD, bool QB>
 hipError_t attend_t(const TreeAttend& a, hipStream_t st) {
   const int tiles = (a.G * a.R + 15) / 16;
-  if (tiles == 1) return attend_rt<HD, QB, 1>(a, st);
-  if (!QB || tiles == 2) return attend_rt<HD, QB, 2>(a, st);
-  return attend_rt<HD, QB, QB ? 4 : 2>(a, st);
+  if (tiles == 1) return attend_few<HD, QB, 1>(a, st);
+  if (tiles == 2) return attend_few<HD, QB, 2>(a, st);
+  constexpr int RT = QB ? 2 : 1;
+  if (tiles <= 2 * RT) return attend_wide<HD, QB, 2>(a, st);
+  if (tiles <= 4 * RT) return attend_wide<HD, QB, 4>(a, st);
+  return attend_wide<HD, QB, 8>(a, st);
 }
 
 }  // namespace
@@ -946,9 +1341,10 @@ hipError_t launch_tree_read(const TreeRead& a, hipStream_t st) {
   return a.bf16 ? read_t<64, true>(a, st) : read_t<64, false>(a, st);
 }
 
-// (a workgroup of a split call has at most 64 packed rows)
+// (a split call has at most 1024 workgroups of up to 32 packed rows, or 512 of up to 256)
 size_t tree_part_rows(int G, int max_rows) {
-  return (size_t)kTreeWgs * std::min<int64_t>((int64_t)G * max_rows, 64);
+  const int64_t n = (int64_t)G * max_rows;
+  return (size_t)std::max(1024 * std::min<int64_t>(n, 32), 512 * std::min<int64_t>(n, 256));
 }
 
 hipError_t launch_tree_attend(const TreeAttend& a, hipStream_t st) {

@@ -536,9 +536,9 @@ spade_status spade_tree_append(const spade_tree_shape* shape, int layer, void* d
  * [1, max_len] ([R, max_len] without d_rows), or 0 for max_len; a longer request is
  * cut to it and flagged, as by spade_kvq_attend.  scale: in [2^-50, 2^50].  Float32
  * calls keep queries and probabilities in 24 bits, bfloat16 calls the
- * probabilities in 16; scores and sums are float32.  The last bits of a result
- * depend on B, R and max_keys, not on other requests; the same call gives the
- * same bits. */
+ * probabilities in 16; scores and sums are float32.  How the keys are divided
+ * among workgroups follows the lengths of all requests, so the last bits of a result
+ * do too; the same call gives the same bits. */
 spade_status spade_tree_attend(const spade_tree_shape* shape, int layer, const void* d_cache, int B, int R, int dtype,
                                const void* d_q, int64_t q_ld, float scale, const int32_t* d_parents,
                                const int32_t* d_lens, const int32_t* d_rows, int max_keys, void* d_out, int64_t out_ld,

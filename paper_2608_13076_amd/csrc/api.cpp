@@ -316,9 +316,9 @@ TreeCache tree_cache(const spade_tree_shape* s, const void* d_cache, int layer) 
   uint16_t* k = (uint16_t*)const_cast<void*>(d_cache);
   return TreeCache{k + layer * n, k + s->n_layers * n + layer * n, (int64_t)kv_stride_of(s->max_len) * s->head_dim};
 }
-size_t tree_workspace(int G, int hd, int max_rows) {
+size_t tree_workspace(int G, int hd, int max_rows, int batch) {
   const size_t rows = tree_part_rows(G, max_rows);
-  return align256(rows * hd * 4) + align256(rows * 2 * 4);
+  return align256(rows * hd * 4) + align256(rows * 2 * 4) + align256(((size_t)batch + 1) * 4);
 }
 
 size_t kvq_layer_bytes(const spade_kvq_shape* s) {
@@ -1200,7 +1200,7 @@ size_t spade_tree_workspace_bytes(const spade_tree_shape* s, int max_rows) {
     fail(SPADE_ECAPACITY, "max_rows must be in [1, %d]", kTreeMaxRows);
     return 0;
   }
-  return tree_workspace(s->n_heads / s->n_kv_heads, s->head_dim, max_rows);
+  return tree_workspace(s->n_heads / s->n_kv_heads, s->head_dim, max_rows, s->batch);
 }
 
 spade_status spade_tree_append(const spade_tree_shape* s, int layer, void* d_cache, int B, int R, int dtype,
@@ -1313,7 +1313,7 @@ spade_status spade_tree_attend(const spade_tree_shape* s, int layer, const void*
   if (max_keys < least || max_keys > s->max_len)
     return fail(SPADE_ECAPACITY, "max_keys %d must be in [%d, %d]", max_keys, least, s->max_len);
   const int G = s->n_heads / s->n_kv_heads;
-  if (tree_workspace(G, hd, R) > workspace_bytes)
+  if (tree_workspace(G, hd, R, B) > workspace_bytes)
     return fail(SPADE_ECAPACITY, "workspace of %zu bytes is too small", workspace_bytes);
   const int64_t e = dtype == SPADE_F32 ? 4 : 2, nq = s->n_heads * hd * e;
   if (rows_overlap(d_q, nq, q_ld * e, d_out, nq, out_ld * e, (int64_t)B * R)) return fail(SPADE_EINVAL, "q and out overlap");
@@ -1338,6 +1338,7 @@ spade_status spade_tree_attend(const spade_tree_shape* s, int layer, const void*
   a.part_rows = tree_part_rows(G, R);
   a.part_o = (float*)d_workspace;
   a.part_ml = (float*)((uint8_t*)d_workspace + align256(a.part_rows * hd * 4));
+  a.plan = (int32_t*)((uint8_t*)a.part_ml + align256(a.part_rows * 2 * 4));
   a.err = d_err;
   const hipError_t r2 = launch_tree_attend(a, (hipStream_t)stream);
   if (r2 != hipSuccess) return hipfail(r2, "tree_attend");

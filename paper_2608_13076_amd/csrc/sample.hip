@@ -20,6 +20,7 @@
 #include <algorithm>
 
 #include "device_accept.h"
+#include "device_lanes.h"
 
 namespace spade {
 
@@ -211,68 +212,13 @@ __device__ __forceinline__ float load1(const SampleArgs& a, int row, int v) {
   return x != x ? -INFINITY : fminf(x, FLT_MAX);
 }
 
-// Values of other lanes by data-parallel moves, which cost an instruction where a
-// shuffle goes through the LDS.  After the six steps of a reduction (or inclusive
-// prefix: 1, 2, 4 and 8 lanes down within a row of sixteen, then a row's last lane to
-// the next row, lane 31 to the upper half) the last lane has the whole.
-template <int STEP>
-__device__ __forceinline__ uint32_t lane_step(uint32_t v, uint32_t none) {
-  constexpr int ctrl = STEP < 4 ? 0x110 + (1 << STEP) : STEP == 4 ? 0x142 : 0x143;
-  constexpr int rows = STEP < 4 ? 0xf : STEP == 4 ? 0xa : 0xc;
-  return (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)v, ctrl, rows, 0xf, false);
-}
-template <int STEP>
-__device__ __forceinline__ uint64_t lane_step(uint64_t v, uint64_t none) {
-  return (uint64_t)lane_step<STEP>((uint32_t)(v >> 32), (uint32_t)(none >> 32)) << 32 | lane_step<STEP>((uint32_t)v, (uint32_t)none);
-}
-template <int STEP>
-__device__ __forceinline__ double lane_step(double v, double none) {
-  return __longlong_as_double((long long)lane_step<STEP>((uint64_t)__double_as_longlong(v), (uint64_t)__double_as_longlong(none)));
-}
-template <int STEP>
-__device__ __forceinline__ float lane_step(float v, float none) {
-  return __uint_as_float(lane_step<STEP>(__float_as_uint(v), __float_as_uint(none)));
-}
-template <int STEP>
-__device__ __forceinline__ int lane_step(int v, int none) {
-  return (int)lane_step<STEP>((uint32_t)v, (uint32_t)none);
-}
-// v of lane l, the same for all
-__device__ __forceinline__ uint32_t lane_of(uint32_t v, int l) { return (uint32_t)__builtin_amdgcn_readlane((int)v, l); }
-__device__ __forceinline__ int lane_of(int v, int l) { return __builtin_amdgcn_readlane(v, l); }
-__device__ __forceinline__ float lane_of(float v, int l) { return __uint_as_float(lane_of(__float_as_uint(v), l)); }
-__device__ __forceinline__ uint64_t lane_of(uint64_t v, int l) {
-  return (uint64_t)lane_of((uint32_t)(v >> 32), l) << 32 | lane_of((uint32_t)v, l);
-}
-__device__ __forceinline__ double lane_of(double v, int l) {
-  return __longlong_as_double((long long)lane_of((uint64_t)__double_as_longlong(v), l));
-}
-template <typename T, typename F>
-__device__ __forceinline__ T all_steps(T v, F f) {
-  v = f(v, lane_step<0>(v, v));
-  v = f(v, lane_step<1>(v, v));
-  v = f(v, lane_step<2>(v, v));
-  v = f(v, lane_step<3>(v, v));
-  v = f(v, lane_step<4>(v, v));
-  return f(v, lane_step<5>(v, v));
-}
 __device__ __forceinline__ float wave_max(float v) {
-  return lane_of(all_steps(v, [](float x, float y) { return fmaxf(x, y); }), 63);
+  return from_lane(all_lanes(v, [](float x, float y) { return fmaxf(x, y); }), 63);
 }
 __device__ __forceinline__ int wave_min(int v) {
-  return lane_of(all_steps(v, [](int x, int y) { return min(x, y); }), 63);
+  return from_lane(all_lanes(v, [](int x, int y) { return min(x, y); }), 63);
 }
-// inclusive prefix sums
-template <typename T>
-__device__ __forceinline__ T wave_prefix(T v) {
-  v += lane_step<0>(v, (T)0);
-  v += lane_step<1>(v, (T)0);
-  v += lane_step<2>(v, (T)0);
-  v += lane_step<3>(v, (T)0);
-  v += lane_step<4>(v, (T)0);
-  return v + lane_step<5>(v, (T)0);
-}
-__device__ __forceinline__ double wave_sum(double v) { return lane_of(wave_prefix(v), 63); }
+__device__ __forceinline__ double wave_sum(double v) { return from_lane(prefix_sum(v), 63); }
 
 struct Draw {
   double s;
@@ -280,12 +226,12 @@ struct Draw {
 };
 __device__ __forceinline__ Draw better_draw(Draw x, Draw y) { return y.s > x.s || (y.s == x.s && y.id < x.id) ? y : x; }
 template <int STEP>
-__device__ __forceinline__ Draw lane_step(Draw v, Draw) {
-  return Draw{lane_step<STEP>(v.s, v.s), lane_step<STEP>(v.id, v.id)};
+__device__ __forceinline__ Draw prefix_step(Draw v, Draw) {
+  return Draw{prefix_step<STEP>(v.s, v.s), prefix_step<STEP>(v.id, v.id)};
 }
 __device__ __forceinline__ Draw wave_draw(Draw v) {
-  v = all_steps(v, [](Draw x, Draw y) { return better_draw(x, y); });
-  return Draw{lane_of(v.s, 63), lane_of(v.id, 63)};
+  v = all_lanes(v, [](Draw x, Draw y) { return better_draw(x, y); });
+  return Draw{from_lane(v.s, 63), from_lane(v.id, 63)};
 }
 
 // The draw as a race: argmax(G - d) is the token with the least e = -log(U) exp(d).
@@ -338,7 +284,7 @@ struct Race {
   }
   // the lanes' bounds to all (all lanes of the wave call it)
   __device__ __forceinline__ void share() {
-    bound = lane_of(all_steps(bound, [](float a, float b) { return fminf(a, b); }), 63);
+    bound = from_lane(all_lanes(bound, [](float a, float b) { return fminf(a, b); }), 63);
   }
   // the wave's token
   __device__ __forceinline__ Draw best() {
@@ -523,27 +469,27 @@ __global__ void __launch_bounds__(kThreads) sample_scan_kernel(SampleArgs a) {
         w[e] = (double)(sm.mass[0][b] + sm.mass[1][b]) * 0x1p-38 * sm.factor[b];
         c[e] = (int)(sm.cnt[0][b] + sm.cnt[1][b]);
       }
-      const double sw = wave_prefix(w[0] + w[1]);
-      const int sc = wave_prefix(c[0] + c[1]);
+      const double sw = prefix_sum(w[0] + w[1]);
+      const int sc = prefix_sum(c[0] + c[1]);
       wi[1] = sw;
       wi[0] = sw - w[1];
       ci[1] = sc;
       ci[0] = sc - c[1];
-      const double total = lane_of(sw, 63);
+      const double total = from_lane(sw, 63);
       // the first bin with f, and the counts and weights before it
       auto first = [&](bool f0, bool f1) {
         const uint64_t hit = __ballot(f0 || f1);
         if (hit == 0) return kSampleBins - 1;
         const int l = __ffsll((unsigned long long)hit) - 1;
-        return 2 * l + (lane_of((int)f0, l) ? 0 : 1);
+        return 2 * l + (from_lane((int)f0, l) ? 0 : 1);
       };
       int k_bin = kSampleBins - 1, k_in = 0;
       double least = total, most = total;  // of the weight that top_p refers to
-      if (q.use_k && lane_of(ci[1], 63) > q.top_k) {  // (else all are among the first top_k)
+      if (q.use_k && from_lane(ci[1], 63) > q.top_k) {  // (else all are among the first top_k)
         k_in = 1;
         k_bin = first(ci[0] >= q.top_k, ci[1] >= q.top_k);
-        most = lane_of(k_bin & 1 ? wi[1] : wi[0], k_bin >> 1);
-        least = most - lane_of(k_bin & 1 ? w[1] : w[0], k_bin >> 1);
+        most = from_lane(k_bin & 1 ? wi[1] : wi[0], k_bin >> 1);
+        least = most - from_lane(k_bin & 1 ? w[1] : w[0], k_bin >> 1);
       }
       lo = hi = k_bin;
       if (q.use_p) {
@@ -553,8 +499,8 @@ __global__ void __launch_bounds__(kThreads) sample_scan_kernel(SampleArgs a) {
         hi = min(hi, first(wi[0] >= t1, wi[1] >= t1));
         if (k_in) hi = k_bin;  // the first top_k tokens' weight ends there
       }
-      const double in = lane_of(lo & 1 ? wi[1] : wi[0], lo >> 1), ex = in - lane_of(lo & 1 ? w[1] : w[0], lo >> 1);
-      const int above = lane_of(lo & 1 ? ci[1] : ci[0], lo >> 1) - lane_of(lo & 1 ? c[1] : c[0], lo >> 1);
+      const double in = from_lane(lo & 1 ? wi[1] : wi[0], lo >> 1), ex = in - from_lane(lo & 1 ? w[1] : w[0], lo >> 1);
+      const int above = from_lane(lo & 1 ? ci[1] : ci[0], lo >> 1) - from_lane(lo & 1 ? c[1] : c[0], lo >> 1);
       if (lane == 0) {
         sm.row.mass = lo == 0 ? 0.0 : ex;
         sm.row.total = total;
@@ -626,10 +572,10 @@ __global__ void __launch_bounds__(kThreads) sample_scan_kernel(SampleArgs a) {
     race.share();
     if (__any(listed != 0)) {
       const int n = __popc(listed);
-      const int in = wave_prefix(n);
+      const int in = prefix_sum(n);
       uint32_t at = 0;
       if (lane == 63) at = atomicAdd(a.count + row, (uint32_t)in);
-      at = lane_of(at, 63) + (uint32_t)(in - n);
+      at = from_lane(at, 63) + (uint32_t)(in - n);
 #pragma unroll
       for (int k = 0; k < 16; ++k)
         if (listed >> k & 1u) {
@@ -737,7 +683,7 @@ __device__ __forceinline__ bool find_digit(FinishSmem& sm, int tid, int& turn, u
       v[e] = MASS ? sm.mass[now][b] : (uint64_t)sm.cnt[now][b];
       s += v[e];
     }
-    const uint64_t in = wave_prefix(s);
+    const uint64_t in = prefix_sum(s);
     const uint64_t hit = __ballot(in >= target);
     if (hit == 0) {
       if (tid == 0) sm.digit = -1;
@@ -843,8 +789,8 @@ __device__ __forceinline__ void finish_list(const L& ls, FinishSmem& sm, int tid
     sm.mass[0][tid] = 0;
   }
   __syncthreads();
-  lo = lane_of(all_steps(lo, [](uint32_t x, uint32_t y) { return min(x, y); }), 63);
-  hi = lane_of(all_steps(hi, [](uint32_t x, uint32_t y) { return max(x, y); }), 63);
+  lo = from_lane(all_lanes(lo, [](uint32_t x, uint32_t y) { return min(x, y); }), 63);
+  hi = from_lane(all_lanes(hi, [](uint32_t x, uint32_t y) { return max(x, y); }), 63);
   if ((tid & 63) == 0 && lo <= hi) {
     atomicMin(&sm.key_lo, lo);
     atomicMax(&sm.key_hi, hi);

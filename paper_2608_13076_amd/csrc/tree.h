@@ -66,14 +66,15 @@ struct TreeAttend {
   int max_keys;
   void* out;
   int64_t out_ld;
-  float* part_o;      // [(request, K/V head, split)][G R][hd]
+  float* part_o;      // [request, K/V head, split, packed row][hd]
   float* part_ml;     // ... [2]
+  int32_t* plan;      // [B + 1] blocks of 32 positions of a split; a request's first row in part_o
   size_t part_rows;   // rows that part_o holds
   uint32_t* err;
   // set by the launcher
-  int RB;  // workgroups over the packed rows of a K/V head
-  int NS;  // splits of the keys
-  int CB;  // blocks of 32 positions of a split
+  int tile;  // packed rows of a workgroup
+  int RB;    // workgroups over the packed rows of a K/V head
+  int WG;    // 0: a workgroup takes all keys; else most workgroups of a call whose keys are split
 };
 // rows of part_o that any call of up to max_rows rows needs
 size_t tree_part_rows(int G, int max_rows);

@@ -14,7 +14,7 @@
 #include <atomic>
 #include <type_traits>
 
-#include "device_util.h"
+#include "device_lanes.h"
 
 namespace spade {
 
@@ -388,27 +388,90 @@ __device__ __forceinline__ void zero_rows(const TreeAttend& p, int b, int kvh, i
   }
 }
 
-// Which part of the call a workgroup has.  Workgroup i runs on XCD i % 8: those
-// that read the same keys for other rows follow each other there and share its L2.
+// Which part of the call a workgroup has.
+//
+// With keys enough and few heads the keys are split: the workgroups, WG at most (one
+// round), have equal counts of blocks of 32 positions whatever the requests' lengths.
+// The count follows from all of them: the least CB for which the splits of all heads and
+// tiles of rows fit (kLeast at least, two rounds of a wave).  Every wave works it out
+// from the lengths, the first workgroup leaves it for the merge.
+constexpr int kLeast = 8;
 struct Part {
-  unsigned unit, head;
+  unsigned head;
   int b, kvh, rb, L, n, rows, nb, lo, hi;
-  __device__ __forceinline__ bool init(const TreeAttend& p, int tid) {
-    const unsigned xcd = blockIdx.x & 7, jj = blockIdx.x >> 3, tt = jj / (unsigned)p.RB;
-    rb = (int)(jj - tt * p.RB);
-    unit = 8 * tt + xcd;
-    if (unit >= (unsigned)(p.B * p.KVH * p.NS)) return false;
-    head = unit / (unsigned)p.NS;
-    const int split = (int)(unit - head * p.NS);
-    b = (int)(head / (unsigned)p.KVH);
-    kvh = (int)(head - (unsigned)b * p.KVH);
-    const TreeRows rr = tree_rows(p, b, split == 0 && rb == 0 && kvh == 0 && tid == 0);
+  int part;  // the first row of the split's part in part_o
+  __device__ __forceinline__ void request(const TreeAttend& p, int tid) {
+    head = (unsigned)(b * p.KVH + kvh);
+    const TreeRows rr = tree_rows(p, b, rb == 0 && kvh == 0 && lo == 0 && tid == 0);
     L = rr.L;
     n = rr.n;
     rows = p.G * n;
     nb = (L + n + 31) / 32;
-    lo = split * p.CB;
-    hi = min(nb, lo + p.CB);
+  }
+  // false: nothing to do
+  __device__ __forceinline__ bool init(const TreeAttend& p, int tid) {
+    lo = part = 0;
+    if (p.WG == 0) {
+      // Workgroup i runs on XCD i % 8: those that read the same keys for other rows
+      // follow each other there and share its L2.
+      const unsigned xcd = blockIdx.x & 7, jj = blockIdx.x >> 3, tt = jj / (unsigned)p.RB, unit = 8 * tt + xcd;
+      rb = (int)(jj - tt * p.RB);
+      if (unit >= (unsigned)(p.B * p.KVH)) return false;
+      b = (int)(unit / (unsigned)p.KVH);
+      kvh = (int)(unit - (unsigned)b * p.KVH);
+      request(p, tid);
+      hi = nb;
+      return true;
+    }
+    const int lane = tid & 63, want = (int)blockIdx.x;
+    // a request's blocks, tiles and packed rows
+    struct One { int nb, tiles, rows; };
+    auto one = [&](int r) {
+      One x{0, 0, 0};
+      if (r < p.B) {
+        const TreeRows rr = tree_rows(p, r, false);
+        x.nb = rr.n > 0 ? (rr.L + rr.n + 31) / 32 : 0;
+        x.rows = p.G * rr.n;
+        x.tiles = (x.rows + p.tile - 1) / p.tile;
+      }
+      return x;
+    };
+    const One first = one(lane);
+    auto total = [&](auto f) {
+      int s = prefix_sum(f(first));
+      for (int r0 = 64; r0 < p.B; r0 += 64) s += prefix_sum(f(one(r0 + lane)));
+      return from_lane(s, 63);
+    };
+    int cb = max(kLeast, (total([&](One x) { return p.KVH * x.tiles * x.nb; }) + p.WG - 1) / p.WG);
+    auto units = [&](One x) { return p.KVH * x.tiles * ((x.nb + cb - 1) / cb); };
+    while (total(units) > p.WG) cb += max(1, cb >> 3);
+    if (want == 0 && tid == 0) p.plan[0] = cb;
+    int before = 0, row = 0;
+    bool found = false;
+    for (int r0 = 0; r0 < p.B; r0 += 64) {
+      const One x = r0 == 0 ? first : one(r0 + lane);
+      const int u = units(x), iu = before + prefix_sum(u);
+      const int pr = p.KVH * ((x.nb + cb - 1) / cb) * x.rows, ir = row + prefix_sum(pr);
+      if (want == 0 && tid < 64 && r0 + lane < p.B) p.plan[1 + r0 + lane] = ir - pr;
+      const uint64_t hit = __ballot(iu > want);
+      if (hit != 0 && !found) {
+        const int l = __ffsll((unsigned long long)hit) - 1;
+        found = true;
+        b = r0 + l;
+        const int at = want - from_lane(iu - u, l), ns = (from_lane(x.nb, l) + cb - 1) / cb;
+        const int h = at / ns, split = at - h * ns;
+        rb = h / p.KVH;
+        kvh = h - rb * p.KVH;
+        lo = split * cb;
+        part = from_lane(ir - pr, l) + (kvh * ns + split) * from_lane(x.rows, l);
+        if (want != 0) break;
+      }
+      before = from_lane(iu, 63);
+      row = from_lane(ir, 63);
+    }
+    if (!found) return false;
+    request(p, tid);
+    hi = min(nb, lo + cb);
     return true;
   }
 };
@@ -643,12 +706,12 @@ struct Rows {
 // reference mx and sum s.
 template <int HD, bool QB>
 __device__ __forceinline__ void put(const TreeAttend& p, const Part& w, int m, int f, floatx4 x, float mx, float s) {
-  if (p.NS == 1) {
+  if (p.WG == 0) {
     const int g = m / w.n, i = m - g * w.n;
     const float y[4] = {x[0] / s, x[1] / s, x[2] / s, x[3] / s};
     store4<QB>(p.out, ((int64_t)w.b * p.R + i) * p.out_ld + ((int64_t)w.kvh * p.G + g) * HD + f, y);
   } else {
-    const int64_t at = (int64_t)w.unit * p.G * p.R + m;
+    const int64_t at = (int64_t)w.part + m;
     *(floatx4*)(p.part_o + at * HD + f) = x;
     if (f == 0) {
       p.part_ml[2 * at] = mx;
@@ -737,7 +800,7 @@ tree_attend_kernel(TreeAttend p) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   Part w;
   if (!w.init(p, tid)) return;
-  if (p.NS == 1 && w.rb == 0 && w.n < p.R) zero_rows<HD, QB>(p, w.b, w.kvh, w.n, tid, kWaves * 64);
+  if (p.WG == 0 && w.rb == 0 && w.n < p.R) zero_rows<HD, QB>(p, w.b, w.kvh, w.n, tid, kWaves * 64);
   const int r0 = w.rb * RT * 16;
   if (r0 >= w.rows || w.lo >= w.hi) return;
   KvLoader<HD> ld;
@@ -999,27 +1062,30 @@ __device__ __forceinline__ void join32(const TreeAttend& p, const Part& w, Rows3
   }
 }
 
-template <int HD, bool QB, int RW>
+template <int HD, bool QB, int RW, int W>
 struct Wide {
-  static constexpr int KW = 8 / RW, RT = QB ? 2 : 1, D = KW == 1 ? 3 : KW == 2 ? 2 : 1;
+  static constexpr int KW = W / RW, RT = QB ? 2 : 1, kThreads = W * 64;
   static constexpr int kRows = RW * RT * 16;
   static constexpr int kPieces = 8 * HD;                    // 16-byte pieces of a block, keys first
-  static constexpr int kLoads = KW * kPieces / 512;         // of a thread and round
-  static constexpr size_t kRing = 2 * KW * kPieces * 16, kJoin = KW == 1 ? 0 : sizeof(JoinSmem<HD, RT, 8>);
+  static constexpr int kLoads = KW * kPieces / kThreads;    // of a thread and round
+  static constexpr int D = kLoads >= 8 ? 1 : kLoads >= 4 ? 2 : 3;
+  static constexpr size_t kRing = 2 * KW * kPieces * 16, kJoin = KW == 1 ? 0 : sizeof(JoinSmem<HD, RT, W>);
   static constexpr size_t kSmem = kRing > kJoin ? kRing : kJoin;
 };
 
-template <int HD, bool QB, int RW>
-__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) tree_attend_wide_kernel(TreeAttend p) {
-  using C = Wide<HD, QB, RW>;
-  constexpr int S = HD / 32, RT = C::RT, KW = C::KW, D = C::D, N = C::kLoads;
+template <int HD, bool QB, int RW, int W>
+__global__ void __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(2))) tree_attend_wide_kernel(TreeAttend p) {
+  using C = Wide<HD, QB, RW, W>;
+  constexpr int S = HD / 32, RT = C::RT, KW = C::KW, D = C::D, N = C::kLoads, T = C::kThreads;
   extern __shared__ __align__(16) uint8_t smem_raw[];
   uint4* ring = reinterpret_cast<uint4*>(smem_raw);  // [2][KW][kPieces]
   const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), rw = wave % RW, kw = wave / RW;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // (wave i runs on SIMD i % 4: the waves of the first rows, which every request has, are spread)
+  const int rw = KW == 2 ? (wave & 1) + 2 * (wave >> 2) : wave / KW, kw = KW == 2 ? wave >> 1 & 1 : wave % KW;
   Part w;
   if (!w.init(p, tid)) return;
-  if (p.NS == 1 && w.rb == 0 && w.n < p.R) zero_rows<HD, QB>(p, w.b, w.kvh, w.n, tid, 512);
+  if (p.WG == 0 && w.rb == 0 && w.n < p.R) zero_rows<HD, QB>(p, w.b, w.kvh, w.n, tid, T);
   if (w.rb * C::kRows >= w.rows || w.lo >= w.hi) return;
   const int r0 = (w.rb * RW + rw) * RT * 16;
   const bool work = r0 < w.rows;
@@ -1027,14 +1093,24 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) t
   ld.init(p.cache, (int64_t)w.head);
   std::conditional_t<QB, Rows32<HD>, Rows<HD, QB, RT>> R;
   R.load(p, w, r0, lane);
-  // piece x of a round: block x / kPieces of it, keys before values
+  // Piece e T + tid of a round: of block e T / kPieces of it, keys before values.  Which of them
+  // follows from e or (T pieces are a whole block) from the wave: no load is under a branch, or
+  // the wait for one would be a wait for all.
+  const bool keys = wave < 2 * S;
+  const Rsrc mine = keys ? ld.k : ld.v;
   auto load = [&](int round, int e) {
-    const int x = e * 512 + wave * 64, blk = w.lo + round * KW + x / C::kPieces, f = x % C::kPieces / 64;
-    return f < 2 * S ? ld.key(blk, f, lane, blk < w.hi) : ld.value(blk, f - 2 * S, lane, blk < w.hi);
+    const int blk = w.lo + round * KW + e * T / C::kPieces, f0 = e * T % C::kPieces / 64;
+    const bool there = blk < w.hi;
+    if (f0 + W <= 2 * S) return ld.key(blk, f0 + wave, lane, there);
+    if (f0 >= 2 * S) return ld.value(blk, f0 + wave - 2 * S, lane, there);
+    const uint32_t ko = (uint32_t)blk * (64 * HD) + wave * 1024,
+                   vo = (uint32_t)(blk >> 3) * (512 * HD) + (uint32_t)(blk & 7) * 1024 + (wave - 2 * S) * 8192;
+    return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(mine, (int)(there ? 16u * lane : kOob),
+                                                                           (int)(there ? (keys ? ko : vo) : 0u), 0));
   };
   uint4 reg[D][N];
 #pragma unroll
-  for (int e = 0; e < N; ++e) ring[e * 512 + tid] = load(0, e);
+  for (int e = 0; e < N; ++e) ring[e * T + tid] = load(0, e);
 #pragma unroll
   for (int d = 0; d < D; ++d)
 #pragma unroll
@@ -1045,7 +1121,7 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) t
   auto round = [&](auto tail, int it, uint4 (&next_regs)[N]) {
     uint4* next = ring + ((it + 1) & 1) * (KW * C::kPieces);
 #pragma unroll
-    for (int e = 0; e < N; ++e) next[e * 512 + tid] = next_regs[e];
+    for (int e = 0; e < N; ++e) next[e * T + tid] = next_regs[e];
 #pragma unroll
     for (int e = 0; e < N; ++e) next_regs[e] = load(it + 1 + D, e);
     const int blk = w.lo + it * KW + kw;
@@ -1076,8 +1152,8 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) t
   if (__any(R.broken))
     for (int e = w.lo + kw; e < w.hi; e += KW)
       if (32 * e + 32 > w.L) R.mend(ld, e, w, lane);
-  if constexpr (QB) join32<HD, RW, KW>(p, w, R, *reinterpret_cast<JoinSmem32<HD, 8>*>(smem_raw), rw, kw, tid);
-  else join<HD, QB, RT, RW, KW>(p, w, R, *reinterpret_cast<JoinSmem<HD, RT, 8>*>(smem_raw), rw, kw, tid);
+  if constexpr (QB) join32<HD, RW, KW>(p, w, R, *reinterpret_cast<JoinSmem32<HD, W>*>(smem_raw), rw, kw, tid);
+  else join<HD, QB, RT, RW, KW>(p, w, R, *reinterpret_cast<JoinSmem<HD, RT, W>*>(smem_raw), rw, kw, tid);
 }
 
 // The splits of a row, in order: GR groups of HD / 4 lanes take every GR-th one.
@@ -1094,8 +1170,8 @@ __global__ void __launch_bounds__(256) tree_merge_kernel(TreeAttend p) {
   const int b = (int)(bh / p.KVH), kvh = (int)(bh - (int64_t)b * p.KVH);
   const TreeRows rr = tree_rows(p, b, false);
   const bool used = live && i < rr.n;
-  const int nb = (rr.L + rr.n + 31) / 32, ns = used ? (nb + p.CB - 1) / p.CB : 0;
-  const int64_t at0 = bh * p.NS * p.G * p.R + (int64_t)g * rr.n + i, step = (int64_t)p.G * p.R;
+  const int cb = p.plan[0], ns = used ? ((rr.L + rr.n + 31) / 32 + cb - 1) / cb : 0;
+  const int64_t step = (int64_t)p.G * rr.n, at0 = p.plan[1 + b] + (int64_t)kvh * ns * step + g * rr.n + i;
   float m = -INFINITY, s = 0.f;
   floatx4 x = {0.f, 0.f, 0.f, 0.f};
   constexpr int U = 4;
@@ -1281,41 +1357,39 @@ hipError_t allow_lds(size_t bytes) {
   return hipSuccess;
 }
 
-// rows: packed rows of a workgroup; want: workgroups of one round; step: blocks that a
-// workgroup takes at once
+// tile: packed rows of a workgroup; wgs: workgroups of one round
 template <int HD, bool QB, auto KERNEL>
-hipError_t attend_with(TreeAttend a, int rows, int want, int step, int threads, size_t lds, hipStream_t st) {
-  a.RB = (a.G * a.R + rows - 1) / rows;
-  const int blocks = (a.max_keys + 31) / 32;
-  const int64_t items = (int64_t)a.B * a.KVH * a.RB;
-  int64_t ns = std::min<int64_t>((a.B > 1 ? 2 : 1) * want / items, (blocks + 2 * step - 1) / (2 * step));
-  ns = std::max<int64_t>(ns, 1);
-  a.CB = (int)((blocks + ns - 1) / ns);
-  a.NS = (blocks + a.CB - 1) / a.CB;
-  const int64_t units = (int64_t)a.B * a.KVH * a.NS, grid = 8 * a.RB * ((units + 7) / 8);
+hipError_t attend_with(TreeAttend a, int tile, int wgs, int threads, size_t lds, hipStream_t st) {
+  a.tile = tile;
+  a.RB = (a.G * a.R + tile - 1) / tile;
+  const int64_t heads = (int64_t)a.B * a.KVH;
+  a.WG = (a.max_keys + 31) / 32 > kLeast && heads * a.RB < wgs ? wgs : 0;
+  const int64_t grid = a.WG > 0 ? a.WG : 8 * a.RB * ((heads + 7) / 8);
   if (grid > 0x7fffffff) return hipErrorInvalidValue;
-  if (a.NS > 1 && units * a.G * a.R > (int64_t)a.part_rows) return hipErrorInvalidValue;
+  // (a split's part has the rows of its workgroups)
+  if (a.WG > 0 && std::min<int64_t>((int64_t)wgs * tile, (int64_t)wgs * a.G * a.R) > (int64_t)a.part_rows) return hipErrorInvalidValue;
   hipError_t e = allow_lds<KERNEL>(lds);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(KERNEL, dim3((unsigned)grid), dim3(threads), lds, st, a);
   e = hipGetLastError();
-  if (e != hipSuccess || a.NS == 1) return e;
+  if (e != hipSuccess || a.WG == 0) return e;
   constexpr int LPR = HD / 4, per = 256 / LPR;
   const int64_t out = (int64_t)a.B * a.H * a.R;
-  if (a.NS >= 8) hipLaunchKernelGGL((tree_merge_kernel<HD, QB, per>), dim3((unsigned)out), dim3(256), 0, st, a);
+  // (about wgs / heads splits of a row)
+  if (wgs >= 8 * heads * a.RB) hipLaunchKernelGGL((tree_merge_kernel<HD, QB, per>), dim3((unsigned)out), dim3(256), 0, st, a);
   else hipLaunchKernelGGL((tree_merge_kernel<HD, QB, 1>), dim3((unsigned)((out + per - 1) / per)), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
 template <int HD, bool QB, int RT>
 hipError_t attend_few(const TreeAttend& a, hipStream_t st) {
-  return attend_with<HD, QB, tree_attend_kernel<HD, QB, RT>>(a, RT * 16, RT == 1 ? 512 : 256, kWaves, kWaves * 64,
+  return attend_with<HD, QB, tree_attend_kernel<HD, QB, RT>>(a, RT * 16, RT == 1 ? 512 : 256, kWaves * 64,
                                                             sizeof(JoinSmem<HD, RT, kWaves>), st);
 }
-template <int HD, bool QB, int RW>
+template <int HD, bool QB, int RW, int W>
 hipError_t attend_wide(const TreeAttend& a, hipStream_t st) {
-  using C = Wide<HD, QB, RW>;
-  return attend_with<HD, QB, tree_attend_wide_kernel<HD, QB, RW>>(a, C::kRows, 256, C::KW, 512, C::kSmem, st);
+  using C = Wide<HD, QB, RW, W>;
+  return attend_with<HD, QB, tree_attend_wide_kernel<HD, QB, RW, W>>(a, C::kRows, 2048 / W, C::kThreads, C::kSmem, st);
 }
 
 template <int HD, bool QB>
@@ -1324,9 +1398,9 @@ hipError_t attend_t(const TreeAttend& a, hipStream_t st) {
   if (tiles == 1) return attend_few<HD, QB, 1>(a, st);
   if (tiles == 2) return attend_few<HD, QB, 2>(a, st);
   constexpr int RT = QB ? 2 : 1;
-  if (tiles <= 2 * RT) return attend_wide<HD, QB, 2>(a, st);
-  if (tiles <= 4 * RT) return attend_wide<HD, QB, 4>(a, st);
-  return attend_wide<HD, QB, 8>(a, st);
+  if (tiles <= 2 * RT) return attend_wide<HD, QB, 2, 8>(a, st);
+  if (tiles <= 4 * RT) return attend_wide<HD, QB, 4, 4>(a, st);
+  return attend_wide<HD, QB, 8, 8>(a, st);
 }
 
 }  // namespace
@@ -1341,10 +1415,10 @@ hipError_t launch_tree_read(const TreeRead& a, hipStream_t st) {
   return a.bf16 ? read_t<64, true>(a, st) : read_t<64, false>(a, st);
 }
 
-// (a split call has at most 1024 workgroups of up to 32 packed rows, or 512 of up to 256)
+// (workgroups of a split call times their rows: 512 of 16 or 128, 256 of up to 256)
 size_t tree_part_rows(int G, int max_rows) {
   const int64_t n = (int64_t)G * max_rows;
-  return (size_t)std::max(1024 * std::min<int64_t>(n, 32), 512 * std::min<int64_t>(n, 256));
+  return (size_t)std::max(512 * std::min<int64_t>(n, 128), 256 * std::min<int64_t>(n, 256));
 }
 
 hipError_t launch_tree_attend(const TreeAttend& a, hipStream_t st) {

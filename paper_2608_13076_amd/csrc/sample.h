@@ -24,6 +24,13 @@ struct SampleRow {
   uint32_t key, id;            // and the token comes no later than this one
 };
 
+// A token of the draw.
+struct SampleDraw {
+  double s;  // its score
+  int id;
+  double d;  // its distance from the largest logit
+};
+
 struct SampleArgs {
   int rows, V, bf16;
   const void* logits;
@@ -44,9 +51,8 @@ struct SampleArgs {
   float* smax;          // [rows][NS] largest logit of a slice
   int32_t* sarg;        // ... its lowest token (greedy rows)
   uint64_t* hist;       // [rows][NS][kSampleBins] count and weight
-  double* best;         // [rows][NS] best score of a part (or slice), its token, the weight of its kept tokens
-  int32_t* best_id;
-  double* sum;
+  SampleDraw* best;     // [rows][NS] of a part (or slice)
+  double* sum;          // ... the weight of its kept tokens
   SampleRow* row;       // [rows]
   uint32_t* count;      // [rows] listed tokens
   uint2* list;          // [rows][kSampleList] token and logit

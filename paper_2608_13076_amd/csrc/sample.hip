@@ -24,6 +24,11 @@
 
 namespace spade {
 
+template <int STEP>
+__device__ __forceinline__ SampleDraw prefix_step(SampleDraw v, SampleDraw) {
+  return SampleDraw{prefix_step<STEP>(v.s, v.s), prefix_step<STEP>(v.id, v.id), prefix_step<STEP>(v.d, v.d)};
+}
+
 namespace {
 
 constexpr int kThreads = 256;
@@ -154,6 +159,11 @@ __device__ __forceinline__ uint32_t key_of(float l) {
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
+// a key's logit
+__device__ __forceinline__ float logit_of(uint32_t key) {
+  return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
+}
+
 // The thread's 16 tokens of a slice: NaN (flagged) and tokens past the end as -inf,
 // infinity as the largest number.
 template <bool BF16>
@@ -220,45 +230,41 @@ __device__ __forceinline__ int wave_min(int v) {
 }
 __device__ __forceinline__ double wave_sum(double v) { return from_lane(prefix_sum(v), 63); }
 
-struct Draw {
-  double s;
-  int id;
-};
+using Draw = SampleDraw;
+constexpr Draw kNoDraw{-INFINITY, 0x7fffffff, 0.0};
 __device__ __forceinline__ Draw better_draw(Draw x, Draw y) { return y.s > x.s || (y.s == x.s && y.id < x.id) ? y : x; }
-template <int STEP>
-__device__ __forceinline__ Draw prefix_step(Draw v, Draw) {
-  return Draw{prefix_step<STEP>(v.s, v.s), prefix_step<STEP>(v.id, v.id)};
-}
 __device__ __forceinline__ Draw wave_draw(Draw v) {
   v = all_lanes(v, [](Draw x, Draw y) { return better_draw(x, y); });
-  return Draw{from_lane(v.s, 63), from_lane(v.id, 63)};
+  return Draw{from_lane(v.s, 63), from_lane(v.id, 63), from_lane(v.d, 63)};
 }
 
 // The draw as a race: argmax(G - d) is the token with the least e = -log(U) exp(d).
-// A token is read with 1 - U <= -log(U) first, so most end without a logarithm, and
-// those that no noise could bring ahead (1 - U is at least 2^-24) without their hash.
-// e is good to 2^-17 in float32: tokens closer than that are told apart in double.
+// 1 - U <= -log(U), so most tokens end without a logarithm.  e is good to 2^-17 in
+// float32: tokens closer than that are told apart in double.
 __device__ __noinline__ double score_of(uint32_t x, double d) {
   const double U = ((double)x + 0.5) * 0x1p-23;
   return -log(-log(U)) - d;
 }
 constexpr float kNear = 0x1p-15f;
 constexpr uint64_t kGolden = 0x9E3779B97F4A7C15ull;  // of SplitMix64's state
+// The 23 bits of the noise: output n of the stream from z = seed + (n + 1) golden (its
+// last step leaves the upper bits alone).
+__device__ __forceinline__ uint32_t noise_bits(uint64_t z) {
+  z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
+  z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
+  return (uint32_t)(z >> 32) >> 9;
+}
+// 1 - U, exact
+__device__ __forceinline__ float noise_rest(uint32_t x) { return ((float)(0x7fffffu - x) + 0.5f) * 0x1p-23f; }
+
 struct Race {
   float bound = INFINITY;  // nothing above it can win
   float e = INFINITY;      // the lane's best
   uint32_t x = 0;
   int id = 0x7fffffff;
   double d = INFINITY;
-  // Token n, whose weight is w: the hash of output n of the stream z0 + (n + 1)
-  // golden (z: that sum), of which 23 bits count: the product's upper word
-  __device__ __forceinline__ void enter(uint64_t z, int n, float w, const double& max, const float& l, const double& inv_T) {
-    const float f = __builtin_amdgcn_rcpf(w);
-    if (f * 0x1p-24f > bound) return;
-    z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
-    z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;  // (z ^ z >> 31 leaves the upper 23 bits alone)
-    const uint32_t xn = (uint32_t)(z >> 32) >> 9;
-    const float y = ((float)(0x7fffffu - xn) + 0.5f) * 0x1p-23f;  // 1 - U, exact
+  // Token n at distance dn with noise xn (y = 1 - U) and f = exp(dn).
+  __device__ __forceinline__ void enter(int n, double dn, float f, uint32_t xn, float y) {
     if (y * f > bound) return;
     // -log(1 - y): a series below 1/8
     float g = __builtin_fmaf(y, 1.f / 6.f, 0.2f);
@@ -268,7 +274,6 @@ struct Race {
     g = __builtin_fmaf(y, g, 1.f) * y;
     if (y >= 0.125f) g = __builtin_amdgcn_logf(1.f - y) * -0.69314718f;
     const float en = g * f;
-    const double dn = (max - (double)l) * inv_T;
     bool first = en < e;
     if (en >= e * (1.f - kNear) && en <= e * (1.f + kNear)) {
       const double a = score_of(xn, dn), b = score_of(x, d);
@@ -289,8 +294,8 @@ struct Race {
   // the wave's token
   __device__ __forceinline__ Draw best() {
     share();
-    Draw r{-INFINITY, 0x7fffffff};
-    if (e <= bound) r = Draw{score_of(x, d), id};
+    Draw r = kNoDraw;
+    if (e <= bound) r = Draw{score_of(x, d), id, d};
     return wave_draw(r);
   }
 };
@@ -311,8 +316,7 @@ __device__ __forceinline__ void store_draw(const SampleArgs& a, int64_t at, Race
       best = better_draw(best, wd[w]);
       sum += ws[w];
     }
-    a.best[at] = best.s;
-    a.best_id[at] = best.id;
+    a.best[at] = best;
     a.sum[at] = sum;
   }
 }
@@ -374,8 +378,12 @@ __global__ void __launch_bounds__(kThreads) sample_slice_kernel(SampleArgs a) {
       if (x[k] > -INFINITY && j < kSampleBins) {
         const double w = place_weight(table, step, rest) * (edge[j] * scale);
         sum += w;
-        const int off = token_of<BF16>(0, 0, k);
-        race.enter(z0 + (uint64_t)off * kGolden, base + off, (float)w, (double)m, x[k], inv_T);
+        const float f = __builtin_amdgcn_rcpf((float)w);
+        if (f * 0x1p-24f <= race.bound) {  // (1 - U is at least 2^-24: no noise brings the others ahead)
+          const int off = token_of<BF16>(0, 0, k);
+          const uint32_t xn = noise_bits(z0 + (uint64_t)off * kGolden);
+          race.enter(base + off, ((double)m - (double)x[k]) * inv_T, f, xn, noise_rest(xn));
+        }
       }
       if (k == 0 || k == 4) race.share();
     }
@@ -408,6 +416,7 @@ struct ScanSmem {
   uint64_t mass[2][kSampleBins];
   uint32_t cnt[2][kSampleBins];
   int off[256];  // bins between a slice's top and the row's (1000: out of reach)
+  float x[16][kThreads];
   float wm[4];
   double ws[4];
   Draw wd[4];
@@ -525,12 +534,37 @@ __global__ void __launch_bounds__(kThreads) sample_scan_kernel(SampleArgs a) {
     r.inv_T = inv_T;
     a.row[row] = r;
   }
-  // a logit that no token of the bins up to hi is below (with room for its rounding)
-  float least = -INFINITY;
+  // The least logits of the window, of the bins up to hi, of those above lo and of min_p: a
+  // first guess, and the place of its neighbours.
+  auto least = [&](double guess, auto in) {
+    float l = (float)fmin(fmax(guess, -3.4e38), 3.4e38);
+    for (int i = 0; i < 8 && !in(l) && l < FLT_MAX; ++i) l = logit_of(key_of(l) + 1);
+    for (int i = 0; i < 8; ++i) {
+      const float below = logit_of(key_of(l) - 1);
+      if (!(below >= -FLT_MAX) || !in(below)) break;
+      l = below;
+    }
+    return l;
+  };
+  auto within = [&](double most) {
+    return least((double)M - most / inv_T, [&](float l) { return ((double)M - (double)l) * inv_T <= most; });
+  };
+  auto from_bin = [&](int bin) {  // of the bins up to `bin` below the top
+    int step;
+    float rest;
+    return least((grid.top - bin) * kSteps / grid.c, [&](float l) { return grid.place(l, step, rest) <= bin; });
+  };
+  float t_window = -FLT_MAX, t_list = -FLT_MAX, t_sure = -FLT_MAX, t_min = -FLT_MAX;
   if (inv_T > 0.0) {
-    const double l = hi < kSampleBins ? (grid.top - hi) * kSteps / grid.c : (double)M - q.min_d / inv_T;
-    least = (float)fmax(l - fabs(l) * 0x1p-20 - fabs((double)M) * 0x1p-40, -3e38);
+    t_window = within(kSpan);
+    if (q.min_d < kSpan) t_min = within(q.min_d);
+    if (hi < kSampleBins - 1) t_list = from_bin(hi);
+    if (lo < kSampleBins) t_sure = lo > 0 ? from_bin(lo - 1) : INFINITY;
+  } else if (q.listed()) {
+    t_sure = INFINITY;  // (all logits are in one bin)
   }
+  t_list = fmaxf(t_list, t_window);
+  t_sure = fmaxf(t_sure, t_window);
   const uint64_t z0 = (uint64_t)__float_as_uint(a.u[row]);
   Race race;
   double sum = 0.0;
@@ -550,26 +584,30 @@ __global__ void __launch_bounds__(kThreads) sample_scan_kernel(SampleArgs a) {
     const int here = s;
     s = after(s + 1);
     if (s < s1) load16<BF16>(a, row, s * kSampleSlice, tid, next);
-    uint32_t listed = 0;
+    uint32_t listed = 0, sure = 0;
 #pragma unroll
     for (int k = 0; k < 16; ++k) {
-      if (x[k] < least) continue;
-      const double d = ((double)M - (double)x[k]) * inv_T;
-      if (!(x[k] > -INFINITY && d <= kSpan)) continue;
-      int step;
-      float rest;
-      const int j = min(grid.place(x[k], step, rest), kSampleBins - 1);
-      if (j > hi) continue;
-      if (j >= lo) {
-        listed |= 1u << k;
-      } else if (d <= q.min_d) {
+      sm.x[k][tid] = x[k];
+      const bool above = x[k] >= t_sure;
+      sure |= (above && x[k] >= t_min ? 1u : 0u) << k;
+      listed |= (!above && x[k] >= t_list && q.listed() ? 1u : 0u) << k;
+    }
+    // the tokens above, every lane its own
+    while (__any(sure != 0)) {
+      if (sure != 0) {
+        const int k = __builtin_ctz(sure);
+        sure &= sure - 1;
+        const float l = sm.x[k][tid];
+        int step;
+        float rest;
+        const int j = min(max(grid.place(l, step, rest), 0), kSampleBins - 1), id = token_of<BF16>(here * kSampleSlice, tid, k);
         const double w = place_weight(sm.table, step, rest) * sm.factor[j];
         sum += w;
-        const int id = token_of<BF16>(here * kSampleSlice, tid, k);
-        race.enter(z0 + (uint64_t)(id + 1) * kGolden, id, (float)w, (double)M, x[k], inv_T);
+        const uint32_t xn = noise_bits(z0 + (uint64_t)(id + 1) * kGolden);
+        race.enter(id, ((double)M - (double)l) * inv_T, __builtin_amdgcn_rcpf((float)w), xn, noise_rest(xn));
       }
+      race.share();
     }
-    race.share();
     if (__any(listed != 0)) {
       const int n = __popc(listed);
       const int in = prefix_sum(n);
@@ -590,11 +628,12 @@ __global__ void __launch_bounds__(kThreads) sample_scan_kernel(SampleArgs a) {
 
 // ---------------------------------------------------------------------------
 constexpr int kFinish = 1024;                     // threads of a row's last workgroup
-constexpr int kStaged = kSampleList;               // listed tokens kept in LDS
+constexpr int kStaged = kSampleList;               // listed tokens, all kept in LDS
 constexpr int kListBits = 40;  // of a listed weight: 2^20 of them stay below 2^61
 
 struct FinishSmem {
-  uint2 list[kStaged];
+  uint2 list[kStaged];  // key, id
+  uint64_t weight[kStaged];
   double table[kSteps];
   double factor[kSampleBins];  // weight of a bin's edge over that of the list's first
   uint64_t mass[2][256];  // of this digit and, cleared meanwhile, of the next
@@ -625,8 +664,14 @@ struct Tokens {
     if (tid < kSteps) sm.table[tid] = kTables.step[tid];
     // (bin j's over bin 0's: the same steps down, from 1)
     if (tid < kSampleBins) sm.factor[tid] = tid == 0 ? 1.0 : kTables.edge[tid] / kTables.edge[0];
+    __syncthreads();
     if (n <= kStaged)
-      for (uint32_t i = tid; i < n; i += kFinish) sm.list[i] = a.list[(int64_t)row * kSampleList + i];
+      for (uint32_t i = tid; i < n; i += kFinish) {
+        const uint2 e = a.list[(int64_t)row * kSampleList + i];
+        const float l = __uint_as_float(e.y);
+        sm.list[i] = make_uint2(key_of(l), e.x);
+        sm.weight[i] = weight(l);
+      }
     __syncthreads();
   }
   // a listed token's weight over that of the first listed bin's edge
@@ -638,27 +683,25 @@ struct Tokens {
     const double w = (double)fixed<kMassBits>(place_weight(sm.table, step, rest)) * 0x1p-38;
     return fixed<kListBits>(w * sm.factor[j]);
   }
+  // f(id, key, weight()) of every listed token
   template <typename F>
   __device__ __forceinline__ void each(F f) const {
-    const uint32_t count = n <= kSampleList ? n : (uint32_t)a.V;
+    if (n <= kStaged) {
 #pragma unroll 1
-    for (uint32_t i = tid; i < count; i += kFinish) {
-      uint2 e;
-      if (n <= kStaged) {
-        e = sm.list[i];
-      } else if (n <= kSampleList) {
-        e = a.list[(int64_t)row * kSampleList + i];
-      } else {
-        const float l = load1<BF16>(a, row, (int)i);
-        if (!(l > -INFINITY && (M - (double)l) * inv_T <= kSpan)) continue;
-        int step;
-        float rest;
-        const int j = min(grid.place(l, step, rest), kSampleBins - 1);
-        if (j < lo || j > hi) continue;
-        e = make_uint2(i, __float_as_uint(l));
+      for (uint32_t i = tid; i < n; i += kFinish) {
+        const uint2 e = sm.list[i];
+        f((int)e.y, e.x, [&] { return sm.weight[i]; });
       }
-      const float l = __uint_as_float(e.y);
-      f((int)e.x, key_of(l), l);
+      return;
+    }
+#pragma unroll 1
+    for (int v = tid; v < a.V; v += kFinish) {
+      const float l = load1<BF16>(a, row, v);
+      if (!(l > -INFINITY && (M - (double)l) * inv_T <= kSpan)) continue;
+      int step;
+      float rest;
+      const int j = min(grid.place(l, step, rest), kSampleBins - 1);
+      if (j >= lo && j <= hi) f(v, key_of(l), [&] { return weight(l); });
     }
   }
 };
@@ -723,12 +766,12 @@ __device__ __forceinline__ Border find_key(const L& ls, FinishSmem& sm, int tid,
   int shift = max(0, 32 - __clz((int)span) - 8), last = 32;
 #pragma unroll 1
   for (;;) {
-    ls.each([&](int id, uint32_t key, float l) {
+    ls.each([&](int id, uint32_t key, auto w) {
       const uint32_t v = key - base;
       if (!in(id, key) || (last < 32 && v >> last != b.key)) return;
       const uint32_t dg = last < 32 ? v >> shift & ((1u << (last - shift)) - 1) : v >> shift;
       atomicAdd(&sm.cnt[turn][dg], 1u);
-      if (MASS) atomicAdd((unsigned long long*)&sm.mass[turn][dg], (unsigned long long)ls.weight(l));
+      if (MASS) atomicAdd((unsigned long long*)&sm.mass[turn][dg], (unsigned long long)w());
     });
     if (!find_digit<MASS, false>(sm, tid, turn, target)) {
       b.found = false;
@@ -753,7 +796,7 @@ __device__ __forceinline__ uint32_t find_id(const L& ls, FinishSmem& sm, int tid
   uint64_t target = n;
 #pragma unroll 1
   for (int shift = 16; shift >= 0; shift -= 8) {
-    ls.each([&](int id, uint32_t k, float) {
+    ls.each([&](int id, uint32_t k, auto) {
       if (k == key && (shift == 16 || ((uint32_t)id ^ found) >> (shift + 8) == 0)) atomicAdd(&sm.cnt[turn][(uint32_t)id >> shift & 255u], 1u);
     });
     if (!find_digit<false, true>(sm, tid, turn, target)) return 0xffffffffu;
@@ -763,18 +806,13 @@ __device__ __forceinline__ uint32_t find_id(const L& ls, FinishSmem& sm, int tid
   return found;
 }
 
-// a key's logit
-__device__ __forceinline__ float logit_of(uint32_t key) {
-  return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
-}
-
 // The row's border (key, id) among its listed tokens, and their part in the draw.
 template <typename L>
 __device__ __forceinline__ void finish_list(const L& ls, FinishSmem& sm, int tid, const Request& q, const SampleRow& r,
                                             uint64_t z0, uint32_t& key, uint32_t& id_to, Race& race, double& sum) {
   const double factor = kTables.edge[min(r.lo, kSampleBins - 1)] * top_scale(ls.grid, sm.table, r.max);
   uint32_t lo = 0xffffffffu, hi = 0u;
-  ls.each([&](int, uint32_t k, float) {
+  ls.each([&](int, uint32_t k, auto) {
     lo = min(lo, k);
     hi = max(hi, k);
   });
@@ -807,8 +845,8 @@ __device__ __forceinline__ void finish_list(const L& ls, FinishSmem& sm, int tid
     }
     if (q.use_p) {  // the weight of the first top_k
       uint64_t mine = 0;
-      ls.each([&](int id, uint32_t k, float l) {
-        if (k > key || (k == key && (uint32_t)id <= id_to)) mine += ls.weight(l);
+      ls.each([&](int id, uint32_t k, auto w) {
+        if (k > key || (k == key && (uint32_t)id <= id_to)) mine += w();
       });
       atomicAdd((unsigned long long*)&sm.total, (unsigned long long)mine);
       __syncthreads();
@@ -831,13 +869,14 @@ __device__ __forceinline__ void finish_list(const L& ls, FinishSmem& sm, int tid
       if (n < b.ties) id_to = find_id(ls, sm, tid, turn, key, n);
     }
   }
-  ls.each([&](int id, uint32_t k, float l) {
+  ls.each([&](int id, uint32_t k, auto weight) {
     if (!(k > key || (k == key && (uint32_t)id <= id_to))) return;
-    const double d = ((double)r.max - (double)l) * r.inv_T;
+    const double d = ((double)r.max - (double)logit_of(k)) * r.inv_T;
     if (d > q.min_d) return;
-    const double w = (double)ls.weight(l) * 0x1p-40 * factor;
+    const double w = (double)weight() * 0x1p-40 * factor;
     sum += w;
-    race.enter(z0 + (uint64_t)(id + 1) * kGolden, id, fmaxf((float)w, 1e-14f), (double)r.max, l, r.inv_T);
+    const uint32_t xn = noise_bits(z0 + (uint64_t)(id + 1) * kGolden);
+    race.enter(id, d, __builtin_amdgcn_rcpf(fmaxf((float)w, 1e-14f)), xn, noise_rest(xn));
   });
 }
 
@@ -885,7 +924,7 @@ __global__ void __launch_bounds__(kFinish) sample_finish_kernel(SampleArgs a) {
   SampleRow r = r0;
   const uint64_t z0 = (uint64_t)__float_as_uint(a.u[row]);
   Race race;
-  Draw best{-INFINITY, 0x7fffffff};  // of the earlier passes
+  Draw best = kNoDraw;  // of the earlier passes
   double sum = 0.0;
   uint32_t key = 0, id_to = 0xffffffffu;
   if (q.listed()) {
@@ -901,12 +940,14 @@ __global__ void __launch_bounds__(kFinish) sample_finish_kernel(SampleArgs a) {
     const double d = ((double)M - (double)ms) * r.inv_T;
     if (tid < a.NS && ms > -INFINITY && d <= kSpan) {
       const int64_t at = (int64_t)row * a.NS + tid;
-      best = Draw{a.best[at] - d, a.best_id[at]};
+      best = a.best[at];
+      best.s -= d;
+      best.d += d;
       sum = a.sum[at] * exp(-d);
     }
   } else if (tid * a.spw < a.NS) {  // the second pass's
     const int64_t at = (int64_t)row * a.NS + tid;
-    best = Draw{a.best[at], a.best_id[at]};
+    best = a.best[at];
     sum += a.sum[at];
   }
   best = better_draw(wave_draw(best), race.best());
@@ -916,15 +957,12 @@ __global__ void __launch_bounds__(kFinish) sample_finish_kernel(SampleArgs a) {
     sm.ws[wave] = sum;
   }
   __syncthreads();
-  if (tid == 0) {
-    for (int w = 1; w < W; ++w) {
-      best = better_draw(best, sm.wd[w]);
-      sum += sm.ws[w];
-    }
-    best.id = min(best.id, a.V - 1);
-    a.tokens[row] = best.id;
-    const double d = ((double)M - (double)load1<BF16>(a, row, best.id)) * r.inv_T;
-    if (a.chosen != nullptr) a.chosen[row] = (float)(exp(-d) / sum);
+  if (wave != 0) return;
+  best = wave_draw(lane < W ? sm.wd[lane] : kNoDraw);
+  sum = wave_sum(lane < W ? sm.ws[lane] : 0.0);
+  if (lane == 0) {
+    a.tokens[row] = min(best.id, a.V - 1);
+    if (a.chosen != nullptr) a.chosen[row] = (float)(exp(-best.d) / sum);
     r.cut = q.min_d;
     r.inv_sum = 1.0 / sum;
     r.key = key;
@@ -996,8 +1034,7 @@ size_t sample_workspace(int rows, int V, SampleArgs* a, uint8_t* base) {
   uint8_t* smax = take(R * NS * 4);
   uint8_t* sarg = take(R * NS * 4);
   uint8_t* hist = take(R * NS * kSampleBins * 8);
-  uint8_t* best = take(R * NS * 8);
-  uint8_t* best_id = take(R * NS * 4);
+  uint8_t* best = take(R * NS * sizeof(SampleDraw));
   uint8_t* sum = take(R * NS * 8);
   uint8_t* row = take(R * sizeof(SampleRow));
   uint8_t* count = take(R * 4);
@@ -1006,8 +1043,7 @@ size_t sample_workspace(int rows, int V, SampleArgs* a, uint8_t* base) {
     a->smax = (float*)smax;
     a->sarg = (int32_t*)sarg;
     a->hist = (uint64_t*)hist;
-    a->best = (double*)best;
-    a->best_id = (int32_t*)best_id;
+    a->best = (SampleDraw*)best;
     a->sum = (double*)sum;
     a->row = (SampleRow*)row;
     a->count = (uint32_t*)count;

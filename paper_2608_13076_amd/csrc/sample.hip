@@ -423,6 +423,27 @@ struct ScanSmem {
   SampleRow row;
 };
 
+// The least finite logit that `in`, true from some logit on, holds for (infinity: none).
+// Among the 64 numbers around a guess at once; rounding can put it further away near 0,
+// then by all numbers, 64 parts at a time.
+template <typename In>
+__device__ __forceinline__ float least_logit(double guess, In in) {
+  const int64_t first = key_of(-FLT_MAX), last = key_of(FLT_MAX);
+  const int64_t at = key_of((float)fmin(fmax(guess, -(double)FLT_MAX), (double)FLT_MAX)) - 32;
+  const int lane = threadIdx.x & 63;
+  auto number = [&](int64_t key) { return logit_of((uint32_t)min(max(key, first), last)); };
+  uint64_t hits = __ballot(in(number(at + lane)));
+  if (hits != 0 && (hits & 1) == 0) return number(at + __ffsll((unsigned long long)hits) - 1);
+  int64_t below = first - 1;  // (below, below + 64 step] holds it
+#pragma unroll 1
+  for (int bits = 27;; bits = max(0, bits - 6)) {
+    hits = __ballot(in(number(below + ((int64_t)(lane + 1) << bits))));
+    if (hits == 0) return INFINITY;
+    below += (int64_t)(__ffsll((unsigned long long)hits) - 1) << bits;
+    if (bits == 0) return number(below + 1);
+  }
+}
+
 template <bool BF16>
 __global__ void __launch_bounds__(kThreads) sample_scan_kernel(SampleArgs a) {
   __shared__ ScanSmem sm;
@@ -534,25 +555,14 @@ __global__ void __launch_bounds__(kThreads) sample_scan_kernel(SampleArgs a) {
     r.inv_T = inv_T;
     a.row[row] = r;
   }
-  // The least logits of the window, of the bins up to hi, of those above lo and of min_p: a
-  // first guess, and the place of its neighbours.
-  auto least = [&](double guess, auto in) {
-    float l = (float)fmin(fmax(guess, -3.4e38), 3.4e38);
-    for (int i = 0; i < 8 && !in(l) && l < FLT_MAX; ++i) l = logit_of(key_of(l) + 1);
-    for (int i = 0; i < 8; ++i) {
-      const float below = logit_of(key_of(l) - 1);
-      if (!(below >= -FLT_MAX) || !in(below)) break;
-      l = below;
-    }
-    return l;
-  };
+  // The least logits of the window, of the bins up to hi, of those above lo and of min_p
   auto within = [&](double most) {
-    return least((double)M - most / inv_T, [&](float l) { return ((double)M - (double)l) * inv_T <= most; });
+    return least_logit((double)M - most / inv_T, [&](float l) { return ((double)M - (double)l) * inv_T <= most; });
   };
   auto from_bin = [&](int bin) {  // of the bins up to `bin` below the top
     int step;
     float rest;
-    return least((grid.top - bin) * kSteps / grid.c, [&](float l) { return grid.place(l, step, rest) <= bin; });
+    return least_logit((grid.top - bin) * kSteps / grid.c, [&](float l) { return grid.place(l, step, rest) <= bin; });
   };
   float t_window = -FLT_MAX, t_list = -FLT_MAX, t_sure = -FLT_MAX, t_min = -FLT_MAX;
   if (inv_T > 0.0) {
@@ -629,6 +639,7 @@ __global__ void __launch_bounds__(kThreads) sample_scan_kernel(SampleArgs a) {
 // ---------------------------------------------------------------------------
 constexpr int kFinish = 1024;                     // threads of a row's last workgroup
 constexpr int kStaged = kSampleList;               // listed tokens, all kept in LDS
+static_assert(kSampleList >= kFinish, "an entry per thread");
 constexpr int kListBits = 40;  // of a listed weight: 2^20 of them stay below 2^61
 
 struct FinishSmem {
@@ -660,14 +671,14 @@ struct Tokens {
   double M, inv_T;
   Grid grid;
   int lo, hi;
-  __device__ __forceinline__ void stage() {
-    if (tid < kSteps) sm.table[tid] = kTables.step[tid];
+  __device__ __forceinline__ void stage(uint2 e, double step, double edge) {
+    if (tid < kSteps) sm.table[tid] = step;
     // (bin j's over bin 0's: the same steps down, from 1)
-    if (tid < kSampleBins) sm.factor[tid] = tid == 0 ? 1.0 : kTables.edge[tid] / kTables.edge[0];
+    if (tid < kSampleBins) sm.factor[tid] = tid == 0 ? 1.0 : edge / kTables.edge[0];
     __syncthreads();
     if (n <= kStaged)
       for (uint32_t i = tid; i < n; i += kFinish) {
-        const uint2 e = a.list[(int64_t)row * kSampleList + i];
+        if (i >= kFinish) e = a.list[(int64_t)row * kSampleList + i];
         const float l = __uint_as_float(e.y);
         sm.list[i] = make_uint2(key_of(l), e.x);
         sm.weight[i] = weight(l);
@@ -806,11 +817,63 @@ __device__ __forceinline__ uint32_t find_id(const L& ls, FinishSmem& sm, int tid
   return found;
 }
 
-// The row's border (key, id) among its listed tokens, and their part in the draw.
+// Both borders of a short list at once: kPer lanes per token add up the counts and
+// weights of the tokens from the first to it.
+constexpr int kFew = 256, kPer = kFinish / kFew;
+__device__ __forceinline__ uint64_t quad_sum(uint64_t v) {
+  v += (uint64_t)__shfl_xor((unsigned long long)v, 1);
+  return v + (uint64_t)__shfl_xor((unsigned long long)v, 2);
+}
+static_assert(kPer == 4, "quad_sum");
+__device__ __forceinline__ void border_of_few(FinishSmem& sm, int tid, uint32_t n, const Request& q, const SampleRow& r,
+                                              double factor, uint32_t& key, uint32_t& id_to) {
+  const uint32_t i = (uint32_t)tid / kPer;
+  const bool mine = i < n;
+  const uint2 e = sm.list[mine ? i : 0];
+  uint64_t sum = 0;
+  uint32_t count = 0;
+  if (mine)
+    for (uint32_t j = tid % kPer; j < n; j += kPer) {
+      const uint2 o = sm.list[j];
+      const uint64_t w = sm.weight[j];
+      const bool before = o.x > e.x || (o.x == e.x && o.y <= e.y);
+      count += before ? 1u : 0u;
+      sum += before ? w : 0ull;
+    }
+  count = (uint32_t)quad_sum(count);
+  sum = quad_sum(sum);
+  const bool teller = mine && tid % kPer == 0;
+  const uint32_t last = r.k_in ? min((uint32_t)(q.top_k - r.above), n) : n;
+  if (teller && count == last) {
+    sm.key_lo = e.x;
+    sm.key_hi = e.y;
+    sm.total = sum;
+  }
+  __syncthreads();
+  if (r.k_in) {
+    key = sm.key_lo;
+    id_to = sm.key_hi;
+  }
+  if (!q.use_p) return;
+  const double total = r.k_in ? r.mass + (double)sm.total * 0x1p-40 * factor : r.total;
+  const uint64_t target = (uint64_t)fmax(ceil(((q.top_p - kSlack) * total - r.mass) / factor * 0x1p40), 1.0);
+  const bool reached = sm.total >= target;
+  __syncthreads();
+  if (teller && count <= last && sum >= target && sum - sm.weight[i] < target) {
+    sm.key_lo = e.x;
+    sm.key_hi = e.y;
+  }
+  __syncthreads();
+  if (reached) {
+    key = sm.key_lo;
+    id_to = sm.key_hi;
+  }
+}
+
+// The same for more: digit by digit.
 template <typename L>
-__device__ __forceinline__ void finish_list(const L& ls, FinishSmem& sm, int tid, const Request& q, const SampleRow& r,
-                                            uint64_t z0, uint32_t& key, uint32_t& id_to, Race& race, double& sum) {
-  const double factor = kTables.edge[min(r.lo, kSampleBins - 1)] * top_scale(ls.grid, sm.table, r.max);
+__device__ __forceinline__ void border_of_many(const L& ls, FinishSmem& sm, int tid, const Request& q, const SampleRow& r,
+                                               double factor, uint32_t& key, uint32_t& id_to) {
   uint32_t lo = 0xffffffffu, hi = 0u;
   ls.each([&](int, uint32_t k, auto) {
     lo = min(lo, k);
@@ -869,6 +932,18 @@ __device__ __forceinline__ void finish_list(const L& ls, FinishSmem& sm, int tid
       if (n < b.ties) id_to = find_id(ls, sm, tid, turn, key, n);
     }
   }
+}
+
+// The row's border (key, id) among its listed tokens, and their part in the draw.
+template <typename L>
+__device__ __forceinline__ void finish_list(const L& ls, FinishSmem& sm, int tid, const Request& q, const SampleRow& r,
+                                            uint64_t z0, uint32_t& key, uint32_t& id_to, Race& race, double& sum) {
+  const double factor = kTables.edge[min(r.lo, kSampleBins - 1)] * top_scale(ls.grid, sm.table, r.max);
+  if (ls.n == 0) return;
+  if (ls.n <= kFew)
+    border_of_few(sm, tid, ls.n, q, r, factor, key, id_to);
+  else
+    border_of_many(ls, sm, tid, q, r, factor, key, id_to);
   ls.each([&](int id, uint32_t k, auto weight) {
     if (!(k > key || (k == key && (uint32_t)id <= id_to))) return;
     const double d = ((double)r.max - (double)logit_of(k)) * r.inv_T;
@@ -888,6 +963,9 @@ __global__ void __launch_bounds__(kFinish) sample_finish_kernel(SampleArgs a) {
   const Request q = request_of(a, row);
   const SampleRow r0 = a.row[row];
   const uint32_t n = a.count[row];
+  // (asked for before it is known whether they are used: the list holds kFinish entries, written or not)
+  const uint2 entry = a.list[(int64_t)row * kSampleList + tid];
+  const double step = kTables.step[tid & (kSteps - 1)], edge = kTables.edge[tid & (kSampleBins - 1)];
   // the row's maximum
   const float ms = tid < a.NS ? a.smax[(int64_t)row * a.NS + tid] : -INFINITY;
   const float m0 = wave_max(ms);
@@ -929,7 +1007,7 @@ __global__ void __launch_bounds__(kFinish) sample_finish_kernel(SampleArgs a) {
   uint32_t key = 0, id_to = 0xffffffffu;
   if (q.listed()) {
     Tokens<BF16> ls{a, sm, row, tid, n, (double)M, r.inv_T, Grid(r.inv_T, M), r.lo, r.hi};
-    ls.stage();
+    ls.stage(entry, step, edge);
     finish_list(ls, sm, tid, q, r, z0, key, id_to, race, sum);
   }
   if (q.plain()) {

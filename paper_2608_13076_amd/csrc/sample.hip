@@ -18,6 +18,7 @@
 #include <float.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "device_accept.h"
 #include "device_lanes.h"
@@ -92,8 +93,13 @@ struct Grid {
   // bins below the top (below 0 or beyond the bins: not of the row's window), the
   // step in its bin and the rest of a step
   __device__ __forceinline__ int place(float l, int& step, float& rest) const {
+    return wide ? place<true>(l, step, rest) : place<false>(l, step, rest);
+  }
+  // (the same without its branch: WIDE is `wide`)
+  template <bool WIDE>
+  __device__ __forceinline__ int place(float l, int& step, float& rest) const {
     const double z = (double)l * c;
-    if (wide) {
+    if (WIDE) {
       const double bin = floor(z * (1.0 / kSteps));
       const double t = fmin(fmax(__builtin_fma((double)l, c, -bin * kSteps), 0.0), kSteps - 0x1p-20);
       step = (int)t;
@@ -370,35 +376,48 @@ __global__ void __launch_bounds__(kThreads) sample_slice_kernel(SampleArgs a) {
     Race race;
     double sum = 0.0;
     const double scale = top_scale(grid, table, m);
+    auto draw = [&](auto wide) {
 #pragma unroll
-    for (int k = 0; k < 16; ++k) {
-      int step;
-      float rest;
-      const int j = grid.place(x[k], step, rest);
-      if (x[k] > -INFINITY && j < kSampleBins) {
-        const double w = place_weight(table, step, rest) * (edge[j] * scale);
-        sum += w;
-        const float f = __builtin_amdgcn_rcpf((float)w);
-        if (f * 0x1p-24f <= race.bound) {  // (1 - U is at least 2^-24: no noise brings the others ahead)
-          const int off = token_of<BF16>(0, 0, k);
-          const uint32_t xn = noise_bits(z0 + (uint64_t)off * kGolden);
-          race.enter(base + off, ((double)m - (double)x[k]) * inv_T, f, xn, noise_rest(xn));
+      for (int k = 0; k < 16; ++k) {
+        int step;
+        float rest;
+        const int j = grid.template place<wide.value>(x[k], step, rest);
+        if (x[k] > -INFINITY && j < kSampleBins) {
+          const double w = place_weight(table, step, rest) * (edge[j] * scale);
+          sum += w;
+          const float f = __builtin_amdgcn_rcpf((float)w);
+          if (f * 0x1p-24f <= race.bound) {  // (1 - U is at least 2^-24: no noise brings the others ahead)
+            const int off = token_of<BF16>(0, 0, k);
+            const uint32_t xn = noise_bits(z0 + (uint64_t)off * kGolden);
+            race.enter(base + off, ((double)m - (double)x[k]) * inv_T, f, xn, noise_rest(xn));
+          }
         }
+        if (k == 0 || k == 4) race.share();
       }
-      if (k == 0 || k == 4) race.share();
-    }
+    };
+    if (grid.wide)
+      draw(std::true_type{});
+    else
+      draw(std::false_type{});
     store_draw<4>(a, (int64_t)row * a.NS + s, race, sum, wd, ws, tid);
     return;
   }
   if (!q.listed()) return;
+  auto count = [&](auto wide) {
 #pragma unroll
-  for (int k = 0; k < 16; ++k) {
-    int step;
-    float rest;
-    const int j = grid.place(x[k], step, rest);
-    if (x[k] > -INFINITY && j < kSampleBins)
-      atomicAdd((unsigned long long*)&bins[j * kCopies + (tid & (kCopies - 1))], (unsigned long long)(fixed<kMassBits>(place_weight(table, step, rest)) | 1ull << 51));
-  }
+    for (int k = 0; k < 16; ++k) {
+      int step;
+      float rest;
+      const int j = grid.template place<wide.value>(x[k], step, rest);
+      if (x[k] > -INFINITY && j < kSampleBins)
+        atomicAdd((unsigned long long*)&bins[j * kCopies + (tid & (kCopies - 1))],
+                  (unsigned long long)(fixed<kMassBits>(place_weight(table, step, rest)) | 1ull << 51));
+    }
+  };
+  if (grid.wide)
+    count(std::true_type{});
+  else
+    count(std::false_type{});
   __syncthreads();
   if (tid < kSampleBins) {
     uint64_t w = 0;

@@ -37,7 +37,7 @@ struct TreeAppend {
   int64_t qo_ld;
   uint32_t* err;
   // set by the launcher
-  int run;        // groups of heads that a wave of the rotated part goes through
+  int run;        // heads that a wave of the rotated part goes through
   int qk_blocks;  // workgroups of that part; the values' follow
 };
 hipError_t launch_tree_append(const TreeAppend& a, hipStream_t st);

@@ -57,38 +57,55 @@ __device__ __forceinline__ void store4(void* base, int64_t at, const float* x) {
 // ---------------------------------------------------------------------------
 // Append.  hd / 8 lanes hold a head: pair group p < pairs / 4 the features of
 // pairs 4 p .. + 3 (halves: 4 p .. + 3 and pairs + 4 p .. + 3; neighbours: 8 p ..
-// + 7), the lanes behind the eight features each that are not rotated.  A wave
-// takes a row and computes its lanes' four angles once, for all heads that it
-// goes through.  The angle pos f is a product in double whose whole turns are
-// taken off exactly, so far positions lose nothing but the product's rounding
+// + 7), the lanes behind the eight features each that are not rotated.  A workgroup
+// takes 16 rows (hd 64: 32) and goes through heads: each lane computes its row's
+// four angles once, and the 16-byte pieces of neighbouring positions, which share
+// the keys' cache lines, leave from one place.  The angle pos f is a product in
+// double whose whole turns are taken off exactly, so far positions lose nothing but
+// the product's rounding
 // (2^-53 of the angle; a float32 angle is off by 0.004 at 100 thousand
 // positions); sine and cosine are rounded once to float32.
 //
 // Values are stored by feature: a lane takes two features of eight neighbouring
 // positions, whole 16-byte pieces where the rows cover them.
+//
+// Bound by memory: 4003 rows of 32 + 32 heads of 128 in bfloat16 read and write
+// 197 MB in 55 us, 3.6 TB/s (a large copy: 5.1).  A wave that takes four heads of one
+// row instead, so that a line of keys is written from eight places, takes 78 us.
+// More loads in flight, other numbers of heads per workgroup (a twentieth to a
+// quarter of them) and 16-byte loads change less than a tenth; without the angles
+// it takes as long.
 // ---------------------------------------------------------------------------
 template <int HD, bool BF16>
 __device__ __forceinline__ void append_qk(const TreeAppend& p, int block) {
-  constexpr int LPH = HD / 8, HPW = 64 / LPH;  // lanes a head, heads at a time
-  const int lane = threadIdx.x & 63, c = lane % LPH, slot = lane / LPH;
+  constexpr int LPH = HD / 8, RPW = 64 / LPH;  // lanes a head, rows a wave
+  const int lane = threadIdx.x & 63, c = lane % LPH;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const int HQ = p.q != nullptr ? p.H : 0, heads = HQ + p.KVH;
-  const int groups = (heads + HPW - 1) / HPW, parts = (groups + p.run - 1) / p.run;
-  const int64_t id = (int64_t)block * 4 + wave, row = id / parts;
-  const int part = (int)(id - row * parts);
+  const int HQ = p.q != nullptr ? p.H : 0, heads = HQ + p.KVH, parts = (heads + p.run - 1) / p.run;
+  const int rows16 = block / parts, part = block - rows16 * parts;
+  const int64_t row = ((int64_t)rows16 * 4 + wave) * RPW + lane / LPH;
   if (row >= (int64_t)p.B * p.R) return;
   const int b = (int)(row / p.R), i = (int)(row - (int64_t)b * p.R);
   const int L = p.lens[b], n = p.rows != nullptr ? min(p.rows[b], p.R) : p.R;
   const bool used = i < n;
   const int t = add_sat(L, i);
   const bool fits = t >= 0 && t < p.max_len;
-  if (used && !fits && part == 0 && lane == 0) flag_error(p.err, SPADE_DERR_CAPACITY);
+  if (used && !fits && part == 0 && c == 0) flag_error(p.err, SPADE_DERR_CAPACITY);
   // the lane's features f0 .. + 3 and f1 .. + 3
   const bool turns = 4 * c < p.pairs;
   const int f0 = turns ? (p.interleaved ? 8 * c : 4 * c) : 8 * c + 0;
   const int f1 = turns ? (p.interleaved ? 8 * c + 4 : p.pairs + 4 * c) : 8 * c + 4;
+  const int first = part * p.run, end = min(heads, first + p.run);
+  if (!used) {
+    const float z[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int h = first; h < min(end, HQ); ++h) {
+      store4<BF16>(p.q_out, row * p.qo_ld + h * HD + f0, z);
+      store4<BF16>(p.q_out, row * p.qo_ld + h * HD + f1, z);
+    }
+    return;
+  }
   float co[4] = {1.f, 1.f, 1.f, 1.f}, sn[4] = {0.f, 0.f, 0.f, 0.f};
-  if (turns && used) {
+  if (turns) {
     const double at = (double)(p.pos != nullptr ? p.pos[b] : L) + (double)(p.depth != nullptr ? p.depth[row] : i);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -102,20 +119,9 @@ __device__ __forceinline__ void append_qk(const TreeAppend& p, int block) {
       sn[j] = (float)(s * (double)p.amplitude);
     }
   }
-  for (int g = part * p.run, end = min(groups, g + p.run); g < end; ++g) {
-    const int h = g * HPW + slot;
-    if (h >= heads) break;
+  for (int h = first; h < end; ++h) {
     const bool query = h < HQ;
-    const int hh = query ? h : h - HQ;
-    if (!used) {
-      if (query) {
-        const float z[4] = {0.f, 0.f, 0.f, 0.f};
-        store4<BF16>(p.q_out, row * p.qo_ld + hh * HD + f0, z);
-        store4<BF16>(p.q_out, row * p.qo_ld + hh * HD + f1, z);
-      }
-      continue;
-    }
-    const int64_t in = row * (query ? p.q_ld : p.k_ld) + hh * HD;
+    const int64_t in = row * (query ? p.q_ld : p.k_ld) + (query ? h : h - HQ) * HD;
     float a[4], d[4];
     load4<BF16>(query ? p.q : p.k, in + f0, a);
     load4<BF16>(query ? p.q : p.k, in + f1, d);
@@ -139,10 +145,10 @@ __device__ __forceinline__ void append_qk(const TreeAppend& p, int block) {
       }
     }
     if (query) {
-      store4<BF16>(p.q_out, row * p.qo_ld + hh * HD + f0, a);
-      store4<BF16>(p.q_out, row * p.qo_ld + hh * HD + f1, d);
+      store4<BF16>(p.q_out, row * p.qo_ld + h * HD + f0, a);
+      store4<BF16>(p.q_out, row * p.qo_ld + h * HD + f1, d);
     } else if (fits) {
-      uint16_t* dst = p.cache.k + ((int64_t)b * p.KVH + hh) * p.cache.head_elems;
+      uint16_t* dst = p.cache.k + ((int64_t)b * p.KVH + h - HQ) * p.cache.head_elems;
       store4<true>(dst, k_cache_index(f0, t, HD), a);
       store4<true>(dst, k_cache_index(f1, t, HD), d);
     }
@@ -1316,12 +1322,12 @@ __global__ void __launch_bounds__(kMoveThreads) tree_move_kernel(TreeCommit p) {
 
 template <int HD, bool BF16>
 hipError_t append_t(TreeAppend a, hipStream_t st) {
-  constexpr int HPW = 64 / (HD / 8), VHPW = 64 / (HD / 2);
-  const int heads = (a.q != nullptr ? a.H : 0) + a.KVH, groups = (heads + HPW - 1) / HPW;
-  const int64_t rows = (int64_t)a.B * a.R;
-  // enough waves for the chip, then several groups of heads for one computation of the angles
-  a.run = (int)std::min<int64_t>(std::max<int64_t>(rows * groups / 8192, 1), groups);
-  const int64_t qk = (rows * ((groups + a.run - 1) / a.run) + 3) / 4;
+  constexpr int VHPW = 64 / (HD / 2), RPG = 4 * 64 / (HD / 8);  // rows a workgroup
+  const int heads = (a.q != nullptr ? a.H : 0) + a.KVH;
+  const int64_t rows = (int64_t)a.B * a.R, groups = (rows + RPG - 1) / RPG;
+  // enough workgroups for the chip, then several heads for one computation of the angles
+  a.run = (int)std::min<int64_t>(std::max<int64_t>(groups * heads / 1024, 1), heads);
+  const int64_t qk = groups * ((heads + a.run - 1) / a.run);
   const int64_t vb = ((int64_t)a.B * ((a.R + 14) / 8) * ((a.KVH + VHPW - 1) / VHPW) + 3) / 4;
   if (qk + vb > 0x7fffffff) return hipErrorInvalidValue;
   a.qk_blocks = (int)qk;

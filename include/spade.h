@@ -531,8 +531,9 @@ spade_status spade_tree_append(const spade_tree_shape* shape, int layer, void* d
  *   out = softmax(scale q . k) v   per query head.
  * d_q and d_out: [B R] rows of n_heads heads in `dtype` that do not overlap; rows
  * that a request does not use give zeros.  What a row does not see has no part in
- * its output, infinities and NaN among it; a value that is not finite gives NaN in
- * the rows that see it.  max_keys: the host's bound of lens[b] + the rows in use, in
+ * its output, infinities and NaN among it; a value that is not finite makes its
+ * feature of the rows that see it NaN or infinite, a key that is not finite their
+ * scores.  (Sums can pass float32's range for values beyond 2^64.)  max_keys: the host's bound of lens[b] + the rows in use, in
  * [1, max_len] ([R, max_len] without d_rows), or 0 for max_len; a longer request is
  * cut to it and flagged, as by spade_kvq_attend.  scale: in [2^-50, 2^50].  Float32
  * calls keep queries and probabilities in 24 bits, bfloat16 calls the

@@ -98,6 +98,7 @@ struct Grid {
   // (the same without its branch: WIDE is `wide`)
   template <bool WIDE>
   __device__ __forceinline__ int place(float l, int& step, float& rest) const {
+#pragma clang fp contract(off)  // (the same place in every kernel)
     const double z = (double)l * c;
     if (WIDE) {
       const double bin = floor(z * (1.0 / kSteps));
@@ -670,6 +671,7 @@ struct FinishSmem {
   uint32_t cnt[2][256];
   Draw wd[kFinish / 64];
   double ws[kFinish / 64];
+  uint64_t wl[kFinish / 64];
   float wm[kFinish / 64];
   int wi[kFinish / 64];
   uint32_t key_lo, key_hi;
@@ -956,8 +958,8 @@ __device__ __forceinline__ void border_of_many(const L& ls, FinishSmem& sm, int 
 // The row's border (key, id) among its listed tokens, and their part in the draw.
 template <typename L>
 __device__ __forceinline__ void finish_list(const L& ls, FinishSmem& sm, int tid, const Request& q, const SampleRow& r,
-                                            uint64_t z0, uint32_t& key, uint32_t& id_to, Race& race, double& sum) {
-  const double factor = kTables.edge[min(r.lo, kSampleBins - 1)] * top_scale(ls.grid, sm.table, r.max);
+                                            uint64_t z0, double factor, uint32_t& key, uint32_t& id_to, Race& race,
+                                            uint64_t& sum) {
   if (ls.n == 0) return;
   if (ls.n <= kFew)
     border_of_few(sm, tid, ls.n, q, r, factor, key, id_to);
@@ -967,10 +969,10 @@ __device__ __forceinline__ void finish_list(const L& ls, FinishSmem& sm, int tid
     if (!(k > key || (k == key && (uint32_t)id <= id_to))) return;
     const double d = ((double)r.max - (double)logit_of(k)) * r.inv_T;
     if (d > q.min_d) return;
-    const double w = (double)weight() * 0x1p-40 * factor;
+    const uint64_t w = weight();
     sum += w;
     const uint32_t xn = noise_bits(z0 + (uint64_t)(id + 1) * kGolden);
-    race.enter(id, d, __builtin_amdgcn_rcpf(fmaxf((float)w, 1e-14f)), xn, noise_rest(xn));
+    race.enter(id, d, __builtin_amdgcn_rcpf(fmaxf((float)((double)w * 0x1p-40 * factor), 1e-14f)), xn, noise_rest(xn));
   });
 }
 
@@ -1022,12 +1024,16 @@ __global__ void __launch_bounds__(kFinish) sample_finish_kernel(SampleArgs a) {
   const uint64_t z0 = (uint64_t)__float_as_uint(a.u[row]);
   Race race;
   Draw best = kNoDraw;  // of the earlier passes
-  double sum = 0.0;
+  // weights of the kept tokens: the earlier passes', and of the list, whose order changes from
+  // call to call, as integers over `factor`
+  double sum = 0.0, factor = 0.0;
+  uint64_t in_list = 0;
   uint32_t key = 0, id_to = 0xffffffffu;
   if (q.listed()) {
     Tokens<BF16> ls{a, sm, row, tid, n, (double)M, r.inv_T, Grid(r.inv_T, M), r.lo, r.hi};
     ls.stage(entry, step, edge);
-    finish_list(ls, sm, tid, q, r, z0, key, id_to, race, sum);
+    factor = kTables.edge[min(r.lo, kSampleBins - 1)] * top_scale(ls.grid, sm.table, r.max);
+    finish_list(ls, sm, tid, q, r, z0, factor, key, id_to, race, in_list);
   }
   if (q.plain()) {
     // the slices' own draws, relative to their maxima
@@ -1045,18 +1051,21 @@ __global__ void __launch_bounds__(kFinish) sample_finish_kernel(SampleArgs a) {
   } else if (tid * a.spw < a.NS) {  // the second pass's
     const int64_t at = (int64_t)row * a.NS + tid;
     best = a.best[at];
-    sum += a.sum[at];
+    sum = a.sum[at];
   }
   best = better_draw(wave_draw(best), race.best());
   sum = wave_sum(sum);
+  in_list = from_lane(prefix_sum(in_list), 63);
   if (lane == 0) {
     sm.wd[wave] = best;
     sm.ws[wave] = sum;
+    sm.wl[wave] = in_list;
   }
   __syncthreads();
   if (wave != 0) return;
   best = wave_draw(lane < W ? sm.wd[lane] : kNoDraw);
-  sum = wave_sum(lane < W ? sm.ws[lane] : 0.0);
+  in_list = from_lane(prefix_sum(lane < W ? sm.wl[lane] : (uint64_t)0), 63);
+  sum = wave_sum(lane < W ? sm.ws[lane] : 0.0) + (double)in_list * 0x1p-40 * factor;
   if (lane == 0) {
     a.tokens[row] = min(best.id, a.V - 1);
     if (a.chosen != nullptr) a.chosen[row] = (float)(exp(-best.d) / sum);

@@ -408,7 +408,7 @@ struct Part {
   int part;  // the first row of the split's part in part_o
   __device__ __forceinline__ void request(const TreeAttend& p, int tid) {
     head = (unsigned)(b * p.KVH + kvh);
-    const TreeRows rr = tree_rows(p, b, rb == 0 && kvh == 0 && lo == 0 && tid == 0);
+    const TreeRows rr = tree_rows(p, b, p.WG == 0 && rb == 0 && kvh == 0 && tid == 0);
     L = rr.L;
     n = rr.n;
     rows = p.G * n;
@@ -458,7 +458,10 @@ struct Part {
       const One x = r0 == 0 ? first : one(r0 + lane);
       const int u = units(x), iu = before + prefix_sum(u);
       const int pr = p.KVH * ((x.nb + cb - 1) / cb) * x.rows, ir = row + prefix_sum(pr);
-      if (want == 0 && tid < 64 && r0 + lane < p.B) p.plan[1 + r0 + lane] = ir - pr;
+      if (want == 0 && tid < 64 && r0 + lane < p.B) {
+        p.plan[1 + r0 + lane] = ir - pr;
+        tree_rows(p, r0 + lane, true);
+      }
       const uint64_t hit = __ballot(iu > want);
       if (hit != 0 && !found) {
         const int l = __ffsll((unsigned long long)hit) - 1;

@@ -225,6 +225,85 @@ def test_distribution_of_the_draw():
     assert chi < k + 3.3 * np.sqrt(2 * k) + 6  # (0.1%)
 
 
+@pytest.mark.parametrize("n", [1, 2, 63, 64, 255, 256, 257, 1024, 1025, 8191, 8192, 8193, 12000])
+def test_borders_among_n_close_tokens(n):
+    """n logits within a quarter of each other hold nearly all the weight, some of
+    them equal: the borders lie among them, however they are looked for.  Calls
+    in a row give the same bits."""
+    rng = np.random.default_rng(n)
+    V, sets = 20011, []
+    for k in sorted({1, 2, n // 3 + 1, n - 1 or 1, n, n + 1}):
+        sets += [dict(top_k=k), dict(top_k=k, top_p=0.6, min_p=0.9)]
+    sets += [dict(top_p=p) for p in (1e-6, 0.1, 0.5, 0.97)]
+    x = rng.uniform(-14, -12, size=(len(sets), V)).astype(np.float32)
+    for r in range(len(sets)):
+        x[r, rng.choice(V, n, replace=False)] = np.round(rng.uniform(0, 0.25, n) * 4096) / 4096
+    logits, u = torch.from_numpy(x).to(DEV), torch.from_numpy(rng.random(len(sets), np.float32)).to(DEV)
+    base = dict(temperature=1.0, top_k=0, top_p=1.0, min_p=0.0)
+    cols = {k: np.array([{**base, **s}[k] for s in sets], np.int32 if k == "top_k" else np.float32) for k in base}
+    tok, ch, pr, s = run(logits, u, cols)
+    check(logits, u, pr, tok, ch, 1, **cols)
+    for _ in range(4):
+        t2, c2, p2, _ = run(logits, u, cols, sampler=s)
+        assert torch.equal(tok, t2) and torch.equal(ch, c2) and torch.equal(pr, p2)
+
+
+def test_the_largest_vocabulary():
+    rng = np.random.default_rng(20)
+    V = 1 << 20
+    logits = torch.from_numpy(rng.normal(size=(5, V)).astype(np.float32) * 3).to(DEV)
+    u = torch.from_numpy(rng.random(5, np.float32)).to(DEV)
+    kw = dict(temperature=np.array([1, 1, 0.7, 0, 1.5], np.float32), top_k=np.array([0, 0, 900000, 0, 300], np.int32),
+              top_p=np.array([1, 0.9, 0.99, 1, 0.8], np.float32), min_p=np.array([0, 0, 1e-6, 0, 0.01], np.float32))
+    tok, ch, pr, s = run(logits, u, kw)
+    check(logits, u, pr, tok, ch, 1, **kw)
+    assert s.device_error() == 0
+
+
+def test_a_last_request_of_fewer_rows():
+    """Five rows, two a request: the third has one."""
+    rng = np.random.default_rng(21)
+    rows, V = 5, 3001
+    logits = torch.from_numpy(rng.normal(size=(rows, V)).astype(np.float32) * 2).to(DEV)
+    u = torch.from_numpy(rng.random(rows, np.float32)).to(DEV)
+    s = sampling.Sampler(rows, V, device=DEV)
+    k = torch.tensor([1, 40, 7], dtype=torch.int32, device=DEV)
+    tok, ch = torch.zeros(rows, dtype=torch.int32, device=DEV), torch.zeros(rows, device=DEV)
+    spade._check(s.lib.spade_sample(rows, V, spade.F32, logits.data_ptr(), V, 2, None, None, k.data_ptr(), None, None,
+                                    u.data_ptr(), tok.data_ptr(), ch.data_ptr(), None, s._at_ws, s._bytes, s._at_err,
+                                    torch.cuda.current_stream().cuda_stream))
+    check(logits, u, None, tok, ch, 2, top_k=[1, 40, 7])
+
+
+def test_captured_draws():
+    """A graph whose distribution takes the logits' place, replayed with eager draws of
+    other settings in between."""
+    rng = np.random.default_rng(22)
+    rows, V = 6, 40009
+    s, e = (sampling.Sampler(rows, V, device=DEV) for _ in range(2))
+    x, u = torch.zeros(rows, V, device=DEV), torch.zeros(rows, device=DEV)
+    k = torch.zeros(rows, dtype=torch.int32, device=DEV)
+    p = torch.ones(rows, device=DEV)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        s.draw(x, u, top_k=k, top_p=p, probs=x)
+    torch.cuda.current_stream().wait_stream(side)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        tok, ch = s.draw(x, u, top_k=k, top_p=p, probs=x)
+    for i in range(4):
+        logits = torch.from_numpy(rng.normal(size=(rows, V)).astype(np.float32) * (i + 1)).to(DEV)
+        x.copy_(logits)
+        u.copy_(torch.from_numpy(rng.random(rows, np.float32)))
+        k.copy_(torch.from_numpy(rng.integers(0, 3, rows).astype(np.int32) * 60))
+        p.copy_(torch.from_numpy(rng.choice([1.0, 0.9, 0.3], rows).astype(np.float32)))
+        g.replay()
+        e.draw(logits, u, temperature=0.5, min_p=0.1)
+        torch.cuda.synchronize()
+        check(logits, u, x, tok, ch, 1, top_k=k.tolist(), top_p=p.tolist())
+
+
 def test_draw_refuses():
     s = sampling.Sampler(4, 100, device=DEV)
     x, u = torch.zeros(4, 100, device=DEV), torch.zeros(4, device=DEV)

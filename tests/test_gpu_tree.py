@@ -241,6 +241,40 @@ def test_attend(b, r, h, kvh, hd, lens, rows, dtype):
     assert cache.device_error() == 0
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("b,r,h,kvh", [(130, 3, 2, 1), (70, 40, 2, 2), (44, 3, 16, 16), (9, 5, 64, 64)])
+def test_attend_large_batches(b, r, h, kvh, dtype):
+    """More requests than a wave has lanes, their keys split or not; ragged lengths,
+    requests without rows among them, whose output rows are zeros over what was there."""
+    rng = np.random.default_rng(b + r)
+    hd = 64
+    cache = tree.TreeCache(1, b, h, kvh, hd, 900, max_rows=r, device=DEV)
+    poison(cache)
+    lens = [int(x) for x in np.exp(rng.uniform(0, math.log(800), b))]
+    used = [int(x) for x in rng.integers(0, r + 1, b)]
+    used[:3], used[-1] = [0, r, 0], 0
+    n = max(a + m for a, m in zip(lens, used))
+    k, v = (rand(rng, b, n, kvh, hd, dtype="bf16") for _ in range(2))
+    cache.append(0, k, v, rows=i32([a + m for a, m in zip(lens, used)]))
+    cache.lens.copy_(i32(lens))
+    q = rand(rng, b, r, h, hd, dtype=dtype)
+    parents = [a_tree(rng, r) for _ in range(b)]
+    out = torch.full_like(q, 7)
+    cache.attend(0, q, parents=i32(parents), rows=i32(used), out=out)
+    assert cache.device_error() == 0
+    some = list(range(0, b, max(1, b * r * h // 1500)))
+    pick = torch.tensor(some, device=DEV)
+    check_attend(cache, 0, q[pick], f64(k[pick]), f64(v[pick]), [lens[i] for i in some], [used[i] for i in some],
+                 [parents[i] for i in some], out[pick], dtype)
+    for i in range(b):
+        assert not out[i, used[i]:].any() and torch.isfinite(out[i].float()).all()
+    # a length outside the cache is flagged, also where a request uses no rows
+    cache.lens[b - 1] = 901
+    again = cache.attend(0, q, parents=i32(parents), rows=i32(used))
+    assert cache.device_error() == spade.DERR_CAPACITY
+    assert torch.equal(out, again)
+
+
 def test_attend_strided_rows():
     """Queries of a fused projection, outputs between other columns."""
     rng = np.random.default_rng(11)

@@ -10,6 +10,7 @@ constexpr int kSampleMaxVocab = 1 << 20;
 constexpr int kSampleSlice = 4096;  // tokens of a workgroup of the first pass: 16 per thread
 constexpr int kSampleBins = 128;    // of a slice's weights
 constexpr int kSampleList = 8192;   // candidates of a row kept apart
+constexpr int kSampleSub = 256;     // parts of the border's bins, where they hold more
 constexpr int kSampleParts = 32;    // most workgroups of a row in the second pass
 
 // What the passes of a row hand on.
@@ -20,6 +21,8 @@ struct SampleRow {
   int lo, hi;     // bins whose tokens are listed (below the top bin)
   int above;      // tokens above bin lo
   int k_in;       // whether the first top_k end in the list
+  int sub;        // bits of a place of these bins below a part of theirs (-1: their tokens are listed)
+  float least, below;  // logits of these bins: from `least` on, below `below`
   double inv_T, cut, inv_sum;  // probabilities: exp(-d) inv_sum where d <= cut
   uint32_t key, id;            // and the token comes no later than this one
 };
@@ -56,6 +59,8 @@ struct SampleArgs {
   SampleRow* row;       // [rows]
   uint32_t* count;      // [rows] listed tokens
   uint2* list;          // [rows][kSampleList] token and logit
+  uint64_t* sub_mass;   // [rows][kSampleSub] weight of a part of the border's bins
+  uint32_t* sub_count;  // ... its tokens
   int NS, NW, spw;      // slices, parts, slices of a part
 };
 size_t sample_workspace(int rows, int V, SampleArgs* a, uint8_t* base);

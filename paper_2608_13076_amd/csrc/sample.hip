@@ -128,11 +128,13 @@ constexpr double const_exp(double x) {
 struct Tables {
   double step[kSteps];       // weight of a step over its bin's upper edge's
   double edge[kSampleBins];  // weight of the upper edge of the bin j below the first over that bin's lower edge's
+  double rel[kSampleBins];   // ... over the first's upper edge's
 };
 constexpr Tables make_tables() {
   Tables t{};
   for (int i = 0; i < kSteps; ++i) t.step[i] = const_exp((i - kSteps) * kStep);
   for (int j = 0; j < kSampleBins; ++j) t.edge[j] = const_exp((1 - j) * kBin);
+  for (int j = 0; j < kSampleBins; ++j) t.rel[j] = t.edge[j] / t.edge[0];
   return t;
 }
 __device__ const Tables kTables = make_tables();
@@ -157,8 +159,18 @@ template <int N>
 __device__ __forceinline__ uint64_t fixed(double w) {
   return (uint64_t)__double_as_longlong(__builtin_fma(w, (double)(1ull << N), 0x1p52)) & 0xfffffffffffffull;
 }
-constexpr int kCopies = 4;     // of a slice's bins, by lane: neighbouring lanes often meet in a bin
 constexpr int kMassBits = 38;  // of a slice's bins: 4096 weights up to 1 below the count at bit 51
+constexpr int kListBits = 40;  // of a listed weight: 2^20 of them stay below 2^61
+// A listed token's weight over that of the first listed bin's edge: in the bins' own steps
+// first, so that equal weights add up to exactly what the bins hold.
+__device__ __forceinline__ uint64_t listed_weight(const double* table, int step, float rest, double rel) {
+  return fixed<kListBits>((double)fixed<kMassBits>(place_weight(table, step, rest)) * 0x1p-38 * rel);
+}
+// A place of the listed bins, j below the first of them, in steps from its upper edge.
+__device__ __forceinline__ int listed_place(int j, int step) { return j * kSteps + (kSteps - 1 - step); }
+constexpr int kSubBits = 8;
+static_assert(kSampleSub == 1 << kSubBits && kSampleSub == 2 * kSampleBins && kSampleSub == kThreads, "two bins' places; in the bins' memory");
+constexpr int kCopies = 4;     // of a slice's bins, by lane: neighbouring lanes often meet in a bin
 
 // Order-preserving integer of a float.
 __device__ __forceinline__ uint32_t key_of(float l) {
@@ -358,6 +370,11 @@ __global__ void __launch_bounds__(kThreads) sample_slice_kernel(SampleArgs a) {
     a.smax[at] = m;
     if (s == 0) a.count[row] = 0;
   }
+  if (s == 0 && q.listed())
+    for (int i = tid; i < kSampleSub; i += kThreads) {
+      a.sub_mass[(int64_t)row * kSampleSub + i] = 0;
+      a.sub_count[(int64_t)row * kSampleSub + i] = 0;
+    }
   if (q.greedy) {
     int id = 0x7fffffff;
 #pragma unroll
@@ -551,6 +568,9 @@ __global__ void __launch_bounds__(kThreads) sample_scan_kernel(SampleArgs a) {
       }
       const double in = from_lane(lo & 1 ? wi[1] : wi[0], lo >> 1), ex = in - from_lane(lo & 1 ? w[1] : w[0], lo >> 1);
       const int above = from_lane(lo & 1 ? ci[1] : ci[0], lo >> 1) - from_lane(lo & 1 ? c[1] : c[0], lo >> 1);
+      // more than the list holds: their counts and weights by finer parts instead
+      const int n = from_lane(hi & 1 ? ci[1] : ci[0], hi >> 1) - above, span = (hi - lo + 1) * kSteps;
+      const int sub = n > kSampleList ? max(0, 32 - __clz(span - 1) - kSubBits) : -1;
       if (lane == 0) {
         sm.row.mass = lo == 0 ? 0.0 : ex;
         sm.row.total = total;
@@ -558,22 +578,12 @@ __global__ void __launch_bounds__(kThreads) sample_scan_kernel(SampleArgs a) {
         sm.row.hi = hi;
         sm.row.above = above;
         sm.row.k_in = k_in;
+        sm.row.sub = sub;
       }
     }
     __syncthreads();
     lo = sm.row.lo;
     hi = sm.row.hi;
-  }
-  if (part == 0 && tid == 0) {
-    SampleRow r = sm.row;
-    if (!q.listed()) {
-      r.mass = r.total = 0.0;
-      r.lo = r.hi = kSampleBins;
-      r.above = r.k_in = 0;
-    }
-    r.max = M;
-    r.inv_T = inv_T;
-    a.row[row] = r;
   }
   // The least logits of the window, of the bins up to hi, of those above lo and of min_p
   auto within = [&](double most) {
@@ -595,6 +605,28 @@ __global__ void __launch_bounds__(kThreads) sample_scan_kernel(SampleArgs a) {
   }
   t_list = fmaxf(t_list, t_window);
   t_sure = fmaxf(t_sure, t_window);
+  if (part == 0 && tid == 0) {
+    SampleRow r = sm.row;
+    if (!q.listed()) {
+      r.mass = r.total = 0.0;
+      r.lo = r.hi = kSampleBins;
+      r.above = r.k_in = 0;
+      r.sub = -1;
+    }
+    r.max = M;
+    r.inv_T = inv_T;
+    r.least = t_list;
+    r.below = t_sure;
+    a.row[row] = r;
+  }
+  const int sub = q.listed() ? sm.row.sub : -1;
+  uint64_t* sub_mass = &sm.mass[0][0];  // (the bins' are used)
+  uint32_t* sub_count = &sm.cnt[0][0];
+  if (sub >= 0) {
+    sub_mass[tid] = 0;
+    sub_count[tid] = 0;
+    __syncthreads();
+  }
   const uint64_t z0 = (uint64_t)__float_as_uint(a.u[row]);
   Race race;
   double sum = 0.0;
@@ -638,7 +670,18 @@ __global__ void __launch_bounds__(kThreads) sample_scan_kernel(SampleArgs a) {
       }
       race.share();
     }
-    if (__any(listed != 0)) {
+    if (sub >= 0) {
+      while (listed != 0) {
+        const int k = __builtin_ctz(listed);
+        listed &= listed - 1;
+        int step;
+        float rest;
+        const int j = min(max(grid.place(sm.x[k][tid], step, rest) - lo, 0), hi - lo);
+        const int at = listed_place(j, step) >> sub;
+        atomicAdd((unsigned long long*)(sub_mass + at), (unsigned long long)listed_weight(sm.table, step, rest, kTables.rel[j]));
+        atomicAdd(sub_count + at, 1u);
+      }
+    } else if (__any(listed != 0)) {
       const int n = __popc(listed);
       const int in = prefix_sum(n);
       uint32_t at = 0;
@@ -653,6 +696,13 @@ __global__ void __launch_bounds__(kThreads) sample_scan_kernel(SampleArgs a) {
         }
     }
   }
+  if (sub >= 0) {
+    __syncthreads();
+    if (sub_count[tid] != 0) {
+      atomicAdd((unsigned long long*)(a.sub_mass + (int64_t)row * kSampleSub + tid), (unsigned long long)sub_mass[tid]);
+      atomicAdd(a.sub_count + (int64_t)row * kSampleSub + tid, sub_count[tid]);
+    }
+  }
   store_draw<4>(a, (int64_t)row * a.NS + part, race, sum, sm.wd, sm.ws, tid);
 }
 
@@ -660,7 +710,6 @@ __global__ void __launch_bounds__(kThreads) sample_scan_kernel(SampleArgs a) {
 constexpr int kFinish = 1024;                     // threads of a row's last workgroup
 constexpr int kStaged = kSampleList;               // listed tokens, all kept in LDS
 static_assert(kSampleList >= kFinish, "an entry per thread");
-constexpr int kListBits = 40;  // of a listed weight: 2^20 of them stay below 2^61
 
 struct FinishSmem {
   uint2 list[kStaged];  // key, id
@@ -679,6 +728,12 @@ struct FinishSmem {
   int digit;
   uint32_t cnt_in;
   uint64_t before, total;
+  // of the border's parts
+  uint64_t part_mass[kSampleSub / 64];
+  uint32_t part_cnt[kSampleSub / 64];
+  int k_part, p_part[2];
+  uint64_t k_mass[2], mass_before;
+  uint32_t cnt_before, count;
 };
 
 // The listed tokens of a row: in LDS, from the list, or, where that was too short
@@ -692,10 +747,9 @@ struct Tokens {
   double M, inv_T;
   Grid grid;
   int lo, hi;
-  __device__ __forceinline__ void stage(uint2 e, double step, double edge) {
+  __device__ __forceinline__ void stage(uint2 e, double step, double rel) {
     if (tid < kSteps) sm.table[tid] = step;
-    // (bin j's over bin 0's: the same steps down, from 1)
-    if (tid < kSampleBins) sm.factor[tid] = tid == 0 ? 1.0 : edge / kTables.edge[0];
+    if (tid < kSampleBins) sm.factor[tid] = rel;
     __syncthreads();
     if (n <= kStaged)
       for (uint32_t i = tid; i < n; i += kFinish) {
@@ -706,14 +760,11 @@ struct Tokens {
       }
     __syncthreads();
   }
-  // a listed token's weight over that of the first listed bin's edge
   __device__ __forceinline__ uint64_t weight(float l) const {
     int step;
     float rest;
     const int j = min(max(grid.place(l, step, rest) - lo, 0), kSampleBins - 1);
-    // (in the bins' own steps first, so that equal weights add up to exactly what the bins hold)
-    const double w = (double)fixed<kMassBits>(place_weight(sm.table, step, rest)) * 0x1p-38;
-    return fixed<kListBits>(w * sm.factor[j]);
+    return listed_weight(sm.table, step, rest, sm.factor[j]);
   }
   // f(id, key, weight()) of every listed token
   template <typename F>
@@ -737,6 +788,109 @@ struct Tokens {
     }
   }
 };
+
+// More tokens in the border's bins than the list holds.  Their counts and weights by
+// parts of those bins tell which parts the border is in: one pass over the row draws
+// the tokens above them and lists theirs (if these are still too many, as where all
+// are equal, every later pass reads the row).
+template <bool BF16>
+__device__ __forceinline__ void narrow(Tokens<BF16>& ls, FinishSmem& sm, int tid, const Request& q, SampleRow& r, uint64_t z0,
+                                       double factor, Race& race, uint64_t& sum) {
+  const SampleArgs& a = ls.a;
+  const int lane = tid & 63, wave = tid >> 6;
+  const bool mine = tid < kSampleSub;
+  const int64_t at = (int64_t)ls.row * kSampleSub + (mine ? tid : 0);
+  const uint64_t w = mine ? a.sub_mass[at] : 0ull;
+  const uint32_t c = mine ? a.sub_count[at] : 0u;
+  uint64_t wi = prefix_sum(w);
+  uint32_t ci = prefix_sum(c);
+  if (mine && lane == 63) {
+    sm.part_mass[wave] = wi;
+    sm.part_cnt[wave] = ci;
+  }
+  if (tid == 0) {
+    sm.k_part = sm.p_part[0] = sm.p_part[1] = kSampleSub - 1;
+    sm.k_mass[0] = sm.k_mass[1] = 0;
+    sm.count = 0;
+  }
+  __syncthreads();
+  if (mine)
+    for (int v = 0; v < wave; ++v) {
+      wi += sm.part_mass[v];
+      ci += sm.part_cnt[v];
+    }
+  if (r.k_in && mine) {
+    const uint32_t n = (uint32_t)(q.top_k - r.above);
+    if (ci >= n && ci - c < n) {
+      sm.k_part = tid;
+      sm.k_mass[0] = wi - w;
+      sm.k_mass[1] = wi;
+    }
+  }
+  __syncthreads();
+  int lo = sm.k_part, hi = lo;
+  if (q.use_p) {
+    // (a little more on either side, as for the bins)
+    const double unit = factor * 0x1p-40;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const double of = r.k_in ? r.mass + (double)sm.k_mass[e] * unit : r.total;
+      const double t = ((q.top_p + (e == 0 ? -0x1p-30 : 0x1p-30)) * of - r.mass) / unit;
+      if (mine && (double)wi >= t && (tid == 0 || (double)(wi - w) < t)) sm.p_part[e] = tid;
+    }
+    __syncthreads();
+    lo = r.k_in ? min(lo, sm.p_part[0]) : sm.p_part[0];
+    if (!r.k_in) hi = sm.p_part[1];
+  }
+  if (mine && tid == lo) {
+    sm.cnt_before = ci - c;
+    sm.mass_before = wi - w;
+  }
+  Race drawn = race;
+  uint64_t weight = sum;
+  for (int s = wave / 4; s < a.NS; s += kFinish / kThreads) {
+    float x[16];
+    load16<BF16>(a, ls.row, s * kSampleSlice, tid % kThreads, x);
+    uint32_t in = 0;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) in |= (x[k] >= r.least && x[k] < r.below ? 1u : 0u) << k;
+    while (in != 0) {  // (every lane its own)
+      const int k = __builtin_ctz(in);
+      in &= in - 1;
+      float l = x[0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) l = k == e ? x[e] : l;
+      int step;
+      float rest;
+      const int j = min(max(ls.grid.place(l, step, rest) - ls.lo, 0), ls.hi - ls.lo), part = listed_place(j, step) >> r.sub;
+      if (part > hi) continue;
+      const int id = token_of<BF16>(s * kSampleSlice, tid % kThreads, k);
+      const uint64_t wl = listed_weight(sm.table, step, rest, sm.factor[j]);
+      if (part >= lo) {
+        const uint32_t i = atomicAdd(&sm.count, 1u);
+        if (i < kStaged) {
+          sm.list[i] = make_uint2(key_of(l), (uint32_t)id);
+          sm.weight[i] = wl;
+        }
+        continue;
+      }
+      const double d = ((double)r.max - (double)l) * r.inv_T;
+      if (d <= q.min_d) {
+        weight += wl;
+        const uint32_t xn = noise_bits(z0 + (uint64_t)(id + 1) * kGolden);
+        drawn.enter(id, d, __builtin_amdgcn_rcpf(fmaxf((float)((double)wl * 0x1p-40 * factor), 1e-14f)), xn, noise_rest(xn));
+      }
+    }
+    drawn.share();
+  }
+  __syncthreads();
+  ls.n = sm.count;
+  if (ls.n > kStaged) return;
+  race = drawn;
+  sum = weight;
+  r.above += (int)sm.cnt_before;
+  r.mass += (double)sm.mass_before * 0x1p-40 * factor;
+}
 
 // The digit at which `target` (a count, or a weight) is reached, from the highest
 // down (UP: from the lowest up), with what comes before it.  False: never.
@@ -986,7 +1140,7 @@ __global__ void __launch_bounds__(kFinish) sample_finish_kernel(SampleArgs a) {
   const uint32_t n = a.count[row];
   // (asked for before it is known whether they are used: the list holds kFinish entries, written or not)
   const uint2 entry = a.list[(int64_t)row * kSampleList + tid];
-  const double step = kTables.step[tid & (kSteps - 1)], edge = kTables.edge[tid & (kSampleBins - 1)];
+  const double step = kTables.step[tid & (kSteps - 1)], rel = kTables.rel[tid & (kSampleBins - 1)];
   // the row's maximum
   const float ms = tid < a.NS ? a.smax[(int64_t)row * a.NS + tid] : -INFINITY;
   const float m0 = wave_max(ms);
@@ -1031,8 +1185,9 @@ __global__ void __launch_bounds__(kFinish) sample_finish_kernel(SampleArgs a) {
   uint32_t key = 0, id_to = 0xffffffffu;
   if (q.listed()) {
     Tokens<BF16> ls{a, sm, row, tid, n, (double)M, r.inv_T, Grid(r.inv_T, M), r.lo, r.hi};
-    ls.stage(entry, step, edge);
+    ls.stage(entry, step, rel);
     factor = kTables.edge[min(r.lo, kSampleBins - 1)] * top_scale(ls.grid, sm.table, r.max);
+    if (r.sub >= 0) narrow(ls, sm, tid, q, r, z0, factor, race, in_list);
     finish_list(ls, sm, tid, q, r, z0, factor, key, id_to, race, in_list);
   }
   if (q.plain()) {
@@ -1145,6 +1300,8 @@ size_t sample_workspace(int rows, int V, SampleArgs* a, uint8_t* base) {
   uint8_t* row = take(R * sizeof(SampleRow));
   uint8_t* count = take(R * 4);
   uint8_t* list = take(R * kSampleList * 8);
+  uint8_t* sub_mass = take(R * kSampleSub * 8);
+  uint8_t* sub_count = take(R * kSampleSub * 4);
   if (a != nullptr) {
     a->smax = (float*)smax;
     a->sarg = (int32_t*)sarg;
@@ -1154,6 +1311,8 @@ size_t sample_workspace(int rows, int V, SampleArgs* a, uint8_t* base) {
     a->row = (SampleRow*)row;
     a->count = (uint32_t*)count;
     a->list = (uint2*)list;
+    a->sub_mass = (uint64_t*)sub_mass;
+    a->sub_count = (uint32_t*)sub_count;
   }
   return off;
 }

@@ -248,6 +248,24 @@ def test_borders_among_n_close_tokens(n):
         assert torch.equal(tok, t2) and torch.equal(ch, c2) and torch.equal(pr, p2)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V,scale", [(40000, 0.05), (128256, 1.0), (128256, 0.3), (262147, 0.5)])
+def test_borders_among_more_tokens_than_a_list_holds(V, scale, dtype):
+    """Flat rows, whose bins at the border hold tens of thousands of tokens."""
+    rng = np.random.default_rng(V)
+    sets = [dict(top_p=p) for p in (0.01, 0.5, 0.9, 0.9999)] + [dict(top_k=V // 2), dict(top_k=V // 2, top_p=0.7),
+            dict(top_k=V - 9, top_p=0.95, min_p=0.3), dict(top_p=0.8, temperature=3.0, min_p=0.8)]
+    logits = torch.from_numpy(rng.normal(size=(len(sets), V)).astype(np.float32) * scale).to(DEV).to(TD[dtype])
+    u = torch.from_numpy(rng.random(len(sets), np.float32)).to(DEV)
+    base = dict(temperature=1.0, top_k=0, top_p=1.0, min_p=0.0)
+    cols = {k: np.array([{**base, **s}[k] for s in sets], np.int32 if k == "top_k" else np.float32) for k in base}
+    tok, ch, pr, s = run(logits, u, cols)
+    check(logits, u, pr, tok, ch, 1, **cols)
+    for _ in range(3):
+        t2, c2, p2, _ = run(logits, u, cols, sampler=s)
+        assert torch.equal(tok, t2) and torch.equal(ch, c2) and torch.equal(pr, p2)
+
+
 def test_the_largest_vocabulary():
     rng = np.random.default_rng(20)
     V = 1 << 20

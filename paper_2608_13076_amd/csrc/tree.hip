@@ -62,9 +62,8 @@ __device__ __forceinline__ void store4(void* base, int64_t at, const float* x) {
 // four angles once, and the 16-byte pieces of neighbouring positions, which share
 // the keys' cache lines, leave from one place.  The angle pos f is a product in
 // double whose whole turns are taken off exactly, so far positions lose nothing but
-// the product's rounding
-// (2^-53 of the angle; a float32 angle is off by 0.004 at 100 thousand
-// positions); sine and cosine are rounded once to float32.
+// the product's rounding (2^-53 of the angle; a float32 angle is off by 0.004 at 100
+// thousand positions); sine and cosine are rounded once to float32.
 //
 // Values are stored by feature: a lane takes two features of eight neighbouring
 // positions, whole 16-byte pieces where the rows cover them.
@@ -230,7 +229,8 @@ __global__ void __launch_bounds__(256) tree_append_kernel(TreeAppend p) {
 }
 
 // ---------------------------------------------------------------------------
-// Read back: keys a lane per 16-byte piece, values as they were appended.
+// Read back: keys a lane per 16-byte piece, values as they were appended.  Bound by
+// memory: 4003 rows of 32 heads of 128 read and write 131 MB in 27 us (4.8 TB/s).
 // ---------------------------------------------------------------------------
 template <int HD, bool BF16>
 __global__ void __launch_bounds__(256) tree_read_kernel(TreeRead p) {
@@ -282,10 +282,9 @@ __global__ void __launch_bounds__(256) tree_read_kernel(TreeRead p) {
 // Attention.
 //
 // The G n rows in use that share a K/V head are packed (row g n + i) into tiles
-// of 16; a workgroup of four waves takes RT tiles over a split of the keys, wave
-// w every fourth block of 32 positions, with a running maximum, sum and output
-// of its own.  The cache's fragments are the A operands of the transposed
-// products, straight from memory, 1 KB per load:
+// of 16.  A workgroup takes tiles of rows over a split of the keys, in blocks of 32
+// positions, with a running reference, sum and output per row (one pass over the keys).
+// The cache's fragments are the A operands of the transposed products, 1 KB per load:
 //   S^T = K Q^T    lane 16 q + c gets the scores of row c at positions 4 q .. + 3
 //                  of either 16-position group
 //   O^T = V^T P^T  k slots 8 q .. + 7 are positions 8 q .. + 7: two swaps of lane
@@ -297,6 +296,12 @@ __global__ void __launch_bounds__(256) tree_read_kernel(TreeRead p) {
 //
 // Only the last blocks hold rows of the tree: there a row's word of ancestors
 // says which it sees.
+//
+// Bound by memory up to about 64 rows of a K/V head (two tiles over 32768 keys of 8
+// heads: 134 MB in 32 us, 4.2 TB/s), by the matrix units and the exponentials beside
+// them beyond (256 rows over 120001 keys of 8 heads, bfloat16: 126 GFLOP of the
+// formula, 189 with the probabilities' second term, in 190 us; a large bfloat16
+// product would take 158).
 // ---------------------------------------------------------------------------
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kWaves = 4;
@@ -400,7 +405,9 @@ __device__ __forceinline__ void zero_rows(const TreeAttend& p, int b, int kvh, i
 // round), have equal counts of blocks of 32 positions whatever the requests' lengths.
 // The count follows from all of them: the least CB for which the splits of all heads and
 // tiles of rows fit (kLeast at least, two rounds of a wave).  Every wave works it out
-// from the lengths, the first workgroup leaves it for the merge.
+// from the lengths, the first workgroup leaves it for the merge.  16 ragged contexts of
+// 256 to 4096 (8 heads, 128 rows) take 45 us with their merge; with as many splits for
+// every request, and loads under branches, they took 66.
 constexpr int kLeast = 8;
 struct Part {
   unsigned head;
@@ -729,72 +736,56 @@ __device__ __forceinline__ void put(const TreeAttend& p, const Part& w, int m, i
   }
 }
 
-// KW waves of the same rows put their parts together; wave kw of rows rw writes to
-// o[kw RW + rw].
-template <int HD, int RT, int WAVES>
+// The waves of the same rows put their parts together.
+template <int HD, int RT>
 struct JoinSmem {
-  float o[WAVES][RT * 16][HD + 4];
-  float m[WAVES][RT * 16], l[WAVES][RT * 16];
+  float o[kWaves][RT * 16][HD + 4];
+  float m[kWaves][RT * 16], l[kWaves][RT * 16];
 };
-template <int HD, bool QB, int RT, int RW, int KW>
-__device__ __forceinline__ void join_rows(const TreeAttend& p, const Part& w, const JoinSmem<HD, RT, RW * KW>& sm, int tid) {
-  constexpr int LPR = HD / 4;  // lanes a row
-  for (int k = tid; k < RW * RT * 16 * LPR; k += RW * KW * 64) {
-    const int r = k / LPR, f = (k - r * LPR) * 4, m = w.rb * RW * RT * 16 + r, v = r / (RT * 16), e = r - v * (RT * 16);
-    if (m >= w.rows) break;
-    float mx = sm.m[v][e];
-#pragma unroll
-    for (int j = 1; j < KW; ++j) mx = fmaxf(mx, sm.m[j * RW + v][e]);
-    float s = 0.f;
-    floatx4 x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int j = 0; j < KW; ++j) {
-      const float mw = sm.m[j * RW + v][e], lw = sm.l[j * RW + v][e];
-      // (a part that is NaN stays so whatever its reference)
-      s += mw == -INFINITY ? lw : lw * __builtin_amdgcn_exp2f(mw - mx);
-      x += *(const floatx4*)&sm.o[j * RW + v][e][f];
-    }
-    put<HD, QB>(p, w, m, f, x, mx, s);
-  }
-}
-template <int HD, bool QB, int RT, int RW, int KW>
-__device__ __forceinline__ void join(const TreeAttend& p, const Part& w, Rows<HD, QB, RT>& R, JoinSmem<HD, RT, RW * KW>& sm,
-                                     int rw, int kw, int tid) {
-  const int lane = tid & 63, q = lane >> 4, c = lane & 15, me = kw * RW + rw;
-  if constexpr (KW == 1) {
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      const int m = (w.rb * RW + rw) * RT * 16 + rt * 16 + c;
-      const float s = sum_q(R.l[rt]);
-      if (m < w.rows)
-#pragma unroll
-        for (int t = 0; t < HD / 16; ++t) put<HD, QB>(p, w, m, 16 * t + 4 * q, R.o[rt][t], R.M[rt], s);
-    }
-    return;
-  }
+template <int HD, bool QB, int RT>
+__device__ __forceinline__ void join(const TreeAttend& p, const Part& w, Rows<HD, QB, RT>& R, JoinSmem<HD, RT>& sm, int wave,
+                                     int tid) {
+  const int lane = tid & 63, q = lane >> 4, c = lane & 15;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const float s = sum_q(R.l[rt]);
     if (q == 0) {
-      sm.m[me][rt * 16 + c] = R.M[rt];
-      sm.l[me][rt * 16 + c] = s;
+      sm.m[wave][rt * 16 + c] = R.M[rt];
+      sm.l[wave][rt * 16 + c] = s;
     }
   }
   __syncthreads();
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    float m = sm.m[rw][rt * 16 + c];
+    float m = sm.m[0][rt * 16 + c];
 #pragma unroll
-    for (int k = 1; k < KW; ++k) m = fmaxf(m, sm.m[k * RW + rw][rt * 16 + c]);
+    for (int k = 1; k < kWaves; ++k) m = fmaxf(m, sm.m[k][rt * 16 + c]);
     const float f = R.M[rt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(R.M[rt] - m);
 #pragma unroll
     for (int t = 0; t < HD / 16; ++t) {
       const floatx4 x = R.o[rt][t] * f;
-      *(floatx4*)&sm.o[me][rt * 16 + c][16 * t + 4 * q] = x;
+      *(floatx4*)&sm.o[wave][rt * 16 + c][16 * t + 4 * q] = x;
     }
   }
   __syncthreads();
-  join_rows<HD, QB, RT, RW, KW>(p, w, sm, tid);
+  constexpr int LPR = HD / 4;  // lanes a row
+  for (int k = tid; k < RT * 16 * LPR; k += kWaves * 64) {
+    const int r = k / LPR, f = (k - r * LPR) * 4, m = w.rb * RT * 16 + r;
+    if (m >= w.rows) break;
+    float mx = sm.m[0][r];
+#pragma unroll
+    for (int j = 1; j < kWaves; ++j) mx = fmaxf(mx, sm.m[j][r]);
+    float s = 0.f;
+    floatx4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < kWaves; ++j) {
+      const float mw = sm.m[j][r], lw = sm.l[j][r];
+      // (a part that is NaN stays so whatever its reference)
+      s += mw == -INFINITY ? lw : lw * __builtin_amdgcn_exp2f(mw - mx);
+      x += *(const floatx4*)&sm.o[j][r][f];
+    }
+    put<HD, QB>(p, w, m, f, x, mx, s);
+  }
 }
 
 // Few rows: four waves with the same RT tiles, wave w every fourth block, two blocks
@@ -804,7 +795,7 @@ __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_e
 tree_attend_kernel(TreeAttend p) {
   constexpr int FT = HD / 16, S = HD / 32;
   extern __shared__ __align__(16) uint8_t smem_raw[];
-  auto& sm = *reinterpret_cast<JoinSmem<HD, RT, kWaves>*>(smem_raw);
+  auto& sm = *reinterpret_cast<JoinSmem<HD, RT>*>(smem_raw);
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   Part w;
@@ -850,12 +841,12 @@ tree_attend_kernel(TreeAttend p) {
   }
   if (__any(R.broken))
     for (int e = first; e < w.hi; e += kWaves) R.mend(ld, e, w, lane);
-  join<HD, QB, RT, 1, kWaves>(p, w, R, sm, 0, wave, tid);
+  join<HD, QB, RT>(p, w, R, sm, wave, tid);
 }
 
-// Many rows: eight waves, RW of them with 32 rows (float32: 16) each over the same
-// keys, KW = 8 / RW blocks at a time, which pass through LDS: every byte enters the
-// compute unit once for RW waves.  Loads run D rounds ahead in registers.
+// Many rows: four or eight waves with 32 rows (float32: 16) each over the same keys,
+// which pass through LDS: every byte enters the compute unit once for all of them.
+// Loads run D blocks ahead in registers.
 //
 // bfloat16 calls use the 32 x 32 products, whose tile is a block's 32 positions by a
 // wave's 32 rows: lane 32 h + c has the scores of row c at positions 8 g + 4 h .. + 3,
@@ -1033,82 +1024,62 @@ struct Rows32 {
   }
 };
 
-// KW groups of RW waves put their parts together; wave kw RW + rw has rows rw.
-template <int HD, int WAVES>
-using JoinSmem32 = JoinSmem<HD, 2, WAVES>;
-template <int HD, int RW, int KW>
-__device__ __forceinline__ void join32(const TreeAttend& p, const Part& w, Rows32<HD>& R, JoinSmem32<HD, RW * KW>& sm, int rw,
-                                       int kw, int tid) {
-  const int lane = tid & 63, h = lane >> 5, c = lane & 31, me = kw * RW + rw;
+// A wave's rows from r0 on are its own: no join.
+template <int HD>
+__device__ __forceinline__ void put_rows(const TreeAttend& p, const Part& w, const Rows32<HD>& R, int r0, int lane) {
+  const int h = lane >> 5, m = r0 + (lane & 31);
   const float s = half_sum(R.l);
-  if constexpr (KW == 1) {
-    const int m = (w.rb * RW + rw) * 32 + c;
-    if (m < w.rows)
-#pragma unroll
-      for (int t = 0; t < HD / 32; ++t)
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
-          put<HD, true>(p, w, m, 32 * t + 8 * g + 4 * h,
-                        floatx4{R.o[t][4 * g], R.o[t][4 * g + 1], R.o[t][4 * g + 2], R.o[t][4 * g + 3]}, R.M, s);
-  } else {
-    if (h == 0) {
-      sm.m[me][c] = R.M;
-      sm.l[me][c] = s;
-    }
-    __syncthreads();
-    float m = sm.m[rw][c];
-#pragma unroll
-    for (int k = 1; k < KW; ++k) m = fmaxf(m, sm.m[k * RW + rw][c]);
-    const float f = R.M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(R.M - m);
+  if (m < w.rows)
 #pragma unroll
     for (int t = 0; t < HD / 32; ++t)
 #pragma unroll
       for (int g = 0; g < 4; ++g)
-        *(floatx4*)&sm.o[me][c][32 * t + 8 * g + 4 * h] =
-            floatx4{R.o[t][4 * g] * f, R.o[t][4 * g + 1] * f, R.o[t][4 * g + 2] * f, R.o[t][4 * g + 3] * f};
-    __syncthreads();
-    join_rows<HD, true, 2, RW, KW>(p, w, sm, tid);
-  }
+        put<HD, true>(p, w, m, 32 * t + 8 * g + 4 * h,
+                      floatx4{R.o[t][4 * g], R.o[t][4 * g + 1], R.o[t][4 * g + 2], R.o[t][4 * g + 3]}, R.M, s);
+}
+template <int HD>
+__device__ __forceinline__ void put_rows(const TreeAttend& p, const Part& w, const Rows<HD, false, 1>& R, int r0, int lane) {
+  const int q = lane >> 4, m = r0 + (lane & 15);
+  const float s = sum_q(R.l[0]);
+  if (m < w.rows)
+#pragma unroll
+    for (int t = 0; t < HD / 16; ++t) put<HD, false>(p, w, m, 16 * t + 4 * q, R.o[0][t], R.M[0], s);
 }
 
-template <int HD, bool QB, int RW, int W>
+template <int HD, bool QB, int W>
 struct Wide {
-  static constexpr int KW = W / RW, RT = QB ? 2 : 1, kThreads = W * 64;
-  static constexpr int kRows = RW * RT * 16;
-  static constexpr int kPieces = 8 * HD;                    // 16-byte pieces of a block, keys first
-  static constexpr int kLoads = KW * kPieces / kThreads;    // of a thread and round
-  static constexpr int D = kLoads >= 8 ? 1 : kLoads >= 4 ? 2 : 3;
-  static constexpr size_t kRing = 2 * KW * kPieces * 16, kJoin = KW == 1 ? 0 : sizeof(JoinSmem<HD, RT, W>);
-  static constexpr size_t kSmem = kRing > kJoin ? kRing : kJoin;
+  static constexpr int kThreads = W * 64, kWaveRows = QB ? 32 : 16, kRows = W * kWaveRows;
+  static constexpr int kPieces = 8 * HD;              // 16-byte pieces of a block, keys first
+  static constexpr int kLoads = kPieces / kThreads;   // of a thread
+  static constexpr int D = kLoads >= 4 ? 2 : 3;       // blocks ahead
+  static constexpr size_t kSmem = 2 * kPieces * 16;
 };
 
-template <int HD, bool QB, int RW, int W>
+template <int HD, bool QB, int W>
 __global__ void __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(2))) tree_attend_wide_kernel(TreeAttend p) {
-  using C = Wide<HD, QB, RW, W>;
-  constexpr int S = HD / 32, RT = C::RT, KW = C::KW, D = C::D, N = C::kLoads, T = C::kThreads;
+  using C = Wide<HD, QB, W>;
+  constexpr int S = HD / 32, D = C::D, N = C::kLoads, T = C::kThreads;
   extern __shared__ __align__(16) uint8_t smem_raw[];
-  uint4* ring = reinterpret_cast<uint4*>(smem_raw);  // [2][KW][kPieces]
+  uint4* ring = reinterpret_cast<uint4*>(smem_raw);  // [2][kPieces]
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // (wave i runs on SIMD i % 4: the waves of the first rows, which every request has, are spread)
-  const int rw = KW == 2 ? (wave & 1) + 2 * (wave >> 2) : wave / KW, kw = KW == 2 ? wave >> 1 & 1 : wave % KW;
   Part w;
   if (!w.init(p, tid)) return;
   if (p.WG == 0 && w.rb == 0 && w.n < p.R) zero_rows<HD, QB>(p, w.b, w.kvh, w.n, tid, T);
   if (w.rb * C::kRows >= w.rows || w.lo >= w.hi) return;
-  const int r0 = (w.rb * RW + rw) * RT * 16;
+  const int r0 = w.rb * C::kRows + wave * C::kWaveRows;
   const bool work = r0 < w.rows;
   KvLoader<HD> ld;
   ld.init(p.cache, (int64_t)w.head);
-  std::conditional_t<QB, Rows32<HD>, Rows<HD, QB, RT>> R;
+  std::conditional_t<QB, Rows32<HD>, Rows<HD, QB, 1>> R;
   R.load(p, w, r0, lane);
-  // Piece e T + tid of a round: of block e T / kPieces of it, keys before values.  Which of them
-  // follows from e or (T pieces are a whole block) from the wave: no load is under a branch, or
-  // the wait for one would be a wait for all.
+  // Piece e T + tid of a block, keys before values.  Which of them follows from e or (T pieces
+  // are a whole block) from the wave: no load is under a branch, or the wait for one would be a
+  // wait for all.
   const bool keys = wave < 2 * S;
   const Rsrc mine = keys ? ld.k : ld.v;
-  auto load = [&](int round, int e) {
-    const int blk = w.lo + round * KW + e * T / C::kPieces, f0 = e * T % C::kPieces / 64;
+  auto load = [&](int blk, int e) {
+    const int f0 = e * T / 64;
     const bool there = blk < w.hi;
     if (f0 + W <= 2 * S) return ld.key(blk, f0 + wave, lane, there);
     if (f0 >= 2 * S) return ld.value(blk, f0 + wave - 2 * S, lane, there);
@@ -1119,53 +1090,51 @@ __global__ void __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(2))
   };
   uint4 reg[D][N];
 #pragma unroll
-  for (int e = 0; e < N; ++e) ring[e * T + tid] = load(0, e);
+  for (int e = 0; e < N; ++e) ring[e * T + tid] = load(w.lo, e);
 #pragma unroll
   for (int d = 0; d < D; ++d)
 #pragma unroll
-    for (int e = 0; e < N; ++e) reg[d][e] = load(1 + d, e);
-  if (32 * w.hi > w.L && work) R.load_ancestors(p, w, r0, lane, w.kvh == 0 && r0 == 0 && kw == 0 && w.hi == w.nb);
+    for (int e = 0; e < N; ++e) reg[d][e] = load(w.lo + 1 + d, e);
+  if (32 * w.hi > w.L && work) R.load_ancestors(p, w, r0, lane, w.kvh == 0 && r0 == 0 && w.hi == w.nb);
   const float sl = p.scale * kLog2e;
-  const int rounds = (w.hi - w.lo + KW - 1) / KW;
-  auto round = [&](auto tail, int it, uint4 (&next_regs)[N]) {
-    uint4* next = ring + ((it + 1) & 1) * (KW * C::kPieces);
+  auto block = [&](auto tail, int it, uint4 (&next_regs)[N]) {
+    uint4* next = ring + ((it + 1) & 1) * C::kPieces;
 #pragma unroll
     for (int e = 0; e < N; ++e) next[e * T + tid] = next_regs[e];
 #pragma unroll
-    for (int e = 0; e < N; ++e) next_regs[e] = load(it + 1 + D, e);
-    const int blk = w.lo + it * KW + kw;
-    if (blk < w.hi && work) {
-      const uint4* here = ring + (it & 1) * (KW * C::kPieces) + kw * C::kPieces;
+    for (int e = 0; e < N; ++e) next_regs[e] = load(w.lo + it + 1 + D, e);
+    if (work) {
+      const uint4* here = ring + (it & 1) * C::kPieces;
       if constexpr (QB) {
-        R.template step<decltype(tail)::value>(blk, w, sl, lane, here);
+        R.template step<decltype(tail)::value>(w.lo + it, w, sl, lane, here);
       } else {
         R.template step<decltype(tail)::value>(
-            blk, w, sl, lane, [&](int u, int s) { return here[(u * S + s) * 64 + lane]; },
+            w.lo + it, w, sl, lane, [&](int u, int s) { return here[(u * S + s) * 64 + lane]; },
             [&](int t) { return here[(2 * S + t) * 64 + lane]; });
       }
     }
     __syncthreads();
   };
   __syncthreads();
-  // rounds whose blocks every row sees, D at a time (the registers' turn); the rest with the masks
-  const int full = min(max((w.L / 32 - w.lo) / KW, 0), rounds) / D * D;
+  // blocks that every row sees, D at a time (the registers' turn); the rest with the masks
+  const int count = w.hi - w.lo, full = min(max(w.L / 32 - w.lo, 0), count) / D * D;
   for (int it = 0; it < full; it += D)
 #pragma unroll
-    for (int d = 0; d < D; ++d) round(std::false_type{}, it + d, reg[d]);
-  for (int it = full; it < rounds; it += D)
+    for (int d = 0; d < D; ++d) block(std::false_type{}, it + d, reg[d]);
+  for (int it = full; it < count; it += D)
 #pragma unroll
     for (int d = 0; d < D; ++d) {
-      if (it + d >= rounds) break;
-      round(std::true_type{}, it + d, reg[d]);
+      if (it + d >= count) break;
+      block(std::true_type{}, it + d, reg[d]);
     }
   if (__any(R.broken))
-    for (int e = w.lo + kw; e < w.hi; e += KW)
-      if (32 * e + 32 > w.L) R.mend(ld, e, w, lane);
-  if constexpr (QB) join32<HD, RW, KW>(p, w, R, *reinterpret_cast<JoinSmem32<HD, W>*>(smem_raw), rw, kw, tid);
-  else join<HD, QB, RT, RW, KW>(p, w, R, *reinterpret_cast<JoinSmem<HD, RT, W>*>(smem_raw), rw, kw, tid);
+    for (int e = max(w.lo, w.L / 32); e < w.hi; ++e) R.mend(ld, e, w, lane);
+  put_rows<HD>(p, w, R, r0, lane);
 }
 
-// The splits of a row, in order: GR groups of HD / 4 lanes take every GR-th one.
+// The splits of a row, in order: GR groups of HD / 4 lanes take every GR-th one.  Bound
+// by memory: 16 requests of 32 rows and 32 heads over about four splits read 34 MB in
+// 7.6 us (4.4 TB/s); one request's 64 splits take 10.8, most of it three round trips.
 template <int HD, bool QB, int GR>
 __global__ void __launch_bounds__(256) tree_merge_kernel(TreeAttend p) {
   constexpr int LPR = HD / 4, PER = 256 / LPR / GR;  // rows of a workgroup
@@ -1239,7 +1208,10 @@ __global__ void __launch_bounds__(256) tree_merge_kernel(TreeAttend p) {
 // ---------------------------------------------------------------------------
 // Commit.  A wave walks a request's tree: lane i holds node i, a vote finds the
 // lowest child of the present node whose token is the drawn one.  Children come
-// after their parents, so the walk ends.
+// after their parents, so the walk ends.  Bound by latency: the walk 1.8 us for one
+// request, 3.5 for 16; the moves 4 us for a layer of one request, 16 for 8 layers of 16
+// requests of 8 heads (2048 workgroups, each two dependent round trips; values are
+// 2-byte elements of 16-byte pieces).
 // ---------------------------------------------------------------------------
 __global__ void __launch_bounds__(64) tree_walk_kernel(TreeCommit p) {
   const int b = blockIdx.x, lane = threadIdx.x;
@@ -1393,23 +1365,46 @@ hipError_t attend_with(TreeAttend a, int tile, int wgs, int threads, size_t lds,
 template <int HD, bool QB, int RT>
 hipError_t attend_few(const TreeAttend& a, hipStream_t st) {
   return attend_with<HD, QB, tree_attend_kernel<HD, QB, RT>>(a, RT * 16, RT == 1 ? 512 : 256, kWaves * 64,
-                                                            sizeof(JoinSmem<HD, RT, kWaves>), st);
+                                                            sizeof(JoinSmem<HD, RT>), st);
 }
-template <int HD, bool QB, int RW, int W>
+template <int HD, bool QB, int W>
 hipError_t attend_wide(const TreeAttend& a, hipStream_t st) {
-  using C = Wide<HD, QB, RW, W>;
-  return attend_with<HD, QB, tree_attend_wide_kernel<HD, QB, RW, W>>(a, C::kRows, 2048 / W, C::kThreads, C::kSmem, st);
+  using C = Wide<HD, QB, W>;
+  return attend_with<HD, QB, tree_attend_wide_kernel<HD, QB, W>>(a, C::kRows, 2048 / W, C::kThreads, C::kSmem, st);
 }
 
+// Which kernel.  Few rows a workgroup cost its keys again for every 16 or 32 rows, from
+// L2; many cost waves that wait at barriers and a part of the chip where the keys are
+// few.  us with 4 query heads on each of 8 K/V heads of 128, bfloat16 calls (kernel by
+// the rows of a workgroup):
+//   requests x keys, rows of a K/V head      16     32     128     256
+//   1 x 2048,   64                         13.6   14.8    16.1    18.0
+//              256                         18.1   19.5    23.2    31.1
+//   1 x 8192,  128                         24.2   23.1    28.8    24.2
+//   1 x 32768,  32                         49.6   32.2    34.9    36.5
+//               64                         50.2   33.0    38.7    39.7
+//              256                         92.9   76.5    71.9    67.8
+//   16 x 2048,  64                         30.0   29.5    38.9    39.9
+//              128                         51.9   51.7    48.4    47.4
+//              256                         94.4   96.6    76.5    72.5
+//   64 x 512,   32                         29.3   36.7    30.1    42.5
+//               64                         45.1   57.4    34.2    45.4
+//              256                         153     206    76.4    84.7
+// and 128 rows over 16 ragged contexts of 256 to 4096 55.9 / 57.7 / 45.6 / 50.1.
+// float32 calls, whose wide kernels have half the rows: 1 x 8192, 256 rows 40.0 / 42.4 /
+// 41.1 / 40.9; 1 x 32768, 32 rows 51.6 / 34.2 / 37.5 / 39.7, 256 rows 106 / 102 / 107 / 101.
 template <int HD, bool QB>
 hipError_t attend_t(const TreeAttend& a, hipStream_t st) {
   const int tiles = (a.G * a.R + 15) / 16;
-  if (tiles == 1) return attend_few<HD, QB, 1>(a, st);
-  if (tiles == 2) return attend_few<HD, QB, 2>(a, st);
-  constexpr int RT = QB ? 2 : 1;
-  if (tiles <= 2 * RT) return attend_wide<HD, QB, 2, 8>(a, st);
-  if (tiles <= 4 * RT) return attend_wide<HD, QB, 4, 4>(a, st);
-  return attend_wide<HD, QB, 8, 8>(a, st);
+  const int64_t heads = (int64_t)a.B * a.KVH;
+  if (heads * ((tiles + 3) / 4) >= 512)  // no split
+    return tiles <= 2 ? attend_few<HD, QB, 1>(a, st) : attend_wide<HD, QB, 4>(a, st);
+  // blocks of keys times tiles of rows, for each workgroup of one round
+  const int64_t work = heads * tiles * ((a.max_keys + 31) / 32) / 512;
+  if (tiles == 1 || work <= 16) return attend_few<HD, QB, 1>(a, st);
+  if (tiles <= 4 || work <= 96) return attend_few<HD, QB, 2>(a, st);
+  if (QB && tiles <= 8) return attend_wide<HD, QB, 4>(a, st);
+  return attend_wide<HD, QB, 8>(a, st);
 }
 
 }  // namespace

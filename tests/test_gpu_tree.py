@@ -275,6 +275,61 @@ def test_attend_large_batches(b, r, h, kvh, dtype):
     assert torch.equal(out, again)
 
 
+def check_picks(picks, kvh, q, k, v, lens, rows, parents, out, dtype):
+    """Like check_attend, for some (request, row, query head) of many."""
+    h, hd = q.shape[2:]
+    scale = hd ** -0.5
+    for i, j, x in picks:
+        if j >= rows[i]:
+            assert not out[i, j, x].any()
+            continue
+        see = list(range(lens[i])) + [lens[i] + a for a in otree.lineage(parents[i], j)]
+        kk, vv = (f64(t[i, :, x // (h // kvh)])[see] for t in (k, v))
+        qq = f64(q[i, j, x])
+        want = otree.attend(qq, kk, vv, scale)
+        dz = 24 * U * scale * (np.abs(kk) @ np.abs(qq)).max() + 2 * U * scale * np.abs(kk @ qq).max()
+        tol = 2 * np.abs(vv).max() * (2.1 * dz + 2.0 ** -22 + (3 * len(see) / 32 + 8) * U + (2.0 ** -17 if dtype == "bf16" else U))
+        tol = tol + np.abs(want) * (HALF if dtype == "bf16" else U)
+        err = np.abs(f64(out[i, j, x]) - want)
+        assert (err <= tol).all(), (i, j, x, err.max(), tol.min())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("b,r,h,kvh,n", [(1, 33, 32, 32, 2900), (2, 64, 64, 64, 700), (1, 40, 200, 100, 3300), (2, 20, 80, 20, 4000),
+                                         (1, 64, 32, 8, 13000), (4, 40, 128, 64, 150), (9, 61, 64, 64, 97), (3, 17, 200, 200, 40)])
+def test_attend_many_rows(b, r, h, kvh, n, hd, dtype):
+    """Trees of up to 64 nodes over heads and contexts enough that every kernel has its
+    turn; ragged lengths, NaN in a row that only its descendants see."""
+    rng = np.random.default_rng(n + hd)
+    cache = tree.TreeCache(1, b, h, kvh, hd, n + r, max_rows=r, device=DEV)
+    poison(cache)
+    lens = [n] + [int(x) for x in rng.integers(0, n + 1, b - 1)]
+    used = [r] + [int(x) for x in rng.integers(1, r + 1, b - 1)]
+    gen = torch.Generator(device=DEV).manual_seed(n)
+    k, v = (torch.randn(b, n + r, kvh, hd, generator=gen, device=DEV).bfloat16() for _ in range(2))
+    cache.append(0, k, v, rows=i32([x + m for x, m in zip(lens, used)]))
+    cache.lens.copy_(i32(lens))
+    q = torch.randn(b, r, h, hd, generator=gen, device=DEV).to(TD[dtype])
+    parents = [a_tree(rng, r) for _ in range(b)]
+    out = cache.attend(0, q, parents=i32(parents), rows=i32(used))
+    picks = [(int(rng.integers(b)), int(rng.integers(r)), int(rng.integers(h))) for _ in range(60)]
+    picks += [(0, 0, 0), (0, r - 1, h - 1), (b - 1, r - 1, 0), (b - 1, used[-1] - 1, h - 1)]
+    check_picks(picks, kvh, q, k, v, lens, used, parents, out, dtype)
+    assert torch.isfinite(out.float()).all() and cache.device_error() == 0
+    bad = r // 2
+    broken = v.clone()
+    broken[0, n + bad, kvh - 1, 7] = float("nan")
+    cache.lens.zero_()
+    cache.append(0, k, broken, rows=i32([x + m for x, m in zip(lens, used)]))
+    cache.lens.copy_(i32(lens))
+    again = cache.attend(0, q, parents=i32(parents), rows=i32(used))
+    see = [i for i in range(r) if bad in otree.lineage(parents[0], i)]
+    mask = torch.zeros_like(out, dtype=torch.bool)
+    mask[0, see, h - h // kvh:, 7] = True
+    assert torch.isnan(again)[mask].all() and torch.equal(again[~mask], out[~mask])
+
+
 def test_attend_strided_rows():
     """Queries of a fused projection, outputs between other columns."""
     rng = np.random.default_rng(11)

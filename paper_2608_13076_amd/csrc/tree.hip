@@ -404,11 +404,14 @@ __device__ __forceinline__ void zero_rows(const TreeAttend& p, int b, int kvh, i
 // With keys enough and few heads the keys are split: the workgroups, WG at most (one
 // round), have equal counts of blocks of 32 positions whatever the requests' lengths.
 // The count follows from all of them: the least CB for which the splits of all heads and
-// tiles of rows fit (kLeast at least, two rounds of a wave).  Every wave works it out
+// tiles of rows fit (kLeast at least, four rounds of a wave).  Every wave works it out
 // from the lengths, the first workgroup leaves it for the merge.  16 ragged contexts of
 // 256 to 4096 (8 heads, 128 rows) take 45 us with their merge; with as many splits for
-// every request, and loads under branches, they took 66.
-constexpr int kLeast = 8;
+// every request, and loads under branches, they took 66.  kLeast of 8 / 16 / 24 / 32, us
+// with the merge, 4 query heads on each of 8 K/V heads, bfloat16: 1 x 2048 keys, 64 rows
+// 13.6 / 11.2 / 12.8 / 13.0; 1 x 8192, 16 rows 15.7 / 12.6 / 14.3 / 14.3, 32 rows 17.9 / 16.2 /
+// 14.5 / 14.6; 1 x 32768, 128 rows 47 / 48 / 51 / 58; 16 x 2048 the same.
+constexpr int kLeast = 16;
 struct Part {
   unsigned head;
   int b, kvh, rb, L, n, rows, nb, lo, hi;
@@ -1134,7 +1137,8 @@ __global__ void __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(2))
 
 // The splits of a row, in order: GR groups of HD / 4 lanes take every GR-th one.  Bound
 // by memory: 16 requests of 32 rows and 32 heads over about four splits read 34 MB in
-// 7.6 us (4.4 TB/s); one request's 64 splits take 10.8, most of it three round trips.
+// 7.6 us (4.4 TB/s; by eight groups 24); one request's 64 splits take 10.8, most of it
+// three round trips (by one group 17).
 template <int HD, bool QB, int GR>
 __global__ void __launch_bounds__(256) tree_merge_kernel(TreeAttend p) {
   constexpr int LPR = HD / 4, PER = 256 / LPR / GR;  // rows of a workgroup

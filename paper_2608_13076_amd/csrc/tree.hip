@@ -31,16 +31,30 @@ __device__ __forceinline__ float hi_f(uint32_t w) { return __uint_as_float(w & 0
 // lengths come from the caller's device memory: sums stop at the type's ends
 __device__ __forceinline__ int add_sat(int a, int b) { return __builtin_elementwise_add_sat(a, b); }
 
-template <bool BF16>
+// STREAM: what a large call reads or writes once goes past the caches.
+typedef __attribute__((ext_vector_type(2))) uint32_t Words2;
+typedef __attribute__((ext_vector_type(4))) float Floats4;
+template <bool STREAM, typename T>
+__device__ __forceinline__ T get(const T* p) {
+  if constexpr (STREAM) return __builtin_nontemporal_load(p);
+  else return *p;
+}
+template <bool STREAM, typename T>
+__device__ __forceinline__ void set(T* p, T v) {
+  if constexpr (STREAM) __builtin_nontemporal_store(v, p);
+  else *p = v;
+}
+
+template <bool BF16, bool STREAM = false>
 __device__ __forceinline__ void load4(const void* base, int64_t at, float* x) {
   if constexpr (BF16) {
-    const uint2 w = *(const uint2*)((const uint16_t*)base + at);
+    const Words2 w = get<STREAM>((const Words2*)((const uint16_t*)base + at));
     x[0] = lo_f(w.x);
     x[1] = hi_f(w.x);
     x[2] = lo_f(w.y);
     x[3] = hi_f(w.y);
   } else {
-    const float4 w = *(const float4*)((const float*)base + at);
+    const Floats4 w = get<STREAM>((const Floats4*)((const float*)base + at));
     x[0] = w.x;
     x[1] = w.y;
     x[2] = w.z;
@@ -48,10 +62,10 @@ __device__ __forceinline__ void load4(const void* base, int64_t at, float* x) {
   }
 }
 
-template <bool BF16>
+template <bool BF16, bool STREAM = false>
 __device__ __forceinline__ void store4(void* base, int64_t at, const float* x) {
-  if constexpr (BF16) *(uint2*)((uint16_t*)base + at) = make_uint2(pk_bf16(x[0], x[1]), pk_bf16(x[2], x[3]));
-  else *(float4*)((float*)base + at) = make_float4(x[0], x[1], x[2], x[3]);
+  if constexpr (BF16) set<STREAM>((Words2*)((uint16_t*)base + at), Words2{pk_bf16(x[0], x[1]), pk_bf16(x[2], x[3])});
+  else set<STREAM>((Floats4*)((float*)base + at), Floats4{x[0], x[1], x[2], x[3]});
 }
 
 // ---------------------------------------------------------------------------
@@ -69,13 +83,13 @@ __device__ __forceinline__ void store4(void* base, int64_t at, const float* x) {
 // positions, whole 16-byte pieces where the rows cover them.
 //
 // Bound by memory: 4003 rows of 32 + 32 heads of 128 in bfloat16 read and write
-// 197 MB in 55 us, 3.6 TB/s (a large copy: 5.1).  A wave that takes four heads of one
-// row instead, so that a line of keys is written from eight places, takes 78 us.
-// More loads in flight, other numbers of heads per workgroup (a twentieth to a
+// 197 MB in 46 us, 4.3 TB/s (a large copy: 5.1).  A wave that takes four heads of one
+// row instead, so that a line of keys is written from eight places, took 78 us where this
+// took 55 (both through the caches).  More loads in flight, other numbers of heads per workgroup (a twentieth to a
 // quarter of them) and 16-byte loads change less than a tenth; without the angles
 // it takes as long.
 // ---------------------------------------------------------------------------
-template <int HD, bool BF16>
+template <int HD, bool BF16, bool STREAM>
 __device__ __forceinline__ void append_qk(const TreeAppend& p, int block) {
   constexpr int LPH = HD / 8, RPW = 64 / LPH;  // lanes a head, rows a wave
   const int lane = threadIdx.x & 63, c = lane % LPH;
@@ -122,8 +136,8 @@ __device__ __forceinline__ void append_qk(const TreeAppend& p, int block) {
     const bool query = h < HQ;
     const int64_t in = row * (query ? p.q_ld : p.k_ld) + (query ? h : h - HQ) * HD;
     float a[4], d[4];
-    load4<BF16>(query ? p.q : p.k, in + f0, a);
-    load4<BF16>(query ? p.q : p.k, in + f1, d);
+    load4<BF16, STREAM>(query ? p.q : p.k, in + f0, a);
+    load4<BF16, STREAM>(query ? p.q : p.k, in + f1, d);
     if (turns) {
       if (p.interleaved) {
 #pragma unroll
@@ -144,8 +158,8 @@ __device__ __forceinline__ void append_qk(const TreeAppend& p, int block) {
       }
     }
     if (query) {
-      store4<BF16>(p.q_out, row * p.qo_ld + h * HD + f0, a);
-      store4<BF16>(p.q_out, row * p.qo_ld + h * HD + f1, d);
+      store4<BF16, STREAM>(p.q_out, row * p.qo_ld + h * HD + f0, a);
+      store4<BF16, STREAM>(p.q_out, row * p.qo_ld + h * HD + f1, d);
     } else if (fits) {
       uint16_t* dst = p.cache.k + ((int64_t)b * p.KVH + h - HQ) * p.cache.head_elems;
       store4<true>(dst, k_cache_index(f0, t, HD), a);
@@ -179,7 +193,7 @@ __device__ __forceinline__ bool octet_of(int64_t block, int B, int R, int KVH, c
   return o.h < KVH;
 }
 
-template <int HD, bool BF16>
+template <int HD, bool BF16, bool STREAM>
 __device__ __forceinline__ void append_v(const TreeAppend& p, int64_t block) {
   Octet o;
   if (!octet_of<HD>(block, p.B, p.R, p.KVH, p.lens, o)) return;
@@ -194,10 +208,10 @@ __device__ __forceinline__ void append_v(const TreeAppend& p, int64_t block) {
       have |= 1u << e;
       const int64_t at = ((int64_t)o.b * p.R + i) * p.v_ld + o.h * HD + o.f;
       if constexpr (BF16) {
-        w[e] = *(const uint32_t*)((const uint16_t*)p.v + at);
+        w[e] = get<STREAM>((const uint32_t*)((const uint16_t*)p.v + at));
       } else {
-        const float2 x = *(const float2*)((const float*)p.v + at);
-        w[e] = pk_bf16(x.x, x.y);
+        const Words2 x = get<STREAM>((const Words2*)((const float*)p.v + at));
+        w[e] = pk_bf16(__uint_as_float(x.x), __uint_as_float(x.y));
       }
     }
   }
@@ -222,10 +236,10 @@ __device__ __forceinline__ void append_v(const TreeAppend& p, int64_t block) {
   }
 }
 
-template <int HD, bool BF16>
+template <int HD, bool BF16, bool STREAM>
 __global__ void __launch_bounds__(256) tree_append_kernel(TreeAppend p) {
-  if ((int)blockIdx.x < p.qk_blocks) append_qk<HD, BF16>(p, (int)blockIdx.x);
-  else append_v<HD, BF16>(p, (int64_t)blockIdx.x - p.qk_blocks);
+  if ((int)blockIdx.x < p.qk_blocks) append_qk<HD, BF16, STREAM>(p, (int)blockIdx.x);
+  else append_v<HD, BF16, STREAM>(p, (int64_t)blockIdx.x - p.qk_blocks);
 }
 
 // ---------------------------------------------------------------------------
@@ -1299,6 +1313,11 @@ __global__ void __launch_bounds__(kMoveThreads) tree_move_kernel(TreeCommit p) {
   }
 }
 
+// Inputs of more than this go past the caches (as do the queries).  us with / without, 4096
+// rows, inputs just written by another kernel: 32 + 2 x 8 heads of float32 (96 MB) 39 / 45, 32 +
+// 2 x 32 of float32 (192 MB) 58 / 70, of bfloat16 (96 MB) 57 / 52, inputs in memory 46 / 55; 2048
+// rows of 32 + 2 x 8 heads of float32 (48 MB) 21 / 18.
+constexpr int64_t kStreamBytes = 64 << 20;
 template <int HD, bool BF16>
 hipError_t append_t(TreeAppend a, hipStream_t st) {
   constexpr int VHPW = 64 / (HD / 2), RPG = 4 * 64 / (HD / 8);  // rows a workgroup
@@ -1310,7 +1329,11 @@ hipError_t append_t(TreeAppend a, hipStream_t st) {
   const int64_t vb = ((int64_t)a.B * ((a.R + 14) / 8) * ((a.KVH + VHPW - 1) / VHPW) + 3) / 4;
   if (qk + vb > 0x7fffffff) return hipErrorInvalidValue;
   a.qk_blocks = (int)qk;
-  hipLaunchKernelGGL((tree_append_kernel<HD, BF16>), dim3((unsigned)(qk + vb)), dim3(256), 0, st, a);
+  const dim3 grid((unsigned)(qk + vb)), block(256);
+  if (rows * (heads + a.KVH) * HD * (BF16 ? 2 : 4) > kStreamBytes)
+    hipLaunchKernelGGL((tree_append_kernel<HD, BF16, true>), grid, block, 0, st, a);
+  else
+    hipLaunchKernelGGL((tree_append_kernel<HD, BF16, false>), grid, block, 0, st, a);
   return hipGetLastError();
 }
 

@@ -123,6 +123,33 @@ def f64_freq(rope):
     return rope.freq.cpu().numpy()
 
 
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("dtype,hd,r", [("bf16", 128, 2100), ("f32", 128, 1300), ("bf16", 64, 4203), ("f32", 64, 2111)])
+def test_append_of_long_prompts_equals_its_pieces(dtype, hd, r, inter):
+    """A call of more than 64 MB, ragged and from strided rows, against calls of a few rows."""
+    b, h, kvh, step = 2, 32, 32, 307
+    gen = torch.Generator(device=DEV).manual_seed(r)
+    qkv = torch.randn(b, r, h + 2 * kvh, hd, generator=gen, device=DEV).to(TD[dtype])
+    q, k, v = qkv[:, :, :h], qkv[:, :, h:h + kvh], qkv[:, :, h + kvh:]
+    rope = tree.Rotary(tree.rotary_frequencies(hd, device=DEV)[0], inter)
+    big, small = (tree.TreeCache(1, b, h, kvh, hd, r + 40, max_rows=1, device=DEV) for _ in range(2))
+    rows = [r, r - 501]
+    for c in (big, small):
+        poison(c)
+        c.lens.copy_(i32([5, 33]))
+    out = torch.full((b, r, h, hd), 7.0, device=DEV).to(TD[dtype])
+    big.append(0, k, v, q=q, rope=rope, rows=i32(rows), q_out=out)
+    for s in range(0, r, step):
+        m = min(step, r - s)
+        part = small.append(0, *(t[:, s:s + m].contiguous() for t in (k, v)), q=q[:, s:s + m].contiguous(), rope=rope,
+                            rows=i32([max(0, min(m, n - s)) for n in rows]))
+        assert torch.equal(part, out[:, s:s + m])
+        small.lens += m
+    assert big.device_error() == 0 and small.device_error() == 0
+    for x, y in zip(big.read(0, r + 40), small.read(0, r + 40)):
+        assert torch.equal(x.view(torch.int16), y.view(torch.int16))
+
+
 def test_append_at_far_positions():
     """Angles of positions up to 2^30 keep their fraction of a turn."""
     rng = np.random.default_rng(5)

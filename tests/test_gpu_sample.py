@@ -322,6 +322,36 @@ def test_captured_draws():
         check(logits, u, x, tok, ch, 1, top_k=k.tolist(), top_p=p.tolist())
 
 
+def test_two_graphs_of_one_sampler():
+    """Graphs that share a workspace, replayed in turn on one stream, with an eager draw
+    of the same sampler in between."""
+    rng = np.random.default_rng(23)
+    rows, V = 7, 30011
+    s = sampling.Sampler(rows, V, device=DEV)
+    x, u = torch.zeros(rows, V, device=DEV), torch.zeros(rows, device=DEV)
+    sets = [dict(top_k=300, top_p=0.8), dict(top_p=0.97, temperature=2.5), dict(min_p=0.02)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        s.draw(x, u)
+    torch.cuda.current_stream().wait_stream(side)
+    graphs = []
+    for kw in sets:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = s.draw(x, u, **kw)
+        graphs.append((g, out))
+    for i in range(3):
+        x.copy_(torch.from_numpy(rng.normal(size=(rows, V)).astype(np.float32) * (1 + i)))
+        u.copy_(torch.from_numpy(rng.random(rows, np.float32)))
+        for (g, (tok, ch)), kw in list(zip(graphs, sets))[::-1 if i % 2 else 1]:
+            g.replay()
+            s.draw(x, u, temperature=0.0)
+            torch.cuda.synchronize()
+            check(x, u, None, tok, ch, rows, **{k: [v] for k, v in kw.items()})
+    assert s.device_error() == 0
+
+
 def test_draw_refuses():
     s = sampling.Sampler(4, 100, device=DEV)
     x, u = torch.zeros(4, 100, device=DEV), torch.zeros(4, device=DEV)

@@ -711,6 +711,40 @@ def test_a_captured_step_equals_the_eager_one():
         assert torch.equal(ka, kc) and torch.equal(va, vc)
 
 
+def test_two_graphs_of_one_workspace():
+    """Attention of few and of many rows captured over one cache, replayed in turn while
+    the lengths change."""
+    rng = np.random.default_rng(10)
+    cache = tree.TreeCache(1, 3, 16, 4, 64, 6000, max_rows=64, device=DEV)
+    k, v = (torch.from_numpy(rng.normal(size=(3, 6000, 4, 64)).astype(np.float32)).to(DEV) for _ in range(2))
+    cache.append(0, k, v)
+    par = [i32([a_tree(rng, r) for _ in range(3)]) for r in (3, 64)]
+    qs = [rand(rng, 3, r, 16, 64, dtype="bf16") for r in (3, 64)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for q, p in zip(qs, par):
+            cache.attend(0, q, parents=p)
+    torch.cuda.current_stream().wait_stream(side)
+    graphs = []
+    for q, p in zip(qs, par):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = cache.attend(0, q, parents=p)
+        graphs.append((g, out))
+    other = tree.TreeCache(1, 3, 16, 4, 64, 6000, max_rows=64, device=DEV, buf=cache.buf)
+    for lens in ([5000, 1, 700], [0, 0, 0], [5936, 5936, 5936], [64, 4000, 31]):
+        cache.lens.copy_(i32(lens))
+        other.lens.copy_(i32(lens))
+        for g, _ in graphs + graphs[::-1]:
+            g.replay()
+        want = [other.attend(0, q, parents=p) for q, p in zip(qs, par)]
+        torch.cuda.synchronize()
+        for (_, out), w in zip(graphs, want):
+            assert torch.equal(out, w)
+    assert cache.device_error() == 0 and other.device_error() == 0
+
+
 def test_calls_on_another_stream():
     """Caches and samplers of their own on two streams at once."""
     rng = np.random.default_rng(9)

@@ -16,11 +16,13 @@ constexpr int kSampleParts = 32;    // most workgroups of a row in the second pa
 // What the passes of a row hand on.
 struct SampleRow {
   double mass;    // of the tokens above bin `lo`, over the largest weight
-  double total;   // of all
+  double total;   // of all (tail: but those of the window's last bin)
   float max;
   int lo, hi;     // bins whose tokens are listed (below the top bin)
   int above;      // tokens above bin lo
   int k_in;       // whether the first top_k end in the list
+  int bits;       // of a listed weight, an integer of 2^-bits of the first listed bin's edge
+  int tail;       // whether the weight of the window's last bin is added up by itself
   int sub;        // bits of a place of these bins below a part of theirs (-1: their tokens are listed)
   float least, below;  // logits of these bins: from `least` on, below `below`
   double inv_T, cut, inv_sum;  // probabilities: exp(-d) inv_sum where d <= cut
@@ -58,6 +60,7 @@ struct SampleArgs {
   double* sum;          // ... the weight of its kept tokens
   SampleRow* row;       // [rows]
   uint32_t* count;      // [rows] listed tokens
+  uint64_t* tail;       // [rows] weight in the window's last bin
   uint2* list;          // [rows][kSampleList] token and logit
   uint64_t* sub_mass;   // [rows][kSampleSub] weight of a part of the border's bins
   uint32_t* sub_count;  // ... its tokens

@@ -43,6 +43,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr double kSpan = 32.0;                       // of d: weights from e^-32 on
 constexpr double kBinsPerUnit = 126.0 / kSpan, kBin = kSpan / 126.0;
+constexpr int kLastBin = 126;                        // the last one that the window reaches, to the top's place in its own
 constexpr int kSteps = 256;                          // of the table of a bin's weights
 constexpr double kSlack = 0x1p-40;                   // of top_p: equal masses count as reached
 
@@ -168,11 +169,15 @@ __device__ __forceinline__ uint64_t fixed(double w) {
   return (uint64_t)__double_as_longlong(__builtin_fma(w, (double)(1ull << N), 0x1p52)) & 0xfffffffffffffull;
 }
 constexpr int kMassBits = 38;  // of a slice's bins: 4096 weights up to 1 below the count at bit 51
-constexpr int kListBits = 40;  // of a listed weight: 2^20 of them stay below 2^61
-// A listed token's weight over that of the first listed bin's edge: in the bins' own steps
-// first, so that equal weights add up to exactly what the bins hold.
-__device__ __forceinline__ uint64_t listed_weight(const double* table, int step, float rest, double rel) {
-  return fixed<kListBits>((double)fixed<kMassBits>(place_weight(table, step, rest)) * 0x1p-38 * rel);
+// A listed token's weight over that of the first listed bin's edge, times `scale` (2^bits):
+// in the bins' own steps first, so that equal weights add up to exactly what the bins
+// hold.  The row's bits are as many as all the listed weights leave in 63, 50 at most: a list
+// from the largest weight down to e^-32 of it keeps sums to 2^-50 a token.
+constexpr int kListBits = 50;
+__device__ __forceinline__ double power_of_2(int n) { return __longlong_as_double((long long)(1023 + n) << 52); }
+__device__ __forceinline__ uint64_t listed_weight(const double* table, int step, float rest, double rel, double scale) {
+  const double w = (double)fixed<kMassBits>(place_weight(table, step, rest)) * 0x1p-38 * rel;
+  return (uint64_t)__double_as_longlong(__builtin_fma(w, scale, 0x1p52)) & 0xfffffffffffffull;
 }
 // A place of the listed bins, j below the first of them, in steps from its upper edge.
 __device__ __forceinline__ int listed_place(int j, int step) { return j * kSteps + (kSteps - 1 - step); }
@@ -379,7 +384,10 @@ __global__ void __launch_bounds__(kThreads) sample_slice_kernel(SampleArgs a) {
   const int64_t at = (int64_t)row * a.NS + s;
   if (tid == 0) {
     a.smax[at] = m;
-    if (s == 0) a.count[row] = 0;
+    if (s == 0) {
+      a.count[row] = 0;
+      a.tail[row] = 0;
+    }
   }
   if (s == 0 && q.listed())
     for (int i = tid; i < kSampleSub; i += kThreads) {
@@ -530,7 +538,7 @@ __global__ void __launch_bounds__(kThreads) sample_scan_kernel(SampleArgs a) {
       uint64_t w[16];
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const int s = s0 + 2 * e, jj = s < a.NS ? j - sm.off[s] : -1;
+        const int s = s0 + 2 * e, jj = s < a.NS && j <= kLastBin ? j - sm.off[s] : -1;
         w[e] = jj >= 0 ? h[s * kSampleBins + jj] : 0ull;
       }
 #pragma unroll
@@ -566,7 +574,9 @@ __global__ void __launch_bounds__(kThreads) sample_scan_kernel(SampleArgs a) {
         return 2 * l + (from_lane((int)f0, l) ? 0 : 1);
       };
       int k_bin = kSampleBins - 1, k_in = 0;
-      double least = total, most = total;  // of the weight that top_p refers to
+      // The window ends within its last bin: what that holds in all is only a bound.
+      const double last = from_lane(w[kLastBin & 1], kLastBin >> 1);
+      double least = total - last, most = total;  // of the weight that top_p refers to
       if (q.use_k && from_lane(ci[1], 63) > q.top_k) {  // (else all are among the first top_k)
         k_in = 1;
         k_bin = first(ci[0] >= q.top_k, ci[1] >= q.top_k);
@@ -582,18 +592,22 @@ __global__ void __launch_bounds__(kThreads) sample_scan_kernel(SampleArgs a) {
         if (k_in) hi = k_bin;  // the first top_k tokens' weight ends there
       }
       const double in = from_lane(lo & 1 ? wi[1] : wi[0], lo >> 1), ex = in - from_lane(lo & 1 ? w[1] : w[0], lo >> 1);
+      const double upto = from_lane(hi & 1 ? wi[1] : wi[0], hi >> 1);
       const int above = from_lane(lo & 1 ? ci[1] : ci[0], lo >> 1) - from_lane(lo & 1 ? c[1] : c[0], lo >> 1);
       // more than the list holds: their counts and weights by finer parts instead
       const int n = from_lane(hi & 1 ? ci[1] : ci[0], hi >> 1) - above, span = (hi - lo + 1) * kSteps;
       const int sub = n > kSampleList ? max(0, 32 - __clz(span - 1) - kSubBits) : -1;
       if (lane == 0) {
         sm.row.mass = lo == 0 ? 0.0 : ex;
-        sm.row.total = total;
+        sm.row.tail = q.use_p && !k_in && last > total * 0x1p-46;
+        sm.row.total = sm.row.tail ? total - last : total;
         sm.row.lo = lo;
         sm.row.hi = hi;
         sm.row.above = above;
         sm.row.k_in = k_in;
         sm.row.sub = sub;
+        const int exponent = (int)(__double_as_longlong((upto - sm.row.mass) / sm.factor[lo]) >> 52) - 1022;
+        sm.row.bits = min(kListBits, 62 - max(exponent, 0));
       }
     }
     __syncthreads();
@@ -609,12 +623,14 @@ __global__ void __launch_bounds__(kThreads) sample_scan_kernel(SampleArgs a) {
     float rest;
     return least_logit((grid.top - bin) * kSteps / grid.c, [&](float l) { return grid.place(l, step, rest) <= bin; });
   };
-  float t_window = -FLT_MAX, t_list = -FLT_MAX, t_sure = -FLT_MAX, t_min = -FLT_MAX;
+  float t_window = -FLT_MAX, t_list = -FLT_MAX, t_sure = -FLT_MAX, t_min = -FLT_MAX, t_tail = -FLT_MAX;
+  const bool tail = q.listed() && sm.row.tail;
   if (inv_T > 0.0) {
     t_window = within(kSpan);
     if (q.min_d < kSpan) t_min = within(q.min_d);
     if (hi < kSampleBins - 1) t_list = from_bin(hi);
     if (lo < kSampleBins) t_sure = lo > 0 ? from_bin(lo - 1) : INFINITY;
+    if (tail) t_tail = from_bin(kLastBin - 1);
   } else if (q.listed()) {
     t_sure = INFINITY;  // (all logits are in one bin)
   }
@@ -625,7 +641,7 @@ __global__ void __launch_bounds__(kThreads) sample_scan_kernel(SampleArgs a) {
     if (!q.listed()) {
       r.mass = r.total = 0.0;
       r.lo = r.hi = kSampleBins;
-      r.above = r.k_in = 0;
+      r.above = r.k_in = r.tail = 0;
       r.sub = -1;
     }
     r.max = M;
@@ -644,8 +660,10 @@ __global__ void __launch_bounds__(kThreads) sample_scan_kernel(SampleArgs a) {
   }
   const uint64_t z0 = (uint64_t)__float_as_uint(a.u[row]);
   Race race;
+  const double scale = q.listed() ? power_of_2(sm.row.bits) : 0.0;
   double sum = 0.0;
-  const int s1 = min(a.NS, (part + 1) * a.spw), reach = min(hi, kSampleBins - 1);
+  uint64_t in_tail = 0;
+  const int s1 = min(a.NS, (part + 1) * a.spw), reach = tail ? kLastBin : min(hi, kSampleBins - 1);
   // the slices that reach these bins, one ahead
   auto after = [&](int s) {
     while (s < s1 && sm.off[s] > reach) ++s;
@@ -668,6 +686,19 @@ __global__ void __launch_bounds__(kThreads) sample_scan_kernel(SampleArgs a) {
       const bool above = x[k] >= t_sure;
       sure |= (above && x[k] >= t_min ? 1u : 0u) << k;
       listed |= (!above && x[k] >= t_list && q.listed() ? 1u : 0u) << k;
+    }
+    if (tail) {
+      uint32_t in = 0;
+#pragma unroll
+      for (int k = 0; k < 16; ++k) in |= (x[k] >= t_window && x[k] < t_tail ? 1u : 0u) << k;
+      while (in != 0) {
+        const int k = __builtin_ctz(in);
+        in &= in - 1;
+        int step;
+        float rest;
+        grid.place(sm.x[k][tid], step, rest);
+        in_tail += fixed<kMassBits>(place_weight(sm.table, step, rest));
+      }
     }
     // the tokens above, every lane its own
     while (__any(sure != 0)) {
@@ -693,7 +724,7 @@ __global__ void __launch_bounds__(kThreads) sample_scan_kernel(SampleArgs a) {
         float rest;
         const int j = min(max(grid.place(sm.x[k][tid], step, rest) - lo, 0), hi - lo);
         const int at = listed_place(j, step) >> sub;
-        atomicAdd((unsigned long long*)(sub_mass + at), (unsigned long long)listed_weight(sm.table, step, rest, kTables.rel[j]));
+        atomicAdd((unsigned long long*)(sub_mass + at), (unsigned long long)listed_weight(sm.table, step, rest, kTables.rel[j], scale));
         atomicAdd(sub_count + at, 1u);
       }
     } else if (__any(listed != 0)) {
@@ -710,6 +741,10 @@ __global__ void __launch_bounds__(kThreads) sample_scan_kernel(SampleArgs a) {
           ++at;
         }
     }
+  }
+  if (tail) {
+    in_tail = from_lane(prefix_sum(in_tail), 63);
+    if (lane == 0 && in_tail != 0) atomicAdd((unsigned long long*)(a.tail + row), (unsigned long long)in_tail);
   }
   if (sub >= 0) {
     __syncthreads();
@@ -764,6 +799,7 @@ struct Tokens {
   double M, inv_T;
   Grid grid;
   int lo, hi;
+  double scale;
   __device__ __forceinline__ void stage(uint2 e, double step, double rel) {
     if (tid < kSteps) sm.table[tid] = step;
     if (tid < kSampleBins) sm.factor[tid] = rel;
@@ -781,7 +817,7 @@ struct Tokens {
     int step;
     float rest;
     const int j = min(max(grid.place(l, step, rest) - lo, 0), kSampleBins - 1);
-    return listed_weight(sm.table, step, rest, sm.factor[j]);
+    return listed_weight(sm.table, step, rest, sm.factor[j], scale);
   }
   // f(id, key, weight()) of every listed token
   template <typename F>
@@ -815,7 +851,7 @@ struct Tokens {
 // us, 400 rows) the second one pays.
 template <bool BF16>
 __device__ __forceinline__ void narrow(Tokens<BF16>& ls, FinishSmem& sm, int tid, const Request& q, SampleRow& r, uint64_t z0,
-                                       double factor, Race& race, uint64_t& sum) {
+                                       double unit, Race& race, uint64_t& sum) {
   const SampleArgs& a = ls.a;
   const int lane = tid & 63, wave = tid >> 6;
   const bool mine = tid < kSampleSub;
@@ -851,7 +887,6 @@ __device__ __forceinline__ void narrow(Tokens<BF16>& ls, FinishSmem& sm, int tid
   int lo = sm.k_part, hi = lo;
   if (q.use_p) {
     // (a little more on either side, as for the bins)
-    const double unit = factor * 0x1p-40;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       const double of = r.k_in ? r.mass + (double)sm.k_mass[e] * unit : r.total;
@@ -885,7 +920,7 @@ __device__ __forceinline__ void narrow(Tokens<BF16>& ls, FinishSmem& sm, int tid
       const int j = min(max(ls.grid.place(l, step, rest) - ls.lo, 0), ls.hi - ls.lo), part = listed_place(j, step) >> r.sub;
       if (part > hi) continue;
       const int id = token_of<BF16>(s * kSampleSlice, tid % kThreads, k);
-      const uint64_t wl = listed_weight(sm.table, step, rest, sm.factor[j]);
+      const uint64_t wl = listed_weight(sm.table, step, rest, sm.factor[j], ls.scale);
       if (part >= lo) {
         const uint32_t i = atomicAdd(&sm.count, 1u);
         if (i < kStaged) {
@@ -898,7 +933,7 @@ __device__ __forceinline__ void narrow(Tokens<BF16>& ls, FinishSmem& sm, int tid
       if (d <= q.min_d) {
         weight += wl;
         const uint32_t xn = noise_bits(z0 + (uint64_t)(id + 1) * kGolden);
-        drawn.enter(id, d, __builtin_amdgcn_rcpf(fmaxf((float)((double)wl * 0x1p-40 * factor), 1e-14f)), xn, noise_rest(xn));
+        drawn.enter(id, d, __builtin_amdgcn_rcpf(fmaxf((float)((double)wl * unit), 1e-14f)), xn, noise_rest(xn));
       }
     }
     drawn.share();
@@ -909,7 +944,7 @@ __device__ __forceinline__ void narrow(Tokens<BF16>& ls, FinishSmem& sm, int tid
   race = drawn;
   sum = weight;
   r.above += (int)sm.cnt_before;
-  r.mass += (double)sm.mass_before * 0x1p-40 * factor;
+  r.mass += (double)sm.mass_before * unit;
 }
 
 // The digit at which `target` (a count, or a weight) is reached, from the highest
@@ -1022,7 +1057,7 @@ __device__ __forceinline__ uint64_t quad_sum(uint64_t v) {
 }
 static_assert(kPer == 4, "quad_sum");
 __device__ __forceinline__ void border_of_few(FinishSmem& sm, int tid, uint32_t n, const Request& q, const SampleRow& r,
-                                              double factor, uint32_t& key, uint32_t& id_to) {
+                                              double unit, uint32_t& key, uint32_t& id_to) {
   const uint32_t i = (uint32_t)tid / kPer;
   const bool mine = i < n;
   const uint2 e = sm.list[mine ? i : 0];
@@ -1051,8 +1086,8 @@ __device__ __forceinline__ void border_of_few(FinishSmem& sm, int tid, uint32_t 
     id_to = sm.key_hi;
   }
   if (!q.use_p) return;
-  const double total = r.k_in ? r.mass + (double)sm.total * 0x1p-40 * factor : r.total;
-  const uint64_t target = (uint64_t)fmax(ceil(((q.top_p - kSlack) * total - r.mass) / factor * 0x1p40), 1.0);
+  const double total = r.k_in ? r.mass + (double)sm.total * unit : r.total;
+  const uint64_t target = (uint64_t)fmax(ceil(((q.top_p - kSlack) * total - r.mass) / unit), 1.0);
   const bool reached = sm.total >= target;
   __syncthreads();
   if (teller && count <= last && sum >= target && sum - sm.weight[i] < target) {
@@ -1069,7 +1104,7 @@ __device__ __forceinline__ void border_of_few(FinishSmem& sm, int tid, uint32_t 
 // The same for more: digit by digit.
 template <typename L>
 __device__ __forceinline__ void border_of_many(const L& ls, FinishSmem& sm, int tid, const Request& q, const SampleRow& r,
-                                               double factor, uint32_t& key, uint32_t& id_to) {
+                                               double unit, uint32_t& key, uint32_t& id_to) {
   uint32_t lo = 0xffffffffu, hi = 0u;
   ls.each([&](int, uint32_t k, auto) {
     lo = min(lo, k);
@@ -1109,11 +1144,11 @@ __device__ __forceinline__ void border_of_many(const L& ls, FinishSmem& sm, int 
       });
       atomicAdd((unsigned long long*)&sm.total, (unsigned long long)mine);
       __syncthreads();
-      total = r.mass + (double)sm.total * 0x1p-40 * factor;
+      total = r.mass + (double)sm.total * unit;
     }
   }
   if (q.use_p) {
-    const uint64_t target = (uint64_t)fmax(ceil(((q.top_p - kSlack) * total - r.mass) / factor * 0x1p40), 1.0);
+    const uint64_t target = (uint64_t)fmax(ceil(((q.top_p - kSlack) * total - r.mass) / unit), 1.0);
     const uint32_t k_key = key, k_id = id_to;
     const Border b = find_key<true>(ls, sm, tid, turn, target, [&](int id, uint32_t k) {
       return k > k_key || (k == k_key && (uint32_t)id <= k_id);
@@ -1133,13 +1168,13 @@ __device__ __forceinline__ void border_of_many(const L& ls, FinishSmem& sm, int 
 // The row's border (key, id) among its listed tokens, and their part in the draw.
 template <typename L>
 __device__ __forceinline__ void finish_list(const L& ls, FinishSmem& sm, int tid, const Request& q, const SampleRow& r,
-                                            uint64_t z0, double factor, uint32_t& key, uint32_t& id_to, Race& race,
+                                            uint64_t z0, double unit, uint32_t& key, uint32_t& id_to, Race& race,
                                             uint64_t& sum) {
   if (ls.n == 0) return;
   if (ls.n <= kFew)
-    border_of_few(sm, tid, ls.n, q, r, factor, key, id_to);
+    border_of_few(sm, tid, ls.n, q, r, unit, key, id_to);
   else
-    border_of_many(ls, sm, tid, q, r, factor, key, id_to);
+    border_of_many(ls, sm, tid, q, r, unit, key, id_to);
   ls.each([&](int id, uint32_t k, auto weight) {
     if (!(k > key || (k == key && (uint32_t)id <= id_to))) return;
     const double d = ((double)r.max - (double)logit_of(k)) * r.inv_T;
@@ -1147,7 +1182,7 @@ __device__ __forceinline__ void finish_list(const L& ls, FinishSmem& sm, int tid
     const uint64_t w = weight();
     sum += w;
     const uint32_t xn = noise_bits(z0 + (uint64_t)(id + 1) * kGolden);
-    race.enter(id, d, __builtin_amdgcn_rcpf(fmaxf((float)((double)w * 0x1p-40 * factor), 1e-14f)), xn, noise_rest(xn));
+    race.enter(id, d, __builtin_amdgcn_rcpf(fmaxf((float)((double)w * unit), 1e-14f)), xn, noise_rest(xn));
   });
 }
 
@@ -1200,16 +1235,17 @@ __global__ void __launch_bounds__(kFinish) sample_finish_kernel(SampleArgs a) {
   Race race;
   Draw best = kNoDraw;  // of the earlier passes
   // weights of the kept tokens: the earlier passes', and of the list, whose order changes from
-  // call to call, as integers over `factor`
-  double sum = 0.0, factor = 0.0;
+  // call to call, as integers of `unit`
+  double sum = 0.0, unit = 0.0;
   uint64_t in_list = 0;
   uint32_t key = 0, id_to = 0xffffffffu;
   if (q.listed()) {
-    Tokens<BF16> ls{a, sm, row, tid, n, (double)M, r.inv_T, Grid(r.inv_T, M), r.lo, r.hi};
+    Tokens<BF16> ls{a, sm, row, tid, n, (double)M, r.inv_T, Grid(r.inv_T, M), r.lo, r.hi, power_of_2(r.bits)};
     ls.stage(entry, step, rel);
-    factor = kTables.edge[min(r.lo, kSampleBins - 1)] * top_scale(ls.grid, sm.table, r.max);
-    if (r.sub >= 0) narrow(ls, sm, tid, q, r, z0, factor, race, in_list);
-    finish_list(ls, sm, tid, q, r, z0, factor, key, id_to, race, in_list);
+    unit = kTables.edge[min(r.lo, kSampleBins - 1)] * top_scale(ls.grid, sm.table, r.max) * power_of_2(-r.bits);
+    if (r.tail) r.total += (double)a.tail[row] * 0x1p-38 * (kTables.edge[kLastBin] * top_scale(ls.grid, sm.table, r.max));
+    if (r.sub >= 0) narrow(ls, sm, tid, q, r, z0, unit, race, in_list);
+    finish_list(ls, sm, tid, q, r, z0, unit, key, id_to, race, in_list);
   }
   if (q.plain()) {
     // the slices' own draws, relative to their maxima
@@ -1241,7 +1277,7 @@ __global__ void __launch_bounds__(kFinish) sample_finish_kernel(SampleArgs a) {
   if (wave != 0) return;
   best = wave_draw(lane < W ? sm.wd[lane] : kNoDraw);
   in_list = from_lane(prefix_sum(lane < W ? sm.wl[lane] : (uint64_t)0), 63);
-  sum = wave_sum(lane < W ? sm.ws[lane] : 0.0) + (double)in_list * 0x1p-40 * factor;
+  sum = wave_sum(lane < W ? sm.ws[lane] : 0.0) + (double)in_list * unit;
   if (lane == 0) {
     a.tokens[row] = min(best.id, a.V - 1);
     if (a.chosen != nullptr) a.chosen[row] = (float)(exp(-best.d) / sum);
@@ -1320,6 +1356,7 @@ size_t sample_workspace(int rows, int V, SampleArgs* a, uint8_t* base) {
   uint8_t* sum = take(R * NS * 8);
   uint8_t* row = take(R * sizeof(SampleRow));
   uint8_t* count = take(R * 4);
+  uint8_t* tail = take(R * 8);
   uint8_t* list = take(R * kSampleList * 8);
   uint8_t* sub_mass = take(R * kSampleSub * 8);
   uint8_t* sub_count = take(R * kSampleSub * 4);
@@ -1331,6 +1368,7 @@ size_t sample_workspace(int rows, int V, SampleArgs* a, uint8_t* base) {
     a->sum = (double*)sum;
     a->row = (SampleRow*)row;
     a->count = (uint32_t*)count;
+    a->tail = (uint64_t*)tail;
     a->list = (uint2*)list;
     a->sub_mass = (uint64_t*)sub_mass;
     a->sub_count = (uint32_t*)sub_count;

@@ -266,6 +266,26 @@ def test_borders_among_more_tokens_than_a_list_holds(V, scale, dtype):
         assert torch.equal(tok, t2) and torch.equal(ch, c2) and torch.equal(pr, p2)
 
 
+@pytest.mark.parametrize("V", [5000, 128256, 1000003])
+def test_tokens_at_the_end_of_the_window(V):
+    """Logits 31.5 to 32.6 below the largest: those beyond 32 have no part in the
+    weight that top_p refers to, not even where it is reached exactly."""
+    rng = np.random.default_rng(V)
+    sets = [dict(top_p=p, temperature=t) for p in (0.5, 0.25, 0.75) for t in (1.0, 0.25)]
+    sets += [dict(top_p=0.5, top_k=k) for k in (3, V // 2)] + [dict(top_p=0.999999), dict(top_k=V // 2), dict(min_p=1e-14)]
+    x = np.empty((len(sets), V), np.float32)
+    for r, st in enumerate(sets):
+        t = st.get("temperature", 1.0)
+        lo, hi = ((32.02, 32.2), (31.9, 32.3), (31.5, 32.6))[r % 3]
+        x[r] = -rng.uniform(lo, hi, V) * t + (0.0, 7.3, -3.21)[r % 3]
+        x[r, rng.choice(V, 4, replace=False)] = (0.0, 7.3, -3.21)[r % 3]
+    logits, u = torch.from_numpy(x).to(DEV), torch.from_numpy(rng.random(len(sets), np.float32)).to(DEV)
+    base = dict(temperature=1.0, top_k=0, top_p=1.0, min_p=0.0)
+    cols = {k: np.array([{**base, **s}[k] for s in sets], np.int32 if k == "top_k" else np.float32) for k in base}
+    tok, ch, pr, _ = run(logits, u, cols)
+    check(logits, u, pr, tok, ch, 1, **cols)
+
+
 def test_the_largest_vocabulary():
     rng = np.random.default_rng(20)
     V = 1 << 20

@@ -14,7 +14,7 @@
 //   sample_finish_kernel  the border among the listed tokens, the draw
 //   sample_probs_kernel   the distribution, where asked
 //
-// One float32 row of 128256 (top_k 50, top_p 0.9): 5.2 + 10.2 + 8.4 us, each a chain
+// One float32 row of 128256 (top_k 50, top_p 0.9): 5.2 + 11.1 + 8.6 us, each a chain
 // of a few round trips on at most 32 compute units.  400 rows, us of the three passes:
 //   greedy                 40 + 5 + 6     the stream, 5.2 TB/s
 //   no filter             132 + 5 + 14    the noise's hash (two 64-bit products a token)

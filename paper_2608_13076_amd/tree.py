@@ -37,8 +37,10 @@ def rotary_frequencies(rot_dim: int, theta: float = 10000.0, scaling: Optional[s
     "bands"   by the turns that a pair makes in ``trained`` positions: at least
               ``fast`` stay, at most ``slow`` are divided, in between a straight
               line over the turns
-    "ramp"    as "bands", with the line over the pairs' numbers (rounded outwards
-              to whole ones) and the amplitude 0.1 log(factor) + 1
+    "ramp"    as "bands", with the line over the pairs' numbers (its ends rounded
+              outwards to whole ones and kept within 0 and rot_dim - 1: behind
+              the last pair where that turns more than ``slow`` times) and the
+              amplitude 0.1 log(factor) + 1
     """
     if rot_dim < 2 or rot_dim % 2 or not theta > 0 or not factor > 0:
         raise ValueError("rot_dim must be even, theta and factor positive")
@@ -62,7 +64,7 @@ def rotary_frequencies(rot_dim: int, theta: float = 10000.0, scaling: Optional[s
     def pair(turns: float) -> float:  # the (fractional) pair that makes so many
         return n * math.log(trained / (2.0 * math.pi * turns)) / math.log(theta)
 
-    lo, hi = max(math.floor(pair(fast)), 0), min(math.ceil(pair(slow)), n - 1)
+    lo, hi = max(math.floor(pair(fast)), 0), min(math.ceil(pair(slow)), rot_dim - 1)
     keep = 1.0 - ((j - lo) / max(hi - lo, 1e-3)).clamp(0.0, 1.0)
     return f * keep + f / factor * (1.0 - keep), (0.1 * math.log(factor) + 1.0 if factor > 1 else 1.0)
 

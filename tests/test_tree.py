@@ -195,6 +195,28 @@ def test_frequencies_refuse(kw):
         tree.rotary_frequencies(device="cpu", **kw)
 
 
+@pytest.mark.parametrize("theta,rot", [(10000.0, 128), (500000.0, 64), (10000.0, 16)])
+@pytest.mark.parametrize("factor", [4.0, 8.0])
+@pytest.mark.parametrize("trained", [64, 4096, 8192, 65536, 131072, 1 << 20, 1 << 23])
+def test_ramp_where_the_slowest_pairs_turn_often(trained, factor, theta, rot):
+    """The line over the pairs' numbers, written out pair by pair: from the last whole
+    number where a pair makes 32 turns or more to the first where it makes one or fewer,
+    also where that is behind the last pair.  (In double: a power of up to 14 natural
+    logarithms, 14 * 2^-53 by its argument's rounding, and a few roundings: below 1e-13.)"""
+    n = rot // 2
+    turns = [trained * theta ** (-2.0 * j / rot) / (2.0 * math.pi) for j in range(-8 * rot, 8 * rot)]
+    lo = max(max(j for j, t in zip(range(-8 * rot, 8 * rot), turns) if t >= 32.0), 0)
+    hi = min(min(j for j, t in zip(range(-8 * rot, 8 * rot), turns) if t <= 1.0), rot - 1)
+    g, _ = tree.rotary_frequencies(rot, theta, "ramp", factor, trained=trained, device="cpu")
+    for j in range(n):
+        keep = 1.0 if j <= lo else 0.0 if j >= hi else (hi - j) / (hi - lo)
+        f = theta ** (-2.0 * j / rot)
+        want = f * keep + f / factor * (1.0 - keep)
+        assert abs(float(g[j]) - want) <= 1e-13 * want, (j, lo, hi)
+        if turns[8 * rot + j] > 1.0:  # only pairs of at most `slow` turns are divided in full
+            assert float(g[j]) > f / factor * (1.0 + 1e-12)
+
+
 # --- the oracle's pins -------------------------------------------------------
 
 

@@ -57,6 +57,8 @@ def rotary_frequencies(rot_dim: int, theta: float = 10000.0, scaling: Optional[s
         raise ValueError(f"scaling: unknown {scaling!r}")
     if not fast > slow > 0 or trained < 1:
         raise ValueError("0 < slow < fast and trained >= 1 required")
+    if scaling == "ramp" and not theta > 1:
+        raise ValueError("a ramp's frequencies must fall from pair to pair: theta above 1 required")
     if scaling == "bands":
         keep = ((trained * f / (2.0 * math.pi) - slow) / (fast - slow)).clamp(0.0, 1.0)
         return f * keep + f / factor * (1.0 - keep), 1.0

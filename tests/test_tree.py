@@ -217,6 +217,14 @@ def test_ramp_where_the_slowest_pairs_turn_often(trained, factor, theta, rot):
             assert float(g[j]) > f / factor * (1.0 + 1e-12)
 
 
+@pytest.mark.parametrize("theta", [1.0, 0.5])
+def test_ramp_refuses_frequencies_that_do_not_fall(theta):
+    with pytest.raises(ValueError):
+        tree.rotary_frequencies(64, theta, "ramp", 4.0, device="cpu")
+    f, _ = tree.rotary_frequencies(64, theta, "bands", 4.0, device="cpu")  # (a band of turns needs no order)
+    assert torch.isfinite(f).all()
+
+
 # --- the oracle's pins -------------------------------------------------------
 
 

@@ -69,12 +69,13 @@ class Sampler:
         if rows > self.max_rows or V > self.vocab:
             raise ValueError(f"the sampler holds {self.max_rows} rows of {self.vocab} tokens")
         f32, i32, arg, all_ = torch.float32, torch.int32, self._arg, self._all
-        n, at = 0, [None] * 4
+        n, at = None, [None] * 4
         for j, (p, t, name) in enumerate(((temperature, f32, "temperature"), (top_k, i32, "top_k"), (top_p, f32, "top_p"),
                                           (min_p, f32, "min_p"))):
             if isinstance(p, torch.Tensor):
-                if n and p.numel() != n:
-                    raise ValueError(f"{name}: expected {n} requests")
+                # (of no requests it has no address, which the library takes as not given)
+                if p.numel() != n and (n is not None or p.numel() == 0):
+                    raise ValueError(f"{name}: expected {n or 'one or more'} requests")
                 n = p.numel()
                 at[j] = arg(p, t, (n,), name)
             elif j == 0:
@@ -85,7 +86,7 @@ class Sampler:
                 all_.top_p = p
             else:
                 all_.min_p = p
-        if n and rows % n:
+        if n is not None and rows % n:
             raise ValueError(f"{rows} rows do not divide into {n} requests")
         one = (rows,)
         if tokens is None:

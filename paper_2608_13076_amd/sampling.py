@@ -9,6 +9,7 @@ stream of its device.
 from __future__ import annotations
 
 import ctypes
+import threading
 from typing import Optional, Tuple, Union
 
 import torch
@@ -23,7 +24,8 @@ _Int = Union[int, torch.Tensor]
 
 class Sampler:
     """Draws for up to ``max_rows`` rows of up to ``vocab`` tokens.  Calls share one
-    workspace, so those on different streams have to be ordered by the program."""
+    workspace, so those on different streams have to be ordered by the program; threads
+    may call at once on one stream (a call's kernels are launched together)."""
 
     def __init__(self, max_rows: int, vocab: int, device="cuda:0"):
         self.lib = load_library()
@@ -39,8 +41,7 @@ class Sampler:
             self.err = torch.zeros(1, dtype=torch.int32, device=self.device)
         self._index, self._bytes = self.device.index, nbytes
         self._at_ws, self._at_err = self.workspace.data_ptr(), self.err.data_ptr()
-        self._all = SamplingArgs(1.0, 0, 1.0, 0.0)
-        self._ref = ctypes.byref(self._all)
+        self._launch = threading.Lock()  # (the library's calls leave the interpreter's lock)
 
     def _arg(self, t: Optional[torch.Tensor], dtype, shape: tuple, name: str):
         if t is None:
@@ -68,7 +69,8 @@ class Sampler:
             raise ValueError("logits: rows must be contiguous")
         if rows > self.max_rows or V > self.vocab:
             raise ValueError(f"the sampler holds {self.max_rows} rows of {self.vocab} tokens")
-        f32, i32, arg, all_ = torch.float32, torch.int32, self._arg, self._all
+        f32, i32, arg = torch.float32, torch.int32, self._arg
+        all_ = SamplingArgs(1.0, 0, 1.0, 0.0)
         n, at = None, [None] * 4
         for j, (p, t, name) in enumerate(((temperature, f32, "temperature"), (top_k, i32, "top_k"), (top_p, f32, "top_p"),
                                           (min_p, f32, "min_p"))):
@@ -93,16 +95,17 @@ class Sampler:
             tokens = uniforms.new_empty(one, dtype=i32)
         if chosen is None:
             chosen = uniforms.new_empty(one)
-        args = (rows, V, _DTYPES[dt], logits.data_ptr(), sr if rows > 1 else V, rows // n if n else max(rows, 1), self._ref,
-                *at, arg(uniforms, f32, one, "uniforms"), arg(tokens, i32, one, "tokens"), arg(chosen, f32, one, "chosen"),
-                arg(probs, f32, (rows, V), "probs"), self._at_ws, self._bytes, self._at_err)
+        args = (rows, V, _DTYPES[dt], logits.data_ptr(), sr if rows > 1 else V, rows // n if n else max(rows, 1),
+                ctypes.byref(all_), *at, arg(uniforms, f32, one, "uniforms"), arg(tokens, i32, one, "tokens"),
+                arg(chosen, f32, one, "chosen"), arg(probs, f32, (rows, V), "probs"), self._at_ws, self._bytes, self._at_err)
         i = self._index
         stream = torch._C._cuda_getCurrentRawStream(i)
-        if torch.cuda.current_device() == i:
-            status = self.lib.spade_sample(*args, stream)
-        else:
-            with torch.cuda.device(i):
+        with self._launch:
+            if torch.cuda.current_device() == i:
                 status = self.lib.spade_sample(*args, stream)
+            else:
+                with torch.cuda.device(i):
+                    status = self.lib.spade_sample(*args, stream)
         if status:
             _check(status)
         return tokens, chosen

@@ -13,6 +13,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+import threading
 from typing import Optional, Tuple
 
 import torch
@@ -92,7 +93,8 @@ class TreeCache:
     holds; only ``commit`` changes it (a program that appends a prompt adds its
     rows itself: ``cache.lens += n``).  ``max_rows``: most rows per request of an
     ``attend`` call.  ``attend`` calls share one workspace, so those on different
-    streams have to be ordered by the program.  No call records a gradient."""
+    streams have to be ordered by the program; threads may call at once on one stream
+    (a call's kernels are launched together).  No call records a gradient."""
 
     def __init__(self, n_layers: int, batch: int, n_heads: int, n_kv_heads: int, head_dim: int, max_len: int,
                  max_rows: int = 64, device="cuda:0", buf: Optional[torch.Tensor] = None,
@@ -121,6 +123,7 @@ class TreeCache:
         # (a call costs the host about as much as a short one costs the GPU)
         self._at_buf, self._at_ws, self._at_err = self.buf.data_ptr(), self.workspace.data_ptr(), self.err.data_ptr()
         self._ws_bytes, self._scale = ws, 1.0 / math.sqrt(head_dim)
+        self._launch = threading.Lock()  # (the library's calls leave the interpreter's lock)
 
     @classmethod
     def over(cls, kv: spade.KVCache, max_rows: int = 64) -> "TreeCache":
@@ -139,11 +142,12 @@ class TreeCache:
         i = self._index
         # (the handle of torch.cuda.current_stream(i), without building the object)
         stream = torch._C._cuda_getCurrentRawStream(i)
-        if torch.cuda.current_device() == i:
-            status = fn(self._sp, *args, stream)
-        else:
-            with torch.cuda.device(i):
+        with self._launch:
+            if torch.cuda.current_device() == i:
                 status = fn(self._sp, *args, stream)
+            else:
+                with torch.cuda.device(i):
+                    status = fn(self._sp, *args, stream)
         if status:
             _check(status)
 

@@ -388,3 +388,32 @@ def test_draw_refuses():
         s.draw(x[:0], u[:0])
     with pytest.raises(spade.SpadeError):
         sampling.Sampler(1, 1, device=DEV)
+
+
+def test_two_threads_of_one_sampler():
+    """Each on the default stream with its own rows and numbers: the draws that it has alone."""
+    import threading
+    rng = np.random.default_rng(12)
+    s = sampling.Sampler(6, 20000, device=DEV)
+    jobs = []
+    for kw in (dict(top_k=40, temperature=0.7), dict(top_p=0.8, min_p=0.01)):
+        x = torch.from_numpy(rng.normal(size=(6, 20000)).astype(np.float32) * 3).to(DEV)
+        u = torch.from_numpy(rng.random(6, np.float32)).to(DEV)
+        jobs.append((x, u, kw, [t.clone() for t in s.draw(x, u, **kw)]))
+    torch.cuda.synchronize()
+    got = [[], []]
+
+    def run(i):
+        for _ in range(20):
+            got[i].append(s.draw(jobs[i][0], jobs[i][1], **jobs[i][2]))
+
+    threads = [threading.Thread(target=run, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    for (_, _, _, (tok, ch)), draws in zip(jobs, got):
+        assert len(draws) == 20
+        for a, b in draws:
+            assert torch.equal(a, tok) and torch.equal(b, ch)

@@ -83,7 +83,7 @@ class Sampler:
             elif j == 0:
                 all_.temperature = p
             elif j == 1:
-                all_.top_k = p
+                all_.top_k = min(max(p, 0), V)  # (the struct's field would take the low 32 bits)
             elif j == 2:
                 all_.top_p = p
             else:
@@ -97,7 +97,8 @@ class Sampler:
             chosen = uniforms.new_empty(one)
         args = (rows, V, _DTYPES[dt], logits.data_ptr(), sr if rows > 1 else V, rows // n if n else max(rows, 1),
                 ctypes.byref(all_), *at, arg(uniforms, f32, one, "uniforms"), arg(tokens, i32, one, "tokens"),
-                arg(chosen, f32, one, "chosen"), arg(probs, f32, (rows, V), "probs"), self._at_ws, self._bytes, self._at_err)
+                arg(chosen, f32, one, "chosen"), arg(probs, f32, (rows, V), "probs"), self._at_ws, self._bytes,
+                self._at_err)
         i = self._index
         stream = torch._C._cuda_getCurrentRawStream(i)
         with self._launch:

@@ -71,3 +71,11 @@ def test_no_requests_are_refused(sampler, name, dtype):
     with pytest.raises(ValueError):
         draw(sampler, temperature=torch.ones(2), min_p=torch.empty(0))
     assert not sampler.lib.calls
+
+
+@pytest.mark.parametrize("k", [V, V + 1, 2 ** 31 - 1, 2 ** 31, 2 ** 32, 2 ** 32 + 3, 2 ** 63 - 1, 10 ** 30, -1, -2 ** 31 - 7,
+                               3 - 2 ** 32])
+def test_a_top_k_beyond_32_bits_is_no_limit(sampler, k):
+    draw(sampler, top_k=k)
+    got = sampler.lib.calls[0].all["top_k"]
+    assert got <= 0 or got >= V

@@ -89,13 +89,11 @@ constexpr double kStep = kBin / kSteps;
 struct Grid {
   double c;
   double top;   // the largest logit's bin
-  double at;    // and its place in it, in steps
   int top_i;
   bool wide;    // step numbers beyond 31 bits: only the difference from the bin is exact then
   __device__ __forceinline__ Grid(double inv_T, float m) {
     c = inv_T * (kSteps * kBinsPerUnit);
     top = floor((double)m * c * (1.0 / kSteps));
-    at = fmin(fmax(__builtin_fma((double)m, c, -top * kSteps), 0.0), kSteps - 0x1p-20);
     wide = !(fabs(top) < 0x1p22);
     top_i = (int)top;
   }

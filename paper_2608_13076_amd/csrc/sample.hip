@@ -30,6 +30,7 @@
 
 #include "device_accept.h"
 #include "device_lanes.h"
+#include "sample_grid.h"
 
 namespace spade {
 
@@ -41,10 +42,6 @@ __device__ __forceinline__ SampleDraw prefix_step(SampleDraw v, SampleDraw) {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr double kSpan = 32.0;                       // of d: weights from e^-32 on
-constexpr double kBinsPerUnit = 126.0 / kSpan, kBin = kSpan / 126.0;
-constexpr int kLastBin = 126;                        // the last one that the window reaches, to the top's place in its own
-constexpr int kSteps = 256;                          // of the table of a bin's weights
 constexpr double kSlack = 0x1p-40;                   // of top_p: equal masses count as reached
 
 struct Request {
@@ -73,54 +70,6 @@ __device__ __forceinline__ Request request_of(const SampleArgs& a, int row) {
   if (!(q.min_d < kSpan)) q.min_d = kSpan;
   return q;
 }
-
-// 1 / T of a row whose largest logit is m, held to |m| / T <= 2^34: there two
-// different logits are 512 apart, so nothing changes.
-__device__ __forceinline__ double row_inv_T(double inv_T, float m) {
-  const double most = 0x1p34 / fmax(fabs((double)m), 0x1p-140);
-  return fmin(inv_T, most);
-}
-
-// Bins of l / T on a grid that all slices of a row share, each cut into steps: l c is
-// the number of a token's step.  A step's weight comes from a table, the rest of the
-// step from a short series (below 2^-10: 2^-34 of the weight; float32's exponential
-// would leave the border of a fine distribution to its rounding).
-constexpr double kStep = kBin / kSteps;
-struct Grid {
-  double c;
-  double top;   // the largest logit's bin
-  int top_i;
-  bool wide;    // step numbers beyond 31 bits: only the difference from the bin is exact then
-  __device__ __forceinline__ Grid(double inv_T, float m) {
-    c = inv_T * (kSteps * kBinsPerUnit);
-    top = floor((double)m * c * (1.0 / kSteps));
-    wide = !(fabs(top) < 0x1p22);
-    top_i = (int)top;
-  }
-  // bins below the top (below 0 or beyond the bins: not of the row's window), the
-  // step in its bin and the rest of a step
-  __device__ __forceinline__ int place(float l, int& step, float& rest) const {
-    return wide ? place<true>(l, step, rest) : place<false>(l, step, rest);
-  }
-  // (the same without its branch: WIDE is `wide`)
-  template <bool WIDE>
-  __device__ __forceinline__ int place(float l, int& step, float& rest) const {
-#pragma clang fp contract(off)  // (the same place in every kernel)
-    const double z = (double)l * c;
-    if (WIDE) {
-      const double bin = floor(z * (1.0 / kSteps));
-      const double t = fmin(fmax(__builtin_fma((double)l, c, -bin * kSteps), 0.0), kSteps - 0x1p-20);
-      step = (int)t;
-      rest = (float)(t - (double)step);
-      return (int)fmin(top - bin, 1e6);
-    }
-    const double q = floor(z);
-    const int i = (int)q;
-    rest = (float)(z - q);
-    step = i & (kSteps - 1);
-    return top_i - (i >> 8);
-  }
-};
 
 // exp of what the tables hold: by its series at x / 64
 constexpr double const_exp(double x) {
@@ -417,7 +366,7 @@ __global__ void __launch_bounds__(kThreads) sample_slice_kernel(SampleArgs a) {
         int step;
         float rest;
         const int j = grid.template place<wide.value>(x[k], step, rest);
-        if (x[k] > -INFINITY && j < kSampleBins) {
+        if (j < kSampleBins) {
           const double w = place_weight(table, step, rest) * (edge[j] * scale);
           sum += w;
           const float f = __builtin_amdgcn_rcpf((float)w);
@@ -444,7 +393,7 @@ __global__ void __launch_bounds__(kThreads) sample_slice_kernel(SampleArgs a) {
       int step;
       float rest;
       const int j = grid.template place<wide.value>(x[k], step, rest);
-      if (x[k] > -INFINITY && j < kSampleBins)
+      if (j < kSampleBins)
         atomicAdd((unsigned long long*)&bins[j * kCopies + (tid & (kCopies - 1))],
                   (unsigned long long)(fixed<kMassBits>(place_weight(table, step, rest)) | 1ull << 51));
     }
@@ -617,9 +566,7 @@ __global__ void __launch_bounds__(kThreads) sample_scan_kernel(SampleArgs a) {
     return least_logit((double)M - most / inv_T, [&](float l) { return ((double)M - (double)l) * inv_T <= most; });
   };
   auto from_bin = [&](int bin) {  // of the bins up to `bin` below the top
-    int step;
-    float rest;
-    return least_logit((grid.top - bin) * kSteps / grid.c, [&](float l) { return grid.place(l, step, rest) <= bin; });
+    return least_logit((grid.top - bin) * kSteps / grid.c, [&](float l) { return grid.reaches(l, bin); });
   };
   float t_window = -FLT_MAX, t_list = -FLT_MAX, t_sure = -FLT_MAX, t_min = -FLT_MAX, t_tail = -FLT_MAX;
   const bool tail = q.listed() && sm.row.tail;

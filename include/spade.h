@@ -569,8 +569,8 @@ spade_status spade_tree_commit(const spade_tree_shape* shape, void* d_cache, int
 
 /* Sampling
  * --------
- * One token per row of logits, and the distribution it was drawn from.  In double,
- * with l a token's logit, T its row's temperature and d = (max l - l) / T, weight
+ * One token per row of logits, and the distribution it was drawn from.  With l a
+ * token's logit, T its row's temperature and d = (max l - l) / T in double, weight
  * exp(-d), the tokens in the order of their logits (equal ones by id) are kept
  * while
  *   d <= 32;
@@ -578,6 +578,9 @@ spade_status spade_tree_commit(const spade_tree_shape* shape, void* d_cache, int
  *   the weight before it is below (top_p - 2^-40) of theirs (top_p >= 1: no limit;
  *     the first token always stays);
  *   exp(-d) >= min(min_p, 1).
+ * Weights are good to 2^-34 of them: where the weight before a token is nearer than
+ * that to what top_p allows, the token may be kept or not.  Equal logits have equal
+ * weights, which add up without rounding: the 2^-40 is for those.
  * The token is argmax (-d + G) over the kept ones (ties: the lowest id), G_v the
  * noise of spade_verify's draws, seeded with the bits of the row's uniform; its
  * probability among them goes to d_chosen, all of them (0 for the others) to

@@ -14,13 +14,13 @@
 //   sample_finish_kernel  the border among the listed tokens, the draw
 //   sample_probs_kernel   the distribution, where asked
 //
-// One float32 row of 128256 (top_k 50, top_p 0.9): 5.2 + 11.1 + 8.6 us, each a chain
+// One float32 row of 128256 (top_k 50, top_p 0.9): 5.1 + 10.8 + 8.6 us, each a chain
 // of a few round trips on at most 32 compute units.  400 rows, us of the three passes:
 //   greedy                 40 + 5 + 6     the stream, 5.2 TB/s
 //   no filter             132 + 5 + 14    the noise's hash (two 64-bit products a token)
 //   top_k 50, top_p 0.9    60 + 78 + 20   the stream twice; vector instructions
 //   min_p                  40 + 50 + 14   the stream twice
-// and of bfloat16, of all kinds, 58 + 41 + 27 (a stream of 103 MB: 20).
+// and of bfloat16, of all kinds, 59 + 42 + 28 (a stream of 103 MB: 20).
 #include "sample.h"
 
 #include <float.h>
@@ -301,9 +301,9 @@ __device__ __forceinline__ void store_draw(const SampleArgs& a, int64_t at, Race
 }
 
 // ---------------------------------------------------------------------------
-// A slice of a row.  Its weights stay at 40 registers: tokens looked up four or sixteen
-// at a time need 56 to 88 and take 65 to 75 us where one by one takes 58 (400 rows of
-// 128256, bfloat16).
+// A slice of a row.  Tokens are looked up one by one (80 registers, six waves a SIMD): four or
+// sixteen at a time need more and take 65 to 75 us where one by one takes 59 (400 rows of
+// 128256, bfloat16; vector instructions fill the time).
 template <bool BF16>
 __global__ void __launch_bounds__(kThreads) sample_slice_kernel(SampleArgs a) {
   __shared__ float wm[4];

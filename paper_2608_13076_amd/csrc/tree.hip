@@ -83,7 +83,7 @@ __device__ __forceinline__ void store4(void* base, int64_t at, const float* x) {
 // positions, whole 16-byte pieces where the rows cover them.
 //
 // Bound by memory: 4003 rows of 32 + 32 heads of 128 in bfloat16 read and write
-// 197 MB in 46 us, 4.3 TB/s (a large copy: 5.1).  A wave that takes four heads of one
+// 197 MB in 47 us, 4.2 TB/s (a large copy: 5.1).  A wave that takes four heads of one
 // row instead, so that a line of keys is written from eight places, took 78 us where this
 // took 55 (both through the caches).  More loads in flight, other numbers of heads per workgroup (a twentieth to a
 // quarter of them) and 16-byte loads change less than a tenth; without the angles
@@ -314,8 +314,9 @@ __global__ void __launch_bounds__(256) tree_read_kernel(TreeRead p) {
 // Bound by memory up to about 64 rows of a K/V head (two tiles over 32768 keys of 8
 // heads: 134 MB in 32 us, 4.2 TB/s), by the matrix units and the exponentials beside
 // them beyond (256 rows over 120001 keys of 8 heads, bfloat16: 126 GFLOP of the
-// formula, 189 with the probabilities' second term, in 190 us; a large bfloat16
-// product would take 158).
+// formula, 189 with the probabilities' second term, 191 us at least and a median of 225
+// where runs follow each other; a large bfloat16 product would take 158.  Matrix
+// instructions fill 0.55 of a SIMD's busy cycles, vector instructions 0.36).
 // ---------------------------------------------------------------------------
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kWaves = 4;
@@ -1420,11 +1421,18 @@ hipError_t attend_wide(const TreeAttend& a, hipStream_t st) {
 // and 128 rows over 16 ragged contexts of 256 to 4096 55.9 / 57.7 / 45.6 / 50.1.
 // float32 calls, whose wide kernels have half the rows: 1 x 8192, 256 rows 40.0 / 42.4 /
 // 41.1 / 40.9; 1 x 32768, 32 rows 51.6 / 34.2 / 37.5 / 39.7, 256 rows 106 / 102 / 107 / 101.
+//
+// From 512 heads times groups of 64 rows on, whole heads fill the chip.  A bfloat16 workgroup
+// takes 128 rows, so of calls with fewer than 512 of those (256 to 511 heads with 65 to 128
+// rows) attend_with still splits long keys.  There too this kernel is about as fast or faster
+// than what the rules below would take, us for 68 / 128 rows of 32 requests of 8 K/V heads: 256
+// keys 18.2 / 19.6 (below: 35.3 / 46.6), 1024 keys 41.5 / 51.5 (50.2 / 52.0), 4096 keys 124 / 143
+// (122 / 144).  (16 x 2048 with 256 rows comes here, 5 % off its best.)
 template <int HD, bool QB>
 hipError_t attend_t(const TreeAttend& a, hipStream_t st) {
   const int tiles = (a.G * a.R + 15) / 16;
   const int64_t heads = (int64_t)a.B * a.KVH;
-  if (heads * ((tiles + 3) / 4) >= 512)  // no split
+  if (heads * ((tiles + 3) / 4) >= 512)
     return tiles <= 2 ? attend_few<HD, QB, 1>(a, st) : attend_wide<HD, QB, 4>(a, st);
   // blocks of keys times tiles of rows, for each workgroup of one round
   const int64_t work = heads * tiles * ((a.max_keys + 31) / 32) / 512;
